@@ -209,6 +209,93 @@ vt_status vt_tree_select(const float* logprobs, const int32_t* target_ids, const
                          void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Token scoring: log probabilities of given tokens under a head, with entropy and the best alternatives.  The target
+ * model needs it to verify what the draft proposed (over W_full), a draft to be trained on its kept vocabulary (over
+ * W_trim, with the gradient below).  For each row m in [0, M):
+ *
+ *   x[m, v]     = sum_j h[m, j] * W[v, j]               fp32 accumulation of exact bf16 products;  z = scale * x
+ *   lse[m]      = log sum_{v < V} exp(z[m, v])
+ *   logprobs[m] = z[m, tokens[m]] - lse[m]
+ *   entropy[m]  = -sum_v p log p,   p = exp(z - lse)
+ *   top_ids[m, :], top_logprobs[m, :]   the k largest x[m, :] in descending order, equal ones by ascending id, and
+ *                                       their z - lse
+ * A row whose token lies outside [0, V) - a padded position, a token the trimmed vocabulary does not keep - is not
+ * scored: logprobs, entropy, lse and top_logprobs are 0 and top_ids -1, whatever its hidden state holds.  With
+ * tokens == NULL every row is scored and logprobs must be NULL.  The logits are never written to memory.
+ *
+ *   h       dev [M, d] bf16, rows ldh elements apart (ldh >= d, a multiple of 8), 16-byte aligned
+ *   W       dev [V, d] bf16, 16-byte aligned              tokens dev [M] int32 or NULL
+ *   logprobs, entropy, lse  dev [M] float (out), each may be NULL
+ *   top_ids, top_logprobs   dev [M, k] int32, float (out); ignored when k == 0
+ *   workspace  dev, 256-byte aligned, vt_score_workspace_bytes(M, d, V, k) bytes; it needs no initialisation except for
+ *              vt_last_status, which reads a status word that vt_workspace_init clears
+ * d % 8 == 0, d >= 8, 0 <= k <= min(V, VT_MAX_K), scale finite and > 0, else VT_ERR_SHAPE; any M >= 1.  Inputs must be
+ * finite in the rows that are scored; a NaN stays in its row.  Asynchronous; results do not depend on timing. */
+size_t    vt_score_workspace_bytes(int M, int d, int V, int k);
+vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32_t* tokens,
+                          int M, int d, int V, float scale, int k,
+                          float* logprobs, float* entropy, float* lse, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of vt_score_tokens.  With upstream gradients gl of the log probability and ge of the entropy:
+ *
+ *   G[m, v]      = scale * ( gl[m] * (1[v == tokens[m]] - p) - ge[m] * p * (log p + entropy[m]) )
+ *   grad_h[m, :] = sum_v G[m, v] * W[v, :]        grad_W[v, :] = sum_m G[m, v] * h[m, :]
+ *
+ * p comes from the logits, multiplied out again, and lse; G is rounded once to bf16 (it is an operand of both products),
+ * the sums are fp32 and rounded once to bf16.  A row that is not scored has G = 0 and adds nothing to grad_W.
+ *
+ *   h, ldh, W, tokens, M, d, V, scale   as in the forward call (tokens required);   lse, entropy  dev [M], its outputs
+ *   grad_logprobs  dev [M] float        grad_entropy  dev [M] float or NULL (then entropy may be NULL, too)
+ *   grad_h  dev [M, d] bf16 (out) or NULL      grad_W  dev [V, d] bf16 (out) or NULL; at least one; 16-byte aligned
+ *   workspace  dev, 256-byte aligned, vt_score_backward_workspace_bytes(M, d, V) bytes (it holds G: 2 M V bytes)
+ * Asynchronous.  Gradients are overwritten, not added to. */
+size_t    vt_score_backward_workspace_bytes(int M, int d, int V);
+vt_status vt_score_tokens_backward(const void* h, int64_t ldh, const void* W, const int32_t* tokens,
+                                   const float* lse, const float* entropy,
+                                   const float* grad_logprobs, const float* grad_entropy,
+                                   int M, int d, int V, float scale, void* grad_h, void* grad_W,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Gated feed-forward block of a draft layer (Table 1, the feed-forward row of the fixed cost F_fixed of Eq. 3):
+ *
+ *   g = x W_gate^T     u = x W_up^T     a = act(g) * u     y = a W_down^T
+ *
+ * fp32 accumulation throughout; a is rounded once to bf16 (it is an operand of the second product), y once to bf16.
+ *
+ *   x       dev [M, d] bf16, rows ldx elements apart (ldx >= d, a multiple of 8)
+ *   W_gate, W_up  dev [f, d] bf16       W_down  dev [d, f] bf16       y  dev [M, d] bf16 (out)
+ *   saved   dev [M, 2 f] float (out) or NULL: g, then u, of each row, for the backward pass
+ *   workspace  dev, 256-byte aligned, vt_gated_ffn_workspace_bytes(M, d, f) bytes; no initialisation needed (see above)
+ * All matrices 16-byte aligned.  d % 8 == 0, f % 8 == 0, both >= 8, any M >= 1; act a vt_act.  Asynchronous. */
+typedef enum vt_act {
+    VT_ACT_SILU = 0,       /* g / (1 + e^-g)                                                 */
+    VT_ACT_GELU = 1        /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2               */
+} vt_act;
+
+size_t    vt_gated_ffn_workspace_bytes(int M, int d, int f);
+vt_status vt_gated_ffn(const void* x, int64_t ldx, const void* W_gate, const void* W_up, const void* W_down,
+                       int M, int d, int f, int act, void* y, float* saved,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward pass of vt_gated_ffn, from its `saved`:
+ *
+ *   da = grad_y W_down      du = da act(g)      dg = da u act'(g)         (fp32; a, dg and du each rounded once to bf16)
+ *   grad_x = dg W_gate + du W_up      grad_W_gate = dg^T x      grad_W_up = du^T x      grad_W_down = grad_y^T a
+ *
+ *   grad_y  dev [M, d] bf16, rows ld_grad_y elements apart (>= d, a multiple of 8)
+ *   grad_x [M, d], grad_W_gate, grad_W_up [f, d], grad_W_down [d, f]  dev bf16 (out), each may be NULL, not all
+ *   workspace  dev, 256-byte aligned, vt_gated_ffn_backward_workspace_bytes(M, d, f) bytes
+ * Asynchronous.  Gradients are overwritten, not added to. */
+size_t    vt_gated_ffn_backward_workspace_bytes(int M, int d, int f);
+vt_status vt_gated_ffn_backward(const void* x, int64_t ldx, const void* W_gate, const void* W_up, const void* W_down,
+                                const float* saved, const void* grad_y, int64_t ld_grad_y,
+                                int M, int d, int f, int act,
+                                void* grad_x, void* grad_W_gate, void* grad_W_up, void* grad_W_down,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Coverage of a token stream by the kept set (Eq. 2 with f(v) = occurrences of v in the
  * stream; the "frequency coverage" of Table 4):
  *

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -21,9 +22,10 @@ VT_ERR_EMPTY, VT_ERR_WORKSPACE, VT_ERR_TIMEOUT, VT_ERR_CUDA, VT_ERR_UNSUPPORTED 
 VT_MAX_K = 64
 VT_PATH_AUTO, VT_PATH_GEMV, VT_PATH_MMA, VT_PATH_MMA_SMALL = 0, 1, 2, 3
 VT_HEAD_STATIC_WEIGHTS, VT_HEAD_D2T_OFFSETS = 0x100, 0x200
+VT_ACT_SILU, VT_ACT_GELU = 0, 1
 
 # every symbol include/vt.h declares: name -> (restype, argtypes)
-_p, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+_p, _i, _i64, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
 SYMBOLS = {
     "vt_strerror": (ctypes.c_char_p, [_i]),
     "vt_last_cuda_error": (_i, []),
@@ -47,6 +49,14 @@ SYMBOLS = {
     "vt_debug_logits": (_i, [_p, _p, _i, _i, _i, _p, _p, _sz, _p, _i]),
     "vt_fuse_features": (_i, [_p, _p, _i, _i, _i, _p, _p, _sz, _p]),
     "vt_tree_select": (_i, [_p, _p, _p, _i, _i, _i, _p, _p, _p, _p, _p]),
+    "vt_score_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "vt_score_tokens": (_i, [_p, _i64, _p, _p, _i, _i, _i, _f, _i, _p, _p, _p, _p, _p, _p, _sz, _p]),
+    "vt_score_backward_workspace_bytes": (_sz, [_i, _i, _i]),
+    "vt_score_tokens_backward": (_i, [_p, _i64, _p, _p, _p, _p, _p, _p, _i, _i, _i, _f, _p, _p, _p, _sz, _p]),
+    "vt_gated_ffn_workspace_bytes": (_sz, [_i, _i, _i]),
+    "vt_gated_ffn": (_i, [_p, _i64, _p, _p, _p, _i, _i, _i, _i, _p, _p, _p, _sz, _p]),
+    "vt_gated_ffn_backward_workspace_bytes": (_sz, [_i, _i, _i]),
+    "vt_gated_ffn_backward": (_i, [_p, _i64, _p, _p, _p, _p, _p, _i64, _i, _i, _i, _i, _p, _p, _p, _p, _p, _sz, _p]),
     "vt_remap": (_i, [_p, _p, _i64, _i, _p, _p]),
     "vt_vocab_maps": (_i, [_p, _i, _i, _p, _p, _p]),
     "vt_last_launch_count": (_i, []),
@@ -105,6 +115,37 @@ def _i32(t: torch.Tensor, name: str) -> torch.Tensor:
     if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous int32 CUDA tensor")
     return t
+
+
+def _bf16_rows(t: torch.Tensor, name: str) -> torch.Tensor:
+    """bf16 rows that may lie further apart than they are long (a slice of a wider buffer)."""
+    if t.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
+        raise TypeError(f"{name}: expected bf16 data (torch.bfloat16 or a 16-bit integer view), got {t.dtype}")
+    if not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name}: expected a 2-D CUDA tensor with contiguous rows")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _f32(t: torch.Tensor, name: str, shape: tuple) -> torch.Tensor:
+    if t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected a contiguous float32 CUDA tensor of shape {shape}")
+    return t
+
+
+def _out(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected a contiguous {dtype} CUDA tensor of shape {shape}")
+    return t
+
+
+def _scratch(workspace: torch.Tensor | None, nbytes: int, device) -> torch.Tensor:
+    return workspace if workspace is not None else torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
 def vt_workspace_bytes(M: int, k: int) -> int:
@@ -316,6 +357,146 @@ def vt_tree_select(logprobs: torch.Tensor, target_ids: torch.Tensor, parent_scor
                                 rows.data_ptr(), slots.data_ptr(), tokens.data_ptr(), scores.data_ptr(), _stream()),
            "vt_tree_select")
     return rows, slots, tokens, scores
+
+
+class VtScores(NamedTuple):
+    """What ``vt_score_tokens`` returns: [M] float32 each, and [M, k] for the alternatives (None for k = 0)."""
+    logprobs: torch.Tensor | None
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: torch.Tensor | None
+    top_logprobs: torch.Tensor | None
+
+
+def vt_score_workspace_bytes(M: int, d: int, V: int, k: int) -> int:
+    return int(lib().vt_score_workspace_bytes(M, d, V, k))
+
+
+def vt_score_backward_workspace_bytes(M: int, d: int, V: int) -> int:
+    return int(lib().vt_score_backward_workspace_bytes(M, d, V))
+
+
+def _score_inputs(h, W, tokens):
+    h, W = _bf16_rows(h, "h"), _bf16(W, "W")
+    if W.shape[1] != h.shape[1]:
+        raise ValueError("h and W disagree on d")
+    if tokens is not None and _i32(tokens, "tokens").shape != (h.shape[0],):
+        raise ValueError("tokens must hold one id per row of h")
+    return h, W
+
+
+def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | None, *, k: int = 0, scale: float = 1.0,
+                    workspace: torch.Tensor | None = None, logprobs: torch.Tensor | None = None,
+                    entropy: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                    top_ids: torch.Tensor | None = None, top_logprobs: torch.Tensor | None = None) -> VtScores:
+    """Log probabilities of ``tokens`` [M] under the head ``W`` [V, d], with entropy, log-sum-exp and the k best alternatives.
+
+    Rows whose token lies outside [0, V) are not scored (zeros, top_ids -1); ``tokens=None`` scores every row without a
+    given token.  Pass tensors for outputs and workspace to have them reused."""
+    h, W = _score_inputs(h, W, tokens)
+    (M, d), V, dev = h.shape, W.shape[0], h.device
+    if tokens is not None:
+        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, dev)
+    elif logprobs is not None:
+        raise ValueError("logprobs needs tokens")
+    entropy = _out(entropy, "entropy", (M,), torch.float32, dev)
+    lse = _out(lse, "lse", (M,), torch.float32, dev)
+    if k > 0:
+        top_ids = _out(top_ids, "top_ids", (M, k), torch.int32, dev)
+        top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, dev)
+    else:
+        top_ids = top_logprobs = None
+    if workspace is None:
+        workspace = _scratch(None, vt_score_workspace_bytes(M, d, V, k), dev)
+    _check(lib().vt_score_tokens(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), M, d, V, scale, k, _ptr(logprobs),
+                                 entropy.data_ptr(), lse.data_ptr(), _ptr(top_ids), _ptr(top_logprobs),
+                                 workspace.data_ptr(), workspace.numel(), _stream()), "vt_score_tokens")
+    return VtScores(logprobs, entropy, lse, top_ids, top_logprobs)
+
+
+def vt_score_tokens_backward(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor,
+                             entropy: torch.Tensor | None, grad_logprobs: torch.Tensor,
+                             grad_entropy: torch.Tensor | None = None, *, scale: float = 1.0,
+                             workspace: torch.Tensor | None = None, grad_h: torch.Tensor | None = None,
+                             grad_W: torch.Tensor | None = None, want_h: bool = True, want_W: bool = True):
+    """(grad_h [M, d], grad_W [V, d]) in bf16 from the forward call's ``lse`` and ``entropy``; one not wanted is None."""
+    h, W = _score_inputs(h, W, tokens)
+    (M, d), V, dev = h.shape, W.shape[0], h.device
+    lse, grad_logprobs = _f32(lse, "lse", (M,)), _f32(grad_logprobs, "grad_logprobs", (M,))
+    if grad_entropy is not None:
+        if entropy is None:
+            raise ValueError("grad_entropy needs the forward call's entropy")
+        _f32(entropy, "entropy", (M,)), _f32(grad_entropy, "grad_entropy", (M,))
+    grad_h = _out(grad_h, "grad_h", (M, d), torch.bfloat16, dev) if want_h else None
+    grad_W = _out(grad_W, "grad_W", (V, d), torch.bfloat16, dev) if want_W else None
+    if workspace is None:
+        workspace = _scratch(None, vt_score_backward_workspace_bytes(M, d, V), dev)
+    _check(lib().vt_score_tokens_backward(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), lse.data_ptr(), _ptr(entropy),
+                                          grad_logprobs.data_ptr(), _ptr(grad_entropy), M, d, V, scale, _ptr(grad_h), _ptr(grad_W),
+                                          workspace.data_ptr(), workspace.numel(), _stream()), "vt_score_tokens_backward")
+    return grad_h, grad_W
+
+
+_ACTS = {"silu": VT_ACT_SILU, "gelu": VT_ACT_GELU}
+
+
+def vt_gated_ffn_workspace_bytes(M: int, d: int, f: int) -> int:
+    return int(lib().vt_gated_ffn_workspace_bytes(M, d, f))
+
+
+def vt_gated_ffn_backward_workspace_bytes(M: int, d: int, f: int) -> int:
+    return int(lib().vt_gated_ffn_backward_workspace_bytes(M, d, f))
+
+
+def _ffn_inputs(x, W_gate, W_up, W_down):
+    x = _bf16_rows(x, "x")
+    _bf16(W_gate, "W_gate"), _bf16(W_up, "W_up"), _bf16(W_down, "W_down")
+    d, f = x.shape[1], W_gate.shape[0]
+    if W_gate.shape != (f, d) or W_up.shape != (f, d) or W_down.shape != (d, f):
+        raise ValueError("x, W_gate, W_up and W_down disagree on d or f")
+    return x, d, f
+
+
+def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, *, act: str | int = "silu",
+                 out: torch.Tensor | None = None, saved: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """y [M, d] bf16 = (act(x W_gate^T) * (x W_up^T)) W_down^T, act "silu" or "gelu" (tanh form).
+
+    Pass ``saved`` [M, 2 f] float32 to receive both projections for ``vt_gated_ffn_backward``."""
+    x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
+    M = x.shape[0]
+    out = _out(out, "out", (M, d), torch.bfloat16, x.device)
+    if saved is not None:
+        _f32(saved, "saved", (M, 2 * f))
+    if workspace is None:
+        workspace = _scratch(None, vt_gated_ffn_workspace_bytes(M, d, f), x.device)
+    _check(lib().vt_gated_ffn(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), M, d, f,
+                              _ACTS.get(act, act), out.data_ptr(), _ptr(saved), workspace.data_ptr(), workspace.numel(),
+                              _stream()), "vt_gated_ffn")
+    return out
+
+
+def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor, saved: torch.Tensor,
+                          grad_y: torch.Tensor, *, act: str | int = "silu", workspace: torch.Tensor | None = None,
+                          grad_x: torch.Tensor | None = None, grad_W_gate: torch.Tensor | None = None,
+                          grad_W_up: torch.Tensor | None = None, grad_W_down: torch.Tensor | None = None):
+    """(grad_x [M, d], grad_W_gate [f, d], grad_W_up [f, d], grad_W_down [d, f]) in bf16 from the forward call's ``saved``."""
+    x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
+    M, dev = x.shape[0], x.device
+    _f32(saved, "saved", (M, 2 * f))
+    if _bf16_rows(grad_y, "grad_y").shape != (M, d):
+        raise ValueError("grad_y must have the shape of x")
+    grad_x = _out(grad_x, "grad_x", (M, d), torch.bfloat16, dev)
+    grad_W_gate = _out(grad_W_gate, "grad_W_gate", (f, d), torch.bfloat16, dev)
+    grad_W_up = _out(grad_W_up, "grad_W_up", (f, d), torch.bfloat16, dev)
+    grad_W_down = _out(grad_W_down, "grad_W_down", (d, f), torch.bfloat16, dev)
+    if workspace is None:
+        workspace = _scratch(None, vt_gated_ffn_backward_workspace_bytes(M, d, f), dev)
+    _check(lib().vt_gated_ffn_backward(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), saved.data_ptr(),
+                                       grad_y.data_ptr(), _ld(grad_y), M, d, f, _ACTS.get(act, act), grad_x.data_ptr(),
+                                       grad_W_gate.data_ptr(), grad_W_up.data_ptr(), grad_W_down.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel(), _stream()), "vt_gated_ffn_backward")
+    return grad_x, grad_W_gate, grad_W_up, grad_W_down
 
 
 def vt_remap(draft_ids: torch.Tensor, d2t: torch.Tensor) -> torch.Tensor:

@@ -3,7 +3,11 @@
 #include <cstdio>
 #include <cstring>
 
+#include <cmath>
+
+#include "vt_ffn.h"
 #include "vt_launch.h"
+#include "vt_score.h"
 
 namespace vt {
 
@@ -396,6 +400,104 @@ vt_status vt_tree_select(const float* logprobs, const int32_t* target_ids, const
         return VT_ERR_ALIGN;
     return launch_tree_select(logprobs, target_ids, parent_scores, M, k, T, out_rows, out_slots, out_tokens, out_scores,
                               (cudaStream_t)stream);
+}
+
+static vt_status check_score_args(const void* h, int64_t ldh, const void* W, int M, int d, int V, float scale) {
+    if (!h || !W) return VT_ERR_NULL;
+    if (d < 8 || d % 8 != 0 || M < 1 || V < 1 || ldh < d || ldh % 8 != 0 || !std::isfinite(scale) || !(scale > 0.0f)) return VT_ERR_SHAPE;
+    if (!aligned(h, 16) || !aligned(W, 16)) return VT_ERR_ALIGN;
+    return VT_OK;
+}
+
+size_t vt_score_workspace_bytes(int M, int d, int V, int k) {
+    if (M < 1 || d < 8 || d % 8 != 0 || V < 1 || k < 0 || k > V || k > VT_MAX_K) return 0;
+    return score_workspace_bytes(M, d, V, k);
+}
+
+vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32_t* tokens, int M, int d, int V, float scale,
+                          int k, float* logprobs, float* entropy, float* lse, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    g_launches = 0;
+    vt_status r = check_score_args(h, ldh, W, M, d, V, scale);
+    if (r != VT_OK) return r;
+    if (k < 0 || k > V || k > VT_MAX_K) return VT_ERR_SHAPE;
+    if ((k > 0 && (!top_ids || !top_logprobs)) || (!tokens && logprobs)) return VT_ERR_NULL;
+    if (!aligned(tokens, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) || !aligned(lse, 4) ||
+        (k > 0 && (!aligned(top_ids, 4) || !aligned(top_logprobs, 4))))
+        return VT_ERR_ALIGN;
+    const size_t need = score_workspace_bytes(M, d, V, k);
+    if (need == 0) return VT_ERR_SHAPE;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return VT_ERR_WORKSPACE;
+    const ScoreCall c{h, ldh, W, tokens, M, d, V, scale};
+    return launch_score(c, ScoreOut{logprobs, entropy, lse, top_ids, top_logprobs, k}, workspace, (cudaStream_t)stream);
+}
+
+size_t vt_score_backward_workspace_bytes(int M, int d, int V) {
+    if (M < 1 || d < 8 || d % 8 != 0 || V < 1) return 0;
+    return score_backward_workspace_bytes(M, d, V);
+}
+
+vt_status vt_score_tokens_backward(const void* h, int64_t ldh, const void* W, const int32_t* tokens, const float* lse,
+                                   const float* entropy, const float* grad_logprobs, const float* grad_entropy, int M, int d,
+                                   int V, float scale, void* grad_h, void* grad_W, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+    g_launches = 0;
+    if (!tokens || !lse || !grad_logprobs || (grad_entropy && !entropy) || (!grad_h && !grad_W)) return VT_ERR_NULL;
+    vt_status r = check_score_args(h, ldh, W, M, d, V, scale);
+    if (r != VT_OK) return r;
+    if (!aligned(tokens, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(grad_logprobs, 4) || !aligned(grad_entropy, 4) ||
+        !aligned(grad_h, 16) || !aligned(grad_W, 16))
+        return VT_ERR_ALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < score_backward_workspace_bytes(M, d, V)) return VT_ERR_WORKSPACE;
+    const ScoreCall c{h, ldh, W, tokens, M, d, V, scale};
+    return launch_score_backward(c, lse, entropy, grad_logprobs, grad_entropy, grad_h, grad_W, workspace, (cudaStream_t)stream);
+}
+
+static vt_status check_ffn_args(const void* x, int64_t ldx, const void* W_gate, const void* W_up, const void* W_down, int M, int d,
+                                int f, int act) {
+    if (!x || !W_gate || !W_up || !W_down) return VT_ERR_NULL;
+    if (d < 8 || d % 8 != 0 || f < 8 || f % 8 != 0 || M < 1 || ldx < d || ldx % 8 != 0 || (act != VT_ACT_SILU && act != VT_ACT_GELU))
+        return VT_ERR_SHAPE;
+    if (!aligned(x, 16) || !aligned(W_gate, 16) || !aligned(W_up, 16) || !aligned(W_down, 16)) return VT_ERR_ALIGN;
+    return VT_OK;
+}
+
+size_t vt_gated_ffn_workspace_bytes(int M, int d, int f) {
+    if (M < 1 || d < 8 || d % 8 != 0 || f < 8 || f % 8 != 0) return 0;
+    return ffn_workspace_bytes(M, d, f);
+}
+size_t vt_gated_ffn_backward_workspace_bytes(int M, int d, int f) {
+    if (M < 1 || d < 8 || d % 8 != 0 || f < 8 || f % 8 != 0) return 0;
+    return ffn_backward_workspace_bytes(M, d, f);
+}
+
+vt_status vt_gated_ffn(const void* x, int64_t ldx, const void* W_gate, const void* W_up, const void* W_down, int M, int d, int f,
+                       int act, void* y, float* saved, void* workspace, size_t workspace_bytes, void* stream) {
+    g_launches = 0;
+    if (!y) return VT_ERR_NULL;
+    vt_status r = check_ffn_args(x, ldx, W_gate, W_up, W_down, M, d, f, act);
+    if (r != VT_OK) return r;
+    if (!aligned(y, 16) || !aligned(saved, 16)) return VT_ERR_ALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < ffn_workspace_bytes(M, d, f)) return VT_ERR_WORKSPACE;
+    const FfnCall c{x, ldx, W_gate, W_up, W_down, M, d, f, act};
+    return launch_ffn(c, y, saved, workspace, (cudaStream_t)stream);
+}
+
+vt_status vt_gated_ffn_backward(const void* x, int64_t ldx, const void* W_gate, const void* W_up, const void* W_down,
+                                const float* saved, const void* grad_y, int64_t ld_grad_y, int M, int d, int f, int act,
+                                void* grad_x, void* grad_W_gate, void* grad_W_up, void* grad_W_down, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    g_launches = 0;
+    if (!saved || !grad_y || (!grad_x && !grad_W_gate && !grad_W_up && !grad_W_down)) return VT_ERR_NULL;
+    vt_status r = check_ffn_args(x, ldx, W_gate, W_up, W_down, M, d, f, act);
+    if (r != VT_OK) return r;
+    if (ld_grad_y < d || ld_grad_y % 8 != 0) return VT_ERR_SHAPE;
+    if (!aligned(saved, 16) || !aligned(grad_y, 16) || !aligned(grad_x, 16) || !aligned(grad_W_gate, 16) || !aligned(grad_W_up, 16) ||
+        !aligned(grad_W_down, 16))
+        return VT_ERR_ALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < ffn_backward_workspace_bytes(M, d, f)) return VT_ERR_WORKSPACE;
+    const FfnCall c{x, ldx, W_gate, W_up, W_down, M, d, f, act};
+    return launch_ffn_backward(c, saved, grad_y, ld_grad_y, grad_x, grad_W_gate, grad_W_up, grad_W_down, workspace, (cudaStream_t)stream);
 }
 
 vt_status vt_remap(const int32_t* draft_ids, const int32_t* d2t, int64_t n, int V_trim, int32_t* target_ids,

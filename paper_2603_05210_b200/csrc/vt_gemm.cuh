@@ -1,0 +1,508 @@
+// The matrix products behind token scoring and the gated feed-forward block: one tcgen05 kernel whose epilogue is a
+// template parameter, for results of any size.
+//
+//   D[m, n] = sum_k A[m, k] * B[n, k]         bf16 operands, exact products, fp32 sums in tensor memory
+//
+// Either operand may be stored with k running fastest ([m][k], "K-major") or with m (n) running fastest ([k][m],
+// "MN-major"): the tensor core takes both from a 128-byte swizzled TMA box, so no gradient needs a transposed copy.
+// A launch takes one to three products (GemmProblem): a product may sum over two pairs of operands one after the other
+// (dg Wg + du Wu), or its columns may come in two halves from two matrices (gate and up rows of one feature side by side
+// in one accumulator).
+//
+// Work is cut into tiles of 128 or 256 rows x NT columns:
+//   PAIR    clusters of two CTAs share each MMA (cta_group::2): 256 rows x NT <= 256 columns, either CTA fetches its
+//           128 rows of A and half the columns of B.  For more than 128 rows: a CTA then moves 32 KB per 64-deep k-block
+//           of 2 * 128 * 256 * 64 FLOP, half of what two separate 128 x 128 tiles would.
+//   single  128 rows x NT <= 256 columns.  With at most 64 (32) rows of A the tile holds them two (four) times, one copy
+//           per group of TMEM lanes: the tensor core has the time, and every epilogue warp then finds rows to work on,
+//           each copy taking its own share of the columns.
+//   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile, lays its partial sums out in
+//           shared memory, and each CTA adds up and finishes its share of the columns through distributed shared
+//           memory, in the order of the CTAs: no atomics, the same bits every time.
+// The CTAs are persistent (except with splits).  Warps 0-7: epilogue, warp 8: TMA producer, warp 9: MMA issuer; two
+// accumulators in tensor memory, so the epilogue of a tile runs under the MMAs of the next.
+// All waits are bounded; one that runs out sets the workspace's status word and the CTA unwinds.
+#pragma once
+
+#include "vt_common.cuh"
+#include "vt_launch.h"
+#include "vt_tc.cuh"
+
+namespace vt {
+
+constexpr int kGemmEpiWarps = 8;
+constexpr int kGemmThreads = (kGemmEpiWarps + 2) * 32;
+constexpr int kGemmMaxStages = 16;
+constexpr int kGemmMaxProblems = 3;
+constexpr int kGemmMaxMaps = 6;
+constexpr int kGemmGroupRows = 8;           // row tiles that share their column tiles before the next group (L2 reuse)
+constexpr int kGemmSms = 148;               // the plans are made for this many SMs; a device with fewer runs them in more waves
+
+struct GemmProblem {
+    int M, N;                    // rows and columns of D (with `dual`: columns of either half)
+    int a0, b0, nk0;             // tensor maps and 64-deep k-blocks of the first pair of operands
+    int a1, b1, nk1;             // ... of the second (nk1 = 0: there is none)
+    int tiles_m, chunks_n;       // row tiles; items along the columns
+    int tiles_n;                 // column tiles
+    int first_item;
+    void* out;                   // for epilogues that just store
+};
+
+struct GemmMaps {
+    CUtensorMap map[kGemmMaxMaps];
+};
+
+struct GemmParams {
+    GemmProblem prob[kGemmMaxProblems];
+    int n_prob, n_items;
+    int tiles_per_item;          // consecutive column tiles of one row tile that a CTA takes in a row
+    int NT;                      // accumulator columns of a tile
+    int dual;                    // 1: columns [0, NT/2) from map b0, [NT/2, NT) from map b1, the same rows of both
+    int rep;                     // copies of A's rows in a tile: 1, 2 or 4 (single only)
+    int splits;                  // CTAs that share one tile's k range (single only)
+    int n_stages;
+    uint32_t a_bytes, b_bytes;   // bytes of one k-block of A (B) in shared memory
+    uint32_t stage_bytes;
+    uint32_t idesc;
+    uint32_t tmem_cols, acc_cols;    // allocation; columns between the two accumulators
+    uint32_t bar_off;            // barriers, from the 1024-aligned base
+    uint32_t total_smem;
+    WsHeader* hdr;
+};
+
+// A tile's place.
+struct GemmItem {
+    int prob, mt, nt0, n_tiles;
+};
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ void acc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+
+// Descriptor of an MN-major bf16 tile as TMA boxes of 64 (m or n) x 64 (k) leave it: 64 elements of m are one 128-byte
+// swizzled row, 8 k rows are 1024 bytes apart, the next 64 elements of m one box (8192 bytes) further on.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr) {
+    uint64_t desc = 0;
+    desc |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+    desc |= (uint64_t)(8192 >> 4) << 16;                 // leading byte offset: between groups of 64 elements of m
+    desc |= (uint64_t)(1024 >> 4) << 32;                 // stride byte offset: between groups of 8 k
+    desc |= (uint64_t)1 << 46;
+    desc |= (uint64_t)2 << 61;
+    return desc;
+}
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ GemmItem gemm_item(const GemmParams& p, int item) {
+    GemmItem it;
+    it.prob = 0;
+    while (it.prob + 1 < p.n_prob && item >= p.prob[it.prob + 1].first_item) ++it.prob;
+    const GemmProblem& q = p.prob[it.prob];
+    const int local = item - q.first_item;
+    const int per_group = kGemmGroupRows * q.chunks_n;
+    const int g = local / per_group, r = local - g * per_group;
+    const int gm = min(kGemmGroupRows, q.tiles_m - g * kGemmGroupRows);
+    const int ch = r / gm;
+    it.mt = g * kGemmGroupRows + (r - ch * gm);
+    it.nt0 = ch * p.tiles_per_item;
+    it.n_tiles = min(p.tiles_per_item, q.tiles_n - it.nt0);
+    return it;
+}
+
+// Eight fp32 values as bf16 (nearest-even) to a 16-byte aligned address.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void store_bf16x8(uint16_t* at, const float* x) {
+    *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// Epilogue that rounds the sums once to bf16 and stores them row-major, N columns a row (N a multiple of 8).
+struct EpiStore {
+    static constexpr bool kDual = false;
+    static constexpr bool kStateful = false;
+    struct Params {};
+    struct State {};
+    static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
+    // eight consecutive columns of one row, all inside D
+    static __device__ __forceinline__ void cols8(State&, const Params&, const GemmProblem& q, int m, int n, const float* x) {
+        store_bf16x8(reinterpret_cast<uint16_t*>(q.out) + (size_t)m * q.N + n, x);
+    }
+};
+
+// An epilogue provides
+//   kDual       its columns come in two halves: cols8(..., x, y) gets eight columns of either
+//   kStateful   it works through all tiles of an item with a state of its own (never with splits): begin(), then
+//               cols16(state, params, row, col, live, x) for runs of 16 columns of which the first `live` are real, then end()
+//   row()       called once per tile and row before its columns (stateless only)
+template <bool PAIR, bool A_MN, bool B_MN, class Epi>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p,
+            const __grid_constant__ typename Epi::Params ep) {
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    unsigned char* smem = smem_raw + (base - raw);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    constexpr int kProducer = kGemmEpiWarps, kIssuer = kGemmEpiWarps + 1;
+    const int S = p.n_stages;
+    const uint32_t rank = (PAIR || p.splits > 1) ? cluster_cta_rank() : 0u;
+    const bool leader = !PAIR || rank == 0u;
+    const int cluster = PAIR ? (int)blockIdx.x >> 1 : p.splits > 1 ? (int)blockIdx.x / p.splits : (int)blockIdx.x;
+    const int n_clusters = PAIR ? (int)gridDim.x >> 1 : p.splits > 1 ? (int)gridDim.x / p.splits : (int)gridDim.x;
+
+    const uint32_t bar_full = base + p.bar_off, bar_empty = bar_full + 8u * S;
+    const uint32_t bar_accf = bar_empty + 8u * S, bar_acce = bar_accf + 16u, bar_drain = bar_acce + 16u;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + p.bar_off + 8u * (2 * S + 5));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    if (warp == kProducer && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.map[p.prob[0].a0]) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.map[p.prob[0].b0]) : "memory");
+    }
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(bar_full + 8u * s, 1);
+            mbar_init(bar_empty + 8u * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar_accf + 8u * b, 1);
+            mbar_init(bar_acce + 8u * b, PAIR ? 2 * kGemmEpiWarps : kGemmEpiWarps);
+        }
+        mbar_init(bar_drain, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == kIssuer) {
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                         ::"r"(smem_u32(tmem_slot)), "r"(p.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                         ::"r"(smem_u32(tmem_slot)), "r"(p.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    fence_proxy_async();
+    tc_fence_before();
+    if constexpr (PAIR) cluster_sync_all();      // the other CTA's barriers are initialised before anything arrives on them
+    else __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    // Nothing above touches global memory (the tensor maps are kernel parameters): under programmatic dependent launch it
+    // overlaps the previous kernel's tail.  From here on that kernel's writes are visible.
+    grid_dependency_wait();
+    if (tid == 0) grid_launch_dependents();
+
+    auto fail = [&]() {
+        *abort_flag = 1;
+        atomicOr(&p.hdr->status, kStatusTimeout);
+    };
+    // the k-blocks of a product that this CTA multiplies
+    auto k_range = [&](const GemmProblem& q, int& k0, int& k1) {
+        const int nk = q.nk0 + q.nk1;
+        k0 = p.splits > 1 ? (int)((long long)nk * (int)rank / p.splits) : 0;
+        k1 = p.splits > 1 ? (int)((long long)nk * ((int)rank + 1) / p.splits) : nk;
+    };
+
+    if (warp == kProducer) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            int s = 0, issued = 0;
+            uint32_t wrap = 0;
+            bool ok = true;
+            const uint32_t tx = (p.a_bytes + p.b_bytes) * (PAIR ? 2u : 1u);
+            const int a_box = 128 / p.rep;
+            for (int item = cluster; item < p.n_items && ok; item += n_clusters) {
+                const GemmItem it = gemm_item(p, item);
+                const GemmProblem& q = p.prob[it.prob];
+                const int row0 = it.mt * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
+                int k0, k1;
+                k_range(q, k0, k1);
+                for (int t = 0; t < it.n_tiles && ok; ++t) {
+                    const int nt = it.nt0 + t;
+                    const int half = p.NT >> 1;
+                    // first row of B this CTA fetches, and the map of a pair's CTA where the halves differ
+                    const int col0 = p.dual ? nt * half : nt * p.NT + (PAIR ? (int)rank * half : 0);
+                    for (int kb = k0; kb < k1; ++kb) {
+                        if (wrap > 0 && !mbar_wait(bar_empty + 8u * s, (wrap - 1) & 1u)) { fail(); ok = false; break; }
+                        if (*abort_flag) { ok = false; break; }
+                        const bool second = kb >= q.nk0;
+                        const int x = (second ? kb - q.nk0 : kb) * kBoxK;
+                        const CUtensorMap* ma = &maps.map[second ? q.a1 : q.a0];
+                        const CUtensorMap* mb = &maps.map[PAIR && p.dual ? (rank ? q.b1 : q.b0) : second ? q.b1 : q.b0];
+                        const uint32_t dst = base + (uint32_t)s * p.stage_bytes;
+                        uint32_t bar = bar_full + 8u * s;
+                        if (leader) mbar_arrive_expect_tx(bar, tx);
+                        if constexpr (PAIR) bar = cluster_map_shared(bar, 0u);     // both CTAs' bytes count on the leader's barrier
+                        auto load = [&](uint32_t to, const CUtensorMap* m, int cx, int cy) {
+                            if constexpr (PAIR) tma_load_2d_pair(to, m, cx, cy, bar);
+                            else tma_load_2d(to, m, cx, cy, bar);
+                        };
+                        if constexpr (A_MN) {
+                            load(dst, ma, row0, x);
+                            load(dst + 8192u, ma, row0 + 64, x);
+                        } else {
+                            for (int r = 0; r < p.rep; ++r) load(dst + (uint32_t)(r * a_box) * 128u, ma, x, row0);
+                        }
+                        const uint32_t dstb = dst + p.a_bytes;
+                        if constexpr (B_MN) {
+                            for (uint32_t o = 0; o < p.b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
+                        } else if (!PAIR && p.dual) {
+                            load(dstb, mb, x, col0);
+                            load(dstb + (uint32_t)half * 128u, &maps.map[q.b1], x, col0);
+                        } else {
+                            load(dstb, mb, x, col0);
+                        }
+                        ++issued;
+                        if (++s == S) { s = 0; ++wrap; }
+                    }
+                }
+            }
+            if (*abort_flag && leader) {       // let copies in flight land before the CTA gives its shared memory back
+                const unsigned long long deadline = global_timer_ns() + kWaitLimitNs;
+                for (int i = max(0, issued - S); i < issued; ++i)
+                    (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, deadline);
+            }
+        }
+    } else if (warp == kIssuer) {
+        // ------------------------------------------------------------------ MMA issuer (of a pair: the leader's)
+        if (lane == 0 && leader) {
+            int s = 0, n = 0;                  // ring stage; tiles so far
+            uint32_t phase = 0;
+            bool ok = true;
+            const uint64_t a_desc0 = A_MN ? smem_desc_sw128_mn(base) : smem_desc_sw128(base);
+            const uint64_t b_desc0 = B_MN ? smem_desc_sw128_mn(base + p.a_bytes) : smem_desc_sw128(base + p.a_bytes);
+            constexpr uint32_t a_step = A_MN ? 128u : 2u, b_step = B_MN ? 128u : 2u;   // 16 of k: two 8-row groups, or 32 bytes of a row
+            const uint32_t stage_units = p.stage_bytes >> 4;
+            for (int item = cluster; item < p.n_items && ok; item += n_clusters) {
+                const GemmItem it = gemm_item(p, item);
+                int k0, k1;
+                k_range(p.prob[it.prob], k0, k1);
+                for (int t = 0; t < it.n_tiles && ok; ++t, ++n) {
+                    const int buf = n & 1;
+                    if (n >= 2 && !mbar_wait(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u)) { fail(); ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t d_tmem = tmem_base + (uint32_t)buf * p.acc_cols;
+                    for (int kb = k0; kb < k1; ++kb) {
+                        if (!mbar_wait(bar_full + 8u * s, phase)) { fail(); ok = false; break; }
+                        if (*abort_flag) { ok = false; break; }
+                        tc_fence_after();
+                        const uint64_t a = a_desc0 + (uint64_t)((uint32_t)s * stage_units);
+                        const uint64_t b = b_desc0 + (uint64_t)((uint32_t)s * stage_units);
+#pragma unroll
+                        for (uint32_t i = 0; i < 4; ++i) {
+                            if constexpr (PAIR) tc_mma_bf16_pair(d_tmem, a + i * a_step, b + i * b_step, p.idesc, (kb != k0 || i != 0) ? 1u : 0u);
+                            else tc_mma_bf16(d_tmem, a + i * a_step, b + i * b_step, p.idesc, (kb != k0 || i != 0) ? 1u : 0u);
+                        }
+                        if constexpr (PAIR) tc_commit_pair_both(bar_empty + 8u * s);
+                        else tc_commit(bar_empty + 8u * s);
+                        if (++s == S) { s = 0; phase ^= 1u; }
+                    }
+                    if (ok) {
+                        if constexpr (PAIR) tc_commit_pair_both(bar_accf + 8u * buf);
+                        else tc_commit(bar_accf + 8u * buf);
+                    }
+                }
+            }
+            if (*abort_flag) {                 // every MMA issued so far must retire before TMEM is freed
+                if constexpr (PAIR) tc_commit_pair(bar_drain);
+                else tc_commit(bar_drain);
+                (void)mbar_wait(bar_drain, 0u);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quad = warp & 3;                                 // the TMEM lanes this warp can read
+        const int tile_rows = 128 / p.rep;                         // distinct rows of this CTA's tile
+        const int r = (quad * 32 + lane) & (tile_rows - 1);        // the thread's row
+        const int part = (warp >> 2) * p.rep + (quad * 32) / tile_rows, parts = 2 * p.rep;
+        const int cols = Epi::kDual ? p.NT >> 1 : p.NT;            // columns of D in a tile
+        const int nch = (cols + 15) >> 4;
+        const int ch0 = part * nch / parts, ch1 = (part + 1) * nch / parts;   // runs of 16 columns this thread takes
+        int n = 0;
+        for (int item = cluster; item < p.n_items; item += n_clusters) {
+            const GemmItem it = gemm_item(p, item);
+            const GemmProblem& q = p.prob[it.prob];
+            const int m = it.mt * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + r;
+            typename Epi::State st;
+            if constexpr (Epi::kStateful) Epi::begin(st, ep, m);
+            for (int t = 0; t < it.n_tiles; ++t, ++n) {
+                const int buf = n & 1;
+                bool got = false;
+                if (!__any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // warp-uniform: tcgen05.ld needs the whole warp
+                    got = __all_sync(0xFFFFFFFFu, mbar_wait(bar_accf + 8u * buf, (uint32_t)(n >> 1) & 1u));
+                    if (!got) fail();
+                }
+                if (!got) continue;
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)buf * p.acc_cols;
+                const int col0 = (it.nt0 + t) * cols;
+                if (p.splits > 1) {
+                    // partial sums to shared memory (the ring is idle: its last k-block has been multiplied)
+                    float* part_row = reinterpret_cast<float*>(smem) + (size_t)r * (p.NT + 4);
+                    for (int ch = part * (p.NT >> 4) / parts; ch < (part + 1) * (p.NT >> 4) / parts; ++ch) {
+                        uint32_t u[16];
+                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<uint4*>(part_row + ch * 16 + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                    }
+                } else if constexpr (Epi::kStateful) {
+                    for (int ch = ch0; ch < ch1; ++ch) {
+                        uint32_t u[16];
+                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
+                        tc_wait_ld();
+                        const int live = q.N - (col0 + ch * 16);
+                        float x[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(u[e]);
+                        if (live > 0) Epi::cols16(st, ep, m, col0 + ch * 16, live, x);
+                    }
+                } else {
+                    if (m < q.M) Epi::row(st, ep, q, m);
+                    for (int ch = ch0; ch < ch1; ++ch) {
+                        const int c = col0 + ch * 16;
+                        uint32_t u[16], w[16];
+                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
+                        if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + ch * 16), w);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 16; e += 8) {
+                            if (m >= q.M || ch * 16 + e >= cols || c + e >= q.N) continue;
+                            float x[8], y[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                x[i] = __uint_as_float(u[e + i]);
+                                if constexpr (Epi::kDual) y[i] = __uint_as_float(w[e + i]);
+                            }
+                            if constexpr (Epi::kDual) Epi::cols8(st, ep, q, m, c + e, x, y);
+                            else Epi::cols8(st, ep, q, m, c + e, x);
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {                                   // the MMAs of the tile after next may start
+                    if constexpr (PAIR) mbar_arrive_cluster(cluster_map_shared(bar_acce + 8u * buf, 0u));
+                    else mbar_arrive(bar_acce + 8u * buf);
+                }
+            }
+            if constexpr (Epi::kStateful) Epi::end(st, ep, m, it.nt0 / p.tiles_per_item * parts + part);
+        }
+    }
+
+    if constexpr (!PAIR && !Epi::kStateful) {
+        if (p.splits > 1) {
+            cluster_sync_all();                                    // every CTA's partial sums are in its shared memory
+            if (warp < kGemmEpiWarps && !*abort_flag) {
+                const GemmItem it = gemm_item(p, cluster);
+                const GemmProblem& q = p.prob[it.prob];
+                const int cols = Epi::kDual ? p.NT >> 1 : p.NT;
+                const int tile_rows = 128 / p.rep;
+                const int rows = min(tile_rows, q.M - it.mt * 128);
+                const int g0 = (int)rank * (cols >> 3) / p.splits, g1 = ((int)rank + 1) * (cols >> 3) / p.splits;   // runs of 8 columns
+                const uint32_t pitch = (uint32_t)(p.NT + 4) * 4u;
+                for (int e = tid; e < rows * (g1 - g0); e += kGemmEpiWarps * 32) {
+                    const int g = e / rows, r = e - g * rows, c = (g0 + g) * 8;
+                    const int col = it.nt0 * cols + c, m = it.mt * 128 + r;
+                    if (col >= q.N) continue;
+                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    const uint32_t at = base + (uint32_t)r * pitch + (uint32_t)c * 4u;
+                    for (int s = 0; s < p.splits; ++s) {
+                        const uint32_t from = cluster_map_shared(at, (uint32_t)s);
+                        const float4 v0 = ld_cluster_f4(from), v1 = ld_cluster_f4(from + 16u);
+                        x[0] += v0.x; x[1] += v0.y; x[2] += v0.z; x[3] += v0.w;
+                        x[4] += v1.x; x[5] += v1.y; x[6] += v1.z; x[7] += v1.w;
+                        if constexpr (Epi::kDual) {
+                            const float4 w0 = ld_cluster_f4(from + (uint32_t)cols * 4u), w1 = ld_cluster_f4(from + (uint32_t)cols * 4u + 16u);
+                            y[0] += w0.x; y[1] += w0.y; y[2] += w0.z; y[3] += w0.w;
+                            y[4] += w1.x; y[5] += w1.y; y[6] += w1.z; y[7] += w1.w;
+                        }
+                    }
+                    typename Epi::State st;
+                    Epi::row(st, ep, q, m);
+                    if constexpr (Epi::kDual) Epi::cols8(st, ep, q, m, col, x, y);
+                    else Epi::cols8(st, ep, q, m, col, x);
+                }
+            }
+            cluster_sync_all();                                    // nobody leaves while its partial sums may be read
+        }
+    }
+
+    tc_fence_before();
+    if constexpr (PAIR) cluster_sync_all();      // neither CTA leaves while the other's MMAs or arrivals may still reach it
+    else __syncthreads();
+    tc_fence_after();
+    if (warp == kIssuer) {
+        if constexpr (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(p.tmem_cols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(p.tmem_cols) : "memory");
+    }
+}
+
+// Launches the kernel for a finished plan (`pair` as the plan chose).
+template <bool A_MN, bool B_MN, class Epi>
+inline vt_status gemm_launch(const GemmMaps& maps, const GemmParams& p, bool pair, const typename Epi::Params& ep, cudaStream_t st) {
+    static std::atomic<unsigned long long> configured_pair{0}, configured_single{0};
+    auto* kernel = pair ? gemm_kernel<true, A_MN, B_MN, Epi> : gemm_kernel<false, A_MN, B_MN, Epi>;
+    if (vt_status rc = ensure_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxDynSmem, pair ? &configured_pair : &configured_single);
+        rc != VT_OK)
+        return rc;
+    int sms = 0;
+    if (vt_status rc = device_sm_count(&sms); rc != VT_OK) return rc;
+    const int cluster = pair ? 2 : p.splits;
+    const int grid = pair ? 2 * std::max(1, std::min(sms / 2, p.n_items)) : p.splits > 1 ? p.n_items * p.splits : std::min(sms, p.n_items);
+    cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, cluster, grid, kGemmThreads, p.total_smem, st, maps, p, ep)
+                                : launch_pdl(kernel, grid, kGemmThreads, p.total_smem, st, maps, p, ep);
+    count_launch();
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? VT_OK : cuda_fail(e);
+}
+
+#endif  // __CUDACC__
+
+// ------------------------------------------------------------------------------------------ host
+inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
+
+// Chooses tile shape, CTA pairs and k-splits for the products in p->prob (M, N, nk0, nk1 set) and fills in the rest of p
+// except the maps' indices, outputs and hdr.  False when the work is too large to number its tiles.
+bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair);
+// The same for token scoring: one product, both operands K-major, whole k range in every CTA, `tiles_per_item` tiles in a row.
+bool gemm_plan_rows(GemmParams* p, bool* pair);
+// Rows of the box each operand's tensor map has (64 columns wide; MN-major operands: 64).
+int gemm_box_a(const GemmParams& p, bool a_mn);
+int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);
+
+// One or more products whose sums are rounded once to bf16 and stored (p->prob[i].out), operands of the given majors.
+vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, cudaStream_t st);
+
+// A bf16 matrix operand in global memory: rows x cols, rows ld elements apart.
+struct GemmOperand {
+    const void* ptr;
+    int rows, cols;
+    int64_t ld;
+};
+inline vt_status gemm_map(CUtensorMap* map, const GemmOperand& o, int box_rows) {
+    return make_tensor_map_bf16_ld(map, o.ptr, o.rows, o.cols, o.ld, box_rows);
+}
+
+}  // namespace vt

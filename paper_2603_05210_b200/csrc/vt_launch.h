@@ -52,9 +52,10 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), int grid, int block, siz
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
-// The same as clusters of two CTAs (the grid must be even).
+// The same as clusters of `cluster` CTAs (the grid must be a multiple of it).
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_pdl_cluster2(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
+inline cudaError_t launch_pdl_cluster(void (*kernel)(KArgs...), int cluster, int grid, int block, size_t smem, cudaStream_t st,
+                                      Args&&... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3((unsigned)block);
@@ -64,12 +65,16 @@ inline cudaError_t launch_pdl_cluster2(void (*kernel)(KArgs...), int grid, int b
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_pdl_cluster2(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
+    return launch_pdl_cluster(kernel, 2, grid, block, smem, st, std::forward<Args>(args)...);
 }
 
 bool gemv_supports(int d);
