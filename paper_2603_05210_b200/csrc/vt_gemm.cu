@@ -7,7 +7,11 @@ namespace vt {
 static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair) {
     p->a_bytes = 128u * 128u;
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
-    p->stage_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
+    p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
+    // A hand-over of a stage costs the issuing threads some 300 cycles, more than the MMAs of a k-block on a narrow tile: as
+    // many k-blocks per stage as leave three stages, at most four.
+    p->kbs = std::max(1, std::min(4, (int)(72 * 1024 / p->blk_bytes)));
+    p->stage_bytes = p->blk_bytes * (uint32_t)p->kbs;
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
     const size_t partial = p->splits > 1 ? (size_t)(128 / p->rep) * (p->NT + 4) * 4 : 0;
     p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128)) / p->stage_bytes));

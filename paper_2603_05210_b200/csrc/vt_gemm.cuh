@@ -61,8 +61,9 @@ struct GemmParams {
     int rep;                     // copies of A's rows in a tile: 1, 2 or 4 (single only)
     int splits;                  // CTAs that share one tile's k range (single only)
     int n_stages;
+    int kbs;                     // k-blocks per ring stage
     uint32_t a_bytes, b_bytes;   // bytes of one k-block of A (B) in shared memory
-    uint32_t stage_bytes;
+    uint32_t blk_bytes, stage_bytes;     // one k-block of both; kbs of them
     uint32_t idesc;
     uint32_t tmem_cols, acc_cols;    // allocation; columns between the two accumulators
     uint32_t bar_off;            // barriers, from the 1024-aligned base
@@ -96,6 +97,17 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr) {
     desc |= (uint64_t)1 << 46;
     desc |= (uint64_t)2 << 61;
     return desc;
+}
+
+// One lane of a converged warp (the same one every time).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// The bounded wait by a whole warp, with an answer the compiler knows to be the same in every lane.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity)) != 0;
 }
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
@@ -219,62 +231,92 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         k0 = p.splits > 1 ? (int)((long long)nk * (int)rank / p.splits) : 0;
         k1 = p.splits > 1 ? (int)((long long)nk * ((int)rank + 1) / p.splits) : nk;
     };
+    // Where every CTA reads the same rows of A, each starts its k range somewhere else and wraps around: in step, they would
+    // all ask for the same few lines of L2 at once.
+    auto k_start = [&](const GemmProblem& q, int k0, int k1) {
+        return !PAIR && q.tiles_m == 1 ? k0 + (int)((long long)(k1 - k0) * cluster / n_clusters) : k0;
+    };
 
     if (warp == kProducer) {
         // ------------------------------------------------------------------ TMA producer
-        if (lane == 0) {
+        // The whole warp runs the loop and one elected lane issues: with uniform control flow the copies' operands are formed
+        // in uniform registers.  Everything the loop needs is read from the parameters ahead of it.
+        {
             int s = 0, issued = 0;
-            uint32_t wrap = 0;
+            uint32_t wrap = 0, dst = base, bar_f = bar_full, bar_e = bar_empty;
             bool ok = true;
-            const uint32_t tx = (p.a_bytes + p.b_bytes) * (PAIR ? 2u : 1u);
-            const int a_box = 128 / p.rep;
-            for (int item = cluster; item < p.n_items && ok; item += n_clusters) {
+            const int kbs = p.kbs;
+            const uint32_t stage_bytes = p.stage_bytes, blk_bytes = p.blk_bytes, a_bytes = p.a_bytes, b_bytes = p.b_bytes;
+            const uint32_t tx = (a_bytes + b_bytes) * (PAIR ? 2u : 1u);
+            const int n_items = p.n_items, NT = p.NT, half = NT >> 1, rep = p.rep;
+            const bool dual = p.dual != 0, two_b = !PAIR && !B_MN && dual;
+            const uint32_t a_box = a_bytes / (uint32_t)rep;
+            const uint32_t bar_shift = PAIR ? cluster_map_shared(base, 0u) - base : 0u;    // both CTAs' bytes count on the leader's barrier
+            for (int item = cluster; item < n_items && ok; item += n_clusters) {
                 const GemmItem it = gemm_item(p, item);
                 const GemmProblem& q = p.prob[it.prob];
                 const int row0 = it.mt * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
+                const CUtensorMap *ma0 = &maps.map[q.a0], *ma1 = &maps.map[q.a1], *mb0 = &maps.map[q.b0], *mb1 = &maps.map[q.b1];
+                if (PAIR && dual && rank) mb0 = mb1;            // the halves of a pair's tile come from one matrix each
+                const int nk0 = q.nk0;
                 int k0, k1;
                 k_range(q, k0, k1);
+                const int kb_first = k_start(q, k0, k1);
                 for (int t = 0; t < it.n_tiles && ok; ++t) {
                     const int nt = it.nt0 + t;
-                    const int half = p.NT >> 1;
-                    // first row of B this CTA fetches, and the map of a pair's CTA where the halves differ
-                    const int col0 = p.dual ? nt * half : nt * p.NT + (PAIR ? (int)rank * half : 0);
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (wrap > 0 && !mbar_wait(bar_empty + 8u * s, (wrap - 1) & 1u)) { fail(); ok = false; break; }
-                        if (*abort_flag) { ok = false; break; }
-                        const bool second = kb >= q.nk0;
-                        const int x = (second ? kb - q.nk0 : kb) * kBoxK;
-                        const CUtensorMap* ma = &maps.map[second ? q.a1 : q.a0];
-                        const CUtensorMap* mb = &maps.map[PAIR && p.dual ? (rank ? q.b1 : q.b0) : second ? q.b1 : q.b0];
-                        const uint32_t dst = base + (uint32_t)s * p.stage_bytes;
-                        uint32_t bar = bar_full + 8u * s;
-                        if (leader) mbar_arrive_expect_tx(bar, tx);
-                        if constexpr (PAIR) bar = cluster_map_shared(bar, 0u);     // both CTAs' bytes count on the leader's barrier
-                        auto load = [&](uint32_t to, const CUtensorMap* m, int cx, int cy) {
-                            if constexpr (PAIR) tma_load_2d_pair(to, m, cx, cy, bar);
-                            else tma_load_2d(to, m, cx, cy, bar);
-                        };
-                        if constexpr (A_MN) {
-                            load(dst, ma, row0, x);
-                            load(dst + 8192u, ma, row0 + 64, x);
-                        } else {
-                            for (int r = 0; r < p.rep; ++r) load(dst + (uint32_t)(r * a_box) * 128u, ma, x, row0);
+                    const int col0 = dual ? nt * half : nt * NT + (PAIR ? (int)rank * half : 0);   // first row of B this CTA fetches
+                    int kb = kb_first;
+                    for (int i = k0; i < k1; i += kbs) {
+                        if (wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u)) { fail(); ok = false; break; }
+                        const int nb = min(kbs, k1 - i);
+                        if (elect_one()) {
+                            if (leader) mbar_arrive_expect_tx(bar_f, tx * (uint32_t)nb);
+                            const uint32_t bar = bar_f + bar_shift;
+                            auto load = [&](uint32_t to, const CUtensorMap* m, int cx, int cy) {
+                                if constexpr (PAIR) tma_load_2d_pair(to, m, cx, cy, bar);
+                                else tma_load_2d(to, m, cx, cy, bar);
+                            };
+                            uint32_t dsta = dst;
+                            int kj = kb;
+                            for (int j = 0; j < nb; ++j, dsta += blk_bytes) {
+                                const bool second = kj >= nk0;
+                                const int x = (second ? kj - nk0 : kj) * kBoxK;
+                                const CUtensorMap *ma = second ? ma1 : ma0, *mb = second ? mb1 : mb0;
+                                const uint32_t dstb = dsta + a_bytes;
+                                if constexpr (B_MN) {
+                                    for (uint32_t o = 0; o < b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
+                                } else {
+                                    load(dstb, mb, x, col0);
+                                    if (two_b) load(dstb + (uint32_t)half * 128u, mb1, x, col0);
+                                }
+                                if constexpr (A_MN) {
+                                    load(dsta, ma, row0, x);
+                                    load(dsta + 8192u, ma, row0 + 64, x);
+                                } else {
+                                    for (int r = 0; r < rep; ++r) load(dsta + (uint32_t)r * a_box, ma, x, row0);
+                                }
+                                if (++kj == k1) kj = k0;
+                            }
                         }
-                        const uint32_t dstb = dst + p.a_bytes;
-                        if constexpr (B_MN) {
-                            for (uint32_t o = 0; o < p.b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
-                        } else if (!PAIR && p.dual) {
-                            load(dstb, mb, x, col0);
-                            load(dstb + (uint32_t)half * 128u, &maps.map[q.b1], x, col0);
-                        } else {
-                            load(dstb, mb, x, col0);
-                        }
+                        __syncwarp();
                         ++issued;
-                        if (++s == S) { s = 0; ++wrap; }
+                        kb += nb;
+                        if (kb >= k1) kb -= k1 - k0;
+                        dst += stage_bytes;
+                        bar_f += 8u;
+                        bar_e += 8u;
+                        if (++s == S) {
+                            s = 0;
+                            ++wrap;
+                            dst = base;
+                            bar_f = bar_full;
+                            bar_e = bar_empty;
+                            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) { ok = false; break; }
+                        }
                     }
                 }
             }
-            if (*abort_flag && leader) {       // let copies in flight land before the CTA gives its shared memory back
+            if (lane == 0 && leader && *abort_flag) {       // let copies in flight land before the CTA gives its shared memory back
                 const unsigned long long deadline = global_timer_ns() + kWaitLimitNs;
                 for (int i = max(0, issued - S); i < issued; ++i)
                     (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, deadline);
@@ -282,45 +324,69 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         }
     } else if (warp == kIssuer) {
         // ------------------------------------------------------------------ MMA issuer (of a pair: the leader's)
-        if (lane == 0 && leader) {
+        if (leader) {
             int s = 0, n = 0;                  // ring stage; tiles so far
             uint32_t phase = 0;
             bool ok = true;
             const uint64_t a_desc0 = A_MN ? smem_desc_sw128_mn(base) : smem_desc_sw128(base);
             const uint64_t b_desc0 = B_MN ? smem_desc_sw128_mn(base + p.a_bytes) : smem_desc_sw128(base + p.a_bytes);
             constexpr uint32_t a_step = A_MN ? 128u : 2u, b_step = B_MN ? 128u : 2u;   // 16 of k: two 8-row groups, or 32 bytes of a row
-            const uint32_t stage_units = p.stage_bytes >> 4;
-            for (int item = cluster; item < p.n_items && ok; item += n_clusters) {
+            const int kbs = p.kbs;
+            const uint32_t stage_units = p.stage_bytes >> 4, blk_units = p.blk_bytes >> 4, idesc = p.idesc, acc_cols = p.acc_cols;
+            const int n_items = p.n_items;
+            uint64_t a = a_desc0, b = b_desc0;
+            uint32_t bar_f = bar_full, bar_e = bar_empty;
+            for (int item = cluster; item < n_items && ok; item += n_clusters) {
                 const GemmItem it = gemm_item(p, item);
                 int k0, k1;
                 k_range(p.prob[it.prob], k0, k1);
                 for (int t = 0; t < it.n_tiles && ok; ++t, ++n) {
                     const int buf = n & 1;
-                    if (n >= 2 && !mbar_wait(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u)) { fail(); ok = false; break; }
+                    if (n >= 2 && !mbar_wait_warp(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u)) { fail(); ok = false; break; }
+                    if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d_tmem = tmem_base + (uint32_t)buf * p.acc_cols;
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (!mbar_wait(bar_full + 8u * s, phase)) { fail(); ok = false; break; }
-                        if (*abort_flag) { ok = false; break; }
+                    const uint32_t d_tmem = tmem_base + (uint32_t)buf * acc_cols;
+                    uint32_t accumulate = 0u;
+                    for (int kb = k0; kb < k1; kb += kbs) {
+                        if (!mbar_wait_warp(bar_f, phase)) { fail(); ok = false; break; }
                         tc_fence_after();
-                        const uint64_t a = a_desc0 + (uint64_t)((uint32_t)s * stage_units);
-                        const uint64_t b = b_desc0 + (uint64_t)((uint32_t)s * stage_units);
+                        const int nb = min(kbs, k1 - kb);
+                        if (elect_one()) {
+                            uint64_t aj = a, bj = b;
+                            for (int j = 0; j < nb; ++j, aj += blk_units, bj += blk_units) {
 #pragma unroll
-                        for (uint32_t i = 0; i < 4; ++i) {
-                            if constexpr (PAIR) tc_mma_bf16_pair(d_tmem, a + i * a_step, b + i * b_step, p.idesc, (kb != k0 || i != 0) ? 1u : 0u);
-                            else tc_mma_bf16(d_tmem, a + i * a_step, b + i * b_step, p.idesc, (kb != k0 || i != 0) ? 1u : 0u);
+                                for (uint32_t i = 0; i < 4; ++i) {
+                                    const uint32_t acc = i == 0 && j == 0 ? accumulate : 1u;
+                                    if constexpr (PAIR) tc_mma_bf16_pair(d_tmem, aj + i * a_step, bj + i * b_step, idesc, acc);
+                                    else tc_mma_bf16(d_tmem, aj + i * a_step, bj + i * b_step, idesc, acc);
+                                }
+                            }
+                            if constexpr (PAIR) tc_commit_pair_both(bar_e);
+                            else tc_commit(bar_e);
                         }
-                        if constexpr (PAIR) tc_commit_pair_both(bar_empty + 8u * s);
-                        else tc_commit(bar_empty + 8u * s);
-                        if (++s == S) { s = 0; phase ^= 1u; }
+                        __syncwarp();
+                        accumulate = 1u;
+                        a += stage_units;
+                        b += stage_units;
+                        bar_f += 8u;
+                        bar_e += 8u;
+                        if (++s == S) {
+                            s = 0;
+                            phase ^= 1u;
+                            a = a_desc0;
+                            b = b_desc0;
+                            bar_f = bar_full;
+                            bar_e = bar_empty;
+                        }
                     }
-                    if (ok) {
+                    if (ok && elect_one()) {
                         if constexpr (PAIR) tc_commit_pair_both(bar_accf + 8u * buf);
                         else tc_commit(bar_accf + 8u * buf);
                     }
+                    __syncwarp();
                 }
             }
-            if (*abort_flag) {                 // every MMA issued so far must retire before TMEM is freed
+            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0) && elect_one()) {   // every MMA issued so far must retire before TMEM is freed
                 if constexpr (PAIR) tc_commit_pair(bar_drain);
                 else tc_commit(bar_drain);
                 (void)mbar_wait(bar_drain, 0u);
