@@ -1,22 +1,32 @@
 // Plans of the matrix products in vt_gemm.cuh, and the products that are stored as they are.
+#include <cmath>
+#include <cstring>
+
 #include "vt_gemm.cuh"
 
 namespace vt {
 
 // Shared memory of a plan whose tile shape is chosen; false if it does not fit.
 static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair) {
-    p->a_bytes = 128u * 128u;
+    int max_m = 0;
+    for (int i = 0; i < p->n_prob; ++i) max_m = std::max(max_m, p->prob[i].M);
+    const int tile_rows = 128 / p->rep;
+    p->a_rows = (uint32_t)(a_mn ? 128 : std::min(tile_rows, (int)round_up(max_m, 8)));
+    p->a_bytes = p->rep > 1 ? 16384u : p->a_rows * 128u;
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
+    p->tx_bytes = p->a_rows * 128u * (uint32_t)p->rep + p->b_bytes;
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
     // A hand-over of a stage costs the issuing threads some 300 cycles, more than the MMAs of a k-block on a narrow tile: as
     // many k-blocks per stage as leave three stages, at most four.
     p->kbs = std::max(1, std::min(4, (int)(72 * 1024 / p->blk_bytes)));
     p->stage_bytes = p->blk_bytes * (uint32_t)p->kbs;
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
-    const size_t partial = p->splits > 1 ? (size_t)(128 / p->rep) * (p->NT + 4) * 4 : 0;
-    p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128)) / p->stage_bytes));
+    const size_t partial = p->splits > 1 ? (size_t)std::min(tile_rows, max_m) * (p->NT + 4) * 4 : 0;
+    // an MMA reads 128 rows of A wherever they end
+    const size_t over = 16384 - p->a_bytes;
+    p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - over) / p->stage_bytes));
     if (p->n_stages < 2) return false;
-    p->bar_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes, partial), 128);
+    p->bar_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes + over, partial), 128);
     p->total_smem = (uint32_t)(p->bar_off + bar_bytes + 1024);
     // D fp32, A and B bf16, M = 128 (a pair: 256), N; bits 15 and 16: A, B MN-major
     p->idesc = (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
@@ -43,10 +53,105 @@ static bool gemm_number_items(GemmParams* p, bool pair) {
     return true;
 }
 
-// Time of a plan in SM cycles, to compare plans with: per 64-deep k-block the tensor core takes 2 cycles per accumulator
-// column (128 rows; a pair the same), at least 130, and the operands come in at about 55 bytes a cycle; weights from HBM
-// at 24 bytes a cycle and SM when all of them stream.  Each tile adds its read-out, each launch its fill.
+// Plans by shape, the last few of each thread: a plan weighs a hundred and more alternatives, which takes longer than the
+// launch it is for.
+struct PlanCache {
+    struct Key {
+        int n[3][4], n_prob, kind;
+        bool operator==(const Key& o) const { return memcmp(this, &o, sizeof(Key)) == 0; }
+    };
+    struct Entry {
+        Key key;
+        GemmParams plan;
+        bool pair, used;
+    };
+    static constexpr int kEntries = 32;
+    Entry e[kEntries];
+    int next;
+
+    static Key key_of(const GemmParams& p, int kind) {
+        Key k;
+        memset(&k, 0, sizeof(k));
+        k.n_prob = p.n_prob;
+        k.kind = kind;
+        for (int i = 0; i < p.n_prob; ++i) {
+            k.n[i][0] = p.prob[i].M;
+            k.n[i][1] = p.prob[i].N;
+            k.n[i][2] = p.prob[i].nk0;
+            k.n[i][3] = p.prob[i].nk1;
+        }
+        return k;
+    }
+    // what a plan does not decide stays the caller's
+    static void take(const GemmParams& plan, GemmParams* p) {
+        GemmParams r = plan;
+        r.hdr = p->hdr;
+        for (int i = 0; i < p->n_prob; ++i) {
+            r.prob[i].a0 = p->prob[i].a0;
+            r.prob[i].b0 = p->prob[i].b0;
+            r.prob[i].a1 = p->prob[i].a1;
+            r.prob[i].b1 = p->prob[i].b1;
+            r.prob[i].out = p->prob[i].out;
+        }
+        *p = r;
+    }
+    bool find(const Key& k, GemmParams* p, bool* pair) const {
+        for (const Entry& x : e)
+            if (x.used && x.key == k) {
+                take(x.plan, p);
+                *pair = x.pair;
+                return true;
+            }
+        return false;
+    }
+    void keep(const Key& k, const GemmParams& p, bool pair) {
+        e[next] = Entry{k, p, pair, true};
+        next = (next + 1) % kEntries;
+    }
+};
+static thread_local PlanCache g_plans{};
+
+// Clusters of `size` single-CTA tiles that the device holds at once (the SMs of a cluster lie in one GPC, so large
+// clusters leave SMs over).  Without a device: what a B200 measured.
+static int cluster_slots(int size) {
+    static std::atomic<int> cached[9];
+    static const int kUsual[9] = {0, 148, 74, 44, 35, 28, 22, 16, 14};
+    int n = cached[size].load(std::memory_order_relaxed);
+    if (n == 0) {
+        n = kUsual[size];
+        if (size > 1) {
+            static std::atomic<unsigned long long> configured{0};
+            auto* kernel = gemm_kernel<false, false, false, EpiStore>;
+            int sms = 0, found = 0;
+            if (device_sm_count(&sms) == VT_OK &&
+                ensure_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxDynSmem, &configured) == VT_OK) {
+                cudaLaunchConfig_t cfg{};
+                cfg.gridDim = dim3((unsigned)(sms / size * size));
+                cfg.blockDim = dim3((unsigned)kGemmThreads);
+                cfg.dynamicSmemBytes = kMaxDynSmem;
+                cudaLaunchAttribute attr[1];
+                attr[0].id = cudaLaunchAttributeClusterDimension;
+                attr[0].val.clusterDim.x = (unsigned)size;
+                attr[0].val.clusterDim.y = 1;
+                attr[0].val.clusterDim.z = 1;
+                cfg.attrs = attr;
+                cfg.numAttrs = 1;
+                if (cudaOccupancyMaxActiveClusters(&found, kernel, &cfg) == cudaSuccess && found > 0) n = found;
+            }
+            (void)cudaGetLastError();
+        }
+        cached[size].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+// Time of a plan in SM cycles, to compare plans with.  Per 64-deep k-block: the tensor core takes 2 cycles per accumulator
+// column (128 rows; a pair the same); the issuing threads take some 120 for the MMAs and copies and share 300 per stage; the
+// operands come in at about 55 bytes a cycle from L2, and weights from HBM at 24 bytes a cycle and SM when all of them
+// stream.  Each round of tiles adds its fill, the last its read-out, and splits the exchange of their partial sums.
 bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
+    const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0));
+    if (g_plans.find(key, p, pair_out)) return true;
     int maxM = 0, max_nk = 0;
     for (int i = 0; i < p->n_prob; ++i) {
         maxM = std::max(maxM, p->prob[i].M);
@@ -57,7 +162,6 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
     double best = -1;
     int best_nt = 0, best_splits = 1;
     bool best_pair = false;
-    const int one_rep = a_mn ? 1 : maxM <= 32 ? 4 : maxM <= 64 ? 2 : 1;
     for (int pair = 0; pair < 2; ++pair) {
         if (pair && maxM <= 128) continue;
         const int step = b_mn ? (pair ? 128 : 64) : pair ? 32 : 16;
@@ -66,15 +170,18 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
             long long tiles = 0;
             for (int i = 0; i < p->n_prob; ++i)
                 tiles += (long long)ceil_div(p->prob[i].M, pair ? 256 : 128) * ceil_div(p->prob[i].N, cols);
+            const double a_rows = std::min(128, maxM);
+            const double blk = (a_rows + (pair ? nt / 2 : nt)) * 128.0;
+            const double per_stage = std::max(1.0, std::min(4.0, floor(72.0 * 1024 / blk)));
+            const double issue = std::max(2.0 * nt, 120.0 + 300.0 / per_stage);
             for (int s = 1; s <= (pair ? 1 : std::min(8, max_nk)); ++s) {
-                const double in_bytes = (128.0 + (pair ? nt / 2 : nt)) * 128.0;
-                double per_kb = std::max(std::max(2.0 * nt, 130.0), in_bytes / 55.0);
-                const long long slots = pair ? kGemmSms / 2 : kGemmSms;
-                const double waves = (double)((tiles * s + slots - 1) / slots);
-                const double share = std::min(1.0, (double)(tiles * s) / (double)slots);
-                per_kb = std::max(per_kb, nt * 128.0 * (pair ? 0.5 : 1.0) / 24.0 * (maxM <= 256 ? share : 0.0));
+                const long long slots = pair ? kGemmSms / 2 : cluster_slots(s);
+                const double rounds = (double)((tiles + slots - 1) / slots);
+                const double busy = std::min(1.0, (double)tiles / (double)slots);
+                double per_kb = std::max(issue, blk / 55.0);
+                per_kb = std::max(per_kb, nt * 128.0 * (pair ? 0.5 : 1.0) / 24.0 * (maxM <= 256 ? busy : 0.0));
                 const double tail = 1500.0 + 12.0 * cols + (s > 1 ? 2500.0 + 4.0 * nt : 0.0);
-                const double cost = waves * (ceil_div(max_nk, s) * per_kb + 300.0) + tail;
+                const double cost = rounds * (ceil_div(max_nk, s) * per_kb + (s > 1 ? 4000.0 : 1200.0)) + tail;
                 if (best < 0 || cost < best) {
                     best = cost;
                     best_nt = nt;
@@ -86,15 +193,19 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
     }
     p->NT = best_nt;
     p->splits = best_splits;
-    p->rep = best_pair ? 1 : one_rep;
+    p->rep = 1;
     *pair_out = best_pair;
-    return gemm_number_items(p, best_pair) && gemm_layout(p, a_mn, b_mn, best_pair);
+    if (!gemm_number_items(p, best_pair) || !gemm_layout(p, a_mn, b_mn, best_pair)) return false;
+    g_plans.keep(key, *p, best_pair);
+    return true;
 }
 
 // Scoring: every row needs all columns, so nothing but the tile width and the number of tiles a CTA takes in a row is
 // free.  Chosen for the fewest rounds of equal work over the SMs (a round costs its columns plus about 24 columns' worth
 // of hand-over); among equals the longer runs, which leave fewer records to merge.
 bool gemm_plan_rows(GemmParams* p, bool* pair_out) {
+    const PlanCache::Key key = PlanCache::key_of(*p, 8);
+    if (g_plans.find(key, p, pair_out)) return true;
     const GemmProblem& q = p->prob[0];
     const bool pair = q.M > 128;
     const int slots = pair ? kGemmSms / 2 : kGemmSms, step = pair ? 32 : 16;
@@ -119,11 +230,13 @@ bool gemm_plan_rows(GemmParams* p, bool* pair_out) {
     p->tiles_per_item = best_c;
     p->splits = 1;
     p->rep = pair ? 1 : q.M <= 32 ? 4 : q.M <= 64 ? 2 : 1;
+    while (p->rep > 1 && 2 * p->rep > p->NT / 16) p->rep /= 2;      // a copy without columns of its own is no use
     *pair_out = pair;
-    return gemm_number_items(p, pair) && gemm_layout(p, false, false, pair);
+    if (!gemm_number_items(p, pair) || !gemm_layout(p, false, false, pair)) return false;
+    g_plans.keep(key, *p, pair);
+    return true;
 }
 
-int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : 128 / p.rep; }
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair) { return b_mn ? 64 : (pair || p.dual) ? p.NT / 2 : p.NT; }
 
 vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, cudaStream_t st) {

@@ -13,9 +13,10 @@
 //   PAIR    clusters of two CTAs share each MMA (cta_group::2): 256 rows x NT <= 256 columns, either CTA fetches its
 //           128 rows of A and half the columns of B.  For more than 128 rows: a CTA then moves 32 KB per 64-deep k-block
 //           of 2 * 128 * 256 * 64 FLOP, half of what two separate 128 x 128 tiles would.
-//   single  128 rows x NT <= 256 columns.  With at most 64 (32) rows of A the tile holds them two (four) times, one copy
-//           per group of TMEM lanes: the tensor core has the time, and every epilogue warp then finds rows to work on,
-//           each copy taking its own share of the columns.
+//   single  128 rows x NT <= 256 columns.  Few rows of A are fetched as a box of their own height; the MMA's other rows
+//           compute on whatever shared memory holds and land in lanes nobody reads.  For an epilogue with work to do per
+//           column (scoring) the tile can hold at most 64 (32) rows of A two (four) times, one copy per group of TMEM
+//           lanes: every epilogue warp then finds rows, each copy taking its own share of the columns.
 //   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile, lays its partial sums out in
 //           shared memory, and each CTA adds up and finishes its share of the columns through distributed shared
 //           memory, in the order of the CTAs: no atomics, the same bits every time.
@@ -62,7 +63,9 @@ struct GemmParams {
     int splits;                  // CTAs that share one tile's k range (single only)
     int n_stages;
     int kbs;                     // k-blocks per ring stage
+    uint32_t a_rows;             // rows of A's box (K-major); `rep` of them, 128 / rep rows apart
     uint32_t a_bytes, b_bytes;   // bytes of one k-block of A (B) in shared memory
+    uint32_t tx_bytes;           // bytes a CTA's copies of one k-block deliver
     uint32_t blk_bytes, stage_bytes;     // one k-block of both; kbs of them
     uint32_t idesc;
     uint32_t tmem_cols, acc_cols;    // allocation; columns between the two accumulators
@@ -247,10 +250,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             bool ok = true;
             const int kbs = p.kbs;
             const uint32_t stage_bytes = p.stage_bytes, blk_bytes = p.blk_bytes, a_bytes = p.a_bytes, b_bytes = p.b_bytes;
-            const uint32_t tx = (a_bytes + b_bytes) * (PAIR ? 2u : 1u);
+            const uint32_t tx = p.tx_bytes * (PAIR ? 2u : 1u);
             const int n_items = p.n_items, NT = p.NT, half = NT >> 1, rep = p.rep;
             const bool dual = p.dual != 0, two_b = !PAIR && !B_MN && dual;
-            const uint32_t a_box = a_bytes / (uint32_t)rep;
+            const uint32_t a_box = 16384u / (uint32_t)rep;
             const uint32_t bar_shift = PAIR ? cluster_map_shared(base, 0u) - base : 0u;    // both CTAs' bytes count on the leader's barrier
             for (int item = cluster; item < n_items && ok; item += n_clusters) {
                 const GemmItem it = gemm_item(p, item);
@@ -555,7 +558,7 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair);
 // The same for token scoring: one product, both operands K-major, whole k range in every CTA, `tiles_per_item` tiles in a row.
 bool gemm_plan_rows(GemmParams* p, bool* pair);
 // Rows of the box each operand's tensor map has (64 columns wide; MN-major operands: 64).
-int gemm_box_a(const GemmParams& p, bool a_mn);
+inline int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : (int)p.a_rows; }
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);
 
 // One or more products whose sums are rounded once to bf16 and stored (p->prob[i].out), operands of the given majors.

@@ -102,14 +102,7 @@ struct EpiScore {
 // ------------------------------------------------------------------------------------------ the join of a row's records
 constexpr int kJoinThreads = 128;
 constexpr int kJoinCand = 1024;
-
-__device__ __forceinline__ float block_sum(float v, float* buf) {
-    v = warp_sum_f32(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return (buf[0] + buf[1]) + (buf[2] + buf[3]);
-}
+constexpr int kJoinHeld = 8;               // lists a thread keeps the best key of in registers
 
 struct ScoreJoin {
     ScoreRecords rec;
@@ -119,13 +112,15 @@ struct ScoreJoin {
     float scale;
 };
 
+// One block per row, bound by the latency of its few loads: all records of a thread's lists are requested together.
 __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoin p) {
-    __shared__ float buf[4];
+    __shared__ float3 parts[kJoinThreads / 32];
     __shared__ unsigned long long heads[kJoinThreads], cand[kJoinCand];
     __shared__ unsigned long long bound_s;
     __shared__ int n_cand;
-    grid_dependency_wait();
     const int m = blockIdx.x, t = threadIdx.x, L = p.rec.L, k = p.out.k;
+    if (t == 0) { n_cand = 0; bound_s = 1ull; }
+    grid_dependency_wait();
     const ScoreOut& o = p.out;
     if (!row_scored(p.tokens, p.V, m)) {
         if (t == 0) {
@@ -141,54 +136,88 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoi
     }
     const float4* stats = p.rec.stats + (size_t)m * L;
     const unsigned long long* keys = p.rec.keys + (size_t)m * L * k;
-    float mx = kMasked;
-    for (int l = t; l < L; l += kJoinThreads) mx = fmaxf(mx, stats[l].x);
-    mx = warp_max_f32(mx);
-    if ((t & 31) == 0) buf[t >> 5] = mx;
-    if (t == 0) { n_cand = 0; bound_s = 1ull; }
-    __syncthreads();
-    mx = fmaxf(fmaxf(buf[0], buf[1]), fmaxf(buf[2], buf[3]));
     const float c = p.scale * kLog2e;
-    float s = 0.0f, e = 0.0f;
-    for (int l = t; l < L; l += kJoinThreads) {
-        const float4 r = stats[l];
-        const float back = r.x - mx, f = ex2_approx(back * c);
-        s = fmaf(f, r.y, s);
-        e = fmaf(f, fmaf(back, r.y, r.z), e);
+    const float given = o.logprobs ? p.rec.given[m] : 0.0f;
+    float mx = kMasked, s = 0.0f, e = 0.0f;
+    unsigned long long held[kJoinHeld], head = 0ull;
+    auto fold = [&](float rmx, float rs, float re) {
+        const float nm = fmaxf(mx, rmx), b0 = mx - nm, b1 = rmx - nm;
+        const float f0 = ex2_approx(b0 * c), f1 = ex2_approx(b1 * c);
+        e = fmaf(f0, fmaf(b0, s, e), f1 * fmaf(b1, rs, re));
+        s = fmaf(f0, s, f1 * rs);
+        mx = nm;
+    };
+    {
+        float4 r[kJoinHeld];
+#pragma unroll
+        for (int i = 0; i < kJoinHeld; ++i) {
+            const int l = t + i * kJoinThreads;
+            r[i] = l < L ? stats[l] : make_float4(kMasked, 0.0f, 0.0f, 0.0f);
+            held[i] = l < L && k > 0 ? keys[(size_t)l * k] : 0ull;
+        }
+#pragma unroll
+        for (int i = 0; i < kJoinHeld; ++i) {
+            fold(r[i].x, r[i].y, r[i].z);
+            head = held[i] > head ? held[i] : head;
+        }
     }
-    s = block_sum(s, buf);
-    e = block_sum(e, buf);
+    for (int l = t + kJoinHeld * kJoinThreads; l < L; l += kJoinThreads) {
+        const float4 r = stats[l];
+        fold(r.x, r.y, r.z);
+        if (k > 0) {
+            const unsigned long long key = keys[(size_t)l * k];
+            head = key > head ? key : head;
+        }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float rmx = __shfl_xor_sync(0xFFFFFFFFu, mx, d), rs = __shfl_xor_sync(0xFFFFFFFFu, s, d), re = __shfl_xor_sync(0xFFFFFFFFu, e, d);
+        // both lanes of a pair must come to the same bits: the lower lane's part first
+        const bool low = (t & d) == 0;
+        const float amx = low ? mx : rmx, as = low ? s : rs, ae = low ? e : re;
+        const float bmx = low ? rmx : mx, bs = low ? rs : s, be = low ? re : e;
+        mx = amx;
+        s = as;
+        e = ae;
+        fold(bmx, bs, be);
+    }
+    if ((t & 31) == 0) parts[t >> 5] = make_float3(mx, s, e);
+    heads[t] = head;
+    __syncthreads();
+    mx = parts[0].x;
+    s = parts[0].y;
+    e = parts[0].z;
+#pragma unroll
+    for (int w = 1; w < kJoinThreads / 32; ++w) fold(parts[w].x, parts[w].y, parts[w].z);
     const float log_s = logf(s);
     if (t == 0) {
         if (o.lse) o.lse[m] = fmaf(p.scale, mx, log_s);
         if (o.entropy) o.entropy[m] = log_s - p.scale * (e / s);
-        if (o.logprobs) o.logprobs[m] = p.scale * (p.rec.given[m] - mx) - log_s;
+        if (o.logprobs) o.logprobs[m] = p.scale * (given - mx) - log_s;
     }
     if (k == 0) return;
 
     // The k best of L descending lists.  The k-th largest of the threads' best heads bounds the winners from below: k keys
     // at least that large exist.  The keys not below it are gathered, and a key's place is the number of keys above it.
-    unsigned long long head = 0ull;
-    for (int l = t; l < L; l += kJoinThreads) {
-        const unsigned long long key = keys[(size_t)l * k];
-        head = key > head ? key : head;
-    }
-    heads[t] = head;
-    __syncthreads();
     if (head != 0ull) {
         int above = 0;
+#pragma unroll 8
         for (int i = 0; i < kJoinThreads; ++i) above += heads[i] > head ? 1 : 0;
         if (above == k - 1) bound_s = head;
     }
     __syncthreads();
     const unsigned long long bound = bound_s;          // 1 (every key) when fewer than k threads have one
-    for (int l = t; l < L; l += kJoinThreads)
-        for (int j = 0; j < k; ++j) {
-            const unsigned long long key = keys[(size_t)l * k + j];
-            if (key < bound) break;
+    auto gather = [&](int l, unsigned long long key) {
+        for (int j = 0; key >= bound;) {
             const int at = atomicAdd(&n_cand, 1);      // the order of the candidates does not matter: their ranks decide
             if (at < kJoinCand) cand[at] = key;
+            if (++j == k) break;
+            key = keys[(size_t)l * k + j];
         }
+    };
+#pragma unroll
+    for (int i = 0; i < kJoinHeld; ++i) gather(t + i * kJoinThreads, held[i]);
+    for (int l = t + kJoinHeld * kJoinThreads; l < L; l += kJoinThreads) gather(l, keys[(size_t)l * k]);
     __syncthreads();
     const int n = n_cand;
     auto emit = [&](int j, unsigned long long key) {
@@ -200,6 +229,7 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoi
         for (int i = t; i < n; i += kJoinThreads) {
             const unsigned long long key = cand[i];
             int above = 0;
+#pragma unroll 4
             for (int q = 0; q < n; ++q) above += cand[q] > key ? 1 : 0;
             if (above < k) emit(above, key);
         }
