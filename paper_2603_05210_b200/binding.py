@@ -96,7 +96,8 @@ def _check(status: int, what: str):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the handle alone: building a Stream object around it takes longer than a launch's other host work together
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t):
@@ -395,10 +396,14 @@ def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | Non
     given token.  Pass tensors for outputs and workspace to have them reused."""
     h, W = _score_inputs(h, W, tokens)
     (M, d), V, dev = h.shape, W.shape[0], h.device
-    if tokens is not None:
-        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, dev)
-    elif logprobs is not None:
+    if tokens is None and logprobs is not None:
         raise ValueError("logprobs needs tokens")
+    if logprobs is None and entropy is None and lse is None:
+        logprobs, entropy, lse = torch.empty((3, M), dtype=torch.float32, device=dev).unbind(0)
+    if tokens is None:
+        logprobs = None
+    else:
+        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, dev)
     entropy = _out(entropy, "entropy", (M,), torch.float32, dev)
     lse = _out(lse, "lse", (M,), torch.float32, dev)
     if k > 0:

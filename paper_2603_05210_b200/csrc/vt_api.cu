@@ -425,11 +425,9 @@ vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32
     if (!aligned(tokens, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) || !aligned(lse, 4) ||
         (k > 0 && (!aligned(top_ids, 4) || !aligned(top_logprobs, 4))))
         return VT_ERR_ALIGN;
-    const size_t need = score_workspace_bytes(M, d, V, k);
-    if (need == 0) return VT_ERR_SHAPE;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return VT_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, 256)) return VT_ERR_WORKSPACE;
     const ScoreCall c{h, ldh, W, tokens, M, d, V, scale};
-    return launch_score(c, ScoreOut{logprobs, entropy, lse, top_ids, top_logprobs, k}, workspace, (cudaStream_t)stream);
+    return launch_score(c, ScoreOut{logprobs, entropy, lse, top_ids, top_logprobs, k}, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 size_t vt_score_backward_workspace_bytes(int M, int d, int V) {

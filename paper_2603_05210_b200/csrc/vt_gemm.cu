@@ -7,7 +7,7 @@
 namespace vt {
 
 // Shared memory of a plan whose tile shape is chosen; false if it does not fit.
-static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair) {
+static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t scratch_bytes = 0) {
     int max_m = 0;
     for (int i = 0; i < p->n_prob; ++i) max_m = std::max(max_m, p->prob[i].M);
     const int tile_rows = 128 / p->rep;
@@ -24,9 +24,10 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair) {
     const size_t partial = p->splits > 1 ? (size_t)std::min(tile_rows, max_m) * (p->NT + 4) * 4 : 0;
     // an MMA reads 128 rows of A wherever they end
     const size_t over = 16384 - p->a_bytes;
-    p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - over) / p->stage_bytes));
+    p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - scratch_bytes - over) / p->stage_bytes));
     if (p->n_stages < 2) return false;
-    p->bar_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes + over, partial), 128);
+    p->scratch_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes + over, partial), 128);
+    p->bar_off = p->scratch_off + scratch_bytes;
     p->total_smem = (uint32_t)(p->bar_off + bar_bytes + 1024);
     // D fp32, A and B bf16, M = 128 (a pair: 256), N; bits 15 and 16: A, B MN-major
     p->idesc = (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
@@ -203,8 +204,8 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
 // Scoring: every row needs all columns, so nothing but the tile width and the number of tiles a CTA takes in a row is
 // free.  Chosen for the fewest rounds of equal work over the SMs (a round costs its columns plus about 24 columns' worth
 // of hand-over); among equals the longer runs, which leave fewer records to merge.
-bool gemm_plan_rows(GemmParams* p, bool* pair_out) {
-    const PlanCache::Key key = PlanCache::key_of(*p, 8);
+bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair_out) {
+    const PlanCache::Key key = PlanCache::key_of(*p, 8 | (int)scratch_bytes << 4);
     if (g_plans.find(key, p, pair_out)) return true;
     const GemmProblem& q = p->prob[0];
     const bool pair = q.M > 128;
@@ -232,7 +233,7 @@ bool gemm_plan_rows(GemmParams* p, bool* pair_out) {
     p->rep = pair ? 1 : q.M <= 32 ? 4 : q.M <= 64 ? 2 : 1;
     while (p->rep > 1 && 2 * p->rep > p->NT / 16) p->rep /= 2;      // a copy without columns of its own is no use
     *pair_out = pair;
-    if (!gemm_number_items(p, pair) || !gemm_layout(p, false, false, pair)) return false;
+    if (!gemm_number_items(p, pair) || !gemm_layout(p, false, false, pair, scratch_bytes)) return false;
     g_plans.keep(key, *p, pair);
     return true;
 }

@@ -69,7 +69,8 @@ struct GemmParams {
     uint32_t blk_bytes, stage_bytes;     // one k-block of both; kbs of them
     uint32_t idesc;
     uint32_t tmem_cols, acc_cols;    // allocation; columns between the two accumulators
-    uint32_t bar_off;            // barriers, from the 1024-aligned base
+    uint32_t scratch_off;        // the epilogue's own shared memory (Epi::kScratch bytes), from the 1024-aligned base
+    uint32_t bar_off;            // barriers
     uint32_t total_smem;
     WsHeader* hdr;
 };
@@ -135,6 +136,22 @@ __device__ __forceinline__ GemmItem gemm_item(const GemmParams& p, int item) {
     return it;
 }
 
+// A thread's share of a finished tile: runs [ch0, ch1) of 16 accumulator columns of its row.
+struct AccColumns {
+    uint32_t taddr;              // tensor-memory address of the row group's column 0
+    int ch0, ch1;
+    int col0, N;                 // the tile's first column of D; columns of D
+    // all lanes must call it; returns how many of the 16 columns lie inside D (<= 0: none)
+    __device__ __forceinline__ int load(int ch, float (&x)[16]) const {
+        uint32_t u[16];
+        acc_ld16(taddr + (uint32_t)(ch * 16), u);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(u[e]);
+        return N - (col0 + ch * 16);
+    }
+};
+
 // Eight fp32 values as bf16 (nearest-even) to a 16-byte aligned address.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
@@ -160,8 +177,8 @@ struct EpiStore {
 
 // An epilogue provides
 //   kDual       its columns come in two halves: cols8(..., x, y) gets eight columns of either
-//   kStateful   it works through all tiles of an item with a state of its own (never with splits): begin(), then
-//               cols16(state, params, row, col, live, x) for runs of 16 columns of which the first `live` are real, then end()
+//   kStateful   it works through all tiles of an item with a state of its own (never with splits): begin(), then tile() per
+//               tile with its share of the columns, in runs of 16 that it reads through an AccColumns, then end()
 //   row()       called once per tile and row before its columns (stateless only)
 template <bool PAIR, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -254,6 +271,9 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             const int n_items = p.n_items, NT = p.NT, half = NT >> 1, rep = p.rep;
             const bool dual = p.dual != 0, two_b = !PAIR && !B_MN && dual;
             const uint32_t a_box = 16384u / (uint32_t)rep;
+            // rows of B that one row tile alone reads are the first to leave L2 again: what is read twice stays
+            const bool b_once = !PAIR && !B_MN && p.prob[0].tiles_m == 1;
+            const uint64_t once = l2_policy_evict_first();
             const uint32_t bar_shift = PAIR ? cluster_map_shared(base, 0u) - base : 0u;    // both CTAs' bytes count on the leader's barrier
             for (int item = cluster; item < n_items && ok; item += n_clusters) {
                 const GemmItem it = gemm_item(p, item);
@@ -289,8 +309,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                                 if constexpr (B_MN) {
                                     for (uint32_t o = 0; o < b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
                                 } else {
-                                    load(dstb, mb, x, col0);
-                                    if (two_b) load(dstb + (uint32_t)half * 128u, mb1, x, col0);
+                                    if (b_once) {
+                                        tma_load_2d_hint(dstb, mb, x, col0, bar, once);
+                                        if (two_b) tma_load_2d_hint(dstb + (uint32_t)half * 128u, mb1, x, col0, bar, once);
+                                    } else {
+                                        load(dstb, mb, x, col0);
+                                        if (two_b) load(dstb + (uint32_t)half * 128u, mb1, x, col0);
+                                    }
                                 }
                                 if constexpr (A_MN) {
                                     load(dsta, ma, row0, x);
@@ -434,16 +459,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                             *reinterpret_cast<uint4*>(part_row + ch * 16 + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
                     }
                 } else if constexpr (Epi::kStateful) {
-                    for (int ch = ch0; ch < ch1; ++ch) {
-                        uint32_t u[16];
-                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
-                        tc_wait_ld();
-                        const int live = q.N - (col0 + ch * 16);
-                        float x[16];
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(u[e]);
-                        if (live > 0) Epi::cols16(st, ep, m, col0 + ch * 16, live, x);
-                    }
+                    Epi::tile(st, ep, m, AccColumns{taddr, ch0, ch1, col0, q.N}, smem + p.scratch_off);
                 } else {
                     if (m < q.M) Epi::row(st, ep, q, m);
                     for (int ch = ch0; ch < ch1; ++ch) {
@@ -556,7 +572,7 @@ inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 // except the maps' indices, outputs and hdr.  False when the work is too large to number its tiles.
 bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair);
 // The same for token scoring: one product, both operands K-major, whole k range in every CTA, `tiles_per_item` tiles in a row.
-bool gemm_plan_rows(GemmParams* p, bool* pair);
+bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair);
 // Rows of the box each operand's tensor map has (64 columns wide; MN-major operands: 64).
 inline int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : (int)p.a_rows; }
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);

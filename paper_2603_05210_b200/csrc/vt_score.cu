@@ -3,12 +3,18 @@
 //   x[m, v] = sum_j h[m, j] W[v, j]     z = scale * x     lse = log sum_v e^z     logprob = z[t] - lse
 //   H = -sum_v p log p = log s - E[z - max],  s = sum_v e^(z - max),  E[y] = sum_v e^(z - max) y / s
 //
-// One pass over the head: no logit is written.  gemm_kernel gives every epilogue thread a row of the tile and a range
-// of its columns; the thread folds them into a running (max, s, e = sum of (x - max) e^(z - max)) - kept about the
-// maximum, because lse and E[z] are both large where H is small - and into a register list of its k best logits, and
-// picks the given token's logit when it comes by.  At the end of a run of tiles it writes one record; a second, small
-// kernel (one block per row) joins a row's records.  Records are joined in the order of their columns and the list's
-// keys are distinct, so the result does not depend on which block ran when.
+// One pass over the head.  gemm_kernel gives every epilogue thread a row of the tile and a range of its columns; the thread
+// folds them into a running (max, s, e = sum of (x - max) e^(z - max)) - kept about the maximum, because lse and E[z] are
+// both large where H is small - and picks the given token's logit when it comes by.  At the end of a run of tiles it
+// writes one record; a second, small kernel (one block per row) joins a row's records.  The k best come in one of two ways:
+//   kept    (few logits, kKeptBytes at most): the logits go to the workspace, which is to say to L2, and the join reads back
+//           the handful of ranges whose maximum is not below the k-th largest maximum of all;
+//   listed  (many): no logit is written; every thread keeps a register list of its k best, and the join merges the lists.
+// With few rows nothing hides an epilogue, and the lists took 5 us of 60 (33 rows x 32000, k = 8) and 12 of 105 (100 rows);
+// with many rows the lists fill in the first of a thread's tiles and cost little after it, while the logits would be
+// hundreds of megabytes.
+// Records are joined in the order of their columns and ranked by distinct keys, so the result does not depend on which
+// block ran when.
 #include "vt_score.h"
 
 #include "vt_gemm.cuh"
@@ -19,15 +25,24 @@ constexpr float kMasked = -1e38f;          // stands for a column past the vocab
 
 struct ScoreRecords {
     float4* stats;                         // [M][L]: max, s, e, unused
-    unsigned long long* keys;              // [M][L][k] descending, 0 = none
+    unsigned long long* keys;              // listed: [M][L][k] descending, 0 = none
+    float* logits;                         // kept: [M][ld]
     float* given;                          // [M] the given token's logit
+    int64_t ld;
     int L;                                 // records per row
+    int parts, NT, tiles_per_item;         // record -> columns: parts per item, columns per tile, tiles per item
 };
 
+constexpr int kListQueue = 24;             // candidates a thread queues between insertions
+constexpr size_t kKeptBytes = (size_t)64 << 20;      // logits that stay in L2 beside the stream of weights
+constexpr int kKeepLogits = -1;            // EpiScore<kKeepLogits>: the kept form
+
+// KR: entries of a thread's list (0: no alternatives wanted), or kKeepLogits.
 template <int KR>
 struct EpiScore {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = true;
+    static constexpr uint32_t kScratch = KR > 0 ? kListQueue * kGemmEpiWarps * 32 * 5 : 0;
     struct Params {
         const int32_t* tokens;
         ScoreRecords rec;
@@ -38,6 +53,8 @@ struct EpiScore {
     struct State {
         float mx, s, e;
         int tok;
+        bool first;
+        float bound;                       // k logits of the row are known to be at least this large
         float v[KL];
         int ix[KL];
     };
@@ -45,46 +62,101 @@ struct EpiScore {
         st.mx = kMasked;
         st.s = st.e = 0.0f;
         st.tok = ep.tokens != nullptr && m < ep.M ? ep.tokens[m] : -1;
-        if constexpr (KR > 0) {
+        st.first = true;
+        st.bound = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < KL; ++j) { st.v[j] = kMasked; st.ix[j] = -1; }
-        }
+        for (int j = 0; j < KL; ++j) { st.v[j] = kMasked; st.ix[j] = -1; }
     }
-    static __device__ __forceinline__ void cols16(State& st, const Params& ep, int m, int col, int live, float (&x)[16]) {
+    static __device__ __forceinline__ void mask(float (&x)[16], int live) {
         if (live < 16) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = i < live ? x[i] : kMasked;
         }
-        float cm = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        cm = fmaxf(cm, fmaxf(fmaxf(fmaxf(x[8], x[9]), fmaxf(x[10], x[11])), fmaxf(fmaxf(x[12], x[13]), fmaxf(x[14], x[15]))));
-        const float nm = fmaxf(st.mx, cm);
-        const float back = st.mx - nm, f = ex2_approx(back * ep.c);
-        float s0 = 0.0f, s1 = 0.0f, e0 = 0.0f, e1 = 0.0f;
+    }
+    static __device__ __forceinline__ void tile(State& st, const Params& ep, int m, const AccColumns& cols, unsigned char* scratch) {
+        float g[KL];
+        if constexpr (KR > 0) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            const float y0 = x[i] - nm, y1 = x[i + 1] - nm;
-            const float p0 = ex2_approx(y0 * ep.c), p1 = ex2_approx(y1 * ep.c);
-            s0 += p0;
-            s1 += p1;
-            e0 = fmaf(p0, y0, e0);
-            e1 = fmaf(p1, y1, e1);
+            for (int j = 0; j < KL; ++j) g[j] = kMasked;
         }
-        st.e = fmaf(f, fmaf(back, st.s, st.e), e0 + e1);
-        st.s = fmaf(f, st.s, s0 + s1);
-        st.mx = nm;
-        const int at = st.tok - col;
-        if ((unsigned)at < (unsigned)min(live, 16)) {
-            float g = x[0];
+        for (int ch = cols.ch0; ch < cols.ch1; ++ch) {
+            float x[16];
+            const int live = cols.load(ch, x), col = cols.col0 + ch * 16;
+            if (live <= 0) break;
+            mask(x, live);
+            float gm[4];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) g = at == i ? x[i] : g;
-            ep.rec.given[m] = g;
+            for (int i = 0; i < 4; ++i) gm[i] = fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), fmaxf(x[4 * i + 2], x[4 * i + 3]));
+            const float nm = fmaxf(st.mx, fmaxf(fmaxf(gm[0], gm[1]), fmaxf(gm[2], gm[3])));
+            const float back = st.mx - nm, f = ex2_approx(back * ep.c);
+            float s0 = 0.0f, s1 = 0.0f, e0 = 0.0f, e1 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float y0 = x[i] - nm, y1 = x[i + 1] - nm;
+                const float p0 = ex2_approx(y0 * ep.c), p1 = ex2_approx(y1 * ep.c);
+                s0 += p0;
+                s1 += p1;
+                e0 = fmaf(p0, y0, e0);
+                e1 = fmaf(p1, y1, e1);
+            }
+            st.e = fmaf(f, fmaf(back, st.s, st.e), e0 + e1);
+            st.s = fmaf(f, st.s, s0 + s1);
+            st.mx = nm;
+            const int at = st.tok - col;
+            if ((unsigned)at < (unsigned)min(live, 16)) {
+                float t = x[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) t = at == i ? x[i] : t;
+                ep.rec.given[m] = t;
+            }
+            if constexpr (KR == kKeepLogits) {
+                if (m < ep.M) {            // rows are whole runs of 16 columns long
+                    float4* to = reinterpret_cast<float4*>(ep.rec.logits + (size_t)m * ep.rec.ld + col);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                }
+            }
+            if constexpr (KR > 0) {
+                if (st.first) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) vals_insert<KL>(g, gm[i]);
+                }
+            }
         }
         if constexpr (KR > 0) {
-            if (__any_sync(0xFFFFFFFFu, cm > st.v[KL - 1])) {
+            // The logits that may be among the row's best - above the list's last entry, and in the thread's first tile not
+            // below the KR-th largest of the maxima of groups of four, which KR logits reach - are queued (lanes meet
+            // theirs at different columns) and inserted together, one per lane and turn.
+            if (st.first) st.bound = g[KL - 1];
+            st.first = false;
+            float* qx = reinterpret_cast<float*>(scratch) + threadIdx.x;
+            unsigned char* qc = scratch + kListQueue * kGemmEpiWarps * 32 * 4 + threadIdx.x;
+            int cnt = 0;
+            auto insert_queued = [&]() {
+                const int most = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)cnt);
+                for (int i = 0; i < most; ++i) {
+                    const float x = i < cnt ? qx[i * (kGemmEpiWarps * 32)] : kMasked;      // beats nothing
+                    rows_insert<KL>(st.v, st.ix, x, cols.col0 + (int)qc[i * (kGemmEpiWarps * 32)]);
+                }
+                cnt = 0;
+            };
+            for (int ch = cols.ch0; ch < cols.ch1; ++ch) {
+                float x[16];
+                const int live = cols.load(ch, x);
+                if (live <= 0) break;
+                mask(x, live);
+                const float tau = st.v[KL - 1];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (__any_sync(0xFFFFFFFFu, x[i] > st.v[KL - 1])) rows_insert<KL>(st.v, st.ix, x[i], col + i);
+                for (int i = 0; i < 16; ++i) {
+                    if (x[i] > tau && x[i] >= st.bound) {
+                        qx[cnt * (kGemmEpiWarps * 32)] = x[i];
+                        qc[cnt * (kGemmEpiWarps * 32)] = (unsigned char)(ch * 16 + i);
+                        ++cnt;
+                    }
+                }
+                if (__any_sync(0xFFFFFFFFu, cnt > kListQueue - 16)) insert_queued();
             }
+            insert_queued();
         }
     }
     static __device__ __forceinline__ void end(State& st, const Params& ep, int m, int list) {
@@ -100,9 +172,8 @@ struct EpiScore {
 };
 
 // ------------------------------------------------------------------------------------------ the join of a row's records
-constexpr int kJoinThreads = 128;
-constexpr int kJoinCand = 1024;
-constexpr int kJoinHeld = 8;               // lists a thread keeps the best key of in registers
+constexpr int kJoinHeld = 8;               // records a thread keeps in registers
+constexpr int kJoinRanges = 512;
 
 struct ScoreJoin {
     ScoreRecords rec;
@@ -112,83 +183,91 @@ struct ScoreJoin {
     float scale;
 };
 
-// One block per row, bound by the latency of its few loads: all records of a thread's lists are requested together.
-__global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoin p) {
-    __shared__ float3 parts[kJoinThreads / 32];
-    __shared__ unsigned long long heads[kJoinThreads], cand[kJoinCand];
-    __shared__ unsigned long long bound_s;
-    __shared__ int n_cand;
+// Sum (SUM) or maximum over the block, the same bits in every thread.
+template <int T, bool SUM>
+__device__ __forceinline__ float block_reduce(float v, float* buf) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float r = __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        v = SUM ? v + r : fmaxf(v, r);
+    }
+    if constexpr (T > 32) {
+        if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = buf[0];
+#pragma unroll
+        for (int w = 1; w < T / 32; ++w) v = SUM ? v + buf[w] : fmaxf(v, buf[w]);
+    }
+    return v;
+}
+
+// One block per row.  Nothing but latency bounds it: a thread's records are all requested before the first is used, and
+// the steps between barriers are short.  256 threads for few rows, one warp where the rows fill the SMs by themselves
+// (4096 rows, k = 4: 29 us of 128-thread blocks before, see the launch rule).
+template <int T, bool KEPT>
+__global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
+    constexpr int kCand = T >= 128 ? 1024 : 256;
+    __shared__ float buf[3][T / 32];
+    __shared__ __align__(16) uint32_t heads[T];
+    __shared__ unsigned long long cand[kCand], wins[T / 32];
+    __shared__ int n_cand, n_ranges, ranges[KEPT ? kJoinRanges : 1];
     const int m = blockIdx.x, t = threadIdx.x, L = p.rec.L, k = p.out.k;
-    if (t == 0) { n_cand = 0; bound_s = 1ull; }
-    grid_dependency_wait();
     const ScoreOut& o = p.out;
-    if (!row_scored(p.tokens, p.V, m)) {
+    if (t == 0) n_cand = n_ranges = 0;
+    grid_dependency_wait();
+    const float4* stats = p.rec.stats + (size_t)m * L;
+    const unsigned long long* keys = p.rec.keys + (size_t)m * L * k;
+    const float c = p.scale * kLog2e;
+    const bool scored = row_scored(p.tokens, p.V, m);
+    const float given = p.tokens != nullptr ? p.rec.given[m] : 0.0f;      // stale where the row is not scored, and then not used
+    // a thread's records in registers, with the best key of each; kept: the range by its maximum
+    float4 r[kJoinHeld];
+    unsigned long long held[kJoinHeld];
+#pragma unroll
+    for (int i = 0; i < kJoinHeld; ++i) {
+        const int l = t + i * T;
+        r[i] = l < L ? stats[l] : make_float4(kMasked, 0.0f, 0.0f, 0.0f);
+        if constexpr (!KEPT) held[i] = l < L && k > 0 ? keys[(size_t)l * k] : 0ull;
+    }
+    if (!scored) {
         if (t == 0) {
             if (o.logprobs) o.logprobs[m] = 0.0f;
             if (o.entropy) o.entropy[m] = 0.0f;
             if (o.lse) o.lse[m] = 0.0f;
         }
-        for (int j = t; j < k; j += kJoinThreads) {
+        for (int j = t; j < k; j += T) {
             o.top_ids[(size_t)m * k + j] = -1;
             o.top_logprobs[(size_t)m * k + j] = 0.0f;
         }
         return;
     }
-    const float4* stats = p.rec.stats + (size_t)m * L;
-    const unsigned long long* keys = p.rec.keys + (size_t)m * L * k;
-    const float c = p.scale * kLog2e;
-    const float given = o.logprobs ? p.rec.given[m] : 0.0f;
-    float mx = kMasked, s = 0.0f, e = 0.0f;
-    unsigned long long held[kJoinHeld], head = 0ull;
-    auto fold = [&](float rmx, float rs, float re) {
-        const float nm = fmaxf(mx, rmx), b0 = mx - nm, b1 = rmx - nm;
-        const float f0 = ex2_approx(b0 * c), f1 = ex2_approx(b1 * c);
-        e = fmaf(f0, fmaf(b0, s, e), f1 * fmaf(b1, rs, re));
-        s = fmaf(f0, s, f1 * rs);
-        mx = nm;
-    };
-    {
-        float4 r[kJoinHeld];
+    auto range_key = [](const float4& q) { return q.y > 0.0f ? make_key(q.x, 0) : 0ull; };
+    float mx = kMasked;
+    uint32_t head = 0u;
 #pragma unroll
-        for (int i = 0; i < kJoinHeld; ++i) {
-            const int l = t + i * kJoinThreads;
-            r[i] = l < L ? stats[l] : make_float4(kMasked, 0.0f, 0.0f, 0.0f);
-            held[i] = l < L && k > 0 ? keys[(size_t)l * k] : 0ull;
-        }
-#pragma unroll
-        for (int i = 0; i < kJoinHeld; ++i) {
-            fold(r[i].x, r[i].y, r[i].z);
-            head = held[i] > head ? held[i] : head;
-        }
+    for (int i = 0; i < kJoinHeld; ++i) {
+        if constexpr (KEPT) held[i] = range_key(r[i]);
+        mx = fmaxf(mx, r[i].x);
+        head = max(head, (uint32_t)(held[i] >> 32));
     }
-    for (int l = t + kJoinHeld * kJoinThreads; l < L; l += kJoinThreads) {
-        const float4 r = stats[l];
-        fold(r.x, r.y, r.z);
-        if (k > 0) {
-            const unsigned long long key = keys[(size_t)l * k];
-            head = key > head ? key : head;
-        }
+    for (int l = t + kJoinHeld * T; l < L; l += T) {
+        const float4 q = stats[l];
+        mx = fmaxf(mx, q.x);
+        if (k > 0) head = max(head, (uint32_t)((KEPT ? range_key(q) : keys[(size_t)l * k]) >> 32));
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float rmx = __shfl_xor_sync(0xFFFFFFFFu, mx, d), rs = __shfl_xor_sync(0xFFFFFFFFu, s, d), re = __shfl_xor_sync(0xFFFFFFFFu, e, d);
-        // both lanes of a pair must come to the same bits: the lower lane's part first
-        const bool low = (t & d) == 0;
-        const float amx = low ? mx : rmx, as = low ? s : rs, ae = low ? e : re;
-        const float bmx = low ? rmx : mx, bs = low ? rs : s, be = low ? re : e;
-        mx = amx;
-        s = as;
-        e = ae;
-        fold(bmx, bs, be);
-    }
-    if ((t & 31) == 0) parts[t >> 5] = make_float3(mx, s, e);
     heads[t] = head;
-    __syncthreads();
-    mx = parts[0].x;
-    s = parts[0].y;
-    e = parts[0].z;
+    mx = block_reduce<T, false>(mx, buf[0]);
+    float s = 0.0f, e = 0.0f;
+    auto fold = [&](const float4& q) {
+        const float back = q.x - mx, f = ex2_approx(back * c);
+        s = fmaf(f, q.y, s);
+        e = fmaf(f, fmaf(back, q.y, q.z), e);
+    };
 #pragma unroll
-    for (int w = 1; w < kJoinThreads / 32; ++w) fold(parts[w].x, parts[w].y, parts[w].z);
+    for (int i = 0; i < kJoinHeld; ++i) fold(r[i]);
+    for (int l = t + kJoinHeld * T; l < L; l += T) fold(stats[l]);
+    s = block_reduce<T, true>(s, buf[1]);
+    e = block_reduce<T, true>(e, buf[2]);
     const float log_s = logf(s);
     if (t == 0) {
         if (o.lse) o.lse[m] = fmaf(p.scale, mx, log_s);
@@ -197,27 +276,83 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoi
     }
     if (k == 0) return;
 
-    // The k best of L descending lists.  The k-th largest of the threads' best heads bounds the winners from below: k keys
-    // at least that large exist.  The keys not below it are gathered, and a key's place is the number of keys above it.
-    if (head != 0ull) {
-        int above = 0;
-#pragma unroll 8
-        for (int i = 0; i < kJoinThreads; ++i) above += heads[i] > head ? 1 : 0;
-        if (above == k - 1) bound_s = head;
-    }
+    // The k-th largest of the maxima of 64 (32) groups of ranges bounds the winners from below: k logits at least that large
+    // exist.  The logits not below it are gathered, and a key's place is the number of keys above it.  Every warp finds the
+    // bound for itself, in k rounds of a warp-wide maximum (equal maxima leave together: the bound is then lower, and holds).
     __syncthreads();
-    const unsigned long long bound = bound_s;          // 1 (every key) when fewer than k threads have one
-    auto gather = [&](int l, unsigned long long key) {
-        for (int j = 0; key >= bound;) {
-            const int at = atomicAdd(&n_cand, 1);      // the order of the candidates does not matter: their ranks decide
-            if (at < kJoinCand) cand[at] = key;
-            if (++j == k) break;
-            key = keys[(size_t)l * k + j];
-        }
-    };
+    uint32_t g0 = 0u, g1 = 0u, b = 0u;
+    if constexpr (T == 32) {
+        g0 = head;
+    } else {
 #pragma unroll
-    for (int i = 0; i < kJoinHeld; ++i) gather(t + i * kJoinThreads, held[i]);
-    for (int l = t + kJoinHeld * kJoinThreads; l < L; l += kJoinThreads) gather(l, keys[(size_t)l * k]);
+        for (int i = 0; i < T / 64; ++i) {
+            const uint2 h = *reinterpret_cast<const uint2*>(heads + 64 * i + 2 * (t & 31));
+            g0 = max(g0, h.x);
+            g1 = max(g1, h.y);
+        }
+    }
+    for (int j = 0; j < k; ++j) {
+        b = __reduce_max_sync(0xFFFFFFFFu, max(g0, g1));
+        g0 = g0 == b ? 0u : g0;
+        g1 = g1 == b ? 0u : g1;
+    }
+    const unsigned long long bound = b != 0u ? (unsigned long long)b << 32 : 1ull;   // 1 (every key) when fewer than k groups have one
+    auto candidate = [&](unsigned long long key) {
+        const int at = atomicAdd(&n_cand, 1);          // the order of the candidates does not matter: their ranks decide
+        if (at < kCand) cand[at] = key;
+    };
+    const float* row = p.rec.logits + (size_t)m * p.rec.ld;
+    if constexpr (KEPT) {
+        // the ranges that reach the bound ...
+        auto gather = [&](int l, unsigned long long key) {
+            if (key < bound) return;
+            const int at = atomicAdd(&n_ranges, 1);
+            if (at < kJoinRanges) ranges[at] = l;
+        };
+#pragma unroll
+        for (int i = 0; i < kJoinHeld; ++i) gather(t + i * T, held[i]);
+        for (int l = t + kJoinHeld * T; l < L; l += T) gather(l, range_key(stats[l]));
+        __syncthreads();
+        // ... and their logits: a warp per range, a lane per four columns, four tiles in flight
+        const float bound_x = b != 0u ? key_logit(bound) : -INFINITY;
+        const bool all = n_ranges > kJoinRanges;       // more than the buffer names: every range
+        const int nr = all ? L : n_ranges, nch = p.rec.NT >> 4, tiles = p.rec.tiles_per_item;
+        for (int i = t >> 5; i < nr; i += T / 32) {
+            const int l = all ? i : ranges[i];
+            const int item = l / p.rec.parts, part = l - item * p.rec.parts;
+            const int c0 = part * nch / p.rec.parts * 16 + (t & 31) * 4, c1 = (part + 1) * nch / p.rec.parts * 16;
+            const int first = item * tiles * p.rec.NT;
+            for (int cc = c0; cc < c1; cc += 128)
+                for (int tile = 0; tile < tiles; tile += 4) {
+                    float4 x[4];
+                    int col[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        col[u] = first + (tile + u) * p.rec.NT + cc;
+                        if (tile + u >= tiles) col[u] = p.V;
+                        if (col[u] < p.V) x[u] = *reinterpret_cast<const float4*>(row + col[u]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const float v[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            if (col[u] + q < p.V && v[q] >= bound_x) candidate(make_key(v[q], col[u] + q));
+                    }
+                }
+        }
+    } else {
+        auto gather = [&](int l, unsigned long long key) {
+            for (int j = 0; key >= bound;) {
+                candidate(key);
+                if (++j == k) break;
+                key = keys[(size_t)l * k + j];
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kJoinHeld; ++i) gather(t + i * T, held[i]);
+        for (int l = t + kJoinHeld * T; l < L; l += T) gather(l, keys[(size_t)l * k]);
+    }
     __syncthreads();
     const int n = n_cand;
     auto emit = [&](int j, unsigned long long key) {
@@ -225,90 +360,126 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(const ScoreJoi
         o.top_ids[at] = key != 0ull ? key_index(key) : -1;
         o.top_logprobs[at] = key != 0ull ? p.scale * (key_logit(key) - mx) - log_s : -INFINITY;
     };
-    if (n <= kJoinCand) {
-        for (int i = t; i < n; i += kJoinThreads) {
+    if (n <= kCand) {
+        for (int i = t; i < n; i += T) {
             const unsigned long long key = cand[i];
             int above = 0;
 #pragma unroll 4
             for (int q = 0; q < n; ++q) above += cand[q] > key ? 1 : 0;
             if (above < k) emit(above, key);
         }
-        for (int j = n + t; j < k; j += kJoinThreads) emit(j, 0ull);
+        for (int j = n + t; j < k; j += T) emit(j, 0ull);
         return;
     }
-    // Too many for the buffer (the winners sit in few lists): the largest key below the last winner, k times.
+    // Too many for the buffer (ties, or winners in few lists): the largest key below the last winner, k times.
     unsigned long long last = ~0ull;
     for (int j = 0; j < k; ++j) {
         unsigned long long best = 0ull;
-        for (int l = t; l < L; l += kJoinThreads)
-            for (int i = 0; i < k; ++i) {
-                const unsigned long long key = keys[(size_t)l * k + i];
-                if (key < last) { best = key > best ? key : best; break; }
+        if constexpr (KEPT) {
+            for (int col = t; col < p.V; col += T) {
+                const unsigned long long key = make_key(row[col], col);
+                if (key < last && key > best) best = key;
             }
+        } else {
+            for (int l = t; l < L; l += T)
+                for (int i = 0; i < k; ++i) {
+                    const unsigned long long key = keys[(size_t)l * k + i];
+                    if (key < last) { best = key > best ? key : best; break; }
+                }
+        }
         best = warp_max_key(best);
         __syncthreads();
-        if ((t & 31) == 0) heads[t >> 5] = best;
+        if ((t & 31) == 0) wins[t >> 5] = best;
         __syncthreads();
-        for (int i = 0; i < kJoinThreads / 32; ++i) best = heads[i] > best ? heads[i] : best;
+        for (int i = 0; i < T / 32; ++i) best = wins[i] > best ? wins[i] : best;
         if (t == 0) emit(j, best);
         last = best;
     }
 }
 
 // ------------------------------------------------------------------------------------------ host
-static bool score_plan(int M, int d, int V, GemmParams* p, bool* pair) {
-    p->n_prob = 1;
-    p->prob[0] = GemmProblem{};
-    p->prob[0].M = M;
-    p->prob[0].N = V;
-    p->prob[0].b0 = 1;
-    p->prob[0].nk0 = ceil_div(d, kBoxK);
-    return gemm_plan_rows(p, pair);
+static int list_entries(int k) { return k == 0 ? 0 : k <= 4 ? 4 : k <= 8 ? 8 : k <= 20 ? 20 : VT_MAX_K; }
+
+struct ScorePlan {
+    GemmParams p;
+    bool pair;
+    int KR;
+    int64_t ld;
+    int L;
+    size_t stats, keys, logits, given, total;      // offsets in the workspace
+};
+
+static bool score_plan(int M, int d, int V, int k, ScorePlan* s) {
+    s->p = GemmParams{};
+    s->p.n_prob = 1;
+    s->p.prob[0].M = M;
+    s->p.prob[0].N = V;
+    s->p.prob[0].b0 = 1;
+    s->p.prob[0].nk0 = ceil_div(d, kBoxK);
+    s->ld = (int64_t)round_up((size_t)V, 16);
+    const size_t kept = (size_t)M * s->ld * 4;
+    s->KR = k > 0 && kept <= kKeptBytes ? kKeepLogits : list_entries(k);
+    if (!gemm_plan_rows(&s->p, s->KR > 0 ? EpiScore<4>::kScratch : 0u, &s->pair)) return false;
+    s->L = s->p.prob[0].chunks_n * 2 * s->p.rep;
+    const size_t rows = (size_t)M * s->L;
+    s->stats = kHeaderBytes;
+    s->keys = s->stats + round_up(rows * sizeof(float4), 256);
+    s->logits = s->keys + (s->KR > 0 ? round_up(rows * k * 8, 256) : 0);
+    s->given = s->logits + (s->KR == kKeepLogits ? round_up(kept, 256) : 0);
+    s->total = s->given + round_up((size_t)M * 4, 256);
+    return true;
 }
-static int score_records(const GemmParams& p) { return p.prob[0].chunks_n * 2 * p.rep; }
 
 size_t score_workspace_bytes(int M, int d, int V, int k) {
-    GemmParams p{};
-    bool pair = false;
-    if (!score_plan(M, d, V, &p, &pair)) return 0;
-    const size_t rows = (size_t)M * score_records(p);
-    return kHeaderBytes + round_up(rows * sizeof(float4), 256) + round_up(rows * k * 8, 256) + round_up((size_t)M * 4, 256);
+    ScorePlan s;
+    return score_plan(M, d, V, k, &s) ? s.total : 0;
 }
 
 template <int KR>
-static vt_status run_score(const GemmMaps& maps, const GemmParams& p, bool pair, const ScoreCall& c, const ScoreRecords& rec, int k,
+static vt_status run_score(const GemmMaps& maps, const ScorePlan& s, const ScoreCall& c, const ScoreRecords& rec, const ScoreOut& o,
                            cudaStream_t st) {
-    const typename EpiScore<KR>::Params ep{c.tokens, rec, c.scale * kLog2e, c.M, c.V, k};
-    return gemm_launch<false, false, EpiScore<KR>>(maps, p, pair, ep, st);
-}
-
-vt_status launch_score(const ScoreCall& c, const ScoreOut& o, void* workspace, cudaStream_t st) {
-    GemmMaps maps{};
-    GemmParams p{};
-    bool pair = false;
-    if (!score_plan(c.M, c.d, c.V, &p, &pair)) return VT_ERR_SHAPE;
-    unsigned char* base = reinterpret_cast<unsigned char*>(workspace);
-    p.hdr = reinterpret_cast<WsHeader*>(base);
-    ScoreRecords rec;
-    rec.L = score_records(p);
-    const size_t rows = (size_t)c.M * rec.L;
-    rec.stats = reinterpret_cast<float4*>(base + kHeaderBytes);
-    rec.keys = reinterpret_cast<unsigned long long*>(base + kHeaderBytes + round_up(rows * sizeof(float4), 256));
-    rec.given = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(rec.keys) + round_up(rows * o.k * 8, 256));
-    vt_status r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(p, false));
-    if (r != VT_OK) return r;
-    if ((r = gemm_map(&maps.map[1], GemmOperand{c.W, c.V, c.d, c.d}, gemm_box_b(p, false, pair))) != VT_OK) return r;
-    if (o.k == 0) r = run_score<0>(maps, p, pair, c, rec, o.k, st);
-    else if (o.k <= 4) r = run_score<4>(maps, p, pair, c, rec, o.k, st);
-    else if (o.k <= 8) r = run_score<8>(maps, p, pair, c, rec, o.k, st);
-    else if (o.k <= 20) r = run_score<20>(maps, p, pair, c, rec, o.k, st);
-    else r = run_score<VT_MAX_K>(maps, p, pair, c, rec, o.k, st);
+    const typename EpiScore<KR>::Params ep{c.tokens, rec, c.scale * kLog2e, c.M, c.V, o.k};
+    vt_status r = gemm_launch<false, false, EpiScore<KR>>(maps, s.p, s.pair, ep, st);
     if (r != VT_OK) return r;
     const ScoreJoin join{rec, o, c.tokens, c.V, c.scale};
-    cudaError_t e = launch_pdl(score_join_kernel, c.M, kJoinThreads, 0, st, join);
+    constexpr bool kept = KR == kKeepLogits;
+    // one warp per row needs the rows' heads to bound k winners, and pays where rows are plenty
+    const bool narrow = c.M > 4 * kGemmSms && o.k <= 32;
+    cudaError_t e = narrow ? launch_pdl(score_join_kernel<32, kept>, c.M, 32, 0, st, join)
+                           : launch_pdl(score_join_kernel<256, kept>, c.M, 256, 0, st, join);
     count_launch();
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? VT_OK : cuda_fail(e);
+}
+
+vt_status launch_score(const ScoreCall& c, const ScoreOut& o, void* workspace, size_t workspace_bytes, cudaStream_t st) {
+    ScorePlan s;
+    if (!score_plan(c.M, c.d, c.V, o.k, &s)) return VT_ERR_SHAPE;
+    if (workspace_bytes < s.total) return VT_ERR_WORKSPACE;
+    unsigned char* base = reinterpret_cast<unsigned char*>(workspace);
+    s.p.hdr = reinterpret_cast<WsHeader*>(base);
+    ScoreRecords rec;
+    rec.stats = reinterpret_cast<float4*>(base + s.stats);
+    rec.keys = reinterpret_cast<unsigned long long*>(base + s.keys);
+    rec.logits = reinterpret_cast<float*>(base + s.logits);
+    rec.given = reinterpret_cast<float*>(base + s.given);
+    rec.ld = s.ld;
+    rec.L = s.L;
+    rec.parts = 2 * s.p.rep;
+    rec.NT = s.p.NT;
+    rec.tiles_per_item = s.p.tiles_per_item;
+    GemmMaps maps{};
+    vt_status r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(s.p, false));
+    if (r != VT_OK) return r;
+    if ((r = gemm_map(&maps.map[1], GemmOperand{c.W, c.V, c.d, c.d}, gemm_box_b(s.p, false, s.pair))) != VT_OK) return r;
+    switch (s.KR) {
+        case kKeepLogits: return run_score<kKeepLogits>(maps, s, c, rec, o, st);
+        case 0: return run_score<0>(maps, s, c, rec, o, st);
+        case 4: return run_score<4>(maps, s, c, rec, o, st);
+        case 8: return run_score<8>(maps, s, c, rec, o, st);
+        case 20: return run_score<20>(maps, s, c, rec, o, st);
+        default: return run_score<VT_MAX_K>(maps, s, c, rec, o, st);
+    }
 }
 
 }  // namespace vt

@@ -29,7 +29,7 @@ __device__ __forceinline__ bool row_scored(const int32_t* tokens, int V, int m) 
 
 size_t score_workspace_bytes(int M, int d, int V, int k);
 size_t score_backward_workspace_bytes(int M, int d, int V);
-vt_status launch_score(const ScoreCall& c, const ScoreOut& o, void* workspace, cudaStream_t st);
+vt_status launch_score(const ScoreCall& c, const ScoreOut& o, void* workspace, size_t workspace_bytes, cudaStream_t st);   // checks the size itself
 vt_status launch_score_backward(const ScoreCall& c, const float* lse, const float* entropy, const float* grad_logprobs,
                                 const float* grad_entropy, void* grad_h, void* grad_W, void* workspace, cudaStream_t st);
 
