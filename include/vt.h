@@ -266,7 +266,7 @@ vt_status vt_score_tokens_backward(const void* h, int64_t ldh, const void* W, co
  *
  *   x       dev [M, d] bf16, rows ldx elements apart (ldx >= d, a multiple of 8)
  *   W_gate, W_up  dev [f, d] bf16       W_down  dev [d, f] bf16       y  dev [M, d] bf16 (out)
- *   saved   dev [M, 2 f] float (out) or NULL: g, then u, of each row, for the backward pass
+ *   saved   dev 2 M f floats (out) or NULL: g and u for the backward pass, in fp32, in a layout of the library's own
  *   workspace  dev, 256-byte aligned, vt_gated_ffn_workspace_bytes(M, d, f) bytes; no initialisation needed (see above)
  * All matrices 16-byte aligned.  d % 8 == 0, f % 8 == 0, both >= 8, any M >= 1; act a vt_act.  Asynchronous. */
 typedef enum vt_act {

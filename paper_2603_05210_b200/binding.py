@@ -467,7 +467,7 @@ def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_do
                  workspace: torch.Tensor | None = None) -> torch.Tensor:
     """y [M, d] bf16 = (act(x W_gate^T) * (x W_up^T)) W_down^T, act "silu" or "gelu" (tanh form).
 
-    Pass ``saved`` [M, 2 f] float32 to receive both projections for ``vt_gated_ffn_backward``."""
+    Pass ``saved`` [M, 2 f] float32 to receive what ``vt_gated_ffn_backward`` needs (its layout is the library's own)."""
     x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
     M = x.shape[0]
     out = _out(out, "out", (M, d), torch.bfloat16, x.device)

@@ -39,66 +39,86 @@ __device__ __forceinline__ ActValue act_eval(int act, float g) {
     return r;
 }
 
+// The kept projections, [M, 2 f] floats: g of all features, then u, in blocks of 32 rows (the last block: of the rows left) x 4
+// features, rows of a block one after the other.  The 32 rows of a warp's accumulators are then one contiguous run, read
+// and written at full width whatever tiles either pass uses.
+__device__ __forceinline__ float* saved_at(float* saved, int M, int f2, int m, int col) {
+    const int m0 = m & ~31, rows = min(32, M - m0);
+    return saved + (size_t)m0 * f2 + (size_t)(col >> 2) * (rows * 4) + (m - m0) * 4;
+}
+
 struct EpiGateUp {
     static constexpr bool kDual = true;
     static constexpr bool kStateful = false;
+    static constexpr int kOuts = 1;
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
         uint16_t* a;        // [M, f] bf16
-        float* saved;       // [M, 2f] (g, then u), or null
+        float* saved;       // see saved_at, or null
         int act;
     };
     struct State {};
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    static __device__ __forceinline__ void cols8(State&, const Params& ep, const GemmProblem& q, int m, int n, const float* g, const float* u) {
-        float a[8];
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void cols8(State&, const Params& ep, const GemmProblem& q, int m, int n, int, const float (&g)[8],
+                                                 const float (&u)[8], float (&out)[1][8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = act_eval(ep.act, g[i]).value * u[i];
-        store_bf16x8(ep.a + (size_t)m * q.N + n, a);
-        if (ep.saved) {
-            float* gs = ep.saved + (size_t)m * 2 * q.N + n;
-            float* us = gs + q.N;
-            *reinterpret_cast<float4*>(gs) = make_float4(g[0], g[1], g[2], g[3]);
-            *reinterpret_cast<float4*>(gs + 4) = make_float4(g[4], g[5], g[6], g[7]);
-            *reinterpret_cast<float4*>(us) = make_float4(u[0], u[1], u[2], u[3]);
-            *reinterpret_cast<float4*>(us + 4) = make_float4(u[4], u[5], u[6], u[7]);
+        for (int i = 0; i < 8; ++i) out[0][i] = act_eval(ep.act, g[i]).value * u[i];
+        if (ep.saved && m < q.M && n < q.N) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                *reinterpret_cast<float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, n + i)) = make_float4(g[i], g[i + 1], g[i + 2], g[i + 3]);
+                *reinterpret_cast<float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, q.N + n + i)) = make_float4(u[i], u[i + 1], u[i + 2], u[i + 3]);
+            }
         }
     }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int, int m, int n) { return ep.a + (size_t)m * q.N + n; }
 };
 
 struct EpiActGrad {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
+    static constexpr int kOuts = 3;         // dg, du, a
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
-        const float* saved;     // [M, 2f]
+        float* saved;           // see saved_at; only read
         uint16_t* dgu;          // [M, 2f] bf16: dg, then du
         uint16_t* a;            // [M, f] bf16
         int act;
     };
-    struct State {};
+    struct State {
+        float4 g[4], u[4];      // the next 16 columns
+    };
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    static __device__ __forceinline__ void cols8(State&, const Params& ep, const GemmProblem& q, int m, int n, const float* da) {
-        const size_t at = (size_t)m * 2 * q.N + n;
-        float g[8], u[8], dg[8], du[8], a[8];
-        *reinterpret_cast<float4*>(g) = *reinterpret_cast<const float4*>(ep.saved + at);
-        *reinterpret_cast<float4*>(g + 4) = *reinterpret_cast<const float4*>(ep.saved + at + 4);
-        *reinterpret_cast<float4*>(u) = *reinterpret_cast<const float4*>(ep.saved + at + q.N);
-        *reinterpret_cast<float4*>(u + 4) = *reinterpret_cast<const float4*>(ep.saved + at + q.N + 4);
+    static __device__ __forceinline__ void ahead(State& st, const Params& ep, const GemmProblem& q, int m, int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + 4 * i < q.N) {
+                st.g[i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, n + 4 * i));
+                st.u[i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, q.N + n + 4 * i));
+            }
+    }
+    static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int, int, int e, const float (&da)[8],
+                                                 const float (&)[8], float (&out)[3][8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const ActValue v = act_eval(ep.act, g[i]);
-            dg[i] = da[i] * u[i] * v.slope;
-            du[i] = da[i] * v.value;
-            a[i] = v.value * u[i];
+            const float4 g4 = st.g[(e + i) >> 2], u4 = st.u[(e + i) >> 2];
+            const float g = (i & 3) == 0 ? g4.x : (i & 3) == 1 ? g4.y : (i & 3) == 2 ? g4.z : g4.w;
+            const float u = (i & 3) == 0 ? u4.x : (i & 3) == 1 ? u4.y : (i & 3) == 2 ? u4.z : u4.w;
+            const ActValue v = act_eval(ep.act, g);
+            out[0][i] = da[i] * u * v.slope;
+            out[1][i] = da[i] * v.value;
+            out[2][i] = v.value * u;
         }
-        store_bf16x8(ep.dgu + at, dg);
-        store_bf16x8(ep.dgu + at + q.N, du);
-        store_bf16x8(ep.a + (size_t)m * q.N + n, a);
+    }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int o, int m, int n) {
+        return o == 2 ? ep.a + (size_t)m * q.N + n : ep.dgu + (size_t)m * 2 * q.N + (o == 1 ? q.N : 0) + n;
     }
 };
 
 static inline int k_blocks(int k) { return (k + kBoxK - 1) / kBoxK; }
 
-static GemmProblem problem(int M, int N, int a0, int b0, int nk0, void* out, int a1 = 0, int b1 = 0, int nk1 = 0) {
+static GemmProblem problem(int M, int N, int a0, int b0, int nk0, int a1 = 0, int b1 = 0, int nk1 = 0) {
     GemmProblem q{};
     q.M = M;
     q.N = N;
@@ -108,7 +128,6 @@ static GemmProblem problem(int M, int N, int a0, int b0, int nk0, void* out, int
     q.a1 = a1;
     q.b1 = b1;
     q.nk1 = nk1;
-    q.out = out;
     return q;
 }
 
@@ -132,12 +151,13 @@ vt_status launch_ffn(const FfnCall& c, void* y, float* saved, void* workspace, c
         GemmParams p{};
         bool pair = false;
         p.n_prob = 1;
-        p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d), nullptr, 0, 2, 0);
+        p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d), 0, 2, 0);
         p.hdr = reinterpret_cast<WsHeader*>(base);
-        if (!gemm_plan(&p, false, false, true, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, false, true, EpiGateUp::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], x, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wg, gemm_box_b(p, false, pair))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[2], wu, gemm_box_b(p, false, pair))) != VT_OK) return r;
+        if ((r = make_tensor_map_bf16_store(&maps.out[0], a, c.M, c.f, c.f)) != VT_OK) return r;
         const EpiGateUp::Params ep{a, saved, c.act};
         if ((r = gemm_launch<false, false, EpiGateUp>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
@@ -145,12 +165,12 @@ vt_status launch_ffn(const FfnCall& c, void* y, float* saved, void* workspace, c
     GemmParams p{};
     bool pair = false;
     p.n_prob = 1;
-    p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f), y);
+    p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f));
     p.hdr = reinterpret_cast<WsHeader*>(base);
-    if (!gemm_plan(&p, false, false, false, &pair)) return VT_ERR_SHAPE;
+    if (!gemm_plan(&p, false, false, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
     if ((r = gemm_map(&maps.map[0], GemmOperand{a, c.M, c.f, c.f}, gemm_box_a(p, false))) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[1], wd, gemm_box_b(p, false, pair))) != VT_OK) return r;
-    return gemm_store(maps, p, pair, false, false, st);
+    return gemm_store(maps, p, pair, false, false, &y, st);
 }
 
 vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* grad_y, int64_t ld_grad_y, void* grad_x,
@@ -168,12 +188,15 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
         GemmParams p{};
         bool pair = false;
         p.n_prob = 1;
-        p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d), nullptr);
+        p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d));
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, true, false, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, true, false, EpiActGrad::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], dy, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wd, gemm_box_b(p, true, pair))) != VT_OK) return r;
-        const EpiActGrad::Params ep{saved, dgu, a, c.act};
+        if ((r = make_tensor_map_bf16_store(&maps.out[0], dgu, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
+        if ((r = make_tensor_map_bf16_store(&maps.out[1], dgu + c.f, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
+        if ((r = make_tensor_map_bf16_store(&maps.out[2], a, c.M, c.f, c.f)) != VT_OK) return r;
+        const EpiActGrad::Params ep{const_cast<float*>(saved), dgu, a, c.act};
         if ((r = gemm_launch<false, true, EpiActGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
     if (grad_x) {   // dx = dg Wg + du Wu: [M, d], summed over f twice
@@ -181,14 +204,14 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
         GemmParams p{};
         bool pair = false;
         p.n_prob = 1;
-        p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f), grad_x, 2, 3, k_blocks(c.f));
+        p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f), 2, 3, k_blocks(c.f));
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, true, false, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], dg, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wg, gemm_box_b(p, true, pair))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[2], du, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[3], wu, gemm_box_b(p, true, pair))) != VT_OK) return r;
-        if ((r = gemm_store(maps, p, pair, false, true, st)) != VT_OK) return r;
+        if ((r = gemm_store(maps, p, pair, false, true, &grad_x, st)) != VT_OK) return r;
     }
     // dWg = dg^T x, dWu = du^T x: [f, d]; dWd = dy^T a: [d, f]; all summed over the M rows
     GemmMaps maps{};
@@ -196,18 +219,24 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
     bool pair = false;
     const int nk = k_blocks(c.M);
     p.hdr = hdr;
-    if (grad_W_gate) p.prob[p.n_prob++] = problem(c.f, c.d, 0, 3, nk, grad_W_gate);
-    if (grad_W_up) p.prob[p.n_prob++] = problem(c.f, c.d, 1, 3, nk, grad_W_up);
-    if (grad_W_down) p.prob[p.n_prob++] = problem(c.d, c.f, 2, 4, nk, grad_W_down);
+    void* outs[kGemmMaxProblems];
+    auto add = [&](void* out, const GemmProblem& q) {
+        if (!out) return;
+        outs[p.n_prob] = out;
+        p.prob[p.n_prob++] = q;
+    };
+    add(grad_W_gate, problem(c.f, c.d, 0, 3, nk));
+    add(grad_W_up, problem(c.f, c.d, 1, 3, nk));
+    add(grad_W_down, problem(c.d, c.f, 2, 4, nk));
     if (p.n_prob == 0) return VT_OK;
-    if (!gemm_plan(&p, true, true, false, &pair)) return VT_ERR_SHAPE;
+    if (!gemm_plan(&p, true, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
     const int box_a = gemm_box_a(p, true), box_b = gemm_box_b(p, true, pair);
     if ((r = gemm_map(&maps.map[0], dg, box_a)) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[1], du, box_a)) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[2], dy, box_a)) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[3], x, box_b)) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[4], av, box_b)) != VT_OK) return r;
-    return gemm_store(maps, p, pair, true, true, st);
+    return gemm_store(maps, p, pair, true, true, outs, st);
 }
 
 }  // namespace vt

@@ -7,7 +7,7 @@
 namespace vt {
 
 // Shared memory of a plan whose tile shape is chosen; false if it does not fit.
-static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t scratch_bytes = 0) {
+static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t scratch_bytes) {
     int max_m = 0;
     for (int i = 0; i < p->n_prob; ++i) max_m = std::max(max_m, p->prob[i].M);
     const int tile_rows = 128 / p->rep;
@@ -16,17 +16,17 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
     p->tx_bytes = p->a_rows * 128u * (uint32_t)p->rep + p->b_bytes;
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
-    // A hand-over of a stage costs the issuing threads some 300 cycles, more than the MMAs of a k-block on a narrow tile: as
-    // many k-blocks per stage as leave three stages, at most four.
-    p->kbs = std::max(1, std::min(4, (int)(72 * 1024 / p->blk_bytes)));
-    p->stage_bytes = p->blk_bytes * (uint32_t)p->kbs;
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
     const size_t partial = p->splits > 1 ? (size_t)std::min(tile_rows, max_m) * (p->NT + 4) * 4 : 0;
-    // an MMA reads 128 rows of A wherever they end
-    const size_t over = 16384 - p->a_bytes;
-    p->n_stages = std::min<int>(kGemmMaxStages, (int)((kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - scratch_bytes - over) / p->stage_bytes));
+    const size_t over = 16384 - p->a_bytes;      // an MMA reads 128 rows of A wherever they end
+    const size_t room = kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - scratch_bytes - over;
+    // A hand-over of a stage costs the issuing threads some 300 cycles, more than the MMAs of a k-block on a narrow tile: as
+    // many k-blocks per stage as leave three stages, at most four.
+    p->kbs = std::max(1, std::min(4, (int)(room / (3 * p->blk_bytes))));
+    p->stage_bytes = p->blk_bytes * (uint32_t)p->kbs;
+    p->n_stages = std::min<int>(kGemmMaxStages, (int)(room / p->stage_bytes));
     if (p->n_stages < 2) return false;
-    p->scratch_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes + over, partial), 128);
+    p->scratch_off = (uint32_t)round_up(std::max((size_t)p->n_stages * p->stage_bytes + over, partial), 1024);
     p->bar_off = p->scratch_off + scratch_bytes;
     p->total_smem = (uint32_t)(p->bar_off + bar_bytes + 1024);
     // D fp32, A and B bf16, M = 128 (a pair: 256), N; bits 15 and 16: A, B MN-major
@@ -92,7 +92,6 @@ struct PlanCache {
             r.prob[i].b0 = p->prob[i].b0;
             r.prob[i].a1 = p->prob[i].a1;
             r.prob[i].b1 = p->prob[i].b1;
-            r.prob[i].out = p->prob[i].out;
         }
         *p = r;
     }
@@ -150,8 +149,8 @@ static int cluster_slots(int size) {
 // column (128 rows; a pair the same); the issuing threads take some 120 for the MMAs and copies and share 300 per stage; the
 // operands come in at about 55 bytes a cycle from L2, and weights from HBM at 24 bytes a cycle and SM when all of them
 // stream.  Each round of tiles adds its fill, the last its read-out, and splits the exchange of their partial sums.
-bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
-    const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0));
+bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_bytes, bool* pair_out) {
+    const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0) | (int)scratch_bytes << 4);
     if (g_plans.find(key, p, pair_out)) return true;
     int maxM = 0, max_nk = 0;
     for (int i = 0; i < p->n_prob; ++i) {
@@ -196,7 +195,7 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair_out) {
     p->splits = best_splits;
     p->rep = 1;
     *pair_out = best_pair;
-    if (!gemm_number_items(p, best_pair) || !gemm_layout(p, a_mn, b_mn, best_pair)) return false;
+    if (!gemm_number_items(p, best_pair) || !gemm_layout(p, a_mn, b_mn, best_pair, scratch_bytes)) return false;
     g_plans.keep(key, *p, best_pair);
     return true;
 }
@@ -240,11 +239,16 @@ bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair_out) {
 
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair) { return b_mn ? 64 : (pair || p.dual) ? p.NT / 2 : p.NT; }
 
-vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, cudaStream_t st) {
-    const EpiStore::Params none{};
-    if (!a_mn && !b_mn) return gemm_launch<false, false, EpiStore>(maps, p, pair, none, st);
-    if (!a_mn) return gemm_launch<false, true, EpiStore>(maps, p, pair, none, st);
-    return gemm_launch<true, true, EpiStore>(maps, p, pair, none, st);
+vt_status gemm_store(GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st) {
+    EpiStore::Params ep{};
+    for (int i = 0; i < p.n_prob; ++i) {
+        ep.out[i] = reinterpret_cast<uint16_t*>(out[i]);
+        const vt_status r = make_tensor_map_bf16_store(&maps.out[i], out[i], p.prob[i].M, p.prob[i].N, p.prob[i].N);
+        if (r != VT_OK) return r;
+    }
+    if (!a_mn && !b_mn) return gemm_launch<false, false, EpiStore>(maps, p, pair, ep, st);
+    if (!a_mn) return gemm_launch<false, true, EpiStore>(maps, p, pair, ep, st);
+    return gemm_launch<true, true, EpiStore>(maps, p, pair, ep, st);
 }
 
 }  // namespace vt

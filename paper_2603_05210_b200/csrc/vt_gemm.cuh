@@ -17,6 +17,8 @@
 //           compute on whatever shared memory holds and land in lanes nobody reads.  For an epilogue with work to do per
 //           column (scoring) the tile can hold at most 64 (32) rows of A two (four) times, one copy per group of TMEM
 //           lanes: every epilogue warp then finds rows, each copy taking its own share of the columns.
+// bf16 results leave through shared memory: a warp lays 32 rows x 32 columns out in a swizzled buffer and TMA stores them.  A
+// thread's own 16-byte stores, 32 rows apart, held the tiles of short sums (dW of 300 rows) to 1.3 TB/s.
 //   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile, lays its partial sums out in
 //           shared memory, and each CTA adds up and finishes its share of the columns through distributed shared
 //           memory, in the order of the CTAs: no atomics, the same bits every time.
@@ -36,6 +38,7 @@ constexpr int kGemmThreads = (kGemmEpiWarps + 2) * 32;
 constexpr int kGemmMaxStages = 16;
 constexpr int kGemmMaxProblems = 3;
 constexpr int kGemmMaxMaps = 6;
+constexpr int kGemmMaxOuts = 3;             // bf16 matrices a launch writes
 constexpr int kGemmGroupRows = 8;           // row tiles that share their column tiles before the next group (L2 reuse)
 constexpr int kGemmSms = 148;               // the plans are made for this many SMs; a device with fewer runs them in more waves
 
@@ -46,11 +49,11 @@ struct GemmProblem {
     int tiles_m, chunks_n;       // row tiles; items along the columns
     int tiles_n;                 // column tiles
     int first_item;
-    void* out;                   // for epilogues that just store
 };
 
 struct GemmMaps {
     CUtensorMap map[kGemmMaxMaps];
+    CUtensorMap out[kGemmMaxOuts];   // [problem * outputs of the epilogue + output]
 };
 
 struct GemmParams {
@@ -152,6 +155,10 @@ struct AccColumns {
     }
 };
 
+// Staging of bf16 results: per warp two buffers of 32 rows x 32 columns for each output.
+constexpr uint32_t kStageBytes = 32 * 64;
+constexpr uint32_t gemm_stage_bytes(int outs) { return kGemmEpiWarps * 2 * (uint32_t)outs * kStageBytes; }
+
 // Eight fp32 values as bf16 (nearest-even) to a 16-byte aligned address.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
@@ -162,24 +169,40 @@ __device__ __forceinline__ void store_bf16x8(uint16_t* at, const float* x) {
     *reinterpret_cast<uint4*>(at) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
-// Epilogue that rounds the sums once to bf16 and stores them row-major, N columns a row (N a multiple of 8).
+__device__ __forceinline__ void st_shared_bf16x8(uint32_t at, const float (&x)[8]) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(pack_bf16(x[0], x[1])), "r"(pack_bf16(x[2], x[3])),
+                 "r"(pack_bf16(x[4], x[5])), "r"(pack_bf16(x[6], x[7])) : "memory");
+}
+
+// Epilogue that rounds the sums once to bf16 and stores them row-major.
 struct EpiStore {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
-    struct Params {};
+    static constexpr int kOuts = 1;
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
+    struct Params {
+        uint16_t* out[kGemmMaxProblems];      // [M, N] of each product
+    };
     struct State {};
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    // eight consecutive columns of one row, all inside D
-    static __device__ __forceinline__ void cols8(State&, const Params&, const GemmProblem& q, int m, int n, const float* x) {
-        store_bf16x8(reinterpret_cast<uint16_t*>(q.out) + (size_t)m * q.N + n, x);
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void cols8(State&, const Params&, const GemmProblem&, int, int, int, const float (&x)[8], const float (&)[8], float (&out)[1][8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[0][i] = x[i];
+    }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int prob, int, int m, int n) {
+        return ep.out[prob] + (size_t)m * q.N + n;
     }
 };
 
-// An epilogue provides
-//   kDual       its columns come in two halves: cols8(..., x, y) gets eight columns of either
+// An epilogue provides kDual (its columns come in two halves) and either
 //   kStateful   it works through all tiles of an item with a state of its own (never with splits): begin(), then tile() per
 //               tile with its share of the columns, in runs of 16 that it reads through an AccColumns, then end()
-//   row()       called once per tile and row before its columns (stateless only)
+// or kOuts bf16 matrices, each value from its own column(s):
+//   row()       once per tile and row, before the accumulator is waited for
+//   ahead()     before each run of 16 columns and one run in advance: requests what cols8 will need for it
+//   cols8()     eight columns (of either half): out[o][i] are the values to round and store
+//   at()        where output o's row m, column n lies
 template <bool PAIR, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p,
@@ -427,8 +450,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         const int r = (quad * 32 + lane) & (tile_rows - 1);        // the thread's row
         const int part = (warp >> 2) * p.rep + (quad * 32) / tile_rows, parts = 2 * p.rep;
         const int cols = Epi::kDual ? p.NT >> 1 : p.NT;            // columns of D in a tile
-        const int nch = (cols + 15) >> 4;
-        const int ch0 = part * nch / parts, ch1 = (part + 1) * nch / parts;   // runs of 16 columns this thread takes
+        const int nch = (cols + 15) >> 4, ng = (cols + 31) >> 5;
+        const int ch0 = part * nch / parts, ch1 = (part + 1) * nch / parts;   // runs of 16 columns this thread takes,
+        const int g0 = part * ng / parts, g1 = (part + 1) * ng / parts;       // or of 32 where they are stored in bulk
+        constexpr uint32_t kStageBufs = 2;
+        const uint32_t stage_at = base + p.scratch_off + (uint32_t)warp * (Epi::kScratch / kGemmEpiWarps);
+        uint32_t n_staged = 0;
         int n = 0;
         for (int item = cluster; item < p.n_items; item += n_clusters) {
             const GemmItem it = gemm_item(p, item);
@@ -438,6 +465,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             if constexpr (Epi::kStateful) Epi::begin(st, ep, m);
             for (int t = 0; t < it.n_tiles; ++t, ++n) {
                 const int buf = n & 1;
+                const int col0 = (it.nt0 + t) * cols;
+                if constexpr (!Epi::kStateful) {
+                    if (p.splits == 1 && m < q.M) {
+                        Epi::row(st, ep, q, m);
+                        Epi::ahead(st, ep, q, m, col0 + g0 * 32);
+                    }
+                }
                 bool got = false;
                 if (!__any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // warp-uniform: tcgen05.ld needs the whole warp
                     got = __all_sync(0xFFFFFFFFu, mbar_wait(bar_accf + 8u * buf, (uint32_t)(n >> 1) & 1u));
@@ -446,7 +480,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 if (!got) continue;
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)buf * p.acc_cols;
-                const int col0 = (it.nt0 + t) * cols;
                 if (p.splits > 1) {
                     // partial sums to shared memory (the ring is idle: its last k-block has been multiplied)
                     float* part_row = reinterpret_cast<float*>(smem) + (size_t)r * (p.NT + 4);
@@ -460,25 +493,55 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     }
                 } else if constexpr (Epi::kStateful) {
                     Epi::tile(st, ep, m, AccColumns{taddr, ch0, ch1, col0, q.N}, smem + p.scratch_off);
-                } else {
-                    if (m < q.M) Epi::row(st, ep, q, m);
-                    for (int ch = ch0; ch < ch1; ++ch) {
-                        const int c = col0 + ch * 16;
-                        uint32_t u[16], w[16];
-                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
-                        if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + ch * 16), w);
-                        tc_wait_ld();
+                } else if (m - lane < q.M) {                       // some row of this warp exists
+                    for (int g = g0; g < g1; ++g) {
+                        const bool staged = g * 32 + 32 <= cols;   // a shorter last run would reach into the next tile's columns
+                        const uint32_t buf_at = stage_at + (n_staged & (kStageBufs - 1)) * (uint32_t)(Epi::kOuts * kStageBytes);
+                        if (staged) {
+                            if (elect_one()) bulk_wait_read<kStageBufs - 1>();     // the buffer's last copy has been read
+                            __syncwarp();
+                        }
 #pragma unroll
-                        for (int e = 0; e < 16; e += 8) {
-                            if (m >= q.M || ch * 16 + e >= cols || c + e >= q.N) continue;
-                            float x[8], y[8];
+                        for (int h = 0; h < 32; h += 16) {
+                            const int c = g * 32 + h;
+                            if (c >= cols) break;
+                            uint32_t u[16], w[16];
+                            acc_ld16(taddr + (uint32_t)c, u);
+                            if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + c), w);
+                            tc_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                x[i] = __uint_as_float(u[e + i]);
-                                if constexpr (Epi::kDual) y[i] = __uint_as_float(w[e + i]);
+                            for (int e = 0; e < 16; e += 8) {
+                                if (c + e >= cols) break;          // the other half, or the next tile's
+                                float x[8], y[8], out[Epi::kOuts][8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    x[i] = __uint_as_float(u[e + i]);
+                                    y[i] = Epi::kDual ? __uint_as_float(w[e + i]) : 0.0f;
+                                }
+                                Epi::cols8(st, ep, q, m, col0 + c + e, e, x, y, out);
+#pragma unroll
+                                for (int o = 0; o < Epi::kOuts; ++o) {
+                                    if (staged)
+                                        st_shared_bf16x8(buf_at + (uint32_t)o * kStageBytes + (uint32_t)lane * 64u +
+                                                         (((uint32_t)(h + e) >> 3 ^ ((uint32_t)lane >> 1 & 3u)) << 4), out[o]);
+                                    else if (m < q.M && col0 + c + e < q.N)
+                                        store_bf16x8(Epi::at(ep, q, it.prob, o, m, col0 + c + e), out[o]);
+                                }
                             }
-                            if constexpr (Epi::kDual) Epi::cols8(st, ep, q, m, c + e, x, y);
-                            else Epi::cols8(st, ep, q, m, c + e, x);
+                            if (m < q.M) Epi::ahead(st, ep, q, m, col0 + c + 16);
+                        }
+                        if (staged) {
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int o = 0; o < Epi::kOuts; ++o)
+                                    tma_store_2d(&maps.out[it.prob * Epi::kOuts + o], col0 + g * 32, m - lane,
+                                                 buf_at + (uint32_t)o * kStageBytes);
+                                bulk_commit();
+                            }
+                            __syncwarp();
+                            ++n_staged;
                         }
                     }
                 }
@@ -490,6 +553,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 }
             }
             if constexpr (Epi::kStateful) Epi::end(st, ep, m, it.nt0 / p.tiles_per_item * parts + part);
+        }
+        if constexpr (!Epi::kStateful) {
+            if (elect_one()) bulk_wait_all();                      // what is on its way has arrived before the CTA is gone
+            __syncwarp();
         }
     }
 
@@ -505,11 +572,15 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 const int g0 = (int)rank * (cols >> 3) / p.splits, g1 = ((int)rank + 1) * (cols >> 3) / p.splits;   // runs of 8 columns
                 const uint32_t pitch = (uint32_t)(p.NT + 4) * 4u;
                 for (int e = tid; e < rows * (g1 - g0); e += kGemmEpiWarps * 32) {
-                    const int g = e / rows, r = e - g * rows, c = (g0 + g) * 8;
+                    const int r = e / (g1 - g0), g = e - r * (g1 - g0), c = (g0 + g) * 8;
                     const int col = it.nt0 * cols + c, m = it.mt * 128 + r;
                     if (col >= q.N) continue;
-                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    typename Epi::State st;
+                    Epi::row(st, ep, q, m);
+                    Epi::ahead(st, ep, q, m, col);
+                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0}, out[Epi::kOuts][8];
                     const uint32_t at = base + (uint32_t)r * pitch + (uint32_t)c * 4u;
+#pragma unroll 4
                     for (int s = 0; s < p.splits; ++s) {
                         const uint32_t from = cluster_map_shared(at, (uint32_t)s);
                         const float4 v0 = ld_cluster_f4(from), v1 = ld_cluster_f4(from + 16u);
@@ -521,10 +592,9 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                             y[4] += w1.x; y[5] += w1.y; y[6] += w1.z; y[7] += w1.w;
                         }
                     }
-                    typename Epi::State st;
-                    Epi::row(st, ep, q, m);
-                    if constexpr (Epi::kDual) Epi::cols8(st, ep, q, m, col, x, y);
-                    else Epi::cols8(st, ep, q, m, col, x);
+                    Epi::cols8(st, ep, q, m, col, 0, x, y, out);
+#pragma unroll
+                    for (int o = 0; o < Epi::kOuts; ++o) store_bf16x8(Epi::at(ep, q, it.prob, o, m, col), out[o]);
                 }
             }
             cluster_sync_all();                                    // nobody leaves while its partial sums may be read
@@ -570,15 +640,17 @@ inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 
 // Chooses tile shape, CTA pairs and k-splits for the products in p->prob (M, N, nk0, nk1 set) and fills in the rest of p
 // except the maps' indices, outputs and hdr.  False when the work is too large to number its tiles.
-bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, bool* pair);
+// scratch_bytes: the epilogue's kScratch.
+bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_bytes, bool* pair);
 // The same for token scoring: one product, both operands K-major, whole k range in every CTA, `tiles_per_item` tiles in a row.
 bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair);
 // Rows of the box each operand's tensor map has (64 columns wide; MN-major operands: 64).
 inline int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : (int)p.a_rows; }
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);
 
-// One or more products whose sums are rounded once to bf16 and stored (p->prob[i].out), operands of the given majors.
-vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, cudaStream_t st);
+// One or more products whose sums are rounded once to bf16 and stored in out[i] (row-major, N columns a row), operands of the
+// given majors.  Adds the outputs' maps.
+vt_status gemm_store(GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st);
 
 // A bf16 matrix operand in global memory: rows x cols, rows ld elements apart.
 struct GemmOperand {

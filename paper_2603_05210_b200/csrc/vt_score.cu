@@ -42,6 +42,7 @@ template <int KR>
 struct EpiScore {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = true;
+    static constexpr int kOuts = 0;
     static constexpr uint32_t kScratch = KR > 0 ? kListQueue * kGemmEpiWarps * 32 * 5 : 0;
     struct Params {
         const int32_t* tokens;

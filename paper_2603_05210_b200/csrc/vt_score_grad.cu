@@ -16,6 +16,8 @@ namespace vt {
 struct EpiScoreGrad {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
+    static constexpr int kOuts = 1;
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
         const int32_t* tokens;
         const float *lse, *entropy, *grad_logprobs, *grad_entropy;
@@ -35,18 +37,19 @@ struct EpiScoreGrad {
         st.ge = ep.grad_entropy ? ep.scale * ep.grad_entropy[m] : 0.0f;
         st.H = ep.grad_entropy ? ep.entropy[m] : 0.0f;
     }
-    static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int m, int n, const float* x) {
-        float g[8];
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int, int n, int, const float (&x)[8],
+                                                 const float (&)[8], float (&out)[1][8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float logp = fmaf(ep.scale, x[i], -st.lse);
             const float p = ex2_approx(logp * kLog2e);
-            g[i] = -p * fmaf(st.ge, logp + st.H, st.gl);
-            if (n + i == st.tok) g[i] += st.gl;
-            if (st.tok < 0) g[i] = 0.0f;
+            float g = -p * fmaf(st.ge, logp + st.H, st.gl);
+            if (n + i == st.tok) g += st.gl;
+            out[0][i] = st.tok < 0 ? 0.0f : g;
         }
-        store_bf16x8(ep.G + (size_t)m * ep.ld + n, g);
     }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem&, int, int, int m, int n) { return ep.G + (size_t)m * ep.ld + n; }
 };
 
 // The hidden states with the rows that are not scored set to zero.  Bound by its bytes: 4 d per row.
@@ -90,9 +93,10 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         p.prob[0].b0 = 1;
         p.prob[0].nk0 = ceil_div(c.d, kBoxK);
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, false, false, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, false, false, EpiScoreGrad::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, false, pair))) != VT_OK) return r;
+        if ((r = make_tensor_map_bf16_store(&maps.out[0], G, c.M, p.prob[0].N, ld)) != VT_OK) return r;
         const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, ld, c.scale, c.V};
         if ((r = gemm_launch<false, false, EpiScoreGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
@@ -105,12 +109,11 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         p.prob[0].N = c.d;
         p.prob[0].b0 = 1;
         p.prob[0].nk0 = ceil_div(c.V, kBoxK);
-        p.prob[0].out = grad_h;
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, true, false, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], g, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, true, pair))) != VT_OK) return r;
-        if ((r = gemm_store(maps, p, pair, false, true, st)) != VT_OK) return r;
+        if ((r = gemm_store(maps, p, pair, false, true, &grad_h, st)) != VT_OK) return r;
     }
     if (!grad_W) return VT_OK;
     {
@@ -131,12 +134,11 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
     p.prob[0].N = c.d;
     p.prob[0].b0 = 1;
     p.prob[0].nk0 = ceil_div(c.M, kBoxK);
-    p.prob[0].out = grad_W;
     p.hdr = hdr;
-    if (!gemm_plan(&p, true, true, false, &pair)) return VT_ERR_SHAPE;
+    if (!gemm_plan(&p, true, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
     if ((r = gemm_map(&maps.map[0], g, gemm_box_a(p, true))) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[1], GemmOperand{h0, c.M, c.d, c.d}, gemm_box_b(p, true, pair))) != VT_OK) return r;
-    return gemm_store(maps, p, pair, true, true, st);
+    return gemm_store(maps, p, pair, true, true, &grad_W, st);
 }
 
 }  // namespace vt
