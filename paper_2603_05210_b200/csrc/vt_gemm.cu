@@ -11,15 +11,19 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     int max_m = 0;
     for (int i = 0; i < p->n_prob; ++i) max_m = std::max(max_m, p->prob[i].M);
     const int tile_rows = 128 / p->rep;
+    if (p->splits > 1) scratch_bytes = 0;        // its results are not staged
     p->a_rows = (uint32_t)(a_mn ? 128 : std::min(tile_rows, (int)round_up(max_m, 8)));
     p->a_bytes = p->rep > 1 ? 16384u : p->a_rows * 128u;
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
     p->tx_bytes = p->a_rows * 128u * (uint32_t)p->rep + p->b_bytes;
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
-    const size_t partial = p->splits > 1 ? (size_t)std::min(tile_rows, max_m) * (p->NT + 4) * 4 : 0;
+    const int groups = (p->dual ? p->NT / 2 : p->NT) / 8;
+    p->x_cols = ceil_div(groups, p->splits) * (p->dual ? 16 : 8);
+    p->x_part = (uint32_t)(std::min(128, max_m) * (p->x_cols + 4) * 4);
+    const size_t partial = p->splits > 1 ? (size_t)p->x_part * p->splits : 0;
     const size_t over = 16384 - p->a_bytes;      // an MMA reads 128 rows of A wherever they end
-    const size_t room = kMaxDynSmem - 1024 - round_up(bar_bytes, 128) - scratch_bytes - over;
+    const size_t room = kMaxDynSmem - 2048 - round_up(bar_bytes, 128) - scratch_bytes - over;
     // A hand-over of a stage costs the issuing threads some 300 cycles, more than the MMAs of a k-block on a narrow tile: as
     // many k-blocks per stage as leave three stages, at most four.
     p->kbs = std::max(1, std::min(4, (int)(room / (3 * p->blk_bytes))));
@@ -145,10 +149,11 @@ static int cluster_slots(int size) {
     return n;
 }
 
-// Time of a plan in SM cycles, to compare plans with.  Per 64-deep k-block: the tensor core takes 2 cycles per accumulator
-// column (128 rows; a pair the same); the issuing threads take some 120 for the MMAs and copies and share 300 per stage; the
-// operands come in at about 55 bytes a cycle from L2, and weights from HBM at 24 bytes a cycle and SM when all of them
-// stream.  Each round of tiles adds its fill, the last its read-out, and splits the exchange of their partial sums.
+// Time of a plan in SM cycles, to compare plans with.  Per 64-deep k-block the tensor core takes 2 cycles per accumulator
+// column (128 rows; a pair the same); the issuing threads take some 250 for the MMAs and copies of a narrow tile and share
+// 400 per stage; an SM takes in 40 bytes a cycle from HBM and 58 from L2 (measured with 22 and with 148 CTAs at work), and
+// weights stream at 24 bytes a cycle and SM when all of them take part.  Each round of tiles adds its fill, the last its
+// read-out, and splits the exchange of their partial sums.
 bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_bytes, bool* pair_out) {
     const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0) | (int)scratch_bytes << 4);
     if (g_plans.find(key, p, pair_out)) return true;
@@ -172,16 +177,16 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_
                 tiles += (long long)ceil_div(p->prob[i].M, pair ? 256 : 128) * ceil_div(p->prob[i].N, cols);
             const double a_rows = std::min(128, maxM);
             const double blk = (a_rows + (pair ? nt / 2 : nt)) * 128.0;
-            const double per_stage = std::max(1.0, std::min(4.0, floor(72.0 * 1024 / blk)));
-            const double issue = std::max(2.0 * nt, 120.0 + 300.0 / per_stage);
-            for (int s = 1; s <= (pair ? 1 : std::min(8, max_nk)); ++s) {
+            const double per_stage = std::max(1.0, std::min(4.0, floor(64.0 * 1024 / blk)));
+            const double issue = std::max(2.0 * nt, 250.0 + 400.0 / per_stage);
+            for (int s = 1; s <= (pair ? 1 : std::min(std::min(8, max_nk), cols / 8)); ++s) {      // every CTA a k-block and a run of columns
                 const long long slots = pair ? kGemmSms / 2 : cluster_slots(s);
                 const double rounds = (double)((tiles + slots - 1) / slots);
                 const double busy = std::min(1.0, (double)tiles / (double)slots);
-                double per_kb = std::max(issue, blk / 55.0);
+                double per_kb = std::max(issue, blk / (maxM <= 256 ? 40.0 : 58.0));
                 per_kb = std::max(per_kb, nt * 128.0 * (pair ? 0.5 : 1.0) / 24.0 * (maxM <= 256 ? busy : 0.0));
-                const double tail = 1500.0 + 12.0 * cols + (s > 1 ? 2500.0 + 4.0 * nt : 0.0);
-                const double cost = rounds * (ceil_div(max_nk, s) * per_kb + (s > 1 ? 4000.0 : 1200.0)) + tail;
+                const double tail = 1500.0 + 12.0 * cols;
+                const double cost = rounds * (ceil_div(max_nk, s) * per_kb + (s > 1 ? 5000.0 : 1200.0)) + tail;
                 if (best < 0 || cost < best) {
                     best = cost;
                     best_nt = nt;

@@ -19,9 +19,9 @@
 //           lanes: every epilogue warp then finds rows, each copy taking its own share of the columns.
 // bf16 results leave through shared memory: a warp lays 32 rows x 32 columns out in a swizzled buffer and TMA stores them.  A
 // thread's own 16-byte stores, 32 rows apart, held the tiles of short sums (dW of 300 rows) to 1.3 TB/s.
-//   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile, lays its partial sums out in
-//           shared memory, and each CTA adds up and finishes its share of the columns through distributed shared
-//           memory, in the order of the CTAs: no atomics, the same bits every time.
+//   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile.  Each CTA owns a share of the
+//           columns: the others write their partial sums of it into its shared memory, and it adds them up in the order
+//           of the CTAs and finishes them: no atomics, the same bits every time.
 // The CTAs are persistent (except with splits).  Warps 0-7: epilogue, warp 8: TMA producer, warp 9: MMA issuer; two
 // accumulators in tensor memory, so the epilogue of a tile runs under the MMAs of the next.
 // All waits are bounded; one that runs out sets the workspace's status word and the CTA unwinds.
@@ -64,6 +64,8 @@ struct GemmParams {
     int dual;                    // 1: columns [0, NT/2) from map b0, [NT/2, NT) from map b1, the same rows of both
     int rep;                     // copies of A's rows in a tile: 1, 2 or 4 (single only)
     int splits;                  // CTAs that share one tile's k range (single only)
+    int x_cols;                  // with splits: columns (of both halves) a CTA owns at most
+    uint32_t x_part;             // ... and the bytes of partial sums it gets from each CTA, over the ring
     int n_stages;
     int kbs;                     // k-blocks per ring stage
     uint32_t a_rows;             // rows of A's box (K-major); `rep` of them, 128 / rep rows apart
@@ -117,10 +119,8 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity)) != 0;
 }
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 __device__ __forceinline__ GemmItem gemm_item(const GemmParams& p, int item) {
@@ -155,9 +155,10 @@ struct AccColumns {
     }
 };
 
-// Staging of bf16 results: per warp two buffers of 32 rows x 32 columns for each output.
+// Staging of bf16 results: per warp 32 rows x 32 columns for each output, two buffers of it for a single output.
 constexpr uint32_t kStageBytes = 32 * 64;
-constexpr uint32_t gemm_stage_bytes(int outs) { return kGemmEpiWarps * 2 * (uint32_t)outs * kStageBytes; }
+constexpr uint32_t gemm_stage_bufs(int outs) { return outs > 1 ? 1u : 2u; }
+constexpr uint32_t gemm_stage_bytes(int outs) { return kGemmEpiWarps * gemm_stage_bufs(outs) * (uint32_t)outs * kStageBytes; }
 
 // Eight fp32 values as bf16 (nearest-even) to a 16-byte aligned address.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -453,7 +454,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         const int nch = (cols + 15) >> 4, ng = (cols + 31) >> 5;
         const int ch0 = part * nch / parts, ch1 = (part + 1) * nch / parts;   // runs of 16 columns this thread takes,
         const int g0 = part * ng / parts, g1 = (part + 1) * ng / parts;       // or of 32 where they are stored in bulk
-        constexpr uint32_t kStageBufs = 2;
+        constexpr uint32_t kStageBufs = gemm_stage_bufs(Epi::kOuts);
         const uint32_t stage_at = base + p.scratch_off + (uint32_t)warp * (Epi::kScratch / kGemmEpiWarps);
         uint32_t n_staged = 0;
         int n = 0;
@@ -478,20 +479,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     if (!got) fail();
                 }
                 if (!got) continue;
+                if (p.splits > 1) break;                           // the tile is finished below, with the rest of the cluster
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)buf * p.acc_cols;
-                if (p.splits > 1) {
-                    // partial sums to shared memory (the ring is idle: its last k-block has been multiplied)
-                    float* part_row = reinterpret_cast<float*>(smem) + (size_t)r * (p.NT + 4);
-                    for (int ch = part * (p.NT >> 4) / parts; ch < (part + 1) * (p.NT >> 4) / parts; ++ch) {
-                        uint32_t u[16];
-                        acc_ld16(taddr + (uint32_t)(ch * 16), u);
-                        tc_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; e += 4)
-                            *reinterpret_cast<uint4*>(part_row + ch * 16 + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
-                    }
-                } else if constexpr (Epi::kStateful) {
+                if constexpr (Epi::kStateful) {
                     Epi::tile(st, ep, m, AccColumns{taddr, ch0, ch1, col0, q.N}, smem + p.scratch_off);
                 } else if (m - lane < q.M) {                       // some row of this warp exists
                     for (int g = g0; g < g1; ++g) {
@@ -562,32 +553,59 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
 
     if constexpr (!PAIR && !Epi::kStateful) {
         if (p.splits > 1) {
-            cluster_sync_all();                                    // every CTA's partial sums are in its shared memory
+            const GemmItem it = gemm_item(p, cluster);
+            const GemmProblem& q = p.prob[it.prob];
+            const int cols = Epi::kDual ? p.NT >> 1 : p.NT, groups = cols >> 3;
+            const int rows = min(128, q.M - it.mt * 128);
+            cluster_sync_all();                                    // every ring is idle: the sums go where it was
+            const int r = (warp & 3) * 32 + lane;
+            if (warp < kGemmEpiWarps && (warp & 3) * 32 < rows && __all_sync(0xFFFFFFFFu, *abort_flag == 0)) {
+                // partial sums to the owners of their columns, eight columns at a time
+                const uint32_t taddr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+                const int nch = (cols + 15) >> 4, half = warp >> 2;
+                for (int ch = half * nch / 2; ch < (half + 1) * nch / 2; ++ch) {
+                    uint32_t u[16], w[16];
+                    acc_ld16(taddr + (uint32_t)(ch * 16), u);
+                    if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + ch * 16), w);
+                    tc_wait_ld();
+                    if (r >= rows) continue;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        const int g = ch * 2 + (e >> 3);
+                        if (g >= groups) break;
+                        int owner = (int)((unsigned)(g * p.splits) / (unsigned)groups);
+                        if (g >= (owner + 1) * groups / p.splits) ++owner;     // shares are [owner * groups / splits, ...); splits <= groups
+                        const int local = g - owner * groups / p.splits;
+                        const uint32_t to = cluster_map_shared(base + rank * p.x_part, (uint32_t)owner) +
+                                            (uint32_t)(r * (p.x_cols + 4) + local * (Epi::kDual ? 16 : 8)) * 4u;
+                        st_cluster_v4(to, u[e], u[e + 1], u[e + 2], u[e + 3]);
+                        st_cluster_v4(to + 16u, u[e + 4], u[e + 5], u[e + 6], u[e + 7]);
+                        if constexpr (Epi::kDual) {
+                            st_cluster_v4(to + 32u, w[e], w[e + 1], w[e + 2], w[e + 3]);
+                            st_cluster_v4(to + 48u, w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
+                        }
+                    }
+                }
+            }
+            cluster_sync_all();                                    // every partial sum is where it belongs
             if (warp < kGemmEpiWarps && !*abort_flag) {
-                const GemmItem it = gemm_item(p, cluster);
-                const GemmProblem& q = p.prob[it.prob];
-                const int cols = Epi::kDual ? p.NT >> 1 : p.NT;
-                const int tile_rows = 128 / p.rep;
-                const int rows = min(tile_rows, q.M - it.mt * 128);
-                const int g0 = (int)rank * (cols >> 3) / p.splits, g1 = ((int)rank + 1) * (cols >> 3) / p.splits;   // runs of 8 columns
-                const uint32_t pitch = (uint32_t)(p.NT + 4) * 4u;
+                const int g0 = (int)rank * groups / p.splits, g1 = ((int)rank + 1) * groups / p.splits;   // this CTA's runs of 8 columns
                 for (int e = tid; e < rows * (g1 - g0); e += kGemmEpiWarps * 32) {
-                    const int r = e / (g1 - g0), g = e - r * (g1 - g0), c = (g0 + g) * 8;
-                    const int col = it.nt0 * cols + c, m = it.mt * 128 + r;
+                    const int er = e / (g1 - g0), g = e - er * (g1 - g0);
+                    const int col = it.nt0 * cols + (g0 + g) * 8, m = it.mt * 128 + er;
                     if (col >= q.N) continue;
                     typename Epi::State st;
                     Epi::row(st, ep, q, m);
                     Epi::ahead(st, ep, q, m, col);
                     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0}, out[Epi::kOuts][8];
-                    const uint32_t at = base + (uint32_t)r * pitch + (uint32_t)c * 4u;
-#pragma unroll 4
-                    for (int s = 0; s < p.splits; ++s) {
-                        const uint32_t from = cluster_map_shared(at, (uint32_t)s);
-                        const float4 v0 = ld_cluster_f4(from), v1 = ld_cluster_f4(from + 16u);
+                    const unsigned char* from = smem + (size_t)(er * (p.x_cols + 4) + g * (Epi::kDual ? 16 : 8)) * 4;
+                    for (int s = 0; s < p.splits; ++s, from += p.x_part) {
+                        const float4* f = reinterpret_cast<const float4*>(from);
+                        const float4 v0 = f[0], v1 = f[1];
                         x[0] += v0.x; x[1] += v0.y; x[2] += v0.z; x[3] += v0.w;
                         x[4] += v1.x; x[5] += v1.y; x[6] += v1.z; x[7] += v1.w;
                         if constexpr (Epi::kDual) {
-                            const float4 w0 = ld_cluster_f4(from + (uint32_t)cols * 4u), w1 = ld_cluster_f4(from + (uint32_t)cols * 4u + 16u);
+                            const float4 w0 = f[2], w1 = f[3];
                             y[0] += w0.x; y[1] += w0.y; y[2] += w0.z; y[3] += w0.w;
                             y[4] += w1.x; y[5] += w1.y; y[6] += w1.z; y[7] += w1.w;
                         }
@@ -597,7 +615,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     for (int o = 0; o < Epi::kOuts; ++o) store_bf16x8(Epi::at(ep, q, it.prob, o, m, col), out[o]);
                 }
             }
-            cluster_sync_all();                                    // nobody leaves while its partial sums may be read
         }
     }
 
