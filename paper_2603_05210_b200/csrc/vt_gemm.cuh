@@ -22,8 +22,8 @@
 //   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile.  Each CTA owns a share of the
 //           columns: the others write their partial sums of it into its shared memory, and it adds them up in the order
 //           of the CTAs and finishes them: no atomics, the same bits every time.
-// The CTAs are persistent (except with splits).  Warps 0-7: epilogue, warp 8: TMA producer, warp 9: MMA issuer; two
-// accumulators in tensor memory, so the epilogue of a tile runs under the MMAs of the next.
+// The CTAs are persistent (except with splits).  Warps 0-7: epilogue, warps 8 and 9: TMA producers, warp 10: MMA issuer;
+// two accumulators in tensor memory, so the epilogue of a tile runs under the MMAs of the next.
 // All waits are bounded; one that runs out sets the workspace's status word and the CTA unwinds.
 #pragma once
 
@@ -34,7 +34,8 @@
 namespace vt {
 
 constexpr int kGemmEpiWarps = 8;
-constexpr int kGemmThreads = (kGemmEpiWarps + 2) * 32;
+constexpr int kGemmProducers = 2;           // they take the ring's stages in turn: issuing a stage's copies takes one warp 700 cycles
+constexpr int kGemmThreads = (kGemmEpiWarps + kGemmProducers + 1) * 32;
 constexpr int kGemmMaxStages = 16;
 constexpr int kGemmMaxProblems = 3;
 constexpr int kGemmMaxMaps = 6;
@@ -214,7 +215,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
     unsigned char* smem = smem_raw + (base - raw);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    constexpr int kProducer = kGemmEpiWarps, kIssuer = kGemmEpiWarps + 1;
+    constexpr int kProducer = kGemmEpiWarps, kIssuer = kGemmEpiWarps + kGemmProducers;
     const int S = p.n_stages;
     const uint32_t rank = (PAIR || p.splits > 1) ? cluster_cta_rank() : 0u;
     const bool leader = !PAIR || rank == 0u;
@@ -281,8 +282,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         return !PAIR && q.tiles_m == 1 ? k0 + (int)((long long)(k1 - k0) * cluster / n_clusters) : k0;
     };
 
-    if (warp == kProducer) {
-        // ------------------------------------------------------------------ TMA producer
+    if (warp >= kProducer && warp < kIssuer) {
+        // ------------------------------------------------------------------ TMA producers
         // The whole warp runs the loop and one elected lane issues: with uniform control flow the copies' operands are formed
         // in uniform registers.  Everything the loop needs is read from the parameters ahead of it.
         {
@@ -314,9 +315,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     const int col0 = dual ? nt * half : nt * NT + (PAIR ? (int)rank * half : 0);   // first row of B this CTA fetches
                     int kb = kb_first;
                     for (int i = k0; i < k1; i += kbs) {
-                        if (wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u)) { fail(); ok = false; break; }
                         const int nb = min(kbs, k1 - i);
-                        if (elect_one()) {
+                        const bool mine = (issued & (kGemmProducers - 1)) == warp - kProducer;
+                        if (mine && wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u)) { fail(); ok = false; break; }
+                        if (mine && elect_one()) {
                             if (leader) mbar_arrive_expect_tx(bar_f, tx * (uint32_t)nb);
                             const uint32_t bar = bar_f + bar_shift;
                             auto load = [&](uint32_t to, const CUtensorMap* m, int cx, int cy) {
@@ -368,10 +370,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     }
                 }
             }
-            if (lane == 0 && leader && *abort_flag) {       // let copies in flight land before the CTA gives its shared memory back
+            if (lane == 0 && leader && *abort_flag) {       // let this warp's copies in flight land before the CTA gives its shared memory back
                 const unsigned long long deadline = global_timer_ns() + kWaitLimitNs;
                 for (int i = max(0, issued - S); i < issued; ++i)
-                    (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, deadline);
+                    if ((i & (kGemmProducers - 1)) == warp - kProducer) (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, deadline);
             }
         }
     } else if (warp == kIssuer) {
