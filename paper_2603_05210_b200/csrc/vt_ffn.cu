@@ -166,6 +166,7 @@ vt_status launch_ffn(const FfnCall& c, void* y, float* saved, void* workspace, c
     bool pair = false;
     p.n_prob = 1;
     p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f));
+    p.b_early = 1;
     p.hdr = reinterpret_cast<WsHeader*>(base);
     if (!gemm_plan(&p, false, false, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
     if ((r = gemm_map(&maps.map[0], GemmOperand{a, c.M, c.f, c.f}, gemm_box_a(p, false))) != VT_OK) return r;
@@ -205,6 +206,7 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
         bool pair = false;
         p.n_prob = 1;
         p.prob[0] = problem(c.M, c.d, 0, 1, k_blocks(c.f), 2, 3, k_blocks(c.f));
+        p.b_early = 1;
         p.hdr = hdr;
         if (!gemm_plan(&p, false, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], dg, gemm_box_a(p, false))) != VT_OK) return r;

@@ -91,6 +91,7 @@ struct PlanCache {
     static void take(const GemmParams& plan, GemmParams* p) {
         GemmParams r = plan;
         r.hdr = p->hdr;
+        r.b_early = p->b_early;
         for (int i = 0; i < p->n_prob; ++i) {
             r.prob[i].a0 = p->prob[i].a0;
             r.prob[i].b0 = p->prob[i].b0;

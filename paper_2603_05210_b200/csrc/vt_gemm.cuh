@@ -60,6 +60,10 @@ struct GemmMaps {
 struct GemmParams {
     GemmProblem prob[kGemmMaxProblems];
     int n_prob, n_items;
+    int b_early;                 // 1: B's first stages are fetched ahead of the dependency wait.  For a call's second product and
+                                 // later ones whose B the kernel just before does not write: every kernel here waits for its own
+                                 // predecessor before it lets its successor start, so whatever was written ahead of the call or
+                                 // by its earlier kernels is there.
     int tiles_per_item;          // consecutive column tiles of one row tile that a CTA takes in a row
     int NT;                      // accumulator columns of a tile
     int dual;                    // 1: columns [0, NT/2) from map b0, [NT/2, NT) from map b1, the same rows of both
@@ -262,8 +266,9 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     // Nothing above touches global memory (the tensor maps are kernel parameters): under programmatic dependent launch it
-    // overlaps the previous kernel's tail.  From here on that kernel's writes are visible.
-    grid_dependency_wait();
+    // overlaps the previous kernel's tail.
+    const bool producer = warp >= kProducer && warp < kIssuer;
+    if (!(p.b_early && producer)) grid_dependency_wait();
     if (tid == 0) grid_launch_dependents();
 
     auto fail = [&]() {
@@ -282,7 +287,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         return !PAIR && q.tiles_m == 1 ? k0 + (int)((long long)(k1 - k0) * cluster / n_clusters) : k0;
     };
 
-    if (warp >= kProducer && warp < kIssuer) {
+    if (producer) {
         // ------------------------------------------------------------------ TMA producers
         // The whole warp runs the loop and one elected lane issues: with uniform control flow the copies' operands are formed
         // in uniform registers.  Everything the loop needs is read from the parameters ahead of it.
@@ -300,6 +305,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             const bool b_once = !PAIR && !B_MN && p.prob[0].tiles_m == 1;
             const uint64_t once = l2_policy_evict_first();
             const uint32_t bar_shift = PAIR ? cluster_map_shared(base, 0u) - base : 0u;    // both CTAs' bytes count on the leader's barrier
+            int early = p.b_early ? 0 : -1;       // stages whose B is on its way before the dependency wait; -1: none to be
             for (int item = cluster; item < n_items && ok; item += n_clusters) {
                 const GemmItem it = gemm_item(p, item);
                 const GemmProblem& q = p.prob[it.prob];
@@ -313,45 +319,60 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 for (int t = 0; t < it.n_tiles && ok; ++t) {
                     const int nt = it.nt0 + t;
                     const int col0 = dual ? nt * half : nt * NT + (PAIR ? (int)rank * half : 0);   // first row of B this CTA fetches
+                    // one stage: nb k-blocks from kj on (wrapping at k1), to ring address `to`
+                    auto issue = [&](int kj, int nb, uint32_t to, uint32_t bar_local, bool with_a, bool with_b) {
+                        if (leader && with_b) mbar_arrive_expect_tx(bar_local, tx * (uint32_t)nb);
+                        const uint32_t bar = bar_local + bar_shift;
+                        auto load = [&](uint32_t at, const CUtensorMap* m, int cx, int cy) {
+                            if constexpr (PAIR) tma_load_2d_pair(at, m, cx, cy, bar);
+                            else tma_load_2d(at, m, cx, cy, bar);
+                        };
+                        for (int j = 0; j < nb; ++j, to += blk_bytes) {
+                            const bool second = kj >= nk0;
+                            const int x = (second ? kj - nk0 : kj) * kBoxK;
+                            const CUtensorMap *ma = second ? ma1 : ma0, *mb = second ? mb1 : mb0;
+                            const uint32_t dstb = to + a_bytes;
+                            if (with_b) {
+                                if constexpr (B_MN) {
+                                    for (uint32_t o = 0; o < b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
+                                } else if (b_once) {
+                                    tma_load_2d_hint(dstb, mb, x, col0, bar, once);
+                                    if (two_b) tma_load_2d_hint(dstb + (uint32_t)half * 128u, mb1, x, col0, bar, once);
+                                } else {
+                                    load(dstb, mb, x, col0);
+                                    if (two_b) load(dstb + (uint32_t)half * 128u, mb1, x, col0);
+                                }
+                            }
+                            if (with_a) {
+                                if constexpr (A_MN) {
+                                    load(to, ma, row0, x);
+                                    load(to + 8192u, ma, row0 + 64, x);
+                                } else {
+                                    for (int r = 0; r < rep; ++r) load(to + (uint32_t)r * a_box, ma, x, row0);
+                                }
+                            }
+                            if (++kj == k1) kj = k0;
+                        }
+                    };
+                    if (early == 0) {                           // the ring's first filling, as far as this tile goes
+                        int kj = kb_first;
+                        early = min(S, (k1 - k0 + kbs - 1) / kbs);
+                        for (int i = 0; i < early; ++i) {
+                            const int nb = min(kbs, k1 - k0 - i * kbs);
+                            if ((i & (kGemmProducers - 1)) == warp - kProducer && elect_one())
+                                issue(kj, nb, base + (uint32_t)i * stage_bytes, bar_full + 8u * i, false, true);
+                            __syncwarp();
+                            kj += nb;
+                            if (kj >= k1) kj -= k1 - k0;
+                        }
+                        grid_dependency_wait();
+                    }
                     int kb = kb_first;
                     for (int i = k0; i < k1; i += kbs) {
                         const int nb = min(kbs, k1 - i);
                         const bool mine = (issued & (kGemmProducers - 1)) == warp - kProducer;
                         if (mine && wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u)) { fail(); ok = false; break; }
-                        if (mine && elect_one()) {
-                            if (leader) mbar_arrive_expect_tx(bar_f, tx * (uint32_t)nb);
-                            const uint32_t bar = bar_f + bar_shift;
-                            auto load = [&](uint32_t to, const CUtensorMap* m, int cx, int cy) {
-                                if constexpr (PAIR) tma_load_2d_pair(to, m, cx, cy, bar);
-                                else tma_load_2d(to, m, cx, cy, bar);
-                            };
-                            uint32_t dsta = dst;
-                            int kj = kb;
-                            for (int j = 0; j < nb; ++j, dsta += blk_bytes) {
-                                const bool second = kj >= nk0;
-                                const int x = (second ? kj - nk0 : kj) * kBoxK;
-                                const CUtensorMap *ma = second ? ma1 : ma0, *mb = second ? mb1 : mb0;
-                                const uint32_t dstb = dsta + a_bytes;
-                                if constexpr (B_MN) {
-                                    for (uint32_t o = 0; o < b_bytes; o += 8192u) load(dstb + o, mb, col0 + (int)(o >> 7), x);
-                                } else {
-                                    if (b_once) {
-                                        tma_load_2d_hint(dstb, mb, x, col0, bar, once);
-                                        if (two_b) tma_load_2d_hint(dstb + (uint32_t)half * 128u, mb1, x, col0, bar, once);
-                                    } else {
-                                        load(dstb, mb, x, col0);
-                                        if (two_b) load(dstb + (uint32_t)half * 128u, mb1, x, col0);
-                                    }
-                                }
-                                if constexpr (A_MN) {
-                                    load(dsta, ma, row0, x);
-                                    load(dsta + 8192u, ma, row0 + 64, x);
-                                } else {
-                                    for (int r = 0; r < rep; ++r) load(dsta + (uint32_t)r * a_box, ma, x, row0);
-                                }
-                                if (++kj == k1) kj = k0;
-                            }
-                        }
+                        if (mine && elect_one()) issue(kb, nb, dst, bar_f, true, issued >= early);
                         __syncwarp();
                         ++issued;
                         kb += nb;

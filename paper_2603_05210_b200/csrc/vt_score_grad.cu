@@ -82,6 +82,15 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
     uint16_t* h0 = reinterpret_cast<uint16_t*>(base + kHeaderBytes + round_up((size_t)c.M * ld * 2, 256));
     const GemmOperand W{c.W, c.V, c.d, c.d}, g{G, c.M, c.V, ld};
     vt_status r;
+    if (grad_W) {   // h without the rows that are not scored
+        const long long n = (long long)c.M * (c.d >> 3);
+        const int grid = (int)std::min<long long>((n + 255) / 256, 8 * kGemmSms);
+        cudaError_t e = launch_pdl(score_rows_kernel, grid, 256, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
+                                   c.M, c.d, c.V, h0);
+        count_launch();
+        if (e == cudaSuccess) e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
     {   // G: [M, V], summed over d
         GemmMaps maps{};
         GemmParams p{};
@@ -109,6 +118,7 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         p.prob[0].N = c.d;
         p.prob[0].b0 = 1;
         p.prob[0].nk0 = ceil_div(c.V, kBoxK);
+        p.b_early = 1;
         p.hdr = hdr;
         if (!gemm_plan(&p, false, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], g, gemm_box_a(p, false))) != VT_OK) return r;
@@ -116,15 +126,6 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         if ((r = gemm_store(maps, p, pair, false, true, &grad_h, st)) != VT_OK) return r;
     }
     if (!grad_W) return VT_OK;
-    {
-        const long long n = (long long)c.M * (c.d >> 3);
-        const int grid = (int)std::min<long long>((n + 255) / 256, 8 * kGemmSms);
-        cudaError_t e = launch_pdl(score_rows_kernel, grid, 256, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
-                                   c.M, c.d, c.V, h0);
-        count_launch();
-        if (e == cudaSuccess) e = cudaGetLastError();
-        if (e != cudaSuccess) return cuda_fail(e);
-    }
     // dW = G^T h: [V, d], summed over the M rows
     GemmMaps maps{};
     GemmParams p{};
