@@ -21,21 +21,30 @@ namespace vt {
 struct ActValue {
     float value, slope;
 };
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // act(g) and act'(g).  SiLU: g s, s (1 + g (1 - s)) with s = 1 / (1 + e^-g).  GELU (tanh form): with b = sqrt(2/pi) (g +
-// 0.044715 g^3), (1 + tanh b) / 2 = 1 / (1 + e^-2b) = s, so act = g s and act' = s + g s (1 - s) * 2 b'.
-__device__ __forceinline__ ActValue act_eval(int act, float g) {
-    float b2 = g, slope2 = 1.0f;
-    if (act == VT_ACT_GELU) {
-        constexpr float k2 = 1.5957691216057308f;          // 2 sqrt(2 / pi)
-        b2 = k2 * g * fmaf(0.044715f * g, g, 1.0f);
-        slope2 = k2 * fmaf(0.134145f * g, g, 1.0f);
+// 0.044715 g^3), (1 + tanh b) / 2 = 1 / (1 + e^-2b) = s, so act = g s and act' = s (1 + g (1 - s) 2 b').  1 - s cancels only where
+// s is 1 to the last bit and the term it is in is nothing beside the 1.  The activation is a template parameter: a tile of da
+// spent more time on this than on its product when it was asked for element by element.
+template <int ACT>
+__device__ __forceinline__ ActValue act_eval(float g) {
+    constexpr float kLog2 = 1.4426950408889634f, k2 = 1.5957691216057308f;      // log2 e, 2 sqrt(2 / pi)
+    float s, gg = g;
+    if constexpr (ACT == VT_ACT_GELU) {
+        const float q = g * g;
+        s = rcp_approx(1.0f + ex2_approx(-kLog2 * k2 * g * fmaf(0.044715f, q, 1.0f)));
+        gg = g * (k2 * fmaf(0.134145f, q, 1.0f));
+        if (q > 1e4f) gg = 0.0f;                           // far out s is 0 or 1 and the term nothing, before it overflows
+    } else {
+        s = rcp_approx(1.0f + ex2_approx(-kLog2 * g));
     }
-    const float e = __expf(-b2);
-    const float s = __fdividef(1.0f, 1.0f + e);            // e = inf: 0
-    const float rest = b2 < -40.0f ? 1.0f : e * s;         // 1 - s without cancellation
     ActValue r;
     r.value = g * s;
-    r.slope = fmaf(g * s * rest, slope2, s);
+    r.slope = s * fmaf(gg, 1.0f - s, 1.0f);
     return r;
 }
 
@@ -47,6 +56,7 @@ __device__ __forceinline__ float* saved_at(float* saved, int M, int f2, int m, i
     return saved + (size_t)m0 * f2 + (size_t)(col >> 2) * (rows * 4) + (m - m0) * 4;
 }
 
+template <int ACT>
 struct EpiGateUp {
     static constexpr bool kDual = true;
     static constexpr bool kStateful = false;
@@ -55,15 +65,14 @@ struct EpiGateUp {
     struct Params {
         uint16_t* a;        // [M, f] bf16
         float* saved;       // see saved_at, or null
-        int act;
     };
     struct State {};
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int, int) {}
     static __device__ __forceinline__ void cols8(State&, const Params& ep, const GemmProblem& q, int m, int n, int, const float (&g)[8],
                                                  const float (&u)[8], float (&out)[1][8]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[0][i] = act_eval(ep.act, g[i]).value * u[i];
+        for (int i = 0; i < 8; ++i) out[0][i] = act_eval<ACT>(g[i]).value * u[i];
         if (ep.saved && m < q.M && n < q.N) {
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
@@ -75,6 +84,7 @@ struct EpiGateUp {
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int, int m, int n) { return ep.a + (size_t)m * q.N + n; }
 };
 
+template <int ACT>
 struct EpiActGrad {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
@@ -84,28 +94,27 @@ struct EpiActGrad {
         float* saved;           // see saved_at; only read
         uint16_t* dgu;          // [M, 2f] bf16: dg, then du
         uint16_t* a;            // [M, f] bf16
-        int act;
     };
     struct State {
-        float4 g[4], u[4];      // the next 16 columns
+        float4 g[2][4], u[2][4];      // the next two runs of 16 columns
     };
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    static __device__ __forceinline__ void ahead(State& st, const Params& ep, const GemmProblem& q, int m, int n) {
+    static __device__ __forceinline__ void ahead(State& st, const Params& ep, const GemmProblem& q, int m, int n, int slot) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (n + 4 * i < q.N) {
-                st.g[i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, n + 4 * i));
-                st.u[i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, q.N + n + 4 * i));
+                st.g[slot][i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, n + 4 * i));
+                st.u[slot][i] = *reinterpret_cast<const float4*>(saved_at(ep.saved, q.M, 2 * q.N, m, q.N + n + 4 * i));
             }
     }
     static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int, int, int e, const float (&da)[8],
                                                  const float (&)[8], float (&out)[3][8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float4 g4 = st.g[(e + i) >> 2], u4 = st.u[(e + i) >> 2];
+            const float4 g4 = st.g[e >> 4][(e & 15) + i >> 2], u4 = st.u[e >> 4][(e & 15) + i >> 2];
             const float g = (i & 3) == 0 ? g4.x : (i & 3) == 1 ? g4.y : (i & 3) == 2 ? g4.z : g4.w;
             const float u = (i & 3) == 0 ? u4.x : (i & 3) == 1 ? u4.y : (i & 3) == 2 ? u4.z : u4.w;
-            const ActValue v = act_eval(ep.act, g);
+            const ActValue v = act_eval<ACT>(g);
             out[0][i] = da[i] * u * v.slope;
             out[1][i] = da[i] * v.value;
             out[2][i] = v.value * u;
@@ -153,13 +162,14 @@ vt_status launch_ffn(const FfnCall& c, void* y, float* saved, void* workspace, c
         p.n_prob = 1;
         p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d), 0, 2, 0);
         p.hdr = reinterpret_cast<WsHeader*>(base);
-        if (!gemm_plan(&p, false, false, true, EpiGateUp::kScratch, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, false, true, EpiGateUp<VT_ACT_SILU>::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], x, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wg, gemm_box_b(p, false, pair))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[2], wu, gemm_box_b(p, false, pair))) != VT_OK) return r;
         if ((r = make_tensor_map_bf16_store(&maps.out[0], a, c.M, c.f, c.f)) != VT_OK) return r;
-        const EpiGateUp::Params ep{a, saved, c.act};
-        if ((r = gemm_launch<false, false, EpiGateUp>(maps, p, pair, ep, st)) != VT_OK) return r;
+        r = c.act == VT_ACT_GELU ? gemm_launch<false, false, EpiGateUp<VT_ACT_GELU>>(maps, p, pair, {a, saved}, st)
+                                 : gemm_launch<false, false, EpiGateUp<VT_ACT_SILU>>(maps, p, pair, {a, saved}, st);
+        if (r != VT_OK) return r;
     }
     GemmMaps maps{};
     GemmParams p{};
@@ -191,14 +201,16 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
         p.n_prob = 1;
         p.prob[0] = problem(c.M, c.f, 0, 1, k_blocks(c.d));
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, true, false, EpiActGrad::kScratch, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, true, false, EpiActGrad<VT_ACT_SILU>::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], dy, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wd, gemm_box_b(p, true, pair))) != VT_OK) return r;
         if ((r = make_tensor_map_bf16_store(&maps.out[0], dgu, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
         if ((r = make_tensor_map_bf16_store(&maps.out[1], dgu + c.f, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
         if ((r = make_tensor_map_bf16_store(&maps.out[2], a, c.M, c.f, c.f)) != VT_OK) return r;
-        const EpiActGrad::Params ep{const_cast<float*>(saved), dgu, a, c.act};
-        if ((r = gemm_launch<false, true, EpiActGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
+        float* kept = const_cast<float*>(saved);
+        r = c.act == VT_ACT_GELU ? gemm_launch<false, true, EpiActGrad<VT_ACT_GELU>>(maps, p, pair, {kept, dgu, a}, st)
+                                 : gemm_launch<false, true, EpiActGrad<VT_ACT_SILU>>(maps, p, pair, {kept, dgu, a}, st);
+        if (r != VT_OK) return r;
     }
     if (grad_x) {   // dx = dg Wg + du Wu: [M, d], summed over f twice
         GemmMaps maps{};

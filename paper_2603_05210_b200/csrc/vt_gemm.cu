@@ -19,8 +19,8 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
     const int groups = (p->dual ? p->NT / 2 : p->NT) / 8;
-    p->x_cols = ceil_div(groups, p->splits) * (p->dual ? 16 : 8);
-    p->x_part = (uint32_t)(std::min(128, max_m) * (p->x_cols + 4) * 4);
+    p->x_rows = (uint32_t)std::min(128, (int)round_up(max_m, 8));
+    p->x_part = p->x_rows * (uint32_t)(ceil_div(groups, p->splits) * (p->dual ? 16 : 8) * 4);
     const size_t partial = p->splits > 1 ? (size_t)p->x_part * p->splits : 0;
     const size_t over = 16384 - p->a_bytes;      // an MMA reads 128 rows of A wherever they end
     const size_t room = kMaxDynSmem - 2048 - round_up(bar_bytes, 128) - scratch_bytes - over;
@@ -187,7 +187,9 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_
                 double per_kb = std::max(issue, blk / (maxM <= 256 ? 40.0 : 58.0));
                 per_kb = std::max(per_kb, nt * 128.0 * (pair ? 0.5 : 1.0) / 24.0 * (maxM <= 256 ? busy : 0.0));
                 const double tail = 1500.0 + 12.0 * cols;
-                const double cost = rounds * (ceil_div(max_nk, s) * per_kb + (s > 1 ? 5000.0 : 1200.0)) + tail;
+                // the exchange: two barriers and a last round trip, and its bytes at the 12 a cycle that an SM sends to others
+                const double exchange = s > 1 ? 3500.0 + a_rows * nt * 4.0 * (s - 1) / s / 12.0 : 0.0;
+                const double cost = rounds * (ceil_div(max_nk, s) * per_kb + 1200.0 + exchange) + tail;
                 if (best < 0 || cost < best) {
                     best = cost;
                     best_nt = nt;

@@ -69,8 +69,7 @@ struct GemmParams {
     int dual;                    // 1: columns [0, NT/2) from map b0, [NT/2, NT) from map b1, the same rows of both
     int rep;                     // copies of A's rows in a tile: 1, 2 or 4 (single only)
     int splits;                  // CTAs that share one tile's k range (single only)
-    int x_cols;                  // with splits: columns (of both halves) a CTA owns at most
-    uint32_t x_part;             // ... and the bytes of partial sums it gets from each CTA, over the ring
+    uint32_t x_rows, x_part;     // with splits: rows of the exchanged sums, and bytes an owner gets from each CTA (over the ring)
     int n_stages;
     int kbs;                     // k-blocks per ring stage
     uint32_t a_rows;             // rows of A's box (K-major); `rep` of them, 128 / rep rows apart
@@ -191,7 +190,7 @@ struct EpiStore {
     };
     struct State {};
     static __device__ __forceinline__ void row(State&, const Params&, const GemmProblem&, int) {}
-    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int, int) {}
     static __device__ __forceinline__ void cols8(State&, const Params&, const GemmProblem&, int, int, int, const float (&x)[8], const float (&)[8], float (&out)[1][8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[0][i] = x[i];
@@ -206,8 +205,8 @@ struct EpiStore {
 //               tile with its share of the columns, in runs of 16 that it reads through an AccColumns, then end()
 // or kOuts bf16 matrices, each value from its own column(s):
 //   row()       once per tile and row, before the accumulator is waited for
-//   ahead()     before each run of 16 columns and one run in advance: requests what cols8 will need for it
-//   cols8()     eight columns (of either half): out[o][i] are the values to round and store
+//   ahead()     two runs of 16 columns in advance: requests what cols8 will need for the run at column n, into slot 0 or 1
+//   cols8()     eight columns (of either half), at e in the two slots' 32: out[o][i] are the values to round and store
 //   at()        where output o's row m, column n lies
 template <bool PAIR, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -493,7 +492,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 if constexpr (!Epi::kStateful) {
                     if (p.splits == 1 && m < q.M) {
                         Epi::row(st, ep, q, m);
-                        Epi::ahead(st, ep, q, m, col0 + g0 * 32);
+                        Epi::ahead(st, ep, q, m, col0 + g0 * 32, 0);
+                        Epi::ahead(st, ep, q, m, col0 + g0 * 32 + 16, 1);
                     }
                 }
                 bool got = false;
@@ -532,7 +532,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                                     x[i] = __uint_as_float(u[e + i]);
                                     y[i] = Epi::kDual ? __uint_as_float(w[e + i]) : 0.0f;
                                 }
-                                Epi::cols8(st, ep, q, m, col0 + c + e, e, x, y, out);
+                                Epi::cols8(st, ep, q, m, col0 + c + e, h + e, x, y, out);
 #pragma unroll
                                 for (int o = 0; o < Epi::kOuts; ++o) {
                                     if (staged)
@@ -542,7 +542,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                                         store_bf16x8(Epi::at(ep, q, it.prob, o, m, col0 + c + e), out[o]);
                                 }
                             }
-                            if (m < q.M) Epi::ahead(st, ep, q, m, col0 + c + 16);
+                            if (m < q.M) Epi::ahead(st, ep, q, m, col0 + c + 32, h >> 4);
                         }
                         if (staged) {
                             fence_proxy_async_smem();
@@ -599,13 +599,15 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                         int owner = (int)((unsigned)(g * p.splits) / (unsigned)groups);
                         if (g >= (owner + 1) * groups / p.splits) ++owner;     // shares are [owner * groups / splits, ...); splits <= groups
                         const int local = g - owner * groups / p.splits;
+                        // four columns of all rows in a run: a warp's 16-byte stores lie side by side
+                        const uint32_t run = p.x_rows * 16u;
                         const uint32_t to = cluster_map_shared(base + rank * p.x_part, (uint32_t)owner) +
-                                            (uint32_t)(r * (p.x_cols + 4) + local * (Epi::kDual ? 16 : 8)) * 4u;
+                                            (uint32_t)local * (Epi::kDual ? 4u : 2u) * run + (uint32_t)r * 16u;
                         st_cluster_v4(to, u[e], u[e + 1], u[e + 2], u[e + 3]);
-                        st_cluster_v4(to + 16u, u[e + 4], u[e + 5], u[e + 6], u[e + 7]);
+                        st_cluster_v4(to + run, u[e + 4], u[e + 5], u[e + 6], u[e + 7]);
                         if constexpr (Epi::kDual) {
-                            st_cluster_v4(to + 32u, w[e], w[e + 1], w[e + 2], w[e + 3]);
-                            st_cluster_v4(to + 48u, w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
+                            st_cluster_v4(to + 2u * run, w[e], w[e + 1], w[e + 2], w[e + 3]);
+                            st_cluster_v4(to + 3u * run, w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
                         }
                     }
                 }
@@ -614,21 +616,21 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             if (warp < kGemmEpiWarps && !*abort_flag) {
                 const int g0 = (int)rank * groups / p.splits, g1 = ((int)rank + 1) * groups / p.splits;   // this CTA's runs of 8 columns
                 for (int e = tid; e < rows * (g1 - g0); e += kGemmEpiWarps * 32) {
-                    const int er = e / (g1 - g0), g = e - er * (g1 - g0);
+                    const int g = e / rows, er = e - g * rows;
                     const int col = it.nt0 * cols + (g0 + g) * 8, m = it.mt * 128 + er;
                     if (col >= q.N) continue;
                     typename Epi::State st;
                     Epi::row(st, ep, q, m);
-                    Epi::ahead(st, ep, q, m, col);
+                    Epi::ahead(st, ep, q, m, col, 0);
                     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0}, out[Epi::kOuts][8];
-                    const unsigned char* from = smem + (size_t)(er * (p.x_cols + 4) + g * (Epi::kDual ? 16 : 8)) * 4;
+                    const unsigned char* from = smem + ((size_t)g * (Epi::kDual ? 4 : 2) * p.x_rows + er) * 16;
                     for (int s = 0; s < p.splits; ++s, from += p.x_part) {
                         const float4* f = reinterpret_cast<const float4*>(from);
-                        const float4 v0 = f[0], v1 = f[1];
+                        const float4 v0 = f[0], v1 = f[p.x_rows];
                         x[0] += v0.x; x[1] += v0.y; x[2] += v0.z; x[3] += v0.w;
                         x[4] += v1.x; x[5] += v1.y; x[6] += v1.z; x[7] += v1.w;
                         if constexpr (Epi::kDual) {
-                            const float4 w0 = f[2], w1 = f[3];
+                            const float4 w0 = f[2 * p.x_rows], w1 = f[3 * p.x_rows];
                             y[0] += w0.x; y[1] += w0.y; y[2] += w0.z; y[3] += w0.w;
                             y[4] += w1.x; y[5] += w1.y; y[6] += w1.z; y[7] += w1.w;
                         }

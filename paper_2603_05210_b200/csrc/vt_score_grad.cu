@@ -37,7 +37,7 @@ struct EpiScoreGrad {
         st.ge = ep.grad_entropy ? ep.scale * ep.grad_entropy[m] : 0.0f;
         st.H = ep.grad_entropy ? ep.entropy[m] : 0.0f;
     }
-    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int) {}
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int, int) {}
     static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int, int n, int, const float (&x)[8],
                                                  const float (&)[8], float (&out)[1][8]) {
 #pragma unroll
