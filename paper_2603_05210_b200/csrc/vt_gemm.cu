@@ -156,7 +156,7 @@ static int cluster_slots(int size) {
 // weights stream at 24 bytes a cycle and SM when all of them take part.  Each round of tiles adds its fill, the last its
 // read-out, and splits the exchange of their partial sums.
 bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_bytes, bool* pair_out) {
-    const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0) | (int)scratch_bytes << 4);
+    const PlanCache::Key key = PlanCache::key_of(*p, (a_mn ? 1 : 0) | (b_mn ? 2 : 0) | (dual ? 4 : 0) | (int)scratch_bytes << 5);
     if (g_plans.find(key, p, pair_out)) return true;
     int maxM = 0, max_nk = 0;
     for (int i = 0; i < p->n_prob; ++i) {
@@ -210,9 +210,11 @@ bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_
 
 // Scoring: every row needs all columns, so nothing but the tile width and the number of tiles a CTA takes in a row is
 // free.  Chosen for the fewest rounds of equal work over the SMs (a round costs its columns plus about 24 columns' worth
-// of hand-over); among equals the longer runs, which leave fewer records to merge.
-bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair_out) {
-    const PlanCache::Key key = PlanCache::key_of(*p, 8 | (int)scratch_bytes << 4);
+// of hand-over).  Where the first tile of a run is dear, a run pays for it once: 40 columns' worth, so that up to sixteen
+// tiles in a row are taken as long as they do not leave SMs idle for more than that; elsewhere runs are short, which keeps
+// the ranges that records stand for short.
+bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool long_runs, bool* pair_out) {
+    const PlanCache::Key key = PlanCache::key_of(*p, 8 | (long_runs ? 16 : 0) | (int)scratch_bytes << 5);
     if (g_plans.find(key, p, pair_out)) return true;
     const GemmProblem& q = p->prob[0];
     const bool pair = q.M > 128;
@@ -225,7 +227,7 @@ bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair_out) {
         for (int c = 1; c <= 16; ++c) {
             const long long items = tiles_m * ceil_div(tiles_n, c);
             const double rounds = (double)((items + slots - 1) / slots);
-            const double cost = rounds * c * (nt + 24.0) + 40.0 / c;
+            const double cost = rounds * (c * (nt + 24.0) + (long_runs ? 40.0 : 0.5));
             if (best < 0 || cost < best) {
                 best = cost;
                 best_nt = nt;

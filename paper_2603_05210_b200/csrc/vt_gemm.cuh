@@ -684,8 +684,9 @@ inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 // except the maps' indices, outputs and hdr.  False when the work is too large to number its tiles.
 // scratch_bytes: the epilogue's kScratch.
 bool gemm_plan(GemmParams* p, bool a_mn, bool b_mn, bool dual, uint32_t scratch_bytes, bool* pair);
-// The same for token scoring: one product, both operands K-major, whole k range in every CTA, `tiles_per_item` tiles in a row.
-bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool* pair);
+// The same for token scoring: one product, both operands K-major, whole k range in every CTA.  long_runs: the first tile of a run
+// costs the epilogue far more than the others.
+bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool long_runs, bool* pair);
 // Rows of the box each operand's tensor map has (64 columns wide; MN-major operands: 64).
 inline int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : (int)p.a_rows; }
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);

@@ -7,12 +7,16 @@
 // folds them into a running (max, s, e = sum of (x - max) e^(z - max)) - kept about the maximum, because lse and E[z] are
 // both large where H is small - and picks the given token's logit when it comes by.  At the end of a run of tiles it
 // writes one record; a second, small kernel (one block per row) joins a row's records.  The k best come in one of two ways:
-//   kept    (few logits, kKeptBytes at most): the logits go to the workspace, which is to say to L2, and the join reads back
-//           the handful of ranges whose maximum is not below the k-th largest maximum of all;
-//   listed  (many): no logit is written; every thread keeps a register list of its k best, and the join merges the lists.
-// With few rows nothing hides an epilogue, and the lists took 5 us of 60 (33 rows x 32000, k = 8) and 12 of 105 (100 rows);
-// with many rows the lists fill in the first of a thread's tiles and cost little after it, while the logits would be
-// hundreds of megabytes.
+//   listed  no logit is written; every thread keeps a register list of its k best, and the join merges the lists;
+//   kept    the logits go to the workspace, and the join reads back the handful of ranges whose maximum is not below the
+//           k-th largest maximum of all.
+// Lists cost the epilogue more the longer they are (and their first tile most, so that long runs of tiles pay), kept logits
+// their bytes and a longer join.  Measured, us, listed / kept (and without alternatives):
+//     M = 33, V = 32000, d = 4096       k = 8: 59.4 / 56.2   k = 20: 70.9 / 58.9   k = 40: 122 / 66     (51.2)
+//     M = 128, V = 100000, d = 4096     k = 8: 148 / 156     k = 20: 153 / 158     k = 40: 296 / 163    (137)
+//     M = 600, V = 32000, d = 2048      k = 8: 82 / 101      k = 20: 101 / 107                          (75)
+//     M = 4096, V = 32000, d = 4096     k = 8: 744 / 999     k = 20: 893 / 1037                         (728)
+// hence keep_logits() below.
 // Records are joined in the order of their columns and ranked by distinct keys, so the result does not depend on which
 // block ran when.
 #include "vt_score.h"
@@ -34,7 +38,7 @@ struct ScoreRecords {
 };
 
 constexpr int kListQueue = 24;             // candidates a thread queues between insertions
-constexpr size_t kKeptBytes = (size_t)64 << 20;      // logits that stay in L2 beside the stream of weights
+constexpr int kListMax = 20;                // entries of the longest list
 constexpr int kKeepLogits = -1;            // EpiScore<kKeepLogits>: the kept form
 
 // KR: entries of a thread's list (0: no alternatives wanted), or kKeepLogits.
@@ -67,6 +71,12 @@ struct EpiScore {
         st.bound = -INFINITY;
 #pragma unroll
         for (int j = 0; j < KL; ++j) { st.v[j] = kMasked; st.ix[j] = -1; }
+    }
+    static constexpr int kThreads = kGemmEpiWarps * 32;
+    // the largest float below x
+    static __device__ __forceinline__ float below(float x) {
+        const int b = __float_as_int(x + 0.0f);
+        return b == 0 ? -__int_as_float(1) : __int_as_float(b > 0 ? b - 1 : b + 1);
     }
     static __device__ __forceinline__ void mask(float (&x)[16], int live) {
         if (live < 16) {
@@ -128,34 +138,34 @@ struct EpiScore {
             // The logits that may be among the row's best - above the list's last entry, and in the thread's first tile not
             // below the KR-th largest of the maxima of groups of four, which KR logits reach - are queued (lanes meet
             // theirs at different columns) and inserted together, one per lane and turn.
-            if (st.first) st.bound = g[KL - 1];
+            if (st.first) st.bound = below(g[KL - 1]);
             st.first = false;
-            float* qx = reinterpret_cast<float*>(scratch) + threadIdx.x;
-            unsigned char* qc = scratch + kListQueue * kGemmEpiWarps * 32 * 4 + threadIdx.x;
-            int cnt = 0;
+            const uint32_t qx0 = smem_u32(scratch) + threadIdx.x * 4u;
+            const uint32_t qc0 = smem_u32(scratch) + kListQueue * kThreads * 4u + threadIdx.x;
+            uint32_t qx = qx0, qc = qc0;
             auto insert_queued = [&]() {
+                const int cnt = (int)(qx - qx0) / (kThreads * 4);
                 const int most = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)cnt);
                 for (int i = 0; i < most; ++i) {
-                    const float x = i < cnt ? qx[i * (kGemmEpiWarps * 32)] : kMasked;      // beats nothing
-                    rows_insert<KL>(st.v, st.ix, x, cols.col0 + (int)qc[i * (kGemmEpiWarps * 32)]);
+                    const float x = i < cnt ? reinterpret_cast<const float*>(scratch)[i * kThreads + threadIdx.x] : kMasked;   // beats nothing
+                    rows_insert<KL>(st.v, st.ix, x, cols.col0 + (int)scratch[kListQueue * kThreads * 4 + i * kThreads + threadIdx.x]);
                 }
-                cnt = 0;
+                qx = qx0;
+                qc = qc0;
             };
             for (int ch = cols.ch0; ch < cols.ch1; ++ch) {
                 float x[16];
                 const int live = cols.load(ch, x);
                 if (live <= 0) break;
                 mask(x, live);
-                const float tau = st.v[KL - 1];
+                const float tau = fmaxf(st.v[KL - 1], st.bound);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (x[i] > tau && x[i] >= st.bound) {
-                        qx[cnt * (kGemmEpiWarps * 32)] = x[i];
-                        qc[cnt * (kGemmEpiWarps * 32)] = (unsigned char)(ch * 16 + i);
-                        ++cnt;
-                    }
-                }
-                if (__any_sync(0xFFFFFFFFu, cnt > kListQueue - 16)) insert_queued();
+                for (int i = 0; i < 16; ++i)       // without a branch: a few of a warp's 32 rows queue something at nearly every column
+                    asm volatile(
+                        "{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %2, %3;\n\t@p st.shared.f32 [%0], %2;\n\t@p st.shared.u8 [%1], %4;\n\t"
+                        "@p add.u32 %0, %0, %5;\n\t@p add.u32 %1, %1, %6;\n\t}"
+                        : "+r"(qx), "+r"(qc) : "f"(x[i]), "f"(tau), "r"(ch * 16 + i), "n"(kThreads * 4), "n"(kThreads) : "memory");
+                if (__any_sync(0xFFFFFFFFu, qx - qx0 > (uint32_t)(kListQueue - 16) * kThreads * 4)) insert_queued();
             }
             insert_queued();
         }
@@ -399,7 +409,14 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
 }
 
 // ------------------------------------------------------------------------------------------ host
-static int list_entries(int k) { return k == 0 ? 0 : k <= 4 ? 4 : k <= 8 ? 8 : k <= 20 ? 20 : VT_MAX_K; }
+static int list_entries(int k) { return k == 0 ? 0 : k <= 4 ? 4 : k <= 8 ? 8 : kListMax; }
+// Whether the logits are kept (see the top of this file): always where a list would be too long, up to what stays in L2 for
+// long lists, and for short ones only where so few rows leave the epilogue uncovered.
+static bool keep_logits(int M, int k, size_t bytes) {
+    if (k == 0) return false;
+    if (k > kListMax) return true;
+    return bytes <= (k > 8 ? (size_t)64 << 20 : M <= 128 ? (size_t)16 << 20 : 0);
+}
 
 struct ScorePlan {
     GemmParams p;
@@ -419,8 +436,8 @@ static bool score_plan(int M, int d, int V, int k, ScorePlan* s) {
     s->p.prob[0].nk0 = ceil_div(d, kBoxK);
     s->ld = (int64_t)round_up((size_t)V, 16);
     const size_t kept = (size_t)M * s->ld * 4;
-    s->KR = k > 0 && kept <= kKeptBytes ? kKeepLogits : list_entries(k);
-    if (!gemm_plan_rows(&s->p, s->KR > 0 ? EpiScore<4>::kScratch : 0u, &s->pair)) return false;
+    s->KR = keep_logits(M, k, kept) ? kKeepLogits : list_entries(k);
+    if (!gemm_plan_rows(&s->p, s->KR > 0 ? EpiScore<4>::kScratch : 0u, s->KR > 0, &s->pair)) return false;
     s->L = s->p.prob[0].chunks_n * 2 * s->p.rep;
     const size_t rows = (size_t)M * s->L;
     s->stats = kHeaderBytes;
@@ -444,10 +461,13 @@ static vt_status run_score(const GemmMaps& maps, const ScorePlan& s, const Score
     if (r != VT_OK) return r;
     const ScoreJoin join{rec, o, c.tokens, c.V, c.scale};
     constexpr bool kept = KR == kKeepLogits;
-    // one warp per row needs the rows' heads to bound k winners, and pays where rows are plenty
-    const bool narrow = c.M > 4 * kGemmSms && o.k <= 32;
-    cudaError_t e = narrow ? launch_pdl(score_join_kernel<32, kept>, c.M, 32, 0, st, join)
-                           : launch_pdl(score_join_kernel<256, kept>, c.M, 256, 0, st, join);
+    // Few rows: 256 threads each.  Many: one warp for short lists (it bounds 32 winners at most), four for kept ranges, which
+    // are read one per warp at a time.
+    const bool many = c.M > 2 * kGemmSms;
+    cudaError_t e;
+    if (many && kept) e = launch_pdl(score_join_kernel<128, kept>, c.M, 128, 0, st, join);
+    else if (many && o.k <= 32) e = launch_pdl(score_join_kernel<32, kept>, c.M, 32, 0, st, join);
+    else e = launch_pdl(score_join_kernel<256, kept>, c.M, 256, 0, st, join);
     count_launch();
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? VT_OK : cuda_fail(e);
@@ -478,8 +498,7 @@ vt_status launch_score(const ScoreCall& c, const ScoreOut& o, void* workspace, s
         case 0: return run_score<0>(maps, s, c, rec, o, st);
         case 4: return run_score<4>(maps, s, c, rec, o, st);
         case 8: return run_score<8>(maps, s, c, rec, o, st);
-        case 20: return run_score<20>(maps, s, c, rec, o, st);
-        default: return run_score<VT_MAX_K>(maps, s, c, rec, o, st);
+        default: return run_score<kListMax>(maps, s, c, rec, o, st);
     }
 }
 
