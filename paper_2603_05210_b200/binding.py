@@ -137,9 +137,12 @@ def _f32(t: torch.Tensor, name: str, shape: tuple) -> torch.Tensor:
     return t
 
 
-def _out(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, device) -> torch.Tensor:
+def _out(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, like: torch.Tensor) -> torch.Tensor:
+    """An output given by the caller, checked, or a new one on the device of `like` (of its shape and type: the cheapest way)."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if like.dtype == dtype and like.shape == shape and like.is_contiguous():
+            return torch.empty_like(like)
+        return like.new_empty(shape, dtype=dtype)
     if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
         raise ValueError(f"{name}: expected a contiguous {dtype} CUDA tensor of shape {shape}")
     return t
@@ -403,12 +406,12 @@ def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | Non
     if tokens is None:
         logprobs = None
     else:
-        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, dev)
-    entropy = _out(entropy, "entropy", (M,), torch.float32, dev)
-    lse = _out(lse, "lse", (M,), torch.float32, dev)
+        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, h)
+    entropy = _out(entropy, "entropy", (M,), torch.float32, h)
+    lse = _out(lse, "lse", (M,), torch.float32, h)
     if k > 0:
-        top_ids = _out(top_ids, "top_ids", (M, k), torch.int32, dev)
-        top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, dev)
+        top_ids = _out(top_ids, "top_ids", (M, k), torch.int32, h)
+        top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, h)
     else:
         top_ids = top_logprobs = None
     if workspace is None:
@@ -432,8 +435,8 @@ def vt_score_tokens_backward(h: torch.Tensor, W: torch.Tensor, tokens: torch.Ten
         if entropy is None:
             raise ValueError("grad_entropy needs the forward call's entropy")
         _f32(entropy, "entropy", (M,)), _f32(grad_entropy, "grad_entropy", (M,))
-    grad_h = _out(grad_h, "grad_h", (M, d), torch.bfloat16, dev) if want_h else None
-    grad_W = _out(grad_W, "grad_W", (V, d), torch.bfloat16, dev) if want_W else None
+    grad_h = _out(grad_h, "grad_h", (M, d), torch.bfloat16, h) if want_h else None
+    grad_W = _out(grad_W, "grad_W", (V, d), torch.bfloat16, W) if want_W else None
     if workspace is None:
         workspace = _scratch(None, vt_score_backward_workspace_bytes(M, d, V), dev)
     _check(lib().vt_score_tokens_backward(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), lse.data_ptr(), _ptr(entropy),
@@ -470,7 +473,7 @@ def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_do
     Pass ``saved`` [M, 2 f] float32 to receive what ``vt_gated_ffn_backward`` needs (its layout is the library's own)."""
     x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
     M = x.shape[0]
-    out = _out(out, "out", (M, d), torch.bfloat16, x.device)
+    out = _out(out, "out", (M, d), torch.bfloat16, x)
     if saved is not None:
         _f32(saved, "saved", (M, 2 * f))
     if workspace is None:
@@ -491,10 +494,10 @@ def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Ten
     _f32(saved, "saved", (M, 2 * f))
     if _bf16_rows(grad_y, "grad_y").shape != (M, d):
         raise ValueError("grad_y must have the shape of x")
-    grad_x = _out(grad_x, "grad_x", (M, d), torch.bfloat16, dev)
-    grad_W_gate = _out(grad_W_gate, "grad_W_gate", (f, d), torch.bfloat16, dev)
-    grad_W_up = _out(grad_W_up, "grad_W_up", (f, d), torch.bfloat16, dev)
-    grad_W_down = _out(grad_W_down, "grad_W_down", (d, f), torch.bfloat16, dev)
+    grad_x = _out(grad_x, "grad_x", (M, d), torch.bfloat16, x)
+    grad_W_gate = _out(grad_W_gate, "grad_W_gate", (f, d), torch.bfloat16, W_gate)
+    grad_W_up = _out(grad_W_up, "grad_W_up", (f, d), torch.bfloat16, W_up)
+    grad_W_down = _out(grad_W_down, "grad_W_down", (d, f), torch.bfloat16, W_down)
     if workspace is None:
         workspace = _scratch(None, vt_gated_ffn_backward_workspace_bytes(M, d, f), dev)
     _check(lib().vt_gated_ffn_backward(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), saved.data_ptr(),

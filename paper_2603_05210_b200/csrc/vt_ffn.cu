@@ -82,6 +82,7 @@ struct EpiGateUp {
         }
     }
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int, int m, int n) { return ep.a + (size_t)m * q.N + n; }
+    static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int) { return q.N; }
 };
 
 template <int ACT>
@@ -123,6 +124,7 @@ struct EpiActGrad {
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int o, int m, int n) {
         return o == 2 ? ep.a + (size_t)m * q.N + n : ep.dgu + (size_t)m * 2 * q.N + (o == 1 ? q.N : 0) + n;
     }
+    static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int o) { return o == 2 ? q.N : 2 * q.N; }
 };
 
 static inline int k_blocks(int k) { return (k + kBoxK - 1) / kBoxK; }
@@ -166,7 +168,6 @@ vt_status launch_ffn(const FfnCall& c, void* y, float* saved, void* workspace, c
         if ((r = gemm_map(&maps.map[0], x, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wg, gemm_box_b(p, false, pair))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[2], wu, gemm_box_b(p, false, pair))) != VT_OK) return r;
-        if ((r = make_tensor_map_bf16_store(&maps.out[0], a, c.M, c.f, c.f)) != VT_OK) return r;
         r = c.act == VT_ACT_GELU ? gemm_launch<false, false, EpiGateUp<VT_ACT_GELU>>(maps, p, pair, {a, saved}, st)
                                  : gemm_launch<false, false, EpiGateUp<VT_ACT_SILU>>(maps, p, pair, {a, saved}, st);
         if (r != VT_OK) return r;
@@ -204,9 +205,6 @@ vt_status launch_ffn_backward(const FfnCall& c, const float* saved, const void* 
         if (!gemm_plan(&p, false, true, false, EpiActGrad<VT_ACT_SILU>::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], dy, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], wd, gemm_box_b(p, true, pair))) != VT_OK) return r;
-        if ((r = make_tensor_map_bf16_store(&maps.out[0], dgu, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
-        if ((r = make_tensor_map_bf16_store(&maps.out[1], dgu + c.f, c.M, c.f, 2 * (int64_t)c.f)) != VT_OK) return r;
-        if ((r = make_tensor_map_bf16_store(&maps.out[2], a, c.M, c.f, c.f)) != VT_OK) return r;
         float* kept = const_cast<float*>(saved);
         r = c.act == VT_ACT_GELU ? gemm_launch<false, true, EpiActGrad<VT_ACT_GELU>>(maps, p, pair, {kept, dgu, a}, st)
                                  : gemm_launch<false, true, EpiActGrad<VT_ACT_SILU>>(maps, p, pair, {kept, dgu, a}, st);

@@ -17,7 +17,7 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
     p->tx_bytes = p->a_rows * 128u * (uint32_t)p->rep + p->b_bytes;
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
-    const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 5) * 8 + 16;
+    const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 6) * 8 + sizeof(GemmTable);      // barriers, two words, the problems
     const int groups = (p->dual ? p->NT / 2 : p->NT) / 8;
     p->x_rows = (uint32_t)std::min(128, (int)round_up(max_m, 8));
     p->x_part = p->x_rows * (uint32_t)(ceil_div(groups, p->splits) * (p->dual ? 16 : 8) * 4);
@@ -249,13 +249,9 @@ bool gemm_plan_rows(GemmParams* p, uint32_t scratch_bytes, bool long_runs, bool*
 
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair) { return b_mn ? 64 : (pair || p.dual) ? p.NT / 2 : p.NT; }
 
-vt_status gemm_store(GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st) {
+vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st) {
     EpiStore::Params ep{};
-    for (int i = 0; i < p.n_prob; ++i) {
-        ep.out[i] = reinterpret_cast<uint16_t*>(out[i]);
-        const vt_status r = make_tensor_map_bf16_store(&maps.out[i], out[i], p.prob[i].M, p.prob[i].N, p.prob[i].N);
-        if (r != VT_OK) return r;
-    }
+    for (int i = 0; i < p.n_prob; ++i) ep.out[i] = reinterpret_cast<uint16_t*>(out[i]);
     if (!a_mn && !b_mn) return gemm_launch<false, false, EpiStore>(maps, p, pair, ep, st);
     if (!a_mn) return gemm_launch<false, true, EpiStore>(maps, p, pair, ep, st);
     return gemm_launch<true, true, EpiStore>(maps, p, pair, ep, st);

@@ -17,8 +17,8 @@
 //           compute on whatever shared memory holds and land in lanes nobody reads.  For an epilogue with work to do per
 //           column (scoring) the tile can hold at most 64 (32) rows of A two (four) times, one copy per group of TMEM
 //           lanes: every epilogue warp then finds rows, each copy taking its own share of the columns.
-// bf16 results leave through shared memory: a warp lays 32 rows x 32 columns out in a swizzled buffer and TMA stores them.  A
-// thread's own 16-byte stores, 32 rows apart, held the tiles of short sums (dW of 300 rows) to 1.3 TB/s.
+// bf16 results leave through shared memory, 128 bytes of a row at a time.  A thread's own 16-byte stores, 32 rows apart, held the
+// tiles of short sums (dW of 300 rows) to 1.3 TB/s, TMA stores of 64-byte rows to 1.9.
 //   splits  (single only) a cluster of up to eight CTAs divides the k range of one tile.  Each CTA owns a share of the
 //           columns: the others write their partial sums of it into its shared memory, and it adds them up in the order
 //           of the CTAs and finishes them: no atomics, the same bits every time.
@@ -39,7 +39,6 @@ constexpr int kGemmThreads = (kGemmEpiWarps + kGemmProducers + 1) * 32;
 constexpr int kGemmMaxStages = 16;
 constexpr int kGemmMaxProblems = 3;
 constexpr int kGemmMaxMaps = 6;
-constexpr int kGemmMaxOuts = 3;             // bf16 matrices a launch writes
 constexpr int kGemmGroupRows = 8;           // row tiles that share their column tiles before the next group (L2 reuse)
 constexpr int kGemmSms = 148;               // the plans are made for this many SMs; a device with fewer runs them in more waves
 
@@ -54,7 +53,6 @@ struct GemmProblem {
 
 struct GemmMaps {
     CUtensorMap map[kGemmMaxMaps];
-    CUtensorMap out[kGemmMaxOuts];   // [problem * outputs of the epilogue + output]
 };
 
 struct GemmParams {
@@ -112,6 +110,11 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr) {
     return desc;
 }
 
+// One arrival on an mbarrier of another CTA of the cluster that orders nothing in memory.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar_cluster) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+}
+
 // One lane of a converged warp (the same one every time).
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
@@ -127,19 +130,24 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-__device__ __forceinline__ GemmItem gemm_item(const GemmParams& p, int item) {
+// What the roles need of a launch's problems at every tile, in shared memory: loads from the parameters at a computed offset
+// took each role over a thousand cycles a tile.
+struct GemmTable {
+    GemmProblem prob[kGemmMaxProblems];
+};
+__device__ __forceinline__ GemmItem gemm_item(const GemmTable& tab, int n_prob, int tiles_per_item, int item) {
     GemmItem it;
     it.prob = 0;
-    while (it.prob + 1 < p.n_prob && item >= p.prob[it.prob + 1].first_item) ++it.prob;
-    const GemmProblem& q = p.prob[it.prob];
-    const int local = item - q.first_item;
-    const int per_group = kGemmGroupRows * q.chunks_n;
-    const int g = local / per_group, r = local - g * per_group;
-    const int gm = min(kGemmGroupRows, q.tiles_m - g * kGemmGroupRows);
-    const int ch = r / gm;
-    it.mt = g * kGemmGroupRows + (r - ch * gm);
-    it.nt0 = ch * p.tiles_per_item;
-    it.n_tiles = min(p.tiles_per_item, q.tiles_n - it.nt0);
+    while (it.prob + 1 < n_prob && item >= tab.prob[it.prob + 1].first_item) ++it.prob;
+    const GemmProblem& q = tab.prob[it.prob];
+    const unsigned local = (unsigned)(item - q.first_item);
+    const unsigned per_group = (unsigned)(kGemmGroupRows * q.chunks_n);
+    const unsigned g = local / per_group, r = local - g * per_group;
+    const unsigned gm = (unsigned)min(kGemmGroupRows, q.tiles_m - (int)g * kGemmGroupRows);
+    const unsigned ch = gm == kGemmGroupRows ? r / kGemmGroupRows : r / gm;
+    it.mt = (int)(g * kGemmGroupRows + (r - ch * gm));
+    it.nt0 = (int)ch * tiles_per_item;
+    it.n_tiles = min(tiles_per_item, q.tiles_n - it.nt0);
     return it;
 }
 
@@ -159,10 +167,19 @@ struct AccColumns {
     }
 };
 
-// Staging of bf16 results: per warp 32 rows x 32 columns for each output, two buffers of it for a single output.
-constexpr uint32_t kStageBytes = 32 * 64;
-constexpr uint32_t gemm_stage_bufs(int outs) { return outs > 1 ? 1u : 2u; }
-constexpr uint32_t gemm_stage_bytes(int outs) { return kGemmEpiWarps * gemm_stage_bufs(outs) * (uint32_t)outs * kStageBytes; }
+// Staging of bf16 results: per warp and output 32 rows of two units of 32 columns (one unit where there are several outputs),
+// the 16-byte chunks of a row permuted so that neither a column of chunks nor a row of them meets a bank twice.
+constexpr int gemm_stage_units(int outs) { return outs > 1 ? 1 : 2; }
+constexpr uint32_t gemm_stage_bytes(int outs) { return kGemmEpiWarps * (uint32_t)(gemm_stage_units(outs) * outs) * 32u * 64u; }
+template <int UNITS>
+__device__ __forceinline__ uint32_t stage_offset(int row, int chunk) {
+    return UNITS == 2 ? (uint32_t)row * 128u + (uint32_t)((chunk ^ (row & 7)) << 4) : (uint32_t)row * 64u + (uint32_t)((chunk ^ (row >> 1 & 3)) << 4);
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 
 // Eight fp32 values as bf16 (nearest-even) to a 16-byte aligned address.
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -198,6 +215,7 @@ struct EpiStore {
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int prob, int, int m, int n) {
         return ep.out[prob] + (size_t)m * q.N + n;
     }
+    static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int) { return q.N; }
 };
 
 // An epilogue provides kDual (its columns come in two halves) and either
@@ -207,7 +225,7 @@ struct EpiStore {
 //   row()       once per tile and row, before the accumulator is waited for
 //   ahead()     two runs of 16 columns in advance: requests what cols8 will need for the run at column n, into slot 0 or 1
 //   cols8()     eight columns (of either half), at e in the two slots' 32: out[o][i] are the values to round and store
-//   at()        where output o's row m, column n lies
+//   at(), ld()  where output o's row m, column n lies; elements between its rows
 template <bool PAIR, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p,
@@ -228,6 +246,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
     const uint32_t bar_full = base + p.bar_off, bar_empty = bar_full + 8u * S;
     const uint32_t bar_accf = bar_empty + 8u * S, bar_acce = bar_accf + 16u, bar_drain = bar_acce + 16u;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + p.bar_off + 8u * (2 * S + 5));
+    GemmTable& tab = *reinterpret_cast<GemmTable*>(smem + p.bar_off + 8u * (2 * S + 6));
+    const int n_prob = p.n_prob, tiles_per_item = p.tiles_per_item;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     if (warp == kProducer && lane == 0) {
@@ -247,6 +267,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         *abort_flag = 0;
         fence_mbar_init();
     }
+    if (tid >= 32 && tid < 32 + kGemmMaxProblems) tab.prob[tid - 32] = p.prob[tid - 32];
     if (warp == kIssuer) {
         if constexpr (PAIR) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
@@ -306,8 +327,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             const uint32_t bar_shift = PAIR ? cluster_map_shared(base, 0u) - base : 0u;    // both CTAs' bytes count on the leader's barrier
             int early = p.b_early ? 0 : -1;       // stages whose B is on its way before the dependency wait; -1: none to be
             for (int item = cluster; item < n_items && ok; item += n_clusters) {
-                const GemmItem it = gemm_item(p, item);
-                const GemmProblem& q = p.prob[it.prob];
+                const GemmItem it = gemm_item(tab, n_prob, tiles_per_item, item);
+                const GemmProblem& q = tab.prob[it.prob];
                 const int row0 = it.mt * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
                 const CUtensorMap *ma0 = &maps.map[q.a0], *ma1 = &maps.map[q.a1], *mb0 = &maps.map[q.b0], *mb1 = &maps.map[q.b1];
                 if (PAIR && dual && rank) mb0 = mb1;            // the halves of a pair's tile come from one matrix each
@@ -411,9 +432,9 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             uint64_t a = a_desc0, b = b_desc0;
             uint32_t bar_f = bar_full, bar_e = bar_empty;
             for (int item = cluster; item < n_items && ok; item += n_clusters) {
-                const GemmItem it = gemm_item(p, item);
+                const GemmItem it = gemm_item(tab, n_prob, tiles_per_item, item);
                 int k0, k1;
-                k_range(p.prob[it.prob], k0, k1);
+                k_range(tab.prob[it.prob], k0, k1);
                 for (int t = 0; t < it.n_tiles && ok; ++t, ++n) {
                     const int buf = n & 1;
                     if (n >= 2 && !mbar_wait_warp(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u)) { fail(); ok = false; break; }
@@ -476,13 +497,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         const int nch = (cols + 15) >> 4, ng = (cols + 31) >> 5;
         const int ch0 = part * nch / parts, ch1 = (part + 1) * nch / parts;   // runs of 16 columns this thread takes,
         const int g0 = part * ng / parts, g1 = (part + 1) * ng / parts;       // or of 32 where they are stored in bulk
-        constexpr uint32_t kStageBufs = gemm_stage_bufs(Epi::kOuts);
+        constexpr int kStageUnits = gemm_stage_units(Epi::kOuts);
+        constexpr uint32_t kStageBytes = kStageUnits * 32 * 64;
         const uint32_t stage_at = base + p.scratch_off + (uint32_t)warp * (Epi::kScratch / kGemmEpiWarps);
-        uint32_t n_staged = 0;
         int n = 0;
         for (int item = cluster; item < p.n_items; item += n_clusters) {
-            const GemmItem it = gemm_item(p, item);
-            const GemmProblem& q = p.prob[it.prob];
+            const GemmItem it = gemm_item(tab, n_prob, tiles_per_item, item);
+            const GemmProblem& q = tab.prob[it.prob];
             const int m = it.mt * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + r;
             typename Epi::State st;
             if constexpr (Epi::kStateful) Epi::begin(st, ep, m);
@@ -505,79 +526,87 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 if (p.splits > 1) break;                           // the tile is finished below, with the rest of the cluster
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)buf * p.acc_cols;
+                // The accumulator has been read: the MMAs of the tile after next may start.  Relaxed, as nothing in memory is
+                // handed over: a release would wait for this warp's stores of results, 1600 cycles a tile.
+                bool released = false;
+                auto release = [&]() {
+                    released = true;
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (PAIR) mbar_arrive_cluster_relaxed(cluster_map_shared(bar_acce + 8u * buf, 0u));
+                        else mbar_arrive(bar_acce + 8u * buf);
+                    }
+                };
                 if constexpr (Epi::kStateful) {
                     Epi::tile(st, ep, m, AccColumns{taddr, ch0, ch1, col0, q.N}, smem + p.scratch_off);
                 } else if (m - lane < q.M) {                       // some row of this warp exists
+                    // 32 columns at a time to the warp's staging rows (of kStageCols columns), and from there to memory whenever
+                    // they are full, several lanes to a row
+                    const int rows_here = min(32, q.M - (m - lane));
                     for (int g = g0; g < g1; ++g) {
-                        const bool staged = g * 32 + 32 <= cols;   // a shorter last run would reach into the next tile's columns
-                        const uint32_t buf_at = stage_at + (n_staged & (kStageBufs - 1)) * (uint32_t)(Epi::kOuts * kStageBytes);
-                        if (staged) {
-                            if (elect_one()) bulk_wait_read<kStageBufs - 1>();     // the buffer's last copy has been read
-                            __syncwarp();
+                        const int unit = (g - g0) % kStageUnits;
+                        uint32_t u[32], w[Epi::kDual ? 32 : 1];
+                        acc_ld16(taddr + (uint32_t)(g * 32), reinterpret_cast<uint32_t(&)[16]>(u[0]));
+                        if (g * 32 + 16 < cols) acc_ld16(taddr + (uint32_t)(g * 32 + 16), reinterpret_cast<uint32_t(&)[16]>(u[16]));
+                        if constexpr (Epi::kDual) {
+                            acc_ld16(taddr + (uint32_t)(cols + g * 32), reinterpret_cast<uint32_t(&)[16]>(w[0]));
+                            if (g * 32 + 16 < cols) acc_ld16(taddr + (uint32_t)(cols + g * 32 + 16), reinterpret_cast<uint32_t(&)[16]>(w[16]));
                         }
+                        tc_wait_ld();
+                        if (g + 1 == g1) release();
 #pragma unroll
-                        for (int h = 0; h < 32; h += 16) {
-                            const int c = g * 32 + h;
-                            if (c >= cols) break;
-                            uint32_t u[16], w[16];
-                            acc_ld16(taddr + (uint32_t)c, u);
-                            if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + c), w);
-                            tc_wait_ld();
+                        for (int e = 0; e < 32; e += 8) {
+                            const int c = g * 32 + e;
+                            if (c >= cols) break;                  // the other half, or the next tile's
+                            float x[8], y[8], out[Epi::kOuts][8];
 #pragma unroll
-                            for (int e = 0; e < 16; e += 8) {
-                                if (c + e >= cols) break;          // the other half, or the next tile's
-                                float x[8], y[8], out[Epi::kOuts][8];
+                            for (int i = 0; i < 8; ++i) {
+                                x[i] = __uint_as_float(u[e + i]);
+                                y[i] = Epi::kDual ? __uint_as_float(w[Epi::kDual ? e + i : 0]) : 0.0f;
+                            }
+                            Epi::cols8(st, ep, q, m, col0 + c, e, x, y, out);
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    x[i] = __uint_as_float(u[e + i]);
-                                    y[i] = Epi::kDual ? __uint_as_float(w[e + i]) : 0.0f;
-                                }
-                                Epi::cols8(st, ep, q, m, col0 + c + e, h + e, x, y, out);
+                            for (int o = 0; o < Epi::kOuts; ++o)
+                                st_shared_bf16x8(stage_at + (uint32_t)o * kStageBytes + stage_offset<kStageUnits>(lane, unit * 4 + e / 8), out[o]);
+                            if ((e & 8) && m < q.M) Epi::ahead(st, ep, q, m, col0 + c + 24, e >> 4);      // the next group's run of this slot
+                        }
+                        if (unit + 1 < kStageUnits && g + 1 < g1) continue;
+                        __syncwarp();
+                        const int shift = unit + 2;                // 4 or 8 chunks of 16 bytes are staged per row
+                        const int j = lane & ((1 << shift) - 1), r0 = lane >> shift, c = (g - unit) * 32 + j * 8;
+                        if (c < cols && col0 + c < q.N) {
 #pragma unroll
-                                for (int o = 0; o < Epi::kOuts; ++o) {
-                                    if (staged)
-                                        st_shared_bf16x8(buf_at + (uint32_t)o * kStageBytes + (uint32_t)lane * 64u +
-                                                         (((uint32_t)(h + e) >> 3 ^ ((uint32_t)lane >> 1 & 3u)) << 4), out[o]);
-                                    else if (m < q.M && col0 + c + e < q.N)
-                                        store_bf16x8(Epi::at(ep, q, it.prob, o, m, col0 + c + e), out[o]);
+                            for (int o = 0; o < Epi::kOuts; ++o) {
+                                uint16_t* to = Epi::at(ep, q, it.prob, o, m - lane, col0 + c);
+                                const int64_t ld = Epi::ld(ep, q, o);
+                                uint4 v[4];
+                                for (int half = 0; half <= unit; ++half) {       // all rows: four turns, or twice that
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+                                        v[i] = ld_shared_v4(stage_at + (uint32_t)o * kStageBytes +
+                                                            stage_offset<kStageUnits>(r0 + ((half * 4 + i) << (5 - shift)), j));
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const int r = r0 + ((half * 4 + i) << (5 - shift));
+                                        if (r < rows_here) *reinterpret_cast<uint4*>(to + r * ld) = v[i];
+                                    }
                                 }
                             }
-                            if (m < q.M) Epi::ahead(st, ep, q, m, col0 + c + 32, h >> 4);
                         }
-                        if (staged) {
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            if (elect_one()) {
-#pragma unroll
-                                for (int o = 0; o < Epi::kOuts; ++o)
-                                    tma_store_2d(&maps.out[it.prob * Epi::kOuts + o], col0 + g * 32, m - lane,
-                                                 buf_at + (uint32_t)o * kStageBytes);
-                                bulk_commit();
-                            }
-                            __syncwarp();
-                            ++n_staged;
-                        }
+                        __syncwarp();
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {                                   // the MMAs of the tile after next may start
-                    if constexpr (PAIR) mbar_arrive_cluster(cluster_map_shared(bar_acce + 8u * buf, 0u));
-                    else mbar_arrive(bar_acce + 8u * buf);
-                }
+                if (!released) release();
             }
             if constexpr (Epi::kStateful) Epi::end(st, ep, m, it.nt0 / p.tiles_per_item * parts + part);
-        }
-        if constexpr (!Epi::kStateful) {
-            if (elect_one()) bulk_wait_all();                      // what is on its way has arrived before the CTA is gone
-            __syncwarp();
         }
     }
 
     if constexpr (!PAIR && !Epi::kStateful) {
         if (p.splits > 1) {
-            const GemmItem it = gemm_item(p, cluster);
-            const GemmProblem& q = p.prob[it.prob];
+            const GemmItem it = gemm_item(tab, n_prob, tiles_per_item, cluster);
+            const GemmProblem& q = tab.prob[it.prob];
             const int cols = Epi::kDual ? p.NT >> 1 : p.NT, groups = cols >> 3;
             const int rows = min(128, q.M - it.mt * 128);
             cluster_sync_all();                                    // every ring is idle: the sums go where it was
@@ -692,8 +721,8 @@ inline int gemm_box_a(const GemmParams& p, bool a_mn) { return a_mn ? 64 : (int)
 int gemm_box_b(const GemmParams& p, bool b_mn, bool pair);
 
 // One or more products whose sums are rounded once to bf16 and stored in out[i] (row-major, N columns a row), operands of the
-// given majors.  Adds the outputs' maps.
-vt_status gemm_store(GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st);
+// given majors.
+vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool a_mn, bool b_mn, void* const* out, cudaStream_t st);
 
 // A bf16 matrix operand in global memory: rows x cols, rows ld elements apart.
 struct GemmOperand {

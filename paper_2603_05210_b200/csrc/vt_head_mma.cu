@@ -379,26 +379,19 @@ static vt_status get_encode(EncodeTiledFn* out) {
     return VT_OK;
 }
 
-// bf16 matrix [rows, d], rows ld elements apart, box = box_cols columns x box_rows rows, swizzled in 128-byte or 64-byte rows
-// (64 or 32 columns), zero fill outside.
-static vt_status encode_bf16(CUtensorMap* map, const void* ptr, int rows, int d, int64_t ld, int box_rows, int box_cols) {
+// bf16 matrix [rows, d], rows ld elements apart, box = 64 columns x box_rows rows, 128-byte swizzle, zero fill outside.
+vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, int d, int64_t ld, int box_rows) {
     EncodeTiledFn enc;
     vt_status r = get_encode(&enc);
     if (r != VT_OK) return r;
     const cuuint64_t dims[2] = {(cuuint64_t)d, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {(cuuint32_t)kBoxK, (cuuint32_t)box_rows};
     const cuuint32_t elem[2] = {1, 1};
     CUresult cr = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, elem,
-                      CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == kBoxK ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return cr == CUDA_SUCCESS ? VT_OK : driver_fail((int)cr);
-}
-vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, int d, int64_t ld, int box_rows) {
-    return encode_bf16(map, ptr, rows, d, ld, box_rows, kBoxK);
-}
-vt_status make_tensor_map_bf16_store(CUtensorMap* map, void* ptr, int rows, int cols, int64_t ld) {
-    return encode_bf16(map, ptr, rows, cols, ld, 32, 32);
 }
 vt_status make_tensor_map_bf16(CUtensorMap* map, const void* ptr, int rows, int d, int box_rows) {
     return make_tensor_map_bf16_ld(map, ptr, rows, d, d, box_rows);

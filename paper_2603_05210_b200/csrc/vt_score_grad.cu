@@ -22,7 +22,7 @@ struct EpiScoreGrad {
         const int32_t* tokens;
         const float *lse, *entropy, *grad_logprobs, *grad_entropy;
         uint16_t* G;
-        int64_t ld;
+        int64_t ldg;
         float scale;
         int V;
     };
@@ -49,7 +49,8 @@ struct EpiScoreGrad {
             out[0][i] = st.tok < 0 ? 0.0f : g;
         }
     }
-    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem&, int, int, int m, int n) { return ep.G + (size_t)m * ep.ld + n; }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem&, int, int, int m, int n) { return ep.G + (size_t)m * ep.ldg + n; }
+    static __device__ __forceinline__ int64_t ld(const Params& ep, const GemmProblem&, int) { return ep.ldg; }
 };
 
 // The hidden states with the rows that are not scored set to zero.  Bound by its bytes: 4 d per row.
@@ -105,7 +106,6 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         if (!gemm_plan(&p, false, false, false, EpiScoreGrad::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, false, pair))) != VT_OK) return r;
-        if ((r = make_tensor_map_bf16_store(&maps.out[0], G, c.M, p.prob[0].N, ld)) != VT_OK) return r;
         const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, ld, c.scale, c.V};
         if ((r = gemm_launch<false, false, EpiScoreGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
