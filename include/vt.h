@@ -242,8 +242,9 @@ vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32
  *   G[m, v]      = scale * ( gl[m] * (1[v == tokens[m]] - p) - ge[m] * p * (log p + entropy[m]) )
  *   grad_h[m, :] = sum_v G[m, v] * W[v, :]        grad_W[v, :] = sum_m G[m, v] * h[m, :]
  *
- * p comes from the logits, multiplied out again, and lse; G is rounded once to bf16 (it is an operand of both products),
- * the sums are fp32 and rounded once to bf16.  A row that is not scored has G = 0 and adds nothing to grad_W.
+ * p comes from the logits, multiplied out again, and lse; G is rounded once to bf16 (it is an operand of both products; what
+ * that takes from the given tokens' entries, its largest, is added to the sums), the sums are fp32 and rounded once to
+ * bf16.  A row that is not scored has G = 0 and adds nothing to grad_W.
  *
  *   h, ldh, W, tokens, M, d, V, scale   as in the forward call (tokens required);   lse, entropy  dev [M], its outputs
  *   grad_logprobs  dev [M] float        grad_entropy  dev [M] float or NULL (then entropy may be NULL, too)

@@ -60,6 +60,7 @@ template <int ACT>
 struct EpiGateUp {
     static constexpr bool kDual = true;
     static constexpr bool kStateful = false;
+    static constexpr bool kSums = false;
     static constexpr int kOuts = 1;
     static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
@@ -89,6 +90,7 @@ template <int ACT>
 struct EpiActGrad {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
+    static constexpr bool kSums = false;
     static constexpr int kOuts = 3;         // dg, du, a
     static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {

@@ -200,6 +200,7 @@ __device__ __forceinline__ void st_shared_bf16x8(uint32_t at, const float (&x)[8
 struct EpiStore {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
+    static constexpr bool kSums = false;
     static constexpr int kOuts = 1;
     static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
@@ -226,6 +227,8 @@ struct EpiStore {
 //   ahead()     two runs of 16 columns in advance: requests what cols8 will need for the run at column n, into slot 0 or 1
 //   cols8()     eight columns (of either half), at e in the two slots' 32: out[o][i] are the values to round and store
 //   at(), ld()  where output o's row m, column n lies; elements between its rows
+// With kSums, rows that wants() names also have their sums stored in fp32, from sums() on.  (Not cols8's work: a branch in
+// every eight columns kept them from being worked on side by side, 24 -> 31 us for 13264 x 2048 over 255.)
 template <bool PAIR, bool A_MN, bool B_MN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmParams p,
@@ -555,6 +558,15 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                         }
                         tc_wait_ld();
                         if (g + 1 == g1) release();
+                        if constexpr (Epi::kSums) {
+                            if (m < q.M && Epi::wants(st)) {
+                                float* to = Epi::sums(st, ep, q) + col0 + g * 32;
+#pragma unroll
+                                for (int e = 0; e < 32; e += 4)
+                                    if (g * 32 + e < cols && col0 + g * 32 + e < q.N)
+                                        *reinterpret_cast<uint4*>(to + e) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
                             const int c = g * 32 + e;
@@ -662,6 +674,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                             const float4 w0 = f[2 * p.x_rows], w1 = f[3 * p.x_rows];
                             y[0] += w0.x; y[1] += w0.y; y[2] += w0.z; y[3] += w0.w;
                             y[4] += w1.x; y[5] += w1.y; y[6] += w1.z; y[7] += w1.w;
+                        }
+                    }
+                    if constexpr (Epi::kSums) {
+                        if (Epi::wants(st)) {
+                            float4* to = reinterpret_cast<float4*>(Epi::sums(st, ep, q) + col);
+                            to[0] = make_float4(x[0], x[1], x[2], x[3]);
+                            to[1] = make_float4(x[4], x[5], x[6], x[7]);
                         }
                     }
                     Epi::cols8(st, ep, q, m, col, 0, x, y, out);

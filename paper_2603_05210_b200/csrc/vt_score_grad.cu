@@ -5,23 +5,37 @@
 //
 // The logits are multiplied out again (the forward pass wrote none) and turned into G on the way out of tensor memory;
 // G goes to memory once, in bf16, because it is an operand of both remaining products - the one rounding in between.
+// Nearly all of a row of G that is not next to nothing is one entry, the given token's, so that entry's rounding moves a whole
+// row of dh, and of dW, by up to 2^-8 of itself; with few rows the result's error was 1.4 to 1.6 times that of one rounding.
+// What the rounding took from that entry is therefore kept in fp32 and given back before the products are rounded: times its
+// row of W to dh, times its row of h to its token's row of dW (error now 1.00 to 1.07 times that of one rounding).  For dW that
+// is a kernel of its own over the rows of the given tokens, whose sums the product leaves in fp32: added in the product's
+// epilogue, the rows of h held every tile up.  255 rows, 13264 x 2048, forward and backward: 81.6 us without any of it, 88.2
+// this way, 101 in the epilogue; 4096 rows, 32000 x 4096: 0 to 3 % on 2700.
 // Rows that are not scored have G = 0 and, so that nothing in their hidden state can reach dW (0 * NaN is NaN), the
 // product for dW reads a copy of h in which they are zero.
+#include <climits>
+
 #include "vt_score.h"
 
 #include "vt_gemm.cuh"
 
 namespace vt {
 
+constexpr int kNone = INT_MAX;
+
 struct EpiScoreGrad {
     static constexpr bool kDual = false;
     static constexpr bool kStateful = false;
+    static constexpr bool kSums = false;
     static constexpr int kOuts = 1;
     static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
     struct Params {
         const int32_t* tokens;
         const float *lse, *entropy, *grad_logprobs, *grad_entropy;
         uint16_t* G;
+        float* rest;            // [M] what rounding the given token's entry left over
+        int32_t* first;         // per token: the first row it was given to, or kNone; null when nobody asks
         int64_t ldg;
         float scale;
         int V;
@@ -38,56 +52,202 @@ struct EpiScoreGrad {
         st.H = ep.grad_entropy ? ep.entropy[m] : 0.0f;
     }
     static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int, int) {}
-    static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem&, int, int n, int, const float (&x)[8],
+    static __device__ __forceinline__ void cols8(State& st, const Params& ep, const GemmProblem& q, int m, int n, int, const float (&x)[8],
                                                  const float (&)[8], float (&out)[1][8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float logp = fmaf(ep.scale, x[i], -st.lse);
             const float p = ex2_approx(logp * kLog2e);
-            float g = -p * fmaf(st.ge, logp + st.H, st.gl);
-            if (n + i == st.tok) g += st.gl;
+            const float g = -p * fmaf(st.ge, logp + st.H, st.gl);
             out[0][i] = st.tok < 0 ? 0.0f : g;
+        }
+        // one test for the eight: a branch in every column kept them from being worked on side by side (+2 us of 21)
+        if ((unsigned)(st.tok - n) < 8u && m < q.M) {
+            float rest = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (n + i == st.tok) {
+                    out[0][i] += st.gl;
+                    rest = out[0][i] - __bfloat162float(__float2bfloat16_rn(out[0][i]));
+                }
+            ep.rest[m] = rest;
+            if (ep.first) atomicMin(ep.first + st.tok, m);
         }
     }
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem&, int, int, int m, int n) { return ep.G + (size_t)m * ep.ldg + n; }
     static __device__ __forceinline__ int64_t ld(const Params& ep, const GemmProblem&, int) { return ep.ldg; }
 };
 
-// The hidden states with the rows that are not scored set to zero.  Bound by its bytes: 4 d per row.
-__global__ void __launch_bounds__(256) score_rows_kernel(const uint16_t* h, int64_t ldh, const int32_t* tokens, int M, int d, int V, uint16_t* out) {
+// Adds r times eight bf16 values.
+__device__ __forceinline__ void add_scaled(float (&out)[8], float r, const uint4& v) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[2 * i] = fmaf(r, __uint_as_float(u[i] << 16), out[2 * i]);
+        out[2 * i + 1] = fmaf(r, __uint_as_float(u[i] & 0xFFFF0000u), out[2 * i + 1]);
+    }
+}
+
+// Stores dh: row m, adding rest[m] W[t_m], which is requested two runs of columns ahead.
+struct EpiGradH {
+    static constexpr bool kDual = false;
+    static constexpr bool kStateful = false;
+    static constexpr bool kSums = false;
+    static constexpr int kOuts = 1;
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
+    struct Params {
+        uint16_t* out;
+        const uint16_t* W;
+        const int32_t* tokens;
+        const float* rest;
+        int V;
+    };
+    struct State {
+        float r;                    // 0: nothing to add
+        const uint16_t* src;
+        uint4 v[2][2];
+    };
+    static __device__ __forceinline__ void row(State& st, const Params& ep, const GemmProblem& q, int m) {
+        const int tok = ep.tokens[m];
+        const bool scored = (unsigned)tok < (unsigned)ep.V;
+        st.src = scored ? ep.W + (size_t)tok * q.N : nullptr;
+        st.r = scored ? ep.rest[m] : 0.0f;
+    }
+    static __device__ __forceinline__ void ahead(State& st, const Params&, const GemmProblem& q, int, int n, int slot) {
+        if (st.src == nullptr) return;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (n + 8 * i < q.N) st.v[slot][i] = *reinterpret_cast<const uint4*>(st.src + n + 8 * i);
+    }
+    static __device__ __forceinline__ void cols8(State& st, const Params&, const GemmProblem& q, int m, int n, int e, const float (&x)[8],
+                                                 const float (&)[8], float (&out)[1][8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[0][i] = x[i];
+        if (m < q.M && n < q.N && st.r != 0.0f) add_scaled(out[0], st.r, st.v[e >> 4][(e >> 3) & 1]);
+    }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int, int m, int n) { return ep.out + (size_t)m * q.N + n; }
+    static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int) { return q.N; }
+};
+
+// Stores dW; the sums of a token's row also go, in fp32, to row first[token] of `sums`.
+struct EpiGradW {
+    static constexpr bool kDual = false;
+    static constexpr bool kStateful = false;
+    static constexpr bool kSums = true;
+    static constexpr int kOuts = 1;
+    static constexpr uint32_t kScratch = gemm_stage_bytes(kOuts);
+    struct Params {
+        uint16_t* out;
+        const int32_t* first;
+        float* sums;
+    };
+    struct State {
+        int first;
+    };
+    static __device__ __forceinline__ void row(State& st, const Params& ep, const GemmProblem&, int m) { st.first = ep.first[m]; }
+    static __device__ __forceinline__ bool wants(const State& st) { return st.first != kNone; }
+    static __device__ __forceinline__ float* sums(const State& st, const Params& ep, const GemmProblem& q) { return ep.sums + (size_t)st.first * q.N; }
+    static __device__ __forceinline__ void ahead(State&, const Params&, const GemmProblem&, int, int, int) {}
+    static __device__ __forceinline__ void cols8(State&, const Params&, const GemmProblem&, int, int, int, const float (&x)[8], const float (&)[8],
+                                                 float (&out)[1][8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[0][i] = x[i];
+    }
+    static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem& q, int, int, int m, int n) { return ep.out + (size_t)m * q.N + n; }
+    static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int) { return q.N; }
+};
+
+// Copies rows of h, zeros in place of those that are not scored, and clears `first`.
+constexpr int kRowThreads = 256;
+__global__ void __launch_bounds__(kRowThreads) score_rows_kernel(const uint16_t* h, int64_t ldh, const int32_t* tokens, int d, int V, uint16_t* out,
+                                                                 int32_t* first) {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int per_row = d >> 3;
-    const long long n = (long long)M * per_row;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
-        const int m = (int)(i / per_row), c = (int)(i - (long long)m * per_row);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if ((unsigned)tokens[m] < (unsigned)V) v = *reinterpret_cast<const uint4*>(h + m * ldh + 8 * c);
-        *reinterpret_cast<uint4*>(out + (size_t)m * d + 8 * c) = v;
+    const int m = blockIdx.x;
+    const bool scored = (unsigned)tokens[m] < (unsigned)V;
+    for (int c = threadIdx.x * 8; c < d; c += kRowThreads * 8)
+        *reinterpret_cast<uint4*>(out + (size_t)m * d + c) = scored ? *reinterpret_cast<const uint4*>(h + m * ldh + c) : make_uint4(0, 0, 0, 0);
+    for (int v = m * kRowThreads + threadIdx.x; v < V; v += gridDim.x * kRowThreads) first[v] = kNone;
+}
+
+// dW's rows of the given tokens once more, a block per row m that is the first of its token v:
+//   dW[v] = sums[m] + sum of rest[i] h[i] over the rows i whose token is v, in their order
+// Bound by latencies, or by the 8 d bytes a row.  What is added comes from before the product that this waits for, so the
+// first columns' share is ready by then.
+__global__ void __launch_bounds__(kRowThreads) score_given_kernel(const uint16_t* h, int64_t ldh, const int32_t* tokens, const float* rest,
+                                                                  const int32_t* first, const float* sums, int M, int d, int V, uint16_t* dW) {
+    __shared__ int list[kRowThreads], count;
+    const int m = blockIdx.x, t = threadIdx.x, tok = tokens[m];
+    if ((unsigned)tok >= (unsigned)V || first[tok] != m) {
+        grid_dependency_wait();
+        return;
     }
+    for (int c0 = 0; c0 < d; c0 += kRowThreads * 8) {
+        const int c = c0 + t * 8;
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int i0 = m; i0 < M; i0 += kRowThreads) {
+            if (t < 32) {                  // one warp lists the token's rows among these, in order
+                int n = 0;
+#pragma unroll
+                for (int j = 0; j < kRowThreads; j += 32) {
+                    const int i = i0 + j + t;
+                    const bool mine = i < M && tokens[i] == tok;
+                    const unsigned hit = __ballot_sync(0xFFFFFFFFu, mine);
+                    if (mine) list[n + __popc(hit & ((1u << t) - 1u))] = i;
+                    n += __popc(hit);
+                }
+                if (t == 0) count = n;
+            }
+            __syncthreads();
+            if (c < d)
+                for (int j = 0; j < count; ++j) add_scaled(sum, rest[list[j]], *reinterpret_cast<const uint4*>(h + list[j] * ldh + c));
+            __syncthreads();
+        }
+        if (c0 == 0) grid_dependency_wait();
+        if (c < d) {
+            const float4* from = reinterpret_cast<const float4*>(sums + (size_t)m * d + c);
+            const float4 a = from[0], b = from[1];
+            const float all[8] = {sum[0] + a.x, sum[1] + a.y, sum[2] + a.z, sum[3] + a.w, sum[4] + b.x, sum[5] + b.y, sum[6] + b.z, sum[7] + b.w};
+            store_bf16x8(dW + (size_t)tok * d + c, all);
+        }
+    }
+    grid_launch_dependents();
 }
 
 // G's rows: whole 16-byte runs of columns, so that a tensor map can read them
 static int64_t grad_ld(int V) { return (int64_t)round_up((size_t)V, 64); }
 
-size_t score_backward_workspace_bytes(int M, int d, int V) {
-    return kHeaderBytes + round_up((size_t)M * grad_ld(V) * 2, 256) + round_up((size_t)M * d * 2, 256);
+struct GradSpace {              // offsets in the workspace
+    size_t G, h0, rest, first, sums, total;
+};
+static GradSpace grad_space(int M, int d, int V) {
+    GradSpace w;
+    w.G = kHeaderBytes;
+    w.h0 = w.G + round_up((size_t)M * grad_ld(V) * 2, 256);
+    w.rest = w.h0 + round_up((size_t)M * d * 2, 256);
+    w.first = w.rest + round_up((size_t)M * 4, 256);
+    w.sums = w.first + round_up((size_t)V * 4, 256);
+    w.total = w.sums + round_up((size_t)M * d * 4, 256);
+    return w;
 }
+size_t score_backward_workspace_bytes(int M, int d, int V) { return grad_space(M, d, V).total; }
 
 vt_status launch_score_backward(const ScoreCall& c, const float* lse, const float* entropy, const float* grad_logprobs,
                                 const float* grad_entropy, void* grad_h, void* grad_W, void* workspace, cudaStream_t st) {
     unsigned char* base = reinterpret_cast<unsigned char*>(workspace);
     WsHeader* hdr = reinterpret_cast<WsHeader*>(base);
     const int64_t ld = grad_ld(c.V);
-    uint16_t* G = reinterpret_cast<uint16_t*>(base + kHeaderBytes);
-    uint16_t* h0 = reinterpret_cast<uint16_t*>(base + kHeaderBytes + round_up((size_t)c.M * ld * 2, 256));
+    const GradSpace space = grad_space(c.M, c.d, c.V);
+    uint16_t* G = reinterpret_cast<uint16_t*>(base + space.G);
+    uint16_t* h0 = reinterpret_cast<uint16_t*>(base + space.h0);
+    float* rest = reinterpret_cast<float*>(base + space.rest);
+    int32_t* first = reinterpret_cast<int32_t*>(base + space.first);
+    float* sums = reinterpret_cast<float*>(base + space.sums);
     const GemmOperand W{c.W, c.V, c.d, c.d}, g{G, c.M, c.V, ld};
     vt_status r;
-    if (grad_W) {   // h without the rows that are not scored
-        const long long n = (long long)c.M * (c.d >> 3);
-        const int grid = (int)std::min<long long>((n + 255) / 256, 8 * kGemmSms);
-        cudaError_t e = launch_pdl(score_rows_kernel, grid, 256, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
-                                   c.M, c.d, c.V, h0);
+    if (grad_W) {
+        cudaError_t e = launch_pdl(score_rows_kernel, c.M, kRowThreads, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
+                                   c.d, c.V, h0, first);
         count_launch();
         if (e == cudaSuccess) e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e);
@@ -106,7 +266,7 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         if (!gemm_plan(&p, false, false, false, EpiScoreGrad::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, false, pair))) != VT_OK) return r;
-        const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, ld, c.scale, c.V};
+        const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, rest, grad_W ? first : nullptr, ld, c.scale, c.V};
         if ((r = gemm_launch<false, false, EpiScoreGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
     if (grad_h) {   // dh = G W: [M, d], summed over the vocabulary; W has d running fastest
@@ -120,10 +280,11 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         p.prob[0].nk0 = ceil_div(c.V, kBoxK);
         p.b_early = 1;
         p.hdr = hdr;
-        if (!gemm_plan(&p, false, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
+        if (!gemm_plan(&p, false, true, false, EpiGradH::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], g, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, true, pair))) != VT_OK) return r;
-        if ((r = gemm_store(maps, p, pair, false, true, &grad_h, st)) != VT_OK) return r;
+        const EpiGradH::Params ep{reinterpret_cast<uint16_t*>(grad_h), reinterpret_cast<const uint16_t*>(c.W), c.tokens, rest, c.V};
+        if ((r = gemm_launch<false, true, EpiGradH>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
     if (!grad_W) return VT_OK;
     // dW = G^T h: [V, d], summed over the M rows
@@ -136,10 +297,16 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
     p.prob[0].b0 = 1;
     p.prob[0].nk0 = ceil_div(c.M, kBoxK);
     p.hdr = hdr;
-    if (!gemm_plan(&p, true, true, false, EpiStore::kScratch, &pair)) return VT_ERR_SHAPE;
+    if (!gemm_plan(&p, true, true, false, EpiGradW::kScratch, &pair)) return VT_ERR_SHAPE;
     if ((r = gemm_map(&maps.map[0], g, gemm_box_a(p, true))) != VT_OK) return r;
     if ((r = gemm_map(&maps.map[1], GemmOperand{h0, c.M, c.d, c.d}, gemm_box_b(p, true, pair))) != VT_OK) return r;
-    return gemm_store(maps, p, pair, true, true, &grad_W, st);
+    const EpiGradW::Params ep{reinterpret_cast<uint16_t*>(grad_W), first, sums};
+    if ((r = gemm_launch<true, true, EpiGradW>(maps, p, pair, ep, st)) != VT_OK) return r;
+    cudaError_t e = launch_pdl(score_given_kernel, c.M, kRowThreads, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
+                               rest, first, sums, c.M, c.d, c.V, reinterpret_cast<uint16_t*>(grad_W));
+    count_launch();
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? VT_OK : cuda_fail(e);
 }
 
 }  // namespace vt
