@@ -221,7 +221,8 @@ vt_status vt_tree_select(const float* logprobs, const int32_t* target_ids, const
  *                                       their z - lse
  * A row whose token lies outside [0, V) - a padded position, a token the trimmed vocabulary does not keep - is not
  * scored: logprobs, entropy, lse and top_logprobs are 0 and top_ids -1, whatever its hidden state holds.  With
- * tokens == NULL every row is scored and logprobs must be NULL.  The logits are never written to memory.
+ * tokens == NULL every row is scored and logprobs must be NULL.  (The workspace may hold logits: where k is large or the
+ * rows are few, never more than 40 MB of them unless k > 20.)
  *
  *   h       dev [M, d] bf16, rows ldh elements apart (ldh >= d, a multiple of 8), 16-byte aligned
  *   W       dev [V, d] bf16, 16-byte aligned              tokens dev [M] int32 or NULL
@@ -249,7 +250,7 @@ vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32
  *   h, ldh, W, tokens, M, d, V, scale   as in the forward call (tokens required);   lse, entropy  dev [M], its outputs
  *   grad_logprobs  dev [M] float        grad_entropy  dev [M] float or NULL (then entropy may be NULL, too)
  *   grad_h  dev [M, d] bf16 (out) or NULL      grad_W  dev [V, d] bf16 (out) or NULL; at least one; 16-byte aligned
- *   workspace  dev, 256-byte aligned, vt_score_backward_workspace_bytes(M, d, V) bytes (it holds G: 2 M V bytes)
+ *   workspace  dev, 256-byte aligned, vt_score_backward_workspace_bytes(M, d, V) bytes (it holds G, 2 M V bytes, and 6 M d more)
  * Asynchronous.  Gradients are overwritten, not added to. */
 size_t    vt_score_backward_workspace_bytes(int M, int d, int V);
 vt_status vt_score_tokens_backward(const void* h, int64_t ldh, const void* W, const int32_t* tokens,

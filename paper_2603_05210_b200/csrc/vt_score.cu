@@ -12,10 +12,13 @@
 //           k-th largest maximum of all.
 // Lists cost the epilogue more the longer they are (and their first tile most, so that long runs of tiles pay), kept logits
 // their bytes and a longer join.  Measured, us, listed / kept (and without alternatives):
-//     M = 33, V = 32000, d = 4096       k = 8: 59.4 / 56.2   k = 20: 70.9 / 58.9   k = 40: 122 / 66     (51.2)
-//     M = 128, V = 100000, d = 4096     k = 8: 148 / 156     k = 20: 153 / 158     k = 40: 296 / 163    (137)
-//     M = 600, V = 32000, d = 2048      k = 8: 82 / 101      k = 20: 101 / 107                          (75)
-//     M = 4096, V = 32000, d = 4096     k = 8: 744 / 999     k = 20: 893 / 1037                         (728)
+//     M = 33, V = 32000, d = 4096       k = 8: 55.9 / 53.8   k = 20: 70.9 / 57.3       (48.1)
+//     M = 61, V = 32000, d = 4096       k = 8: 55.2 / 54.6   k = 20: 71.8 / 58.4
+//     M = 128, V = 32000, d = 4096      k = 4: 63.8 / 70.1   k = 20: 84.5 / 72.8       (55.6)
+//     M = 300, V = 8000, d = 2048       k = 8: 39.1 / 43.3   k = 20: 62.0 / 46.2       (27.6)
+//     M = 256, V = 32000, d = 2048      k = 8: 50.8 / 61.1   k = 20: 72.5 / 65.5
+//     M = 128, V = 100000, d = 4096     k = 8: 142 / 153     k = 20: 153 / 165         (134)
+//     M = 4096, V = 32000, d = 4096     k = 8: 754 / 951     k = 20: 894 / 981         (687)
 // hence keep_logits() below.
 // Records are joined in the order of their columns and ranked by distinct keys, so the result does not depend on which
 // block ran when.
@@ -410,12 +413,12 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
 
 // ------------------------------------------------------------------------------------------ host
 static int list_entries(int k) { return k == 0 ? 0 : k <= 4 ? 4 : k <= 8 ? 8 : kListMax; }
-// Whether the logits are kept (see the top of this file): always where a list would be too long, up to what stays in L2 for
-// long lists, and for short ones only where so few rows leave the epilogue uncovered.
+// Whether the logits are kept (see the top of this file): always where a list would be too long, for long lists up to where
+// the bytes cost as much, and for short ones only where so few rows leave the epilogue uncovered.
 static bool keep_logits(int M, int k, size_t bytes) {
     if (k == 0) return false;
     if (k > kListMax) return true;
-    return bytes <= (k > 8 ? (size_t)64 << 20 : M <= 128 ? (size_t)16 << 20 : 0);
+    return bytes <= (k > 8 ? (size_t)40 << 20 : M <= 128 ? (size_t)8 << 20 : 0);
 }
 
 struct ScorePlan {

@@ -246,6 +246,37 @@ def test_gradients(vt, M, d, V, with_entropy):
         assert torch.equal(one[0], gh.t) if want_h_too else torch.equal(one[1], gW.t)
 
 
+@pytest.mark.parametrize("M,d,V", [(1, 8, 5), (2, 2056, 300), (40, 4104, 100), (300, 264, 5000), (700, 72, 259)])
+@pytest.mark.parametrize("shared", [1, 3, 1000])
+def test_given_entries_are_rounded_once(vt, M, d, V, shared):
+    """Up to `shared` rows have the same token.  A given token's entry of G enters dh and dW unrounded: of it only the 2^-14 that stand for
+    its own fp32 errors (2^-16) and the sums' are left, beside the other entries' rounding and the result's."""
+    h, W, _ = case(M, d, V, 5 * M + d)
+    rng = np.random.default_rng(M + shared)
+    tokens = np.resize(np.repeat(rng.permutation(V)[:max(1, M // shared)], min(shared, M)), M).astype(np.int32)
+    tokens[0] = V - 1
+    if M > 2:
+        tokens[rng.permutation(M)[: M // 5]] = -1
+    gl = rng.normal(size=M).astype(np.float32)
+    hd, Wd, t = dev(h), dev(W), dev(tokens, torch.int32)
+    r = vt.vt_score_tokens(hd, Wd, t)
+    gh, gW = Guarded((M, d), torch.bfloat16), Guarded((V, d), torch.bfloat16)
+    ws = torch.full((vt.vt_score_backward_workspace_bytes(M, d, V),), 0xFF, dtype=torch.uint8, device="cuda")
+    ws[:512] = 0
+    vt.vt_score_tokens_backward(hd, Wd, t, r.lse, None, torch.from_numpy(gl).cuda(), None, workspace=ws, grad_h=gh.t, grad_W=gW.t)
+    assert vt.vt_last_status(ws) == vt.VT_OK and gh.intact() and gW.intact()
+    want_h, want_W = so.score_backward(h, W, tokens, gl)
+    _, A = so.grad_logits(h, W, tokens, gl)
+    keep = so.scored_rows(tokens, M, V)
+    others, given = A.copy(), np.zeros_like(A)
+    m = np.flatnonzero(keep)
+    given[m, tokens[m]], others[m, tokens[m]] = A[m, tokens[m]], 0.0
+    E = (2.0 ** -8 + 2.0 ** -14) * others + 2.0 ** -14 * given
+    for got, want, terms in ((gh.t, want_h, E @ np.abs(W)), (gW.t, want_W, E[keep].T @ np.abs(h[keep]))):
+        err = np.abs(got.double().cpu().numpy() - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + terms + 1e-30).all()
+
+
 def test_gradients_against_differences(vt):
     """The GPU's gradients along random directions against central differences of the oracle's loss.  The gradients' relative
     error is 2^-8 per element at most and averages out along a direction; the differences' is eps^2: 1 % of the norms' product
