@@ -401,19 +401,25 @@ def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | Non
     (M, d), V, dev = h.shape, W.shape[0], h.device
     if tokens is None and logprobs is not None:
         raise ValueError("logprobs needs tokens")
-    if logprobs is None and entropy is None and lse is None:
-        logprobs, entropy, lse = torch.empty((3, M), dtype=torch.float32, device=dev).unbind(0)
-    if tokens is None:
-        logprobs = None
+    if logprobs is None and entropy is None and lse is None and top_ids is None and top_logprobs is None:
+        # one allocation cut up: five of them, and checking them, take as long as the call itself
+        if k > 0:
+            logprobs, entropy, lse, top_ids, top_logprobs = h.new_empty((M * (3 + 2 * k),), dtype=torch.float32).split_with_sizes(
+                (M, M, M, M * k, M * k))
+            top_ids, top_logprobs = top_ids.view(torch.int32).view(M, k), top_logprobs.view(M, k)
+        else:
+            logprobs, entropy, lse = h.new_empty((M * 3,), dtype=torch.float32).split_with_sizes((M, M, M))
+        if tokens is None:
+            logprobs = None
     else:
-        logprobs = _out(logprobs, "logprobs", (M,), torch.float32, h)
-    entropy = _out(entropy, "entropy", (M,), torch.float32, h)
-    lse = _out(lse, "lse", (M,), torch.float32, h)
-    if k > 0:
-        top_ids = _out(top_ids, "top_ids", (M, k), torch.int32, h)
-        top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, h)
-    else:
-        top_ids = top_logprobs = None
+        logprobs = None if tokens is None else _out(logprobs, "logprobs", (M,), torch.float32, h)
+        entropy = _out(entropy, "entropy", (M,), torch.float32, h)
+        lse = _out(lse, "lse", (M,), torch.float32, h)
+        if k > 0:
+            top_ids = _out(top_ids, "top_ids", (M, k), torch.int32, h)
+            top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, h)
+        else:
+            top_ids = top_logprobs = None
     if workspace is None:
         workspace = _scratch(None, vt_score_workspace_bytes(M, d, V, k), dev)
     _check(lib().vt_score_tokens(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), M, d, V, scale, k, _ptr(logprobs),
