@@ -26,6 +26,17 @@ def test_two_tokens_by_hand():
         assert list(r["top_ids"][0]) == ([1, 0] if s > 0 else [0, 1])
 
 
+def test_a_common_shift_of_the_logits_moves_only_the_log_sum_exp():
+    rng = np.random.default_rng(9)
+    h, W, t = rng.normal(size=(4, 6)), rng.normal(size=(9, 6)), [0, 3, 5, 8]
+    plain = so.score(h, W, t, k=3)
+    assert np.allclose(plain["lse"], [math.log(sum(math.exp(sum(a * b for a, b in zip(x, w))) for w in W)) for x in h])
+    for c in (-1000.0, 7.0, 1000.0):
+        r = so.score(np.hstack([h, np.full((4, 1), c)]), np.hstack([W, np.ones((9, 1))]), t, k=3)
+        assert np.allclose(r["lse"], plain["lse"] + c) and (r["top_ids"] == plain["top_ids"]).all()
+        assert all(np.allclose(r[n], plain[n], atol=1e-11) for n in ("logprobs", "entropy", "top_logprobs"))
+
+
 def test_scale_is_a_temperature():
     rng = np.random.default_rng(1)
     h, W, t = rng.normal(size=(4, 6)), rng.normal(size=(9, 6)), [0, 1, 2, 3]
