@@ -12,14 +12,15 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     for (int i = 0; i < p->n_prob; ++i) max_m = std::max(max_m, p->prob[i].M);
     const int tile_rows = 128 / p->rep;
     if (p->splits > 1) scratch_bytes = 0;        // its results are not staged
-    p->a_rows = (uint32_t)(a_mn ? 128 : std::min(tile_rows, (int)round_up(max_m, 8)));
+    const int box_m = (int)round_up((size_t)std::min(max_m, 128), 8);
+    p->a_rows = (uint32_t)(a_mn ? 128 : std::min(tile_rows, box_m));
     p->a_bytes = p->rep > 1 ? 16384u : p->a_rows * 128u;
     p->b_bytes = (uint32_t)(pair ? p->NT / 2 : p->NT) * 128u;
     p->tx_bytes = p->a_rows * 128u * (uint32_t)p->rep + p->b_bytes;
     p->blk_bytes = p->a_bytes + (uint32_t)round_up(p->b_bytes, 1024);
     const size_t bar_bytes = (size_t)(2 * kGemmMaxStages + 6) * 8 + sizeof(GemmTable);      // barriers, two words, the problems
     const int groups = (p->dual ? p->NT / 2 : p->NT) / 8;
-    p->x_rows = (uint32_t)std::min(128, (int)round_up(max_m, 8));
+    p->x_rows = (uint32_t)box_m;
     p->x_part = p->x_rows * (uint32_t)(ceil_div(groups, p->splits) * (p->dual ? 16 : 8) * 4);
     const size_t partial = p->splits > 1 ? (size_t)p->x_part * p->splits : 0;
     const size_t over = 16384 - p->a_bytes;      // an MMA reads 128 rows of A wherever they end

@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(kRowThreads) score_rows_kernel(const uint16_t*
     const bool scored = (unsigned)tokens[m] < (unsigned)V;
     for (int c = threadIdx.x * 8; c < d; c += kRowThreads * 8)
         *reinterpret_cast<uint4*>(out + (size_t)m * d + c) = scored ? *reinterpret_cast<const uint4*>(h + m * ldh + c) : make_uint4(0, 0, 0, 0);
-    for (int v = m * kRowThreads + threadIdx.x; v < V; v += gridDim.x * kRowThreads) first[v] = kNone;
+    // in 64 bits: M blocks of 256 threads pass 2^31 from 8388608 rows on
+    for (long long v = (long long)m * kRowThreads + threadIdx.x; v < V; v += (long long)gridDim.x * kRowThreads) first[v] = kNone;
 }
 
 // dW's rows of the given tokens once more, a block per row m that is the first of its token v:

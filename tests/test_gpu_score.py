@@ -366,3 +366,38 @@ def test_offsets_past_32_bits(vt):
     assert (err <= 2.0 ** -7 * (G.abs().T @ h[:, 0].double().abs()) + 1e-12).all()
     assert (gW[:, 1:] == 0).all()
     assert (gh[:, 0].double() - G @ W[:, 0].double()).abs().max() < 2.0 ** -7 * float((G.abs() @ W[:, 0].double().abs()).max())
+
+
+def test_more_rows_than_32_bit_thread_indices(vt):
+    """2^24 + 5 rows: one thread per row and 256 per block pass 2^31 and 2^32.  A handful of rows are scored, the first, the last and
+    those around 2^23 and 2^24; nothing of the others may appear anywhere.  Tolerances as above: h and W lie on binary grids, G
+    is one rounding (the given entries none) from its value, the result one more."""
+    M, d, V = 2 ** 24 + 5, 8, 9
+    at = torch.tensor([0, 1, 2 ** 23 - 1, 2 ** 23, 2 ** 23 + 1, 2 ** 24 - 1, 2 ** 24, M - 1], device="cuda")
+    given = torch.tensor([3, 8, 3, 0, 5, 3, 8, 7], dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    h = torch.full((M, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    h[at] = (torch.randint(-32, 33, (len(at), d), device="cuda", generator=gen) / 16).bfloat16()
+    W = (torch.randint(-255, 256, (V, d), device="cuda", generator=gen) / 256).bfloat16()
+    tokens = torch.full((M,), -1, dtype=torch.int32, device="cuda")
+    tokens[at] = given
+    r = vt.vt_score_tokens(h, W, tokens)
+    rows, w = h[at].double(), W.double()
+    logp = torch.log_softmax(rows @ w.T, 1)
+    want = logp.gather(1, given.long()[:, None])[:, 0]
+    assert ((r.logprobs[at].double() - want).abs() <= 4e-6 + 2.0 ** -22 * want.abs()).all()
+    assert int((r.lse != 0).sum()) == len(at) and int((r.logprobs != 0).sum()) == len(at)
+    gl = torch.ones(M, device="cuda")
+    ws = vt.new_workspace(vt.vt_score_backward_workspace_bytes(M, d, V))
+    dh, dW = vt.vt_score_tokens_backward(h, W, tokens, r.lse, None, gl, workspace=ws)
+    assert vt.vt_last_status(ws) == vt.VT_OK
+    p = logp.exp()
+    G = -p
+    G[torch.arange(len(at)), given.long()] += 1
+    A = p.clone()
+    A[torch.arange(len(at)), given.long()] += 1
+    slack = 2.0 ** -8 + 2.0 ** -14
+    for got, exact, terms in ((dh[at], G @ w, A @ w.abs()), (dW, G.T @ rows, A.T @ rows.abs())):
+        assert ((got.double() - exact).abs() <= 2.0 ** -8 * exact.abs() + slack * terms).all()
+    dh[at] = 0
+    assert not dh.any()
