@@ -526,8 +526,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     if (!got) fail();
                 }
                 if (!got) continue;
-                if (p.splits > 1) break;                           // the tile is finished below, with the rest of the cluster
                 tc_fence_after();
+                if (p.splits > 1) break;                           // the tile is finished below, with the rest of the cluster
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)buf * p.acc_cols;
                 // The accumulator has been read: the MMAs of the tile after next may start.  Relaxed, as nothing in memory is
                 // handed over: a release would wait for this warp's stores of results, 1600 cycles a tile.
@@ -622,6 +622,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             const int cols = Epi::kDual ? p.NT >> 1 : p.NT, groups = cols >> 3;
             const int rows = min(128, q.M - it.mt * 128);
             cluster_sync_all();                                    // every ring is idle: the sums go where it was
+            tc_fence_after();                                      // the barrier may have ordered the sums after other warps' waits
             const int r = (warp & 3) * 32 + lane;
             if (warp < kGemmEpiWarps && (warp & 3) * 32 < rows && __all_sync(0xFFFFFFFFu, *abort_flag == 0)) {
                 // partial sums to the owners of their columns, eight columns at a time

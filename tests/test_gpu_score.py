@@ -401,3 +401,24 @@ def test_more_rows_than_32_bit_thread_indices(vt):
         assert ((got.double() - exact).abs() <= 2.0 ** -8 * exact.abs() + slack * terms).all()
     dh[at] = 0
     assert not dh.any()
+
+
+@pytest.mark.parametrize("M,d,V", [(4096, 512, 300), (1000, 64, 45), (600, 1024, 130)])
+def test_weight_gradients_from_divided_sums(vt, M, d, V):
+    """Many rows and a small vocabulary: the sums of dW (and their fp32 copies for given tokens) are divided among a cluster's CTAs, whose
+    tiles end inside a warp's rows.  Tolerances as in test_gradients."""
+    rng = np.random.default_rng(21)
+    h, W, tokens = case(M, d, V, M + V)
+    tokens[::5] = -1
+    gl, ge = rng.normal(size=M).astype(np.float32), rng.normal(size=M).astype(np.float32)
+    hd, Wd, t = dev(h), dev(W), dev(tokens, torch.int32)
+    r = vt.vt_score_tokens(hd, Wd, t)
+    grads = [vt.vt_score_tokens_backward(hd, Wd, t, r.lse, r.entropy, torch.from_numpy(gl).cuda(), torch.from_numpy(ge).cuda()) for _ in range(2)]
+    assert torch.equal(grads[0][0], grads[1][0]) and torch.equal(grads[0][1], grads[1][1])
+    want_h, want_W = so.score_backward(h, W, tokens, gl, ge)
+    _, A = so.grad_logits(h, W, tokens, gl, ge)
+    keep = so.scored_rows(tokens, M, V)
+    slack = 2.0 ** -8 + 2.0 ** -14
+    for got, want, terms in zip(grads[0], (want_h, want_W), (A @ np.abs(W), A[keep].T @ np.abs(h[keep]))):
+        err = np.abs(got.double().cpu().numpy() - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + slack * terms + 1e-30).all()
