@@ -159,6 +159,7 @@ struct AccColumns {
     // all lanes must call it; returns how many of the 16 columns lie inside D (<= 0: none)
     __device__ __forceinline__ int load(int ch, float (&x)[16]) const {
         uint32_t u[16];
+        __syncwarp();                // the lanes part where rows differ (given tokens, rows past the last)
         acc_ld16(taddr + (uint32_t)(ch * 16), u);
         tc_wait_ld();
 #pragma unroll
@@ -544,12 +545,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 if constexpr (Epi::kStateful) {
                     Epi::tile(st, ep, m, AccColumns{taddr, ch0, ch1, col0, q.N}, smem + p.scratch_off);
                 } else if (m - lane < q.M) {                       // some row of this warp exists
-                    // 32 columns at a time to the warp's staging rows (of kStageCols columns), and from there to memory whenever
+                    // 32 columns at a time to the warp's staging rows (kStageUnits times 32 columns), and from there to memory whenever
                     // they are full, several lanes to a row
                     const int rows_here = min(32, q.M - (m - lane));
                     for (int g = g0; g < g1; ++g) {
                         const int unit = (g - g0) % kStageUnits;
                         uint32_t u[32], w[Epi::kDual ? 32 : 1];
+                        __syncwarp();                              // tcgen05.ld is the whole warp's; rows part in what they ask for and store
                         acc_ld16(taddr + (uint32_t)(g * 32), reinterpret_cast<uint32_t(&)[16]>(u[0]));
                         if (g * 32 + 16 < cols) acc_ld16(taddr + (uint32_t)(g * 32 + 16), reinterpret_cast<uint32_t(&)[16]>(u[16]));
                         if constexpr (Epi::kDual) {
@@ -622,7 +624,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
             const int cols = Epi::kDual ? p.NT >> 1 : p.NT, groups = cols >> 3;
             const int rows = min(128, q.M - it.mt * 128);
             cluster_sync_all();                                    // every ring is idle: the sums go where it was
-            tc_fence_after();                                      // the barrier may have ordered the sums after other warps' waits
             const int r = (warp & 3) * 32 + lane;
             if (warp < kGemmEpiWarps && (warp & 3) * 32 < rows && __all_sync(0xFFFFFFFFu, *abort_flag == 0)) {
                 // partial sums to the owners of their columns, eight columns at a time
@@ -630,14 +631,14 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 const int nch = (cols + 15) >> 4, half = warp >> 2;
                 for (int ch = half * nch / 2; ch < (half + 1) * nch / 2; ++ch) {
                     uint32_t u[16], w[16];
+                    __syncwarp();                                  // lanes past the rows have not stored what the others have
                     acc_ld16(taddr + (uint32_t)(ch * 16), u);
                     if constexpr (Epi::kDual) acc_ld16(taddr + (uint32_t)(cols + ch * 16), w);
                     tc_wait_ld();
-                    if (r >= rows) continue;
 #pragma unroll
                     for (int e = 0; e < 16; e += 8) {
                         const int g = ch * 2 + (e >> 3);
-                        if (g >= groups) break;
+                        if (g >= groups || r >= rows) break;
                         int owner = (int)((unsigned)(g * p.splits) / (unsigned)groups);
                         if (g >= (owner + 1) * groups / p.splits) ++owner;     // shares are [owner * groups / splits, ...); splits <= groups
                         const int local = g - owner * groups / p.splits;
