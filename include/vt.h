@@ -231,7 +231,8 @@ vt_status vt_tree_select(const float* logprobs, const int32_t* target_ids, const
  *   workspace  dev, 256-byte aligned, vt_score_workspace_bytes(M, d, V, k) bytes; it needs no initialisation except for
  *              vt_last_status, which reads a status word that vt_workspace_init clears
  * d % 8 == 0, d >= 8, 0 <= k <= min(V, VT_MAX_K), scale finite and > 0, else VT_ERR_SHAPE; any M >= 1.  Inputs must be
- * finite in the rows that are scored; a NaN stays in its row.  Asynchronous; results do not depend on timing. */
+ * finite in the rows that are scored, and x and z there finite in fp32 and, within a row, no further apart than 2e38; a NaN stays in
+ * its row.  Asynchronous; results do not depend on timing. */
 size_t    vt_score_workspace_bytes(int M, int d, int V, int k);
 vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32_t* tokens,
                           int M, int d, int V, float scale, int k,

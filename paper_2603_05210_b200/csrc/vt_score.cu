@@ -4,8 +4,8 @@
 //   H = -sum_v p log p = log s - E[z - max],  s = sum_v e^(z - max),  E[y] = sum_v e^(z - max) y / s
 //
 // One pass over the head.  gemm_kernel gives every epilogue thread a row of the tile and a range of its columns; the thread
-// folds them into a running (max, s, e = sum of (x - max) e^(z - max)) - kept about the maximum, because lse and E[z] are
-// both large where H is small - and picks the given token's logit when it comes by.  At the end of a run of tiles it
+// folds them into a running (max, s, e = sum of t 2^t, t = (x - max) scale log2 e) - kept about the maximum, because lse and E[z]
+// are both large where H is small, and in units of t, because sums of x - max overflow where the scale is next to nothing - and picks the given token's logit when it comes by.  At the end of a run of tiles it
 // writes one record; a second, small kernel (one block per row) joins a row's records.  The k best come in one of two ways:
 //   listed  no logit is written; every thread keeps a register list of its k best, and the join merges the lists;
 //   kept    the logits go to the workspace, and the join reads back the handful of ranges whose maximum is not below the
@@ -22,13 +22,15 @@
 // hence keep_logits() below.
 // Records are joined in the order of their columns and ranked by distinct keys, so the result does not depend on which
 // block ran when.
+#include <cfloat>
+
 #include "vt_score.h"
 
 #include "vt_gemm.cuh"
 
 namespace vt {
 
-constexpr float kMasked = -1e38f;          // stands for a column past the vocabulary: e^ gives 0, and nothing finite is below it
+constexpr float kLowest = -FLT_MAX;       // the running maximum of no columns: no finite logit is below it
 
 struct ScoreRecords {
     float4* stats;                         // [M][L]: max, s, e, unused
@@ -39,6 +41,10 @@ struct ScoreRecords {
     int L;                                 // records per row
     int parts, NT, tiles_per_item;         // record -> columns: parts per item, columns per tile, tiles per item
 };
+
+constexpr float kLn2 = 0.6931471805599453f;
+// scale * log2(e), finite: (max - max) times it has to be 0
+__host__ __device__ inline float exponent_scale(float scale) { return fminf(scale * kLog2e, FLT_MAX); }
 
 constexpr int kListQueue = 24;             // candidates a thread queues between insertions
 constexpr int kListMax = 20;                // entries of the longest list
@@ -67,31 +73,45 @@ struct EpiScore {
         int ix[KL];
     };
     static __device__ __forceinline__ void begin(State& st, const Params& ep, int m) {
-        st.mx = kMasked;
+        st.mx = kLowest;
         st.s = st.e = 0.0f;
         st.tok = ep.tokens != nullptr && m < ep.M ? ep.tokens[m] : -1;
         st.first = true;
         st.bound = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < KL; ++j) { st.v[j] = kMasked; st.ix[j] = -1; }
+        for (int j = 0; j < KL; ++j) { st.v[j] = -INFINITY; st.ix[j] = -1; }
     }
     static constexpr int kThreads = kGemmEpiWarps * 32;
-    // the largest float below x
+    // the largest float below x (-inf: itself)
     static __device__ __forceinline__ float below(float x) {
+        if (x == -INFINITY) return x;
         const int b = __float_as_int(x + 0.0f);
         return b == 0 ? -__int_as_float(1) : __int_as_float(b > 0 ? b - 1 : b + 1);
     }
+    // columns past the vocabulary: below every logit
     static __device__ __forceinline__ void mask(float (&x)[16], int live) {
         if (live < 16) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = i < live ? x[i] : kMasked;
+            for (int i = 0; i < 16; ++i) x[i] = i < live ? x[i] : -INFINITY;
+        }
+    }
+    // Adds 2^t and t 2^t of a run's columns.  PART: of the first `live` of them; that the others' terms are 0
+    // cannot be left to the exponential, which a scale near 0 takes to 1 for any finite logit.
+    template <bool PART>
+    static __device__ __forceinline__ void add_terms(const float (&x)[16], int live, float nm, float c, float (&s)[2], float (&e)[2]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float t = !PART || i < live ? (x[i] - nm) * c : 0.0f;
+            const float p = !PART || i < live ? ex2_approx(t) : 0.0f;
+            s[i & 1] += p;
+            e[i & 1] = fmaf(p, t, e[i & 1]);
         }
     }
     static __device__ __forceinline__ void tile(State& st, const Params& ep, int m, const AccColumns& cols, unsigned char* scratch) {
         float g[KL];
         if constexpr (KR > 0) {
 #pragma unroll
-            for (int j = 0; j < KL; ++j) g[j] = kMasked;
+            for (int j = 0; j < KL; ++j) g[j] = -INFINITY;
         }
         for (int ch = cols.ch0; ch < cols.ch1; ++ch) {
             float x[16];
@@ -102,19 +122,12 @@ struct EpiScore {
 #pragma unroll
             for (int i = 0; i < 4; ++i) gm[i] = fmaxf(fmaxf(x[4 * i], x[4 * i + 1]), fmaxf(x[4 * i + 2], x[4 * i + 3]));
             const float nm = fmaxf(st.mx, fmaxf(fmaxf(gm[0], gm[1]), fmaxf(gm[2], gm[3])));
-            const float back = st.mx - nm, f = ex2_approx(back * ep.c);
-            float s0 = 0.0f, s1 = 0.0f, e0 = 0.0f, e1 = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float y0 = x[i] - nm, y1 = x[i + 1] - nm;
-                const float p0 = ex2_approx(y0 * ep.c), p1 = ex2_approx(y1 * ep.c);
-                s0 += p0;
-                s1 += p1;
-                e0 = fmaf(p0, y0, e0);
-                e1 = fmaf(p1, y1, e1);
-            }
-            st.e = fmaf(f, fmaf(back, st.s, st.e), e0 + e1);
-            st.s = fmaf(f, st.s, s0 + s1);
+            const float back = st.s > 0.0f ? (st.mx - nm) * ep.c : 0.0f, f = ex2_approx(back);     // nothing summed yet: nothing to rescale
+            float s2[2] = {0.0f, 0.0f}, e2[2] = {0.0f, 0.0f};
+            if (live >= 16) add_terms<false>(x, 16, nm, ep.c, s2, e2);
+            else add_terms<true>(x, live, nm, ep.c, s2, e2);
+            st.e = fmaf(f, fmaf(back, st.s, st.e), e2[0] + e2[1]);
+            st.s = fmaf(f, st.s, s2[0] + s2[1]);
             st.mx = nm;
             const int at = st.tok - col;
             if ((unsigned)at < (unsigned)min(live, 16)) {
@@ -150,7 +163,7 @@ struct EpiScore {
                 const int cnt = (int)(qx - qx0) / (kThreads * 4);
                 const int most = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)cnt);
                 for (int i = 0; i < most; ++i) {
-                    const float x = i < cnt ? reinterpret_cast<const float*>(scratch)[i * kThreads + threadIdx.x] : kMasked;   // beats nothing
+                    const float x = i < cnt ? reinterpret_cast<const float*>(scratch)[i * kThreads + threadIdx.x] : -INFINITY;   // beats nothing
                     rows_insert<KL>(st.v, st.ix, x, cols.col0 + (int)scratch[kListQueue * kThreads * 4 + i * kThreads + threadIdx.x]);
                 }
                 qx = qx0;
@@ -231,7 +244,7 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
     grid_dependency_wait();
     const float4* stats = p.rec.stats + (size_t)m * L;
     const unsigned long long* keys = p.rec.keys + (size_t)m * L * k;
-    const float c = p.scale * kLog2e;
+    const float c = exponent_scale(p.scale);
     const bool scored = row_scored(p.tokens, p.V, m);
     const float given = p.tokens != nullptr ? p.rec.given[m] : 0.0f;      // stale where the row is not scored, and then not used
     // a thread's records in registers, with the best key of each; kept: the range by its maximum
@@ -240,7 +253,7 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
 #pragma unroll
     for (int i = 0; i < kJoinHeld; ++i) {
         const int l = t + i * T;
-        r[i] = l < L ? stats[l] : make_float4(kMasked, 0.0f, 0.0f, 0.0f);
+        r[i] = l < L ? stats[l] : make_float4(kLowest, 0.0f, 0.0f, 0.0f);
         if constexpr (!KEPT) held[i] = l < L && k > 0 ? keys[(size_t)l * k] : 0ull;
     }
     if (!scored) {
@@ -256,7 +269,7 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
         return;
     }
     auto range_key = [](const float4& q) { return q.y > 0.0f ? make_key(q.x, 0) : 0ull; };
-    float mx = kMasked;
+    float mx = kLowest;
     uint32_t head = 0u;
 #pragma unroll
     for (int i = 0; i < kJoinHeld; ++i) {
@@ -273,7 +286,7 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
     mx = block_reduce<T, false>(mx, buf[0]);
     float s = 0.0f, e = 0.0f;
     auto fold = [&](const float4& q) {
-        const float back = q.x - mx, f = ex2_approx(back * c);
+        const float back = q.y > 0.0f ? (q.x - mx) * c : 0.0f, f = ex2_approx(back);       // a record of no columns adds 0
         s = fmaf(f, q.y, s);
         e = fmaf(f, fmaf(back, q.y, q.z), e);
     };
@@ -285,7 +298,7 @@ __global__ void __launch_bounds__(T) score_join_kernel(const ScoreJoin p) {
     const float log_s = logf(s);
     if (t == 0) {
         if (o.lse) o.lse[m] = fmaf(p.scale, mx, log_s);
-        if (o.entropy) o.entropy[m] = log_s - p.scale * (e / s);
+        if (o.entropy) o.entropy[m] = log_s - kLn2 * (e / s);
         if (o.logprobs) o.logprobs[m] = p.scale * (given - mx) - log_s;
     }
     if (k == 0) return;
@@ -459,7 +472,7 @@ size_t score_workspace_bytes(int M, int d, int V, int k) {
 template <int KR>
 static vt_status run_score(const GemmMaps& maps, const ScorePlan& s, const ScoreCall& c, const ScoreRecords& rec, const ScoreOut& o,
                            cudaStream_t st) {
-    const typename EpiScore<KR>::Params ep{c.tokens, rec, c.scale * kLog2e, c.M, c.V, o.k};
+    const typename EpiScore<KR>::Params ep{c.tokens, rec, exponent_scale(c.scale), c.M, c.V, o.k};
     vt_status r = gemm_launch<false, false, EpiScore<KR>>(maps, s.p, s.pair, ep, st);
     if (r != VT_OK) return r;
     const ScoreJoin join{rec, o, c.tokens, c.V, c.scale};

@@ -422,3 +422,30 @@ def test_weight_gradients_from_divided_sums(vt, M, d, V):
     for got, want, terms in zip(grads[0], (want_h, want_W), (A @ np.abs(W), A[keep].T @ np.abs(h[keep]))):
         err = np.abs(got.double().cpu().numpy() - want)
         assert (err <= 2.0 ** -8 * np.abs(want) + slack * terms + 1e-30).all()
+
+
+@pytest.mark.parametrize("M", [3, 200])
+@pytest.mark.parametrize("k", [0, 4, 20, 30])
+@pytest.mark.parametrize("scale", [1e-44, 1e-38, 1e-37, 1e-30, 1e30, 2.5e38])
+def test_any_finite_scale(vt, M, k, scale):
+    """Scales that flatten every difference (columns past the vocabulary must still weigh nothing) and ones that leave one token alone."""
+    V, d = 1003, 64
+    h, W, tokens = case(M, d, V, 22)
+    h, W = h / 16, W / 16                        # exact in bf16: |scale x| stays below the largest float
+    scale = float(np.float32(scale))
+    want = so.score(h, W, tokens, k, scale)
+    assert np.abs(want["lse"]).max() < 3e38
+    check(run(vt, dev(h), dev(W), dev(tokens, torch.int32), k, scale), want, V)
+
+
+@pytest.mark.parametrize("M", [3, 200])
+@pytest.mark.parametrize("k", [0, 4, 20, 30])
+def test_logits_near_the_lowest_float(vt, M, k):
+    """Every logit between -1.1e38 and -2.6e38, scaled to differences of a few units."""
+    V, d = 90, 8
+    h, W = np.zeros((M, d)), np.zeros((V, d))
+    h[:, 0] = 1.0
+    W[:, 0] = -(1.28125 + np.random.default_rng(23).permutation(V) / 64.0) * 2.0 ** 126
+    tokens = (np.arange(M) % V).astype(np.int32)
+    scale = 2.0 ** -126
+    check(run(vt, dev(h), dev(W), dev(tokens, torch.int32), k, scale), so.score(h, W, tokens, k, scale), V)
