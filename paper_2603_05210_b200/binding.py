@@ -148,8 +148,13 @@ def _out(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, li
     return t
 
 
-def _scratch(workspace: torch.Tensor | None, nbytes: int, device) -> torch.Tensor:
-    return workspace if workspace is not None else torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+def _scratch(workspace: torch.Tensor | None, nbytes, *sizes, device) -> torch.Tensor:
+    """The caller's workspace, which must be on the device, or a new one of nbytes(*sizes)."""
+    if workspace is None:
+        return torch.empty(max(nbytes(*sizes), 256), dtype=torch.uint8, device=device)
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous CUDA tensor")
+    return workspace
 
 
 def vt_workspace_bytes(M: int, k: int) -> int:
@@ -420,11 +425,10 @@ def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | Non
             top_logprobs = _out(top_logprobs, "top_logprobs", (M, k), torch.float32, h)
         else:
             top_ids = top_logprobs = None
-    if workspace is None:
-        workspace = _scratch(None, vt_score_workspace_bytes(M, d, V, k), dev)
+    workspace = _scratch(workspace, vt_score_workspace_bytes, M, d, V, k, device=dev)
     _check(lib().vt_score_tokens(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), M, d, V, scale, k, _ptr(logprobs),
                                  entropy.data_ptr(), lse.data_ptr(), _ptr(top_ids), _ptr(top_logprobs),
-                                 workspace.data_ptr(), workspace.numel(), _stream()), "vt_score_tokens")
+                                 workspace.data_ptr(), workspace.nbytes, _stream()), "vt_score_tokens")
     return VtScores(logprobs, entropy, lse, top_ids, top_logprobs)
 
 
@@ -443,11 +447,10 @@ def vt_score_tokens_backward(h: torch.Tensor, W: torch.Tensor, tokens: torch.Ten
         _f32(entropy, "entropy", (M,)), _f32(grad_entropy, "grad_entropy", (M,))
     grad_h = _out(grad_h, "grad_h", (M, d), torch.bfloat16, h) if want_h else None
     grad_W = _out(grad_W, "grad_W", (V, d), torch.bfloat16, W) if want_W else None
-    if workspace is None:
-        workspace = _scratch(None, vt_score_backward_workspace_bytes(M, d, V), dev)
+    workspace = _scratch(workspace, vt_score_backward_workspace_bytes, M, d, V, device=dev)
     _check(lib().vt_score_tokens_backward(h.data_ptr(), _ld(h), W.data_ptr(), _ptr(tokens), lse.data_ptr(), _ptr(entropy),
                                           grad_logprobs.data_ptr(), _ptr(grad_entropy), M, d, V, scale, _ptr(grad_h), _ptr(grad_W),
-                                          workspace.data_ptr(), workspace.numel(), _stream()), "vt_score_tokens_backward")
+                                          workspace.data_ptr(), workspace.nbytes, _stream()), "vt_score_tokens_backward")
     return grad_h, grad_W
 
 
@@ -482,10 +485,9 @@ def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_do
     out = _out(out, "out", (M, d), torch.bfloat16, x)
     if saved is not None:
         _f32(saved, "saved", (M, 2 * f))
-    if workspace is None:
-        workspace = _scratch(None, vt_gated_ffn_workspace_bytes(M, d, f), x.device)
+    workspace = _scratch(workspace, vt_gated_ffn_workspace_bytes, M, d, f, device=x.device)
     _check(lib().vt_gated_ffn(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), M, d, f,
-                              _ACTS.get(act, act), out.data_ptr(), _ptr(saved), workspace.data_ptr(), workspace.numel(),
+                              _ACTS.get(act, act), out.data_ptr(), _ptr(saved), workspace.data_ptr(), workspace.nbytes,
                               _stream()), "vt_gated_ffn")
     return out
 
@@ -504,12 +506,11 @@ def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Ten
     grad_W_gate = _out(grad_W_gate, "grad_W_gate", (f, d), torch.bfloat16, W_gate)
     grad_W_up = _out(grad_W_up, "grad_W_up", (f, d), torch.bfloat16, W_up)
     grad_W_down = _out(grad_W_down, "grad_W_down", (d, f), torch.bfloat16, W_down)
-    if workspace is None:
-        workspace = _scratch(None, vt_gated_ffn_backward_workspace_bytes(M, d, f), dev)
+    workspace = _scratch(workspace, vt_gated_ffn_backward_workspace_bytes, M, d, f, device=dev)
     _check(lib().vt_gated_ffn_backward(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), saved.data_ptr(),
                                        grad_y.data_ptr(), _ld(grad_y), M, d, f, _ACTS.get(act, act), grad_x.data_ptr(),
                                        grad_W_gate.data_ptr(), grad_W_up.data_ptr(), grad_W_down.data_ptr(), workspace.data_ptr(),
-                                       workspace.numel(), _stream()), "vt_gated_ffn_backward")
+                                       workspace.nbytes, _stream()), "vt_gated_ffn_backward")
     return grad_x, grad_W_gate, grad_W_up, grad_W_down
 
 
