@@ -454,7 +454,13 @@ def vt_score_tokens_backward(h: torch.Tensor, W: torch.Tensor, tokens: torch.Ten
     return grad_h, grad_W
 
 
-_ACTS = {"silu": VT_ACT_SILU, "gelu": VT_ACT_GELU}
+_ACTS = {"silu": VT_ACT_SILU, "gelu": VT_ACT_GELU, VT_ACT_SILU: VT_ACT_SILU, VT_ACT_GELU: VT_ACT_GELU}
+
+
+def _act(act: str | int) -> int:
+    if act not in _ACTS:
+        raise ValueError(f"act: expected 'silu' or 'gelu' (or VT_ACT_SILU, VT_ACT_GELU), got {act!r}")
+    return _ACTS[act]
 
 
 def vt_gated_ffn_workspace_bytes(M: int, d: int, f: int) -> int:
@@ -487,7 +493,7 @@ def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_do
         _f32(saved, "saved", (M, 2 * f))
     workspace = _scratch(workspace, vt_gated_ffn_workspace_bytes, M, d, f, device=x.device)
     _check(lib().vt_gated_ffn(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), M, d, f,
-                              _ACTS.get(act, act), out.data_ptr(), _ptr(saved), workspace.data_ptr(), workspace.nbytes,
+                              _act(act), out.data_ptr(), _ptr(saved), workspace.data_ptr(), workspace.nbytes,
                               _stream()), "vt_gated_ffn")
     return out
 
@@ -508,7 +514,7 @@ def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Ten
     grad_W_down = _out(grad_W_down, "grad_W_down", (d, f), torch.bfloat16, W_down)
     workspace = _scratch(workspace, vt_gated_ffn_backward_workspace_bytes, M, d, f, device=dev)
     _check(lib().vt_gated_ffn_backward(x.data_ptr(), _ld(x), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), saved.data_ptr(),
-                                       grad_y.data_ptr(), _ld(grad_y), M, d, f, _ACTS.get(act, act), grad_x.data_ptr(),
+                                       grad_y.data_ptr(), _ld(grad_y), M, d, f, _act(act), grad_x.data_ptr(),
                                        grad_W_gate.data_ptr(), grad_W_up.data_ptr(), grad_W_down.data_ptr(), workspace.data_ptr(),
                                        workspace.nbytes, _stream()), "vt_gated_ffn_backward")
     return grad_x, grad_W_gate, grad_W_up, grad_W_down

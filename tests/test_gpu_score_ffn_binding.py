@@ -37,3 +37,16 @@ def test_workspaces(vt):
             call(torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
         assert e.value.status == vt.VT_ERR_WORKSPACE
         call(torch.empty((need + 3) // 4, dtype=torch.float32, device="cuda"))             # its bytes count, whatever its type
+
+
+def test_activations(vt):
+    M, d, f = 3, 64, 72
+    x, g, u, dn = (torch.randn(r, c, device="cuda").bfloat16() for r, c in ((M, d), (f, d), (f, d), (d, f)))
+    saved = torch.empty(M, 2 * f, device="cuda")
+    for name, number in (("silu", vt.VT_ACT_SILU), ("gelu", vt.VT_ACT_GELU)):
+        assert torch.equal(vt.vt_gated_ffn(x, g, u, dn, act=name, saved=saved), vt.vt_gated_ffn(x, g, u, dn, act=number))
+    for bad in ("relu", "SiLU", 2, -1, None):
+        with pytest.raises(ValueError):
+            vt.vt_gated_ffn(x, g, u, dn, act=bad)
+        with pytest.raises(ValueError):
+            vt.vt_gated_ffn_backward(x, g, u, dn, saved, x, act=bad)
