@@ -36,6 +36,7 @@ struct EpiScoreGrad {
         uint16_t* G;
         float* rest;            // [M] what rounding the given token's entry left over
         int32_t* first;         // per token: the first row it was given to, or kNone; null when nobody asks
+        int32_t* count;         // per token: the rows it was given to
         int64_t ldg;
         float scale;
         int V;
@@ -71,7 +72,10 @@ struct EpiScoreGrad {
                     rest = out[0][i] - __bfloat162float(__float2bfloat16_rn(out[0][i]));
                 }
             ep.rest[m] = rest;
-            if (ep.first) atomicMin(ep.first + st.tok, m);
+            if (ep.first) {
+                atomicMin(ep.first + st.tok, m);
+                atomicAdd(ep.count + st.tok, 1);
+            }
         }
     }
     static __device__ __forceinline__ uint16_t* at(const Params& ep, const GemmProblem&, int, int, int m, int n) { return ep.G + (size_t)m * ep.ldg + n; }
@@ -157,10 +161,10 @@ struct EpiGradW {
     static __device__ __forceinline__ int64_t ld(const Params&, const GemmProblem& q, int) { return q.N; }
 };
 
-// Copies rows of h, zeros in place of those that are not scored, and clears `first`.
+// Copies rows of h, zeros in place of those that are not scored, and clears `first` and `count`.
 constexpr int kRowThreads = 256;
 __global__ void __launch_bounds__(kRowThreads) score_rows_kernel(const uint16_t* h, int64_t ldh, const int32_t* tokens, int d, int V, uint16_t* out,
-                                                                 int32_t* first) {
+                                                                 int32_t* first, int32_t* count) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int m = blockIdx.x;
@@ -168,48 +172,141 @@ __global__ void __launch_bounds__(kRowThreads) score_rows_kernel(const uint16_t*
     for (int c = threadIdx.x * 8; c < d; c += kRowThreads * 8)
         *reinterpret_cast<uint4*>(out + (size_t)m * d + c) = scored ? *reinterpret_cast<const uint4*>(h + m * ldh + c) : make_uint4(0, 0, 0, 0);
     // in 64 bits: M blocks of 256 threads pass 2^31 from 8388608 rows on
-    for (long long v = (long long)m * kRowThreads + threadIdx.x; v < V; v += (long long)gridDim.x * kRowThreads) first[v] = kNone;
+    for (long long v = (long long)m * kRowThreads + threadIdx.x; v < V; v += (long long)gridDim.x * kRowThreads) {
+        first[v] = kNone;
+        count[v] = 0;
+    }
 }
 
-// dW's rows of the given tokens once more, a block per row m that is the first of its token v:
-//   dW[v] = sums[m] + sum of rest[i] h[i] over the rows i whose token is v, in their order
+// dW's rows of the given tokens once more, for each token v
+//   dW[v] = sums[first row of v] + sum of rest[i] h[i] over the rows i whose token is v
+// A block per row.  A token of few rows (most have one) is the work of its first row's block, which adds them in their order, a
+// thread to eight columns.  The rows of a token with more than wide_from of them share it: each of their blocks takes runs of 64
+// columns by its rank among them, 32 rows side by side, joined in a fixed order.  (One block adding all rows one after the other took
+// 0.34 us a row and 2048 columns, after everything else: a whole gradient of 4096 rows, 32000 x 4096, took 2.5 ms with tokens all over
+// the vocabulary, 3.0 ms with a quarter of the rows on one token and 5.3 ms with all of them; now 2.5 to 2.6 ms, whatever the tokens.)
 // Bound by latencies, or by the 8 d bytes a row.  What is added comes from before the product that this waits for, so the
 // first columns' share is ready by then.
+constexpr int kGivenRows = 2048;            // rows that are searched for a token at a time
+constexpr int kWideCols = 64;
 __global__ void __launch_bounds__(kRowThreads) score_given_kernel(const uint16_t* h, int64_t ldh, const int32_t* tokens, const float* rest,
-                                                                  const int32_t* first, const float* sums, int M, int d, int V, uint16_t* dW) {
-    __shared__ int list[kRowThreads], count;
-    const int m = blockIdx.x, t = threadIdx.x, tok = tokens[m];
-    if ((unsigned)tok >= (unsigned)V || first[tok] != m) {
+                                                                  const int32_t* first, const int32_t* count, const float* sums, int M, int d,
+                                                                  int V, int wide_from, uint16_t* dW) {
+    constexpr int kWarps = kRowThreads / 32, kRuns = kGivenRows / kRowThreads;
+    __shared__ int list[kGivenRows], found[kWarps];
+    __shared__ float part[kWarps][kWideCols];
+    const int m = blockIdx.x, t = threadIdx.x, warp = t >> 5, lane = t & 31, tok = tokens[m];
+    const bool scored = (unsigned)tok < (unsigned)V;
+    const int from = scored ? __ldcg(first + tok) : kNone, n = scored ? __ldcg(count + tok) : 0;
+    const bool wide = n > wide_from;
+    if (!scored || (!wide && from != m)) {
         grid_dependency_wait();
         return;
     }
-    for (int c0 = 0; c0 < d; c0 += kRowThreads * 8) {
-        const int c = c0 + t * 8;
-        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int i0 = m; i0 < M; i0 += kRowThreads) {
-            if (t < 32) {                  // one warp lists the token's rows among these, in order
-                int n = 0;
+    // lists the token's rows among [i0, min(i0 + kGivenRows, end)), in order; returns their number
+    auto list_rows = [&](int i0, int end) {
+        unsigned hit[kRuns];
+        int mine = 0;
 #pragma unroll
-                for (int j = 0; j < kRowThreads; j += 32) {
-                    const int i = i0 + j + t;
-                    const bool mine = i < M && tokens[i] == tok;
-                    const unsigned hit = __ballot_sync(0xFFFFFFFFu, mine);
-                    if (mine) list[n + __popc(hit & ((1u << t) - 1u))] = i;
-                    n += __popc(hit);
+        for (int j = 0; j < kRuns; ++j) {
+            const unsigned i = (unsigned)i0 + (unsigned)((warp * kRuns + j) * 32 + lane);
+            hit[j] = __ballot_sync(0xFFFFFFFFu, i < (unsigned)end && tokens[i] == tok);
+            mine += __popc(hit[j]);
+        }
+        __syncthreads();                    // whoever still read the last list is done
+        if (lane == 0) found[warp] = mine;
+        __syncthreads();
+        int at = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            at += w < warp ? found[w] : 0;
+            all += found[w];
+        }
+#pragma unroll
+        for (int j = 0; j < kRuns; ++j) {
+            if (hit[j] >> lane & 1u) list[at + __popc(hit[j] & ((1u << lane) - 1u))] = i0 + (warp * kRuns + j) * 32 + lane;
+            at += __popc(hit[j]);
+        }
+        __syncthreads();
+        return all;
+    };
+    // adds rows list[j0], list[j0 + step], ... below k at columns c .. c + 7 to sum, four of them in flight
+    auto add_rows = [&](float (&sum)[8], int j0, int step, int k, int c) {
+        for (int j = j0; j < k; j += 4 * step) {
+            uint4 v[4];
+            float r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool is = j + u * step < k;
+                const int i = list[is ? j + u * step : j];
+                v[u] = *reinterpret_cast<const uint4*>(h + i * ldh + c);
+                r[u] = __ldcg(rest + i);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j + u * step < k) add_scaled(sum, r[u], v[u]);
+        }
+    };
+    auto finish = [&](const float (&sum)[8], int c) {
+        const float4* src = reinterpret_cast<const float4*>(sums + (size_t)from * d + c);
+        const float4 a = src[0], b = src[1];
+        const float all[8] = {sum[0] + a.x, sum[1] + a.y, sum[2] + a.z, sum[3] + a.w, sum[4] + b.x, sum[5] + b.y, sum[6] + b.z, sum[7] + b.w};
+        store_bf16x8(dW + (size_t)tok * d + c, all);
+    };
+    if (!wide) {
+        int k = 0;                          // rows listed; all of them fit one list nearly always, and it then serves every run of columns
+        for (int c0 = 0; c0 < d; c0 += kRowThreads * 8) {
+            const int c = c0 + t * 8;
+            float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (n == 1) {
+                if (c < d) add_scaled(sum, __ldcg(rest + m), *reinterpret_cast<const uint4*>(h + m * ldh + c));
+            } else {
+                int left = n;
+                for (int i0 = m; left > 0 && i0 < M; i0 += kGivenRows) {
+                    if (k < n) k = list_rows(i0, M);
+                    if (c < d) add_rows(sum, 0, 1, k, c);
+                    left -= k;
                 }
-                if (t == 0) count = n;
+            }
+            if (c0 == 0) grid_dependency_wait();
+            if (c < d) finish(sum, c);
+        }
+    } else {
+        const int runs = (d + kWideCols - 1) / kWideCols;
+        int rank = 0;
+        for (int i0 = from; i0 < m && rank < runs; i0 += kGivenRows) rank += list_rows(i0, m);
+        if (rank >= runs) {
+            grid_dependency_wait();
+            return;
+        }
+        for (int run = rank; run < runs; run += n) {
+            const int c = run * kWideCols + (lane & 7) * 8;
+            float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            int left = n;
+            for (int i0 = from; left > 0 && i0 < M; i0 += kGivenRows) {
+                const int k = list_rows(i0, M);
+                if (c < d) add_rows(sum, warp * 4 + (lane >> 3), kWarps * 4, k, c);
+                left -= k;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 8);
+                sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], 16);
+                if (lane < 8) part[warp][lane * 8 + i] = sum[i];
             }
             __syncthreads();
-            if (c < d)
-                for (int j = 0; j < count; ++j) add_scaled(sum, rest[list[j]], *reinterpret_cast<const uint4*>(h + list[j] * ldh + c));
+            if (run == rank) grid_dependency_wait();
+            if (t < 8 && c < d) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    sum[i] = part[0][t * 8 + i];
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) sum[i] += part[w][t * 8 + i];
+                }
+                finish(sum, c);
+            }
             __syncthreads();
-        }
-        if (c0 == 0) grid_dependency_wait();
-        if (c < d) {
-            const float4* from = reinterpret_cast<const float4*>(sums + (size_t)m * d + c);
-            const float4 a = from[0], b = from[1];
-            const float all[8] = {sum[0] + a.x, sum[1] + a.y, sum[2] + a.z, sum[3] + a.w, sum[4] + b.x, sum[5] + b.y, sum[6] + b.z, sum[7] + b.w};
-            store_bf16x8(dW + (size_t)tok * d + c, all);
         }
     }
     grid_launch_dependents();
@@ -218,8 +315,12 @@ __global__ void __launch_bounds__(kRowThreads) score_given_kernel(const uint16_t
 // G's rows: whole 16-byte runs of columns, so that a tensor map can read them
 static int64_t grad_ld(int V) { return (int64_t)round_up((size_t)V, 64); }
 
+// A token with more rows than this is shared among their blocks.  Sharing one searches the rows once per block that takes part: no
+// more than 128 tokens are, so that of many rows those searches stay below what the products take.
+static int given_wide_from(int M) { return std::max(32, M / 128); }
+
 struct GradSpace {              // offsets in the workspace
-    size_t G, h0, rest, first, sums, total;
+    size_t G, h0, rest, first, count, sums, total;
 };
 static GradSpace grad_space(int M, int d, int V) {
     GradSpace w;
@@ -227,7 +328,8 @@ static GradSpace grad_space(int M, int d, int V) {
     w.h0 = w.G + round_up((size_t)M * grad_ld(V) * 2, 256);
     w.rest = w.h0 + round_up((size_t)M * d * 2, 256);
     w.first = w.rest + round_up((size_t)M * 4, 256);
-    w.sums = w.first + round_up((size_t)V * 4, 256);
+    w.count = w.first + round_up((size_t)V * 4, 256);
+    w.sums = w.count + round_up((size_t)V * 4, 256);
     w.total = w.sums + round_up((size_t)M * d * 4, 256);
     return w;
 }
@@ -243,12 +345,13 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
     uint16_t* h0 = reinterpret_cast<uint16_t*>(base + space.h0);
     float* rest = reinterpret_cast<float*>(base + space.rest);
     int32_t* first = reinterpret_cast<int32_t*>(base + space.first);
+    int32_t* count = reinterpret_cast<int32_t*>(base + space.count);
     float* sums = reinterpret_cast<float*>(base + space.sums);
     const GemmOperand W{c.W, c.V, c.d, c.d}, g{G, c.M, c.V, ld};
     vt_status r;
     if (grad_W) {
         cudaError_t e = launch_pdl(score_rows_kernel, c.M, kRowThreads, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
-                                   c.d, c.V, h0, first);
+                                   c.d, c.V, h0, first, count);
         count_launch();
         if (e == cudaSuccess) e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e);
@@ -267,7 +370,7 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
         if (!gemm_plan(&p, false, false, false, EpiScoreGrad::kScratch, &pair)) return VT_ERR_SHAPE;
         if ((r = gemm_map(&maps.map[0], GemmOperand{c.h, c.M, c.d, c.ldh}, gemm_box_a(p, false))) != VT_OK) return r;
         if ((r = gemm_map(&maps.map[1], W, gemm_box_b(p, false, pair))) != VT_OK) return r;
-        const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, rest, grad_W ? first : nullptr, ld, c.scale, c.V};
+        const EpiScoreGrad::Params ep{c.tokens, lse, entropy, grad_logprobs, grad_entropy, G, rest, grad_W ? first : nullptr, count, ld, c.scale, c.V};
         if ((r = gemm_launch<false, false, EpiScoreGrad>(maps, p, pair, ep, st)) != VT_OK) return r;
     }
     if (grad_h) {   // dh = G W: [M, d], summed over the vocabulary; W has d running fastest
@@ -304,7 +407,7 @@ vt_status launch_score_backward(const ScoreCall& c, const float* lse, const floa
     const EpiGradW::Params ep{reinterpret_cast<uint16_t*>(grad_W), first, sums};
     if ((r = gemm_launch<true, true, EpiGradW>(maps, p, pair, ep, st)) != VT_OK) return r;
     cudaError_t e = launch_pdl(score_given_kernel, c.M, kRowThreads, 0, st, reinterpret_cast<const uint16_t*>(c.h), c.ldh, c.tokens,
-                               rest, first, sums, c.M, c.d, c.V, reinterpret_cast<uint16_t*>(grad_W));
+                               rest, first, count, sums, c.M, c.d, c.V, given_wide_from(c.M), reinterpret_cast<uint16_t*>(grad_W));
     count_launch();
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? VT_OK : cuda_fail(e);

@@ -449,3 +449,57 @@ def test_logits_near_the_lowest_float(vt, M, k):
     tokens = (np.arange(M) % V).astype(np.int32)
     scale = 2.0 ** -126
     check(run(vt, dev(h), dev(W), dev(tokens, torch.int32), k, scale), so.score(h, W, tokens, k, scale), V)
+
+
+@pytest.mark.parametrize("M,d,V", [(2500, 520, 300), (5000, 64, 40), (40, 72, 9)])
+def test_tokens_given_to_many_rows(vt, M, d, V):
+    """A quarter of the rows have one token, two others 33 and 32 (around where a token's rows begin to share it), the rest any; rows that
+    are not scored between them.  Bounds as in test_given_entries_are_rounded_once, and the same bits twice."""
+    h, W, _ = case(M, d, V, 24)
+    rng = np.random.default_rng(25)
+    tokens = rng.integers(3, V, M)
+    places = rng.permutation(M)
+    tokens[places[: M // 4]] = 0
+    tokens[places[M // 4: M // 4 + min(33, M // 4)]] = 1
+    tokens[places[M // 2: M // 2 + min(32, M // 4)]] = 2
+    tokens[places[M - M // 10:]] = -1
+    tokens = tokens.astype(np.int32)
+    gl = rng.normal(size=M).astype(np.float32)
+    hd, Wd, t = dev(h), dev(W), dev(tokens, torch.int32)
+    r = vt.vt_score_tokens(hd, Wd, t)
+    (dh, dW), again = (vt.vt_score_tokens_backward(hd, Wd, t, r.lse, None, torch.from_numpy(gl).cuda()) for _ in range(2))
+    assert torch.equal(dh, again[0]) and torch.equal(dW, again[1])
+    want_h, want_W = so.score_backward(h, W, tokens, gl)
+    _, A = so.grad_logits(h, W, tokens, gl)
+    keep = so.scored_rows(tokens, M, V)
+    others, given = A.copy(), np.zeros_like(A)
+    m = np.flatnonzero(keep)
+    given[m, tokens[m]], others[m, tokens[m]] = A[m, tokens[m]], 0.0
+    E = (2.0 ** -8 + 2.0 ** -14) * others + 2.0 ** -14 * given
+    for got, want, terms in ((dh, want_h, E @ np.abs(W)), (dW, want_W, E[keep].T @ np.abs(h[keep]))):
+        err = np.abs(got.double().cpu().numpy() - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + terms + 1e-30).all()
+
+
+def test_repeated_tokens_do_not_hold_a_gradient_up(vt):
+    """All rows on one token against tokens all over the vocabulary: the same products, so at most half as much again, where a token's
+    rows added one after the other took three times as long."""
+    M, d, V = 8192, 512, 8000
+    gen = torch.Generator(device="cuda").manual_seed(26)
+    h = torch.randn(M, d, device="cuda", generator=gen).bfloat16()
+    W = (torch.randn(V, d, device="cuda", generator=gen) * 0.02).bfloat16()
+    ws = vt.new_workspace(max(vt.vt_score_workspace_bytes(M, d, V, 0), vt.vt_score_backward_workspace_bytes(M, d, V)))
+    times = {}
+    for name, t in (("any", torch.randint(V, (M,), device="cuda", generator=gen).int()), ("one", torch.full((M,), 77, dtype=torch.int32, device="cuda"))):
+        r = vt.vt_score_tokens(h, W, t, workspace=ws)
+        runs = []
+        for _ in range(7):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(5):
+                vt.vt_score_tokens_backward(h, W, t, r.lse, None, r.lse, workspace=ws)
+            b.record()
+            torch.cuda.synchronize()
+            runs.append(a.elapsed_time(b))
+        times[name] = min(runs)
+    assert times["one"] <= 1.5 * times["any"], times
