@@ -418,6 +418,12 @@ int vt_last_launch_count(void);
  * Asynchronous. */
 vt_status vt_test_timeout_probe(void* workspace, int limit_us, void* stream);
 
+/* Failure path of the scoring and feed-forward products: until the calling thread passes 0 again, each of its products counts on
+ * 16 bytes more than its copies bring and gives up waiting after `limit_us` microseconds (1 .. 100,000).  The product then
+ * lets what is in flight end, sets the time-out bit in its workspace's status word and returns without a valid result, as after a copy
+ * that never came; the call's other kernels run on what is there.  Nothing faults, and every wait is bounded. */
+vt_status vt_test_withhold_copies(int limit_us);
+
 /* Stream-order probe: a kernel that releases its programmatic dependents at once, idles for `delay_us`
  * microseconds (0 .. 10,000) and only then copies n_bytes (a multiple of 16; dev pointers, 16-byte aligned)
  * from src to dst.  A head call enqueued right behind it must still see the copied bytes. Asynchronous. */

@@ -62,6 +62,7 @@ SYMBOLS = {
     "vt_last_launch_count": (_i, []),
     "vt_test_timeout_probe": (_i, [_p, _i, _p]),
     "vt_test_late_copy": (_i, [_p, _p, _sz, _i, _p]),
+    "vt_test_withhold_copies": (_i, [_i]),
 }
 
 _lib = None
@@ -545,6 +546,11 @@ def vt_last_launch_count() -> int:
 
 def vt_test_timeout_probe(workspace: torch.Tensor, limit_us: int) -> None:
     _check(lib().vt_test_timeout_probe(workspace.data_ptr(), int(limit_us), _stream()), "vt_test_timeout_probe")
+
+
+def vt_test_withhold_copies(limit_us: int) -> None:
+    """Products of this thread give up waiting after ``limit_us`` (0: back to normal); see ``include/vt.h``."""
+    _check(lib().vt_test_withhold_copies(limit_us), "vt_test_withhold_copies")
 
 
 def vt_test_late_copy(dst: torch.Tensor, src: torch.Tensor, delay_us: int) -> None:

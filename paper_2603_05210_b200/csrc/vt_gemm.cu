@@ -40,6 +40,7 @@ static bool gemm_layout(GemmParams* p, bool a_mn, bool b_mn, bool pair, uint32_t
     p->acc_cols = 32;
     while (p->acc_cols < (uint32_t)p->NT) p->acc_cols *= 2;
     p->tmem_cols = 2 * p->acc_cols;
+    p->wait_ns = kWaitLimitNs;
     return p->total_smem <= (uint32_t)kMaxDynSmem;
 }
 
@@ -258,4 +259,13 @@ vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool 
     return gemm_launch<true, true, EpiStore>(maps, p, pair, ep, st);
 }
 
+static thread_local int g_withheld_us = 0;
+int gemm_withheld_us() { return g_withheld_us; }
+
 }  // namespace vt
+
+extern "C" vt_status vt_test_withhold_copies(int limit_us) {
+    if (limit_us < 0 || limit_us > 100000) return VT_ERR_SHAPE;
+    vt::g_withheld_us = limit_us;
+    return VT_OK;
+}

@@ -79,6 +79,7 @@ struct GemmParams {
     uint32_t scratch_off;        // the epilogue's own shared memory (Epi::kScratch bytes), from the 1024-aligned base
     uint32_t bar_off;            // barriers
     uint32_t total_smem;
+    unsigned long long wait_ns;      // limit of every wait
     WsHeader* hdr;
 };
 
@@ -122,8 +123,8 @@ __device__ __forceinline__ bool elect_one() {
     return p != 0;
 }
 // The bounded wait by a whole warp, with an answer the compiler knows to be the same in every lane.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
-    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity)) != 0;
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, limit_ns)) != 0;
 }
 
 __device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -311,12 +312,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
         return !PAIR && q.tiles_m == 1 ? k0 + (int)((long long)(k1 - k0) * cluster / n_clusters) : k0;
     };
 
+    int issued = 0;                    // a producer warp's ring stages so far, of either warp
     if (producer) {
         // ------------------------------------------------------------------ TMA producers
         // The whole warp runs the loop and one elected lane issues: with uniform control flow the copies' operands are formed
         // in uniform registers.  Everything the loop needs is read from the parameters ahead of it.
         {
-            int s = 0, issued = 0;
+            int s = 0;
             uint32_t wrap = 0, dst = base, bar_f = bar_full, bar_e = bar_empty;
             bool ok = true;
             const int kbs = p.kbs;
@@ -395,7 +397,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     for (int i = k0; i < k1; i += kbs) {
                         const int nb = min(kbs, k1 - i);
                         const bool mine = (issued & (kGemmProducers - 1)) == warp - kProducer;
-                        if (mine && wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u)) { fail(); ok = false; break; }
+                        if (mine && wrap > 0 && !mbar_wait_warp(bar_e, (wrap - 1) & 1u, p.wait_ns)) { fail(); ok = false; break; }
                         if (mine && elect_one()) issue(kb, nb, dst, bar_f, true, issued >= early);
                         __syncwarp();
                         ++issued;
@@ -414,11 +416,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                         }
                     }
                 }
-            }
-            if (lane == 0 && leader && *abort_flag) {       // let this warp's copies in flight land before the CTA gives its shared memory back
-                const unsigned long long deadline = global_timer_ns() + kWaitLimitNs;
-                for (int i = max(0, issued - S); i < issued; ++i)
-                    if ((i & (kGemmProducers - 1)) == warp - kProducer) (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, deadline);
             }
         }
     } else if (warp == kIssuer) {
@@ -441,13 +438,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 k_range(tab.prob[it.prob], k0, k1);
                 for (int t = 0; t < it.n_tiles && ok; ++t, ++n) {
                     const int buf = n & 1;
-                    if (n >= 2 && !mbar_wait_warp(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u)) { fail(); ok = false; break; }
+                    if (n >= 2 && !mbar_wait_warp(bar_acce + 8u * buf, (uint32_t)((n >> 1) - 1) & 1u, p.wait_ns)) { fail(); ok = false; break; }
                     if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d_tmem = tmem_base + (uint32_t)buf * acc_cols;
                     uint32_t accumulate = 0u;
                     for (int kb = k0; kb < k1; kb += kbs) {
-                        if (!mbar_wait_warp(bar_f, phase)) { fail(); ok = false; break; }
+                        if (!mbar_wait_warp(bar_f, phase, p.wait_ns)) { fail(); ok = false; break; }
                         tc_fence_after();
                         const int nb = min(kbs, k1 - kb);
                         if (elect_one()) {
@@ -485,11 +482,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                     __syncwarp();
                 }
             }
-            if (__any_sync(0xFFFFFFFFu, *abort_flag != 0) && elect_one()) {   // every MMA issued so far must retire before TMEM is freed
-                if constexpr (PAIR) tc_commit_pair(bar_drain);
-                else tc_commit(bar_drain);
-                (void)mbar_wait(bar_drain, 0u);
-            }
         }
     } else {
         // ------------------------------------------------------------------ epilogue
@@ -523,7 +515,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
                 }
                 bool got = false;
                 if (!__any_sync(0xFFFFFFFFu, *abort_flag != 0)) {  // warp-uniform: tcgen05.ld needs the whole warp
-                    got = __all_sync(0xFFFFFFFFu, mbar_wait(bar_accf + 8u * buf, (uint32_t)(n >> 1) & 1u));
+                    got = __all_sync(0xFFFFFFFFu, mbar_wait(bar_accf + 8u * buf, (uint32_t)(n >> 1) & 1u, p.wait_ns));
                     if (!got) fail();
                 }
                 if (!got) continue;
@@ -694,8 +686,28 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
     }
 
     tc_fence_before();
+    __syncthreads();                             // every role is done, and knows whether one of them gave up
+    if (__builtin_expect(*abort_flag != 0, 0)) { // MMAs and copies in flight must end before their memory is given back
+        if (warp == kIssuer && leader && elect_one()) {
+            if constexpr (PAIR) tc_commit_pair(bar_drain);
+            else tc_commit(bar_drain);
+            (void)mbar_wait(bar_drain, 0u, p.wait_ns);
+        }
+        if (producer && lane == 0) {
+            const unsigned long long now = global_timer_ns();
+            if (leader) {                        // of a pair: for both, which leave together
+                for (int i = max(0, issued - S); i < issued; ++i)
+                    if ((i & (kGemmProducers - 1)) == warp - kProducer)
+                        (void)mbar_wait_until(bar_full + 8u * (i % S), (uint32_t)(i / S) & 1u, now + p.wait_ns);
+            } else {                             // copies past the leader's last stage are counted nowhere: longer than any takes
+                while (global_timer_ns() - now < 1000000ull) { }
+            }
+        }
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+    }
     if constexpr (PAIR) cluster_sync_all();      // neither CTA leaves while the other's MMAs or arrivals may still reach it
-    else __syncthreads();
     tc_fence_after();
     if (warp == kIssuer) {
         if constexpr (PAIR)
@@ -705,9 +717,14 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
     }
 }
 
+// See vt_test_withhold_copies: 0, or the limit of the calling thread's products' waits in microseconds.
+int gemm_withheld_us();
+
 // Launches the kernel for a finished plan (`pair` as the plan chose).
 template <bool A_MN, bool B_MN, class Epi>
-inline vt_status gemm_launch(const GemmMaps& maps, const GemmParams& p, bool pair, const typename Epi::Params& ep, cudaStream_t st) {
+inline vt_status gemm_launch(const GemmMaps& maps, const GemmParams& plan, bool pair, const typename Epi::Params& ep, cudaStream_t st) {
+    GemmParams withheld;
+    const GemmParams& p = gemm_withheld_us() > 0 ? withheld : plan;
     static std::atomic<unsigned long long> configured_pair{0}, configured_single{0};
     auto* kernel = pair ? gemm_kernel<true, A_MN, B_MN, Epi> : gemm_kernel<false, A_MN, B_MN, Epi>;
     if (vt_status rc = ensure_max_dyn_smem(reinterpret_cast<const void*>(kernel), kMaxDynSmem, pair ? &configured_pair : &configured_single);
@@ -715,6 +732,11 @@ inline vt_status gemm_launch(const GemmMaps& maps, const GemmParams& p, bool pai
         return rc;
     int sms = 0;
     if (vt_status rc = device_sm_count(&sms); rc != VT_OK) return rc;
+    if (const int us = gemm_withheld_us(); us > 0) {     // a test of the unwinding: each stage waits for 16 bytes more than come
+        withheld = plan;
+        withheld.tx_bytes += 16;
+        withheld.wait_ns = (unsigned long long)us * 1000ull;
+    }
     const int cluster = pair ? 2 : p.splits;
     const int grid = pair ? 2 * std::max(1, std::min(sms / 2, p.n_items)) : p.splits > 1 ? p.n_items * p.splits : std::min(sms, p.n_items);
     cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, cluster, grid, kGemmThreads, p.total_smem, st, maps, p, ep)
