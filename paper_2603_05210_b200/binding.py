@@ -402,7 +402,8 @@ def vt_score_tokens(h: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor | Non
     """Log probabilities of ``tokens`` [M] under the head ``W`` [V, d], with entropy, log-sum-exp and the k best alternatives.
 
     Rows whose token lies outside [0, V) are not scored (zeros, top_ids -1); ``tokens=None`` scores every row without a
-    given token.  Pass tensors for outputs and workspace to have them reused."""
+    given token.  Pass tensors for outputs and workspace to have them reused.  A device-side wait that runs out leaves
+    invalid results and is only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
     h, W = _score_inputs(h, W, tokens)
     (M, d), V, dev = h.shape, W.shape[0], h.device
     if tokens is None and logprobs is not None:
@@ -438,7 +439,9 @@ def vt_score_tokens_backward(h: torch.Tensor, W: torch.Tensor, tokens: torch.Ten
                              grad_entropy: torch.Tensor | None = None, *, scale: float = 1.0,
                              workspace: torch.Tensor | None = None, grad_h: torch.Tensor | None = None,
                              grad_W: torch.Tensor | None = None, want_h: bool = True, want_W: bool = True):
-    """(grad_h [M, d], grad_W [V, d]) in bf16 from the forward call's ``lse`` and ``entropy``; one not wanted is None."""
+    """(grad_h [M, d], grad_W [V, d]) in bf16 from the forward call's ``lse`` and ``entropy``; one not wanted is None.
+
+    Time-outs are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
     h, W = _score_inputs(h, W, tokens)
     (M, d), V, dev = h.shape, W.shape[0], h.device
     lse, grad_logprobs = _f32(lse, "lse", (M,)), _f32(grad_logprobs, "grad_logprobs", (M,))
@@ -486,7 +489,8 @@ def vt_gated_ffn(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_do
                  workspace: torch.Tensor | None = None) -> torch.Tensor:
     """y [M, d] bf16 = (act(x W_gate^T) * (x W_up^T)) W_down^T, act "silu" or "gelu" (tanh form).
 
-    Pass ``saved`` [M, 2 f] float32 to receive what ``vt_gated_ffn_backward`` needs (its layout is the library's own)."""
+    Pass ``saved`` [M, 2 f] float32 to receive what ``vt_gated_ffn_backward`` needs (its layout is the library's own).
+    Time-outs are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
     x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
     M = x.shape[0]
     out = _out(out, "out", (M, d), torch.bfloat16, x)
@@ -503,7 +507,9 @@ def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Ten
                           grad_y: torch.Tensor, *, act: str | int = "silu", workspace: torch.Tensor | None = None,
                           grad_x: torch.Tensor | None = None, grad_W_gate: torch.Tensor | None = None,
                           grad_W_up: torch.Tensor | None = None, grad_W_down: torch.Tensor | None = None):
-    """(grad_x [M, d], grad_W_gate [f, d], grad_W_up [f, d], grad_W_down [d, f]) in bf16 from the forward call's ``saved``."""
+    """(grad_x [M, d], grad_W_gate [f, d], grad_W_up [f, d], grad_W_down [d, f]) in bf16 from the forward call's ``saved``.
+
+    Time-outs are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
     x, d, f = _ffn_inputs(x, W_gate, W_up, W_down)
     M, dev = x.shape[0], x.device
     _f32(saved, "saved", (M, 2 * f))

@@ -122,3 +122,8 @@ def test_binding_refuses_what_is_not_on_the_device_or_does_not_fit(vt):
         vt.vt_gated_ffn(h, W, W, W.T.contiguous())
     with pytest.raises(ValueError):
         vt.vt_gated_ffn_backward(h, W, W, W.T.contiguous(), torch.zeros(2, 8), h)
+
+
+def test_docstrings_say_where_a_time_out_is_seen(vt):
+    for name in ("vt_score_tokens", "vt_score_tokens_backward", "vt_gated_ffn", "vt_gated_ffn_backward"):
+        assert "vt_last_status" in getattr(vt, name).__doc__, name
