@@ -424,6 +424,12 @@ vt_status vt_test_timeout_probe(void* workspace, int limit_us, void* stream);
  * that never came; the call's other kernels run on what is there.  Nothing faults, and every wait is bounded. */
 vt_status vt_test_withhold_copies(int limit_us);
 
+/* The forms that the scoring and feed-forward products launched by the calling thread took since the last time this was asked, at
+ * most `max` and 16: five ints each - CTA pairs (1) or single CTAs, accumulator columns of a tile, CTAs that divide a tile's sum,
+ * tiles (scoring: runs of tiles), and how many of these the grid takes at once.  Returns their number and forgets them (out ==
+ * NULL: only forgets). */
+int vt_test_products(int* out, int max);
+
 /* Stream-order probe: a kernel that releases its programmatic dependents at once, idles for `delay_us`
  * microseconds (0 .. 10,000) and only then copies n_bytes (a multiple of 16; dev pointers, 16-byte aligned)
  * from src to dst.  A head call enqueued right behind it must still see the copied bytes. Asynchronous. */

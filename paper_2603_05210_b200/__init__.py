@@ -15,7 +15,7 @@ _BINDING_NAMES = {
     "VT_OK", "VT_ERR_NULL", "VT_ERR_SHAPE", "VT_ERR_ALIGN", "VT_ERR_RANGE", "VT_ERR_DUP", "VT_ERR_EMPTY",
     "VT_ERR_WORKSPACE", "VT_ERR_TIMEOUT", "VT_ERR_CUDA", "VT_ERR_UNSUPPORTED", "VT_MAX_K",
     "VT_PATH_AUTO", "VT_PATH_GEMV", "VT_PATH_MMA", "VT_PATH_MMA_SMALL", "VT_HEAD_STATIC_WEIGHTS", "VT_HEAD_D2T_OFFSETS",
-    "vt_test_timeout_probe", "vt_test_late_copy", "vt_test_withhold_copies",
+    "vt_test_timeout_probe", "vt_test_late_copy", "vt_test_withhold_copies", "vt_test_products",
     "VtScores", "vt_score_tokens", "vt_score_tokens_backward", "vt_score_workspace_bytes", "vt_score_backward_workspace_bytes",
     "vt_gated_ffn", "vt_gated_ffn_backward", "vt_gated_ffn_workspace_bytes", "vt_gated_ffn_backward_workspace_bytes",
     "VT_ACT_SILU", "VT_ACT_GELU",

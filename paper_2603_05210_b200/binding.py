@@ -63,6 +63,7 @@ SYMBOLS = {
     "vt_test_timeout_probe": (_i, [_p, _i, _p]),
     "vt_test_late_copy": (_i, [_p, _p, _sz, _i, _p]),
     "vt_test_withhold_copies": (_i, [_i]),
+    "vt_test_products": (_i, [_p, _i]),
 }
 
 _lib = None
@@ -552,6 +553,13 @@ def vt_last_launch_count() -> int:
 
 def vt_test_timeout_probe(workspace: torch.Tensor, limit_us: int) -> None:
     _check(lib().vt_test_timeout_probe(workspace.data_ptr(), int(limit_us), _stream()), "vt_test_timeout_probe")
+
+
+def vt_test_products() -> list[tuple[int, ...]]:
+    """(pair, NT, splits, items, at once) of each product this thread launched since the last call; see ``include/vt.h``."""
+    rows = (ctypes.c_int * 80)()
+    n = lib().vt_test_products(ctypes.addressof(rows), 16)
+    return [tuple(rows[5 * i:5 * i + 5]) for i in range(n)]
 
 
 def vt_test_withhold_copies(limit_us: int) -> None:

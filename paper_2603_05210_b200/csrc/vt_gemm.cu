@@ -262,10 +262,30 @@ vt_status gemm_store(const GemmMaps& maps, const GemmParams& p, bool pair, bool 
 static thread_local int g_withheld_us = 0;
 int gemm_withheld_us() { return g_withheld_us; }
 
+static thread_local struct {
+    int n, row[16][5];
+} g_noted{};
+void gemm_note(bool pair, int NT, int splits, int items, int at_once) {
+    if (g_noted.n == 16) return;
+    int* r = g_noted.row[g_noted.n++];
+    r[0] = pair;
+    r[1] = NT;
+    r[2] = splits;
+    r[3] = items;
+    r[4] = at_once;
+}
+
 }  // namespace vt
 
 extern "C" vt_status vt_test_withhold_copies(int limit_us) {
     if (limit_us < 0 || limit_us > 100000) return VT_ERR_SHAPE;
     vt::g_withheld_us = limit_us;
     return VT_OK;
+}
+
+extern "C" int vt_test_products(int* out, int max) {
+    const int n = std::min(vt::g_noted.n, std::max(max, 0));
+    if (out) memcpy(out, vt::g_noted.row, (size_t)n * sizeof(vt::g_noted.row[0]));
+    vt::g_noted.n = 0;
+    return out ? n : 0;
 }

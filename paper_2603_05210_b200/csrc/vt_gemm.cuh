@@ -719,6 +719,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmP
 
 // See vt_test_withhold_copies: 0, or the limit of the calling thread's products' waits in microseconds.
 int gemm_withheld_us();
+// Notes a launch for vt_test_products.
+void gemm_note(bool pair, int NT, int splits, int items, int at_once);
 
 // Launches the kernel for a finished plan (`pair` as the plan chose).
 template <bool A_MN, bool B_MN, class Epi>
@@ -742,6 +744,7 @@ inline vt_status gemm_launch(const GemmMaps& maps, const GemmParams& plan, bool 
     cudaError_t e = cluster > 1 ? launch_pdl_cluster(kernel, cluster, grid, kGemmThreads, p.total_smem, st, maps, p, ep)
                                 : launch_pdl(kernel, grid, kGemmThreads, p.total_smem, st, maps, p, ep);
     count_launch();
+    gemm_note(pair, p.NT, p.splits, p.n_items, grid / cluster);
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? VT_OK : cuda_fail(e);
 }
