@@ -776,6 +776,8 @@ struct GemmOperand {
     int rows, cols;
     int64_t ld;
 };
+// make_tensor_map_bf16 for rows that lie ld elements apart (ld a multiple of 8; defined beside it).
+vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, int d, int64_t ld, int box_rows);
 inline vt_status gemm_map(CUtensorMap* map, const GemmOperand& o, int box_rows) {
     return make_tensor_map_bf16_ld(map, o.ptr, o.rows, o.cols, o.ld, box_rows);
 }

@@ -12,8 +12,6 @@ constexpr int kBoxK = 64;                    // bf16 elements per k-block = one 
 // Tensor map of a bf16 matrix [rows, d] row-major for boxes of kBoxK columns x box_rows rows, 128-byte
 // swizzle, zero fill outside the matrix (host; defined in vt_head_mma.cu).
 vt_status make_tensor_map_bf16(CUtensorMap* map, const void* ptr, int rows, int d, int box_rows);
-// The same for rows that lie ld elements apart (ld a multiple of 8).
-vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, int d, int64_t ld, int box_rows);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
