@@ -251,7 +251,8 @@ vt_status vt_score_tokens(const void* h, int64_t ldh, const void* W, const int32
  *   h, ldh, W, tokens, M, d, V, scale   as in the forward call (tokens required);   lse, entropy  dev [M], its outputs
  *   grad_logprobs  dev [M] float        grad_entropy  dev [M] float or NULL (then entropy may be NULL, too)
  *   grad_h  dev [M, d] bf16 (out) or NULL      grad_W  dev [V, d] bf16 (out) or NULL; at least one; 16-byte aligned
- *   workspace  dev, 256-byte aligned, vt_score_backward_workspace_bytes(M, d, V) bytes (it holds G, 2 M V bytes, and 6 M d more)
+ *   workspace  dev, 256-byte aligned, vt_score_backward_workspace_bytes(M, d, V) bytes (it holds G, 2 M V bytes, and 6 M d + 8 V
+ *              more)
  * Asynchronous.  Gradients are overwritten, not added to. */
 size_t    vt_score_backward_workspace_bytes(int M, int d, int V);
 vt_status vt_score_tokens_backward(const void* h, int64_t ldh, const void* W, const int32_t* tokens,
