@@ -169,8 +169,8 @@ vt_status vt_draft_head_host(const void* h_host, const void* W_trim, const int32
                              int32_t* target_ids_host, float* logprobs_host,
                              void* workspace, size_t workspace_bytes, void* stream);
 
-/* Reads the status word of a draft-head workspace.  SYNCHRONISES the stream.  Returns VT_OK,
- * VT_ERR_TIMEOUT, or VT_ERR_CUDA, and clears the word. */
+/* Reads the status word of a workspace.  SYNCHRONISES the stream.  Returns VT_OK, VT_ERR_TIMEOUT, VT_ERR_RANGE (vt_tree_attention met a
+ * page id outside the cache) or VT_ERR_CUDA, and clears the word. */
 vt_status vt_last_status(void* workspace, void* stream);
 
 /* ------------------------------------------------------------------------------------------
@@ -298,6 +298,158 @@ vt_status vt_gated_ffn_backward(const void* x, int64_t ldx, const void* W_gate, 
                                 int M, int d, int f, int act,
                                 void* grad_x, void* grad_W_gate, void* grad_W_up, void* grad_W_down,
                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Rotary positions (the attention of a draft layer, Table 1): each pair of a head's first rot_dim elements is turned by an angle
+ * that grows with the token's position,
+ *
+ *   angle[n, i] = positions[n] * w_i          y1 = a (x1 cos - x2 sin)     y2 = a (x2 cos + x1 sin)       i < rot_dim / 2
+ *
+ * pair i being elements (i, i + rot_dim / 2) of a head, or (2 i, 2 i + 1) with VT_ROPE_INTERLEAVED; the other elements are
+ * copied.  The gradient's way back is the turn by the opposite angle (VT_ROPE_INVERSE; `a` stays).  Sums in fp32, rounded once.
+ *
+ * vt_rope_table writes the frequencies, as fractions of a turn per position in 64-bit fixed point: position * entry modulo 2^64 is
+ * then the angle without its whole turns, exactly, so that far positions are as good as near ones.  With base^(-2 i / rot_dim) = f_i:
+ *
+ *   VT_ROPE_NONE        w_i = f_i
+ *   VT_ROPE_LINEAR      w_i = f_i / factor
+ *   VT_ROPE_BASE        w_i = (base * factor^(rot_dim / (rot_dim - 2)))^(-2 i / rot_dim)
+ *   VT_ROPE_WAVELENGTH  w_i = f_i s + f_i / factor (1 - s),  s = (turns - low) / (high - low) within [0, 1],
+ *                       turns = original_len f_i / (2 pi)
+ *   VT_ROPE_RAMP        w_i = f_i (1 - s) + f_i / factor s,  s = (i - i0) / (i1 - i0) within [0, 1],
+ *                       i0 = floor(e(high)), i1 = ceil(e(low)) within [0, rot_dim - 1],
+ *                       e(turns) = rot_dim log(original_len / (2 pi turns)) / (2 log base): the pair that makes so many turns
+ *                       (its usual amplitude is a = 0.1 log(factor) + 1)
+ *
+ *   table  dev [rot_dim / 2] uint64 (out), 8-byte aligned
+ * rot_dim a multiple of 16, 16 <= rot_dim <= 1024; base > 1, factor > 0, original_len > 0 and finite; low < high for WAVELENGTH,
+ * 0 < low < high for RAMP; else VT_ERR_SHAPE.  Asynchronous. */
+typedef enum vt_rope_scaling {
+    VT_ROPE_NONE = 0,
+    VT_ROPE_LINEAR = 1,
+    VT_ROPE_BASE = 2,
+    VT_ROPE_WAVELENGTH = 3,
+    VT_ROPE_RAMP = 4
+} vt_rope_scaling;
+
+#define VT_ROPE_INTERLEAVED 1  /* pairs side by side */
+#define VT_ROPE_INVERSE     2  /* turn back: the gradient of the call without it */
+
+vt_status vt_rope_table(uint64_t* table, int rot_dim, double base, int scaling, double factor, double low, double high,
+                        double original_len, void* stream);
+
+/* A [tokens, heads, D] bf16 tensor: element (n, h, j) at ptr[n * token_stride + h * head_stride + j].  ptr 16-byte aligned, strides
+ * multiples of 8. */
+typedef struct vt_heads {
+    void* ptr;
+    int64_t token_stride, head_stride;
+} vt_heads;
+
+/* Turns q [N, Hq, D] into q_out and k [N, Hkv, D] into k_out (k, k_out NULL and Hkv = 0: queries alone).
+ *   positions dev [N] int32 (any value)     table as above     amplitude: a, finite     options: VT_ROPE_* bits
+ * Outputs may be the inputs themselves (same pointer and strides); otherwise they must not overlap them.
+ * D a multiple of 16, rot_dim <= D <= 1024; N >= 0, Hq >= 1.  Asynchronous. */
+vt_status vt_rope(const vt_heads* q, const vt_heads* k, const int32_t* positions, const uint64_t* table, int N, int Hq, int Hkv, int D,
+                  int rot_dim, float amplitude, int options, const vt_heads* q_out, const vt_heads* k_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A paged cache of keys and values.  Page p, place i, head h, element j of the keys lies at
+ * k[p * k_page_stride + i * k_token_stride + h * k_head_stride + j] (the values alike); position `at` of request b is place
+ * at % page_size of page page_table[b * table_stride + at / page_size].  lens[b] positions of request b hold earlier tokens; the
+ * tokens of a call are its positions lens[b], lens[b] + 1, ...
+ *
+ *   k, v        dev bf16, 16-byte aligned, strides multiples of 8 (elements)
+ *   page_table  dev [B, max_pages] int32, rows table_stride apart        lens  dev [B] int32
+ * page_size 8, 16, 32, 64 or a multiple of 128.  Neither the table nor the lengths are read before the stream's earlier work is done,
+ * so both may be written by it. */
+typedef struct vt_cache {
+    void* k;
+    void* v;
+    const int32_t* page_table;
+    const int32_t* lens;
+    int64_t k_page_stride, k_token_stride, k_head_stride;
+    int64_t v_page_stride, v_token_stride, v_head_stride;
+    int64_t table_stride;
+    int32_t n_pages, page_size, heads, head_dim, B, max_pages;
+} vt_cache;
+
+/* vt_rope for serving: queries are turned into q_out, keys are turned and stored in the cache, values [N, Hkv, D] are stored beside them.
+ * Token n belongs to the request b with cu_tokens[b] <= n < cu_tokens[b + 1] and goes to position lens[b] + n - cu_tokens[b]; lens
+ * itself stays as it is.
+ *   cu_tokens  dev [B + 1] int32, ascending          positions  dev [N] int32: what the angles go by (in a tree the depth, not the place)
+ * Tokens outside [cu_tokens[0], cu_tokens[B]) are padding: nothing of theirs is written.  A token whose position lies past the table, or
+ * whose page id lies outside [0, n_pages), is not stored (its query is still turned).  Asynchronous. */
+vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v, const int32_t* positions, const int32_t* cu_tokens,
+                         const uint64_t* table, int N, int Hq, int rot_dim, float amplitude, int options, const vt_heads* q_out,
+                         const vt_cache* cache, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Attention of drafted tokens over a paged cache that holds them at its end (their keys and values stored by vt_rope_append).  A
+ * request's tokens may be a tree (mask), a chain (mask NULL: each sees itself and those before it), or one alone.  For token t of
+ * request b, head h, and the positions i it attends - all i < lens[b], and lens[b] + u where bit u % 32 of word u / 32 of its mask row is
+ * set (mask NULL: where u <= t) -
+ *
+ *   x_i = scale * q . k_i      lse = log sum_i exp(x_i)      out = sum_i exp(x_i - lse) v_i
+ *
+ * query head h reads key head h / (Hq / heads).  A token that attends nothing has out = 0 and lse = -infinity.  Keys and values of
+ * positions that nobody attends, behind a request's end or out of every token's mask, may hold anything; where only some tokens attend one, the
+ * others are not touched by it, but for those its value must be finite (infinities and NaN act as the largest finite number).  Products are
+ * exact, sums fp32; the weights exp(x_i - m) are rounded to bf16 as an operand of the second product (not in lse), out once to bf16.
+ *
+ *   q        [N, Hq, D] as vt_heads                     out      [N, Hq, D] as vt_heads (out)      lse  dev [N, Hq] float (out) or NULL
+ *   cu_tokens  dev [B + 1] int32, ascending, within [0, N]; rows outside all requests are left as they were
+ *   mask     dev [N, mask_words] int32 or NULL; tokens from 32 * mask_words on are attended by nobody
+ *   max_tokens  the most tokens a request has (a bound; what a request has beyond it is not computed and not attended)
+ *   workspace   dev, 256-byte aligned, vt_tree_attention_workspace_bytes(Hq, heads, D, max_tokens) bytes; needs no initialisation but for
+ *               vt_last_status (below).  Calls that share one must be ordered on one stream
+ * D (the cache's head_dim) 64 or 128; Hq a multiple of heads, Hq / heads <= 128; max_tokens >= 1; scale finite and > 0; 0 <= N.
+ * Positions past the table's max_pages pages are not attended.  A page id outside [0, n_pages) reads as keys and values of zeros and is reported
+ * by vt_last_status as VT_ERR_RANGE.  Asynchronous; results do not depend on timing. */
+size_t    vt_tree_attention_workspace_bytes(int Hq, int heads, int D, int max_tokens);
+vt_status vt_tree_attention(const vt_heads* q, const int32_t* cu_tokens, const vt_cache* cache, const int32_t* mask, int mask_words,
+                            int N, int Hq, int max_tokens, float scale, const vt_heads* out, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The mask and the positions of drafted trees from their parents: parents[n] is the index, within its request, of the token that
+ * token n follows (an earlier one), or -1.  A token's mask row has the bits of itself and of all tokens on its way up; its depth is the
+ * number of those above it.
+ *   parents dev [N] int32        mask dev [N, mask_words] int32 (out) or NULL        positions dev [N] int32 (out) or NULL:
+ *   lens[b] + depth (lens NULL: the depth)
+ * A parent that is not an earlier token of the request counts as -1.  Bits from 32 * mask_words on are dropped; rows outside all requests
+ * are left as they were.  mask_words >= 1 where there is a mask.  Asynchronous. */
+vt_status vt_tree_mask(const int32_t* parents, const int32_t* cu_tokens, const int32_t* lens, int N, int B, int32_t* mask, int mask_words,
+                       int32_t* positions, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Verification of drafted tokens: which of a request's drafted tree stay, and the token that follows them, distributed exactly as if the
+ * target had generated them alone.  Token 0 of a request is its root (already certain); probs[n, :] is the target's distribution
+ * of what follows token n.  From the root on, at token x with p = probs[x]:
+ *
+ *   the children c of x are taken in ascending order; c is accepted if   u_accept[c] * q(c) * Z < r(c)   and r(c) > 0, and becomes x;
+ *   otherwise what is left of p changes:
+ *     drawn    (draft_probs given: the children of x were drawn from q = draft_probs[x], each alone)
+ *              S += Z;  r(v) = max(p(v) - S q(v), 0);  Z = sum_v r(v)                    (S = 0, Z = 1, r = p at first)
+ *     chosen   (draft_probs NULL: they were picked without chance; q(c) = 1)
+ *              Z -= r(c);  r(c) = 0
+ *   with no child left, the token that follows is the smallest v with  sum_{w <= v} r(w) > u_sample[b] * sum_w r(w).
+ *
+ * All of it in 64 bits.  (Where rounding leaves no r at all, p itself is drawn from.)
+ *
+ *   probs       dev [N, V] float, rows ld_probs apart     tokens  dev [N] int32: ids in the target's vocabulary
+ *   parents     dev [N] int32: index within the request   cu_tokens  dev [B + 1] int32, ascending, within [0, N]
+ *   u_accept    dev [N] float in [0, 1)                   u_sample   dev [B] float in [0, 1)
+ *   draft_probs dev [N, Vd] float or NULL, rows ld_draft apart        draft_ids  dev [N] int32: tokens as draft indices
+ *   d2t         dev [Vd] int32: the draft-to-target map, distinct ids (NULL: a draft index is the target's id)
+ *   n_accepted  dev [B] int32 (out)       path  dev [B, max_tokens] int32 (out): the accepted tokens' indices within the request, then -1
+ *   out_tokens  dev [B, max_tokens] int32 (out): the accepted tokens, the one that follows them, then -1
+ * A token whose parent is not an earlier one of its request, or whose token or draft index lies outside its vocabulary, is left out, with all
+ * that hangs on it.  A request without tokens accepts 0 and has -1 everywhere; one with more than max_tokens loses those past it.
+ * Negative and NaN probabilities count as 0; a row without any positive entry gives -1 as the token that follows.
+ * 1 <= max_tokens <= 1024; V <= 4194304, with draft_probs V <= 393216; Vd >= 1.  Asynchronous; results do not depend on timing. */
+vt_status vt_verify_tokens(const float* probs, int64_t ld_probs, const int32_t* tokens, const int32_t* parents, const int32_t* cu_tokens,
+                           const float* u_accept, const float* u_sample, const float* draft_probs, int64_t ld_draft,
+                           const int32_t* draft_ids, const int32_t* d2t, int N, int B, int V, int Vd, int max_tokens,
+                           int32_t* n_accepted, int32_t* path, int32_t* out_tokens, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Coverage of a token stream by the kept set (Eq. 2 with f(v) = occurrences of v in the

@@ -19,6 +19,9 @@ _BINDING_NAMES = {
     "VtScores", "vt_score_tokens", "vt_score_tokens_backward", "vt_score_workspace_bytes", "vt_score_backward_workspace_bytes",
     "vt_gated_ffn", "vt_gated_ffn_backward", "vt_gated_ffn_workspace_bytes", "vt_gated_ffn_backward_workspace_bytes",
     "VT_ACT_SILU", "VT_ACT_GELU",
+    "VtRope", "vt_rope_table", "vt_rope", "VtCache", "vt_rope_append", "vt_tree_mask", "vt_tree_attention",
+    "vt_tree_attention_workspace_bytes", "VtVerified", "vt_verify_tokens",
+    "VT_ROPE_NONE", "VT_ROPE_LINEAR", "VT_ROPE_BASE", "VT_ROPE_WAVELENGTH", "VT_ROPE_RAMP", "VT_ROPE_INTERLEAVED", "VT_ROPE_INVERSE",
 }
 
 

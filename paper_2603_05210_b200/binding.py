@@ -8,6 +8,7 @@ fallback: if the library cannot be loaded the call raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import NamedTuple
 
@@ -23,6 +24,8 @@ VT_MAX_K = 64
 VT_PATH_AUTO, VT_PATH_GEMV, VT_PATH_MMA, VT_PATH_MMA_SMALL = 0, 1, 2, 3
 VT_HEAD_STATIC_WEIGHTS, VT_HEAD_D2T_OFFSETS = 0x100, 0x200
 VT_ACT_SILU, VT_ACT_GELU = 0, 1
+VT_ROPE_NONE, VT_ROPE_LINEAR, VT_ROPE_BASE, VT_ROPE_WAVELENGTH, VT_ROPE_RAMP = 0, 1, 2, 3, 4
+VT_ROPE_INTERLEAVED, VT_ROPE_INVERSE = 1, 2
 
 # every symbol include/vt.h declares: name -> (restype, argtypes)
 _p, _i, _i64, _sz, _f = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
@@ -57,6 +60,13 @@ SYMBOLS = {
     "vt_gated_ffn": (_i, [_p, _i64, _p, _p, _p, _i, _i, _i, _i, _p, _p, _p, _sz, _p]),
     "vt_gated_ffn_backward_workspace_bytes": (_sz, [_i, _i, _i]),
     "vt_gated_ffn_backward": (_i, [_p, _i64, _p, _p, _p, _p, _p, _i64, _i, _i, _i, _i, _p, _p, _p, _p, _p, _sz, _p]),
+    "vt_rope_table": (_i, [_p, _i, ctypes.c_double, _i, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double, _p]),
+    "vt_rope": (_i, [_p, _p, _p, _p, _i, _i, _i, _i, _i, _f, _i, _p, _p, _p]),
+    "vt_rope_append": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _i, _f, _i, _p, _p, _p]),
+    "vt_tree_attention_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "vt_tree_attention": (_i, [_p, _p, _p, _p, _i, _i, _i, _i, _f, _p, _p, _p, _sz, _p]),
+    "vt_tree_mask": (_i, [_p, _p, _p, _i, _i, _p, _i, _p, _p]),
+    "vt_verify_tokens": (_i, [_p, _i64, _p, _p, _p, _p, _p, _p, _i64, _p, _p, _i, _i, _i, _i, _i, _p, _p, _p, _p]),
     "vt_remap": (_i, [_p, _p, _i64, _i, _p, _p]),
     "vt_vocab_maps": (_i, [_p, _i, _i, _p, _p, _p]),
     "vt_last_launch_count": (_i, []),
@@ -526,6 +536,269 @@ def vt_gated_ffn_backward(x: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Ten
                                        grad_W_gate.data_ptr(), grad_W_up.data_ptr(), grad_W_down.data_ptr(), workspace.data_ptr(),
                                        workspace.nbytes, _stream()), "vt_gated_ffn_backward")
     return grad_x, grad_W_gate, grad_W_up, grad_W_down
+
+
+class _VtHeads(ctypes.Structure):
+    """``vt_heads``: a [tokens, heads, D] bf16 tensor."""
+    _fields_ = [("ptr", _p), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class _VtCacheStruct(ctypes.Structure):
+    _fields_ = [("k", _p), ("v", _p), ("page_table", _p), ("lens", _p)] + \
+        [(n, _i64) for n in ("k_page_stride", "k_token_stride", "k_head_stride", "v_page_stride", "v_token_stride", "v_head_stride",
+                             "table_stride")] + \
+        [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "heads", "head_dim", "B", "max_pages")]
+
+
+def _heads(t: torch.Tensor, name: str, device: int) -> _VtHeads:
+    """bf16 [tokens, heads, D] on the current device, the elements of a head in a row; anything else may be strided."""
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3 or t.get_device() != device or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{name}: expected [tokens, heads, D] with contiguous heads on the current CUDA device")
+    n, h, d = t.shape
+    if n > 1 and h > 1:
+        return _VtHeads(t.data_ptr(), t.stride(0), t.stride(1))
+    return _VtHeads(t.data_ptr(), t.stride(0) if n > 1 else max(h, 1) * d, t.stride(1) if h > 1 else d)     # the stride of one alone says nothing
+
+
+def _vector(t: torch.Tensor, name: str, n: int | None, device: int, dtype: torch.dtype = torch.int32) -> int:
+    """The address of a contiguous vector of n entries (None: any number) on the current device."""
+    if t.dtype is not dtype or t.dim() != 1 or t.get_device() != device or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{name}: expected a contiguous {dtype} vector{'' if n is None else f' of {n}'} on the current CUDA device")
+    return t.data_ptr()
+
+
+def _new_or_given(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, like: torch.Tensor, device: int) -> torch.Tensor:
+    if t is None:
+        return like.new_empty(shape, dtype=dtype)
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on the current CUDA device")
+    return t
+
+
+class VtRope(NamedTuple):
+    """Frequencies and layout of rotary positions, from ``vt_rope_table``."""
+    table: torch.Tensor        # [rot_dim / 2] int64: turns per position, as fractions of 2^64
+    rot_dim: int
+    interleaved: bool
+    amplitude: float
+
+
+_ROPE_SCALINGS = {"none": VT_ROPE_NONE, "linear": VT_ROPE_LINEAR, "base": VT_ROPE_BASE, "wavelength": VT_ROPE_WAVELENGTH, "ramp": VT_ROPE_RAMP}
+
+
+def vt_rope_table(rot_dim: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                  high: float | None = None, original_len: float = 8192.0, interleaved: bool = False, amplitude: float | None = None,
+                  device=None) -> VtRope:
+    """The plan of rotary positions over a head's first ``rot_dim`` elements, pairs (i, i + rot_dim / 2) or, ``interleaved``, (2 i, 2 i + 1).
+
+    ``scaling`` stretches positions for contexts longer than ``original_len``: "linear", "base", "wavelength" (``low`` and ``high`` turns,
+    1 and 4) or "ramp" (1 and 32; the amplitude is then 0.1 log(factor) + 1 unless it is given).  Formulas: ``include/vt.h``."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling: expected one of {', '.join(_ROPE_SCALINGS)}, got {scaling!r}")
+    if high is None:
+        high = 32.0 if scaling == "ramp" else 4.0
+    if amplitude is None:
+        amplitude = 0.1 * math.log(factor) + 1.0 if scaling == "ramp" and factor > 0 else 1.0
+    table = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.int64, device=device or "cuda")
+    if table.get_device() != torch.cuda.current_device():
+        raise ValueError("device: expected the current CUDA device")
+    _check(lib().vt_rope_table(table.data_ptr(), rot_dim, base, _ROPE_SCALINGS[scaling], factor, low, high, original_len, _stream()),
+           "vt_rope_table")
+    return VtRope(table, int(rot_dim), bool(interleaved), float(amplitude))
+
+
+class VtCache:
+    """A paged cache: ``k`` and ``v`` [pages, page_size, heads, D] bf16 (any strides that are multiples of 8, D in a row), ``page_table`` [B, n]
+    int32 and ``lens`` [B] int32.  The tensors are the caller's: the table, the lengths and the cache itself may be written between
+    calls; for other tensors make another ``VtCache``."""
+    __slots__ = ("_k", "_v", "_table", "_lens", "_struct", "_ref", "_device")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor):
+        for name, t in (("k", k), ("v", v)):
+            if t.dtype is not torch.bfloat16:
+                raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
+            if t.dim() != 4 or not t.is_cuda or (t.stride(3) != 1 and t.shape[3] > 1) or t.shape != k.shape or t.device != k.device:
+                raise ValueError(f"{name}: expected [pages, page_size, heads, D] with D in a row on one CUDA device, both alike")
+        B = lens.shape[0] if lens.dim() == 1 else -1
+        if lens.dtype is not torch.int32 or B < 1 or not lens.is_contiguous() or lens.device != k.device:
+            raise ValueError("lens: expected a contiguous int32 vector on the cache's device")
+        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or page_table.device != k.device or \
+                (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+            raise ValueError("page_table: expected int32 [len(lens), pages] with contiguous rows on the cache's device")
+        if page_table.shape[1] < 1 or min(k.shape) < 1:
+            raise ValueError("page_table, k: an empty cache")
+        self._k, self._v, self._table, self._lens, self._device = k, v, page_table, lens, k.get_device()
+        whole = k.numel()
+
+        def strides(t):                # the stride of one alone says nothing
+            return [s if n > 1 else (whole + 7) // 8 * 8 for s, n in zip(t.stride()[:3], t.shape)]
+
+        self._struct = _VtCacheStruct(k.data_ptr(), v.data_ptr(), page_table.data_ptr(), lens.data_ptr(), *strides(k), *strides(v),
+                                      page_table.stride(0), *k.shape, B, page_table.shape[1])
+        self._ref = ctypes.addressof(self._struct)
+
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    page_table = property(lambda self: self._table)
+    lens = property(lambda self: self._lens)
+
+
+def _rope_args(q, k, positions, rope: VtRope):
+    device = torch.cuda.current_device()
+    hq = _heads(q, "q", device)
+    hk = None if k is None else _heads(k, "k", device)
+    if k is not None and (k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]):
+        raise ValueError("q and k disagree on tokens or D")
+    _vector(positions, "positions", q.shape[0], device)
+    if rope.table.get_device() != device:
+        raise ValueError("rope: its table lies on another device")
+    return device, hq, hk
+
+
+def _heads_out(t, name, like, device):
+    if t is None:
+        t = torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
+    elif t.shape != like.shape:
+        raise ValueError(f"{name}: expected the shape of its input")
+    return t, _heads(t, name, device)
+
+
+def vt_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, rope: VtRope, *, inverse: bool = False,
+            out_q: torch.Tensor | None = None, out_k: torch.Tensor | None = None):
+    """(q, k) turned to their ``positions`` [N] int32; q [N, Hq, D], k [N, Hkv, D] or None.
+
+    ``inverse`` turns back, which is the gradient's way: (grad_q, grad_k) = vt_rope(grad of q, grad of k, ..., inverse=True).  The outputs may
+    be the inputs themselves."""
+    device, hq, hk = _rope_args(q, k, positions, rope)
+    out_q, ho = _heads_out(out_q, "out_q", q, device)
+    ko = None
+    if k is not None:
+        out_k, ko = _heads_out(out_k, "out_k", k, device)
+    elif out_k is not None:
+        raise ValueError("out_k needs k")
+    N, Hq, D = q.shape
+    _check(lib().vt_rope(ctypes.byref(hq), None if hk is None else ctypes.byref(hk), positions.data_ptr(), rope.table.data_ptr(), N, Hq,
+                         0 if k is None else k.shape[1], D, rope.rot_dim, rope.amplitude,
+                         (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), ctypes.byref(ho),
+                         None if ko is None else ctypes.byref(ko), _stream()), "vt_rope")
+    return out_q, out_k
+
+
+def vt_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache,
+                   rope: VtRope, *, out_q: torch.Tensor | None = None) -> torch.Tensor:
+    """q [N, Hq, D] turned; k [N, heads, D] turned into the cache and v beside it, at places lens[b], lens[b] + 1, ... of each request.
+
+    Request b has the tokens from ``cu_tokens``[b] to ``cu_tokens``[b + 1]; tokens outside all requests are padding, and left alone."""
+    device, hq, hk = _rope_args(q, k, positions, rope)
+    hv = _heads(v, "v", device)
+    c = cache._struct
+    if k.shape != v.shape or k.shape[1] != c.heads or k.shape[2] != c.head_dim or cache._device != device:
+        raise ValueError("k, v and the cache disagree on tokens, heads, D or device")
+    cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
+    out_q, ho = _heads_out(out_q, "out_q", q, device)
+    _check(lib().vt_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), positions.data_ptr(), cu, rope.table.data_ptr(), q.shape[0],
+                                q.shape[1], rope.rot_dim, rope.amplitude, VT_ROPE_INTERLEAVED if rope.interleaved else 0, ctypes.byref(ho),
+                                cache._ref, _stream()), "vt_rope_append")
+    return out_q
+
+
+def vt_tree_mask(parents: torch.Tensor, cu_tokens: torch.Tensor, max_tokens: int, *, lens: torch.Tensor | None = None,
+                 mask: torch.Tensor | None = None, positions: torch.Tensor | None = None):
+    """(mask [N, ceil(max_tokens / 32)] int32, positions [N] int32) of drafted trees from ``parents`` [N] (index within the request, -1: none).
+
+    A token's row has the bits of the tokens on its way up and its own; its position is lens[b] + its depth (without ``lens`` the depth)."""
+    device = torch.cuda.current_device()
+    N, words = parents.shape[0], (int(max_tokens) + 31) // 32
+    pp, cu = _vector(parents, "parents", N, device), _vector(cu_tokens, "cu_tokens", None, device)
+    B = cu_tokens.shape[0] - 1
+    pl = None if lens is None else _vector(lens, "lens", B, device)
+    mask = _new_or_given(mask, "mask", (N, words), torch.int32, parents, device)
+    positions = _new_or_given(positions, "positions", (N,), torch.int32, parents, device)
+    _check(lib().vt_tree_mask(pp, cu, pl, N, B, mask.data_ptr(), words, positions.data_ptr(), _stream()), "vt_tree_mask")
+    return mask, positions
+
+
+def vt_tree_attention_workspace_bytes(Hq: int, heads: int, D: int, max_tokens: int) -> int:
+    return int(lib().vt_tree_attention_workspace_bytes(Hq, heads, D, max_tokens))
+
+
+def vt_tree_attention(q: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache, *, max_tokens: int, mask: torch.Tensor | None = None,
+                      scale: float | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(out [N, Hq, D] bf16, lse [N, Hq] float32): drafted tokens' attention over the cache, which holds their keys and values at its end.
+
+    ``max_tokens`` bounds the tokens of a request.  ``mask`` [N, words] int32 (``vt_tree_mask``) says which drafted tokens each attends; without
+    it a token attends itself and those before it.  ``scale`` is D^-0.5 unless it is given.  Rows outside all requests are left as they were.
+    Time-outs and page ids outside the cache are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
+    device = torch.cuda.current_device()
+    hq = _heads(q, "q", device)
+    N, Hq, D = q.shape
+    c = cache._struct
+    if D != c.head_dim or cache._device != device:
+        raise ValueError("q and the cache disagree on D or device")
+    cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
+    words = 0
+    if mask is not None:
+        if mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != N or mask.get_device() != device or not mask.is_contiguous():
+            raise ValueError("mask: expected a contiguous int32 tensor with a row per token on the current CUDA device")
+        words = mask.shape[1]
+    out, ho = _heads_out(out, "out", q, device)
+    lse = _new_or_given(lse, "lse", (N, Hq), torch.float32, q, device)
+    if workspace is None:
+        workspace = torch.empty(max(vt_tree_attention_workspace_bytes(Hq, c.heads, D, max_tokens), 256), dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor on the current CUDA device")
+    _check(lib().vt_tree_attention(ctypes.byref(hq), cu, cache._ref, None if mask is None else mask.data_ptr(), words, N, Hq, max_tokens,
+                                   D ** -0.5 if scale is None else scale, ctypes.byref(ho), lse.data_ptr(), workspace.data_ptr(),
+                                   workspace.nbytes, _stream()), "vt_tree_attention")
+    return out, lse
+
+
+class VtVerified(NamedTuple):
+    """What ``vt_verify_tokens`` returns, int32."""
+    n_accepted: torch.Tensor   # [B]
+    path: torch.Tensor         # [B, max_tokens]: accepted tokens as indices within the request, then -1
+    tokens: torch.Tensor       # [B, max_tokens]: the accepted tokens, the one that follows them, then -1
+
+
+def vt_verify_tokens(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, cu_tokens: torch.Tensor, u_accept: torch.Tensor,
+                     u_sample: torch.Tensor, *, max_tokens: int, draft_probs: torch.Tensor | None = None,
+                     draft_ids: torch.Tensor | None = None, d2t: torch.Tensor | None = None, out: VtVerified | None = None) -> VtVerified:
+    """Which drafted tokens stay, given the target's ``probs`` [N, V] after each token and random numbers, and the token that follows them.
+
+    Token 0 of a request is its root.  With ``draft_probs`` [N, Vd] the children of a token were drawn from its row (``draft_ids`` [N]: the tokens
+    as draft indices, ``d2t`` [Vd] the draft-to-target map); without them they were picked without chance (``vt_tree_select``).  The result is
+    distributed as if the target had generated alone; the rule is spelled out in ``include/vt.h``."""
+    device = torch.cuda.current_device()
+    for name, t in (("probs", probs), ("draft_probs", draft_probs)):
+        if t is not None and (t.dtype is not torch.float32 or t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.shape[1] > 1)):
+            raise ValueError(f"{name}: expected float32 [N, vocabulary] with contiguous rows on the current CUDA device")
+    N, V = probs.shape
+    B = u_sample.shape[0]
+    f32 = torch.float32
+    args = (_vector(tokens, "tokens", N, device), _vector(parents, "parents", N, device), _vector(cu_tokens, "cu_tokens", B + 1, device),
+            _vector(u_accept, "u_accept", N, device, f32), _vector(u_sample, "u_sample", B, device, f32))
+    Vd, pq, ldq, pi, pm = 0, None, 0, None, None
+    if draft_probs is not None:
+        if draft_ids is None or draft_probs.shape[0] != N:
+            raise ValueError("draft_probs needs a row per token, and draft_ids")
+        Vd, pq, ldq = draft_probs.shape[1], draft_probs.data_ptr(), draft_probs.stride(0) if N > 1 else draft_probs.shape[1]
+        pi = _vector(draft_ids, "draft_ids", N, device)
+        pm = None if d2t is None else _vector(d2t, "d2t", Vd, device)
+    elif draft_ids is not None or d2t is not None:
+        raise ValueError("draft_ids and d2t need draft_probs")
+    if out is None:                # one allocation cut up
+        n = max(int(max_tokens), 0)
+        a, b, c = tokens.new_empty((B * (1 + 2 * n),)).split_with_sizes((B, B * n, B * n))
+        out = VtVerified(a, b.view(B, n), c.view(B, n))
+    else:
+        for name, t, shape in zip(VtVerified._fields, out, ((B,), (B, max_tokens), (B, max_tokens))):
+            _new_or_given(t, name, shape, torch.int32, tokens, device)
+    _check(lib().vt_verify_tokens(probs.data_ptr(), probs.stride(0) if N > 1 else V, *args, pq, ldq, pi, pm, N, B, V, Vd, max_tokens,
+                                  out.n_accepted.data_ptr(), out.path.data_ptr(), out.tokens.data_ptr(), _stream()), "vt_verify_tokens")
+    return out
 
 
 def vt_remap(draft_ids: torch.Tensor, d2t: torch.Tensor) -> torch.Tensor:

@@ -8,6 +8,7 @@
 #include "vt_ffn.h"
 #include "vt_launch.h"
 #include "vt_score.h"
+#include "vt_step.h"
 
 namespace vt {
 
@@ -146,7 +147,7 @@ const char* vt_strerror(vt_status s) {
         case VT_ERR_NULL: return "a required pointer is NULL";
         case VT_ERR_SHAPE: return "a size or shape argument is outside the supported range";
         case VT_ERR_ALIGN: return "a pointer is not aligned as required";
-        case VT_ERR_RANGE: return "a keep id lies outside [0, V_full)";
+        case VT_ERR_RANGE: return "a keep id lies outside [0, V_full), or a page id outside the cache";
         case VT_ERR_DUP: return "keep_ids names an id more than once";
         case VT_ERR_EMPTY: return "coverage of an empty token stream is undefined";
         case VT_ERR_WORKSPACE: return "workspace is NULL, misaligned or too small";
@@ -316,7 +317,166 @@ vt_status vt_last_status(void* workspace, void* stream) {
         e = cudaMemsetAsync(&hdr->status, 0, 4, st);
         if (e != cudaSuccess) return cuda_fail(e);
     }
-    return (status & kStatusTimeout) ? VT_ERR_TIMEOUT : VT_OK;
+    return (status & kStatusTimeout) ? VT_ERR_TIMEOUT : (status & kStatusPage) ? VT_ERR_RANGE : VT_OK;
+}
+
+vt_status vt_rope_table(uint64_t* table, int rot_dim, double base, int scaling, double factor, double low, double high, double original_len,
+                        void* stream) {
+    g_launches = 0;
+    if (!table) return VT_ERR_NULL;
+    if (rot_dim < 16 || rot_dim % 16 != 0 || rot_dim > 1024 || !(base > 1.0) || !std::isfinite(base)) return VT_ERR_SHAPE;
+    if (scaling < VT_ROPE_NONE || scaling > VT_ROPE_RAMP) return VT_ERR_SHAPE;
+    if (scaling != VT_ROPE_NONE && (!(factor > 0.0) || !std::isfinite(factor))) return VT_ERR_SHAPE;
+    if (scaling >= VT_ROPE_WAVELENGTH &&
+        (!(original_len > 0.0) || !std::isfinite(original_len) || !std::isfinite(low) || !std::isfinite(high) || !(low < high) ||
+         (scaling == VT_ROPE_RAMP && !(low > 0.0))))
+        return VT_ERR_SHAPE;
+    if (!aligned(table, 8)) return VT_ERR_ALIGN;
+    return launch_rope_table(table, rot_dim, base, scaling, factor, low, high, original_len, (cudaStream_t)stream);
+}
+
+static bool heads_strides_ok(const vt_heads& h) {
+    return h.token_stride > 0 && h.head_stride > 0 && h.token_stride % 8 == 0 && h.head_stride % 8 == 0;
+}
+
+static vt_status check_rope_args(const vt_heads* q, const vt_heads* k, const int32_t* positions, const uint64_t* table, int N, int Hq,
+                                 int Hkv, int D, int rot_dim, float amplitude, int options, int known, const vt_heads* q_out) {
+    if (!q || !q_out || !table || (Hkv > 0 && !k) || (N > 0 && (!q->ptr || !q_out->ptr || !positions || (Hkv > 0 && !k->ptr)))) return VT_ERR_NULL;
+    if (N < 0 || Hq < 1 || Hkv < 0 || Hq > 65536 || Hkv > 65536 || D < 16 || D % 16 != 0 || D > 1024 || rot_dim < 16 || rot_dim % 16 != 0 ||
+        rot_dim > D || !std::isfinite(amplitude) || (options & ~known) != 0)
+        return VT_ERR_SHAPE;
+    if (!heads_strides_ok(*q) || !heads_strides_ok(*q_out) || (Hkv > 0 && !heads_strides_ok(*k))) return VT_ERR_SHAPE;
+    if (!aligned(q->ptr, 16) || !aligned(q_out->ptr, 16) || (Hkv > 0 && !aligned(k->ptr, 16)) || !aligned(positions, 4) || !aligned(table, 8))
+        return VT_ERR_ALIGN;
+    return VT_OK;
+}
+
+vt_status vt_rope(const vt_heads* q, const vt_heads* k, const int32_t* positions, const uint64_t* table, int N, int Hq, int Hkv, int D,
+                  int rot_dim, float amplitude, int options, const vt_heads* q_out, const vt_heads* k_out, void* stream) {
+    g_launches = 0;
+    if (Hkv > 0 && (!k_out || (N > 0 && !k_out->ptr))) return VT_ERR_NULL;
+    vt_status r = check_rope_args(q, k, positions, table, N, Hq, Hkv, D, rot_dim, amplitude, options, VT_ROPE_INTERLEAVED | VT_ROPE_INVERSE, q_out);
+    if (r != VT_OK) return r;
+    if (Hkv > 0 && !heads_strides_ok(*k_out)) return VT_ERR_SHAPE;
+    if (Hkv > 0 && !aligned(k_out->ptr, 16)) return VT_ERR_ALIGN;
+    if (N == 0) return VT_OK;
+    RopeCall c{};
+    c.q = *q;
+    c.q_out = *q_out;
+    if (Hkv > 0) {
+        c.k = *k;
+        c.k_out = *k_out;
+    }
+    c.positions = positions;
+    c.table = table;
+    c.N = N;
+    c.Hq = Hq;
+    c.Hkv = Hkv;
+    c.D = D;
+    c.rot_dim = rot_dim;
+    c.amplitude = amplitude;
+    c.options = options;
+    return launch_rope(c, (cudaStream_t)stream);
+}
+
+static vt_status check_cache(const vt_cache* a) {
+    if (!a || !a->k || !a->v || !a->page_table || !a->lens) return VT_ERR_NULL;
+    if (a->n_pages < 1 || a->heads < 1 || a->heads > 65536 || a->B < 1 || a->max_pages < 1 || a->table_stride < 0 || a->head_dim < 16 ||
+        a->head_dim % 16 != 0 || a->head_dim > 1024)
+        return VT_ERR_SHAPE;
+    const int ps = a->page_size;
+    if (!(ps == 8 || ps == 16 || ps == 32 || ps == 64 || (ps >= 128 && ps % 128 == 0))) return VT_ERR_SHAPE;
+    for (int64_t s : {a->k_page_stride, a->k_token_stride, a->k_head_stride, a->v_page_stride, a->v_token_stride, a->v_head_stride})
+        if (s < 8 || s % 8 != 0) return VT_ERR_SHAPE;
+    if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->page_table, 4) || !aligned(a->lens, 4)) return VT_ERR_ALIGN;
+    return VT_OK;
+}
+
+vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v, const int32_t* positions, const int32_t* cu_tokens,
+                         const uint64_t* table, int N, int Hq, int rot_dim, float amplitude, int options, const vt_heads* q_out,
+                         const vt_cache* cache, void* stream) {
+    g_launches = 0;
+    if (!k || !v || !cu_tokens || (N > 0 && !v->ptr)) return VT_ERR_NULL;
+    vt_status r = check_cache(cache);
+    if (r != VT_OK) return r;
+    r = check_rope_args(q, k, positions, table, N, Hq, cache->heads, cache->head_dim, rot_dim, amplitude, options, VT_ROPE_INTERLEAVED, q_out);
+    if (r != VT_OK) return r;
+    if (!heads_strides_ok(*v)) return VT_ERR_SHAPE;
+    if (!aligned(v->ptr, 16) || !aligned(cu_tokens, 4)) return VT_ERR_ALIGN;
+    if (N == 0) return VT_OK;
+    RopeCall c{};
+    c.q = *q;
+    c.k = *k;
+    c.v = *v;
+    c.q_out = *q_out;
+    c.positions = positions;
+    c.cu_tokens = cu_tokens;
+    c.table = table;
+    c.N = N;
+    c.Hq = Hq;
+    c.Hkv = cache->heads;
+    c.D = cache->head_dim;
+    c.rot_dim = rot_dim;
+    c.amplitude = amplitude;
+    c.options = options;
+    c.cache = cache;
+    return launch_rope(c, (cudaStream_t)stream);
+}
+
+static bool attn_shape_ok(int Hq, int heads, int D, int max_tokens) {
+    return heads >= 1 && Hq >= 1 && Hq <= 65536 && Hq % heads == 0 && Hq / heads <= 128 && (D == 64 || D == 128) && max_tokens >= 1;
+}
+
+size_t vt_tree_attention_workspace_bytes(int Hq, int heads, int D, int max_tokens) {
+    return attn_shape_ok(Hq, heads, D, max_tokens) ? attn_workspace_bytes(Hq, heads, D, max_tokens) : 0;
+}
+
+vt_status vt_tree_attention(const vt_heads* q, const int32_t* cu_tokens, const vt_cache* cache, const int32_t* mask, int mask_words, int N,
+                            int Hq, int max_tokens, float scale, const vt_heads* out, float* lse, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    g_launches = 0;
+    if (!q || !cu_tokens || !out || (N > 0 && (!q->ptr || !out->ptr))) return VT_ERR_NULL;
+    vt_status r = check_cache(cache);
+    if (r != VT_OK) return r;
+    if (!attn_shape_ok(Hq, cache->heads, cache->head_dim, max_tokens) || N < 0 || (mask && mask_words < 1) || !(scale > 0.0f) ||
+        !std::isfinite(scale) || !heads_strides_ok(*q) || !heads_strides_ok(*out))
+        return VT_ERR_SHAPE;
+    if (!aligned(q->ptr, 16) || !aligned(out->ptr, 16) || !aligned(cu_tokens, 4) || !aligned(mask, 4) || !aligned(lse, 4)) return VT_ERR_ALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < attn_workspace_bytes(Hq, cache->heads, cache->head_dim, max_tokens))
+        return VT_ERR_WORKSPACE;
+    if (N == 0) return VT_OK;
+    const AttnCall c{*q, *out, cu_tokens, mask, cache, lse, mask_words, N, Hq, max_tokens, scale};
+    return launch_attn(c, workspace, (cudaStream_t)stream);
+}
+
+vt_status vt_tree_mask(const int32_t* parents, const int32_t* cu_tokens, const int32_t* lens, int N, int B, int32_t* mask, int mask_words,
+                       int32_t* positions, void* stream) {
+    g_launches = 0;
+    if (!cu_tokens || (N > 0 && (!parents || (!mask && !positions)))) return VT_ERR_NULL;
+    if (N < 0 || B < 1 || (mask && mask_words < 1)) return VT_ERR_SHAPE;
+    if (!aligned(parents, 4) || !aligned(cu_tokens, 4) || !aligned(lens, 4) || !aligned(mask, 4) || !aligned(positions, 4)) return VT_ERR_ALIGN;
+    if (N == 0) return VT_OK;
+    return launch_tree_mask(parents, cu_tokens, lens, N, B, mask, mask_words, positions, (cudaStream_t)stream);
+}
+
+vt_status vt_verify_tokens(const float* probs, int64_t ld_probs, const int32_t* tokens, const int32_t* parents, const int32_t* cu_tokens,
+                           const float* u_accept, const float* u_sample, const float* draft_probs, int64_t ld_draft,
+                           const int32_t* draft_ids, const int32_t* d2t, int N, int B, int V, int Vd, int max_tokens,
+                           int32_t* n_accepted, int32_t* path, int32_t* out_tokens, void* stream) {
+    g_launches = 0;
+    if (!cu_tokens || !u_sample || !n_accepted || !path || !out_tokens ||
+        (N > 0 && (!probs || !tokens || !parents || !u_accept || (draft_probs && !draft_ids))))
+        return VT_ERR_NULL;
+    if (N < 0 || B < 1 || B > (1 << 24) || V < 1 || max_tokens < 1 || max_tokens > kVerifyMaxTokens || ld_probs < V ||
+        V > (draft_probs ? kVerifyMaxVDrawn : kVerifyMaxV) || (draft_probs && (Vd < 1 || ld_draft < Vd)))
+        return VT_ERR_SHAPE;
+    for (const void* q : {(const void*)probs, (const void*)tokens, (const void*)parents, (const void*)cu_tokens, (const void*)u_accept,
+                          (const void*)u_sample, (const void*)draft_probs, (const void*)draft_ids, (const void*)d2t, (const void*)n_accepted,
+                          (const void*)path, (const void*)out_tokens})
+        if (!aligned(q, 4)) return VT_ERR_ALIGN;
+    const VerifyCall c{probs, u_accept, u_sample, draft_probs, tokens, parents, cu_tokens, draft_ids, d2t, ld_probs, ld_draft,
+                       N, B, V, Vd, max_tokens, n_accepted, path, out_tokens};
+    return launch_verify(c, (cudaStream_t)stream);
 }
 
 vt_status vt_coverage_enqueue(const int32_t* token_ids, int64_t N, const int32_t* keep_ids, int V_trim, int V_full,

@@ -1,0 +1,915 @@
+// Attention of drafted tokens over a paged cache (see vt_tree_attention).
+//
+// out = sum_i e^{x_i - lse} v_i over the attended positions, x = scale q.k: one pass over keys and values, with the running maximum and sum
+// of each row, as two tcgen05 products per tile of 128 positions - S = Q K^T, then O += P V with P = 2^{(S - m) scale log2 e} in bf16.
+//
+// Rows.  All query heads of a key head and all drafted tokens of a request read the same keys, so they are the rows of one product: row
+// t G + g for token t and head g of G.  A block of rows is up to two tiles of 128 TMEM lanes (a TMA box of G heads x 128 / G tokens fills a tile
+// in that order).
+//
+// Two streams.  S, P and O of two streams live in tensor memory: O0, O1, S0, S1, 128 columns each; P takes the place of its S.  While
+// four warps work out one stream's exponentials, the tensor cores multiply for the other.  With two row tiles a stream is a row tile
+// and both read each key tile; with one, the streams take the key tiles in turn, and are joined when the rows are finished.
+//
+// Work.  The lengths are known on the device alone, so the cut is made there: all key tiles of all (request, key head, row block) in a row,
+// an equal run of them to each CTA.  A run begins and ends inside an item, and a long item lies in many runs: a CTA writes what it has
+// of such an item (unnormalised O, m, l in fp32) to the workspace, and a second kernel joins the pieces.  No atomics: the same bits every time.
+// Where the host can see that no item is longer than kAttnWhole tiles, items are not cut and there is one launch.
+//
+// O is rescaled only when a row's maximum grows by more than 2^8 over the one in use (P then stays below 2^8, its sum in fp32): the
+// rescale, done by the stream's own warps, is rare after the first tiles.
+//
+// Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (and the end of an item), warp 8 TMA producer, warp 9 MMA issuer, warp 10 the cleaner: in
+// tiles where something is masked it turns infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
+// All waits are bounded; one that runs out sets the status word and every role leaves.
+#include "vt_step.h"
+#include "vt_tc.cuh"
+
+namespace vt {
+
+int gemm_withheld_us();                      // see vt_test_withhold_copies
+
+constexpr int kAttnKeys = 128;               // positions per tile
+constexpr int kAttnThreads = 11 * 32;
+constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10;
+constexpr int kAttnCtas = 148;               // runs at most
+constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
+constexpr int kAttnMaxStages = 12;
+constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
+constexpr uint32_t kAttnTmemO = 0, kAttnTmemS = 256;
+
+struct AttnSplit {                           // a CTA's first item, where the CTA's run begins inside it and it is the first to do so
+    int rows;                                // 0: none
+    int token0, head0, n_pieces, first_cta;
+    int first_slot;                          // of the first piece: 0 where its CTA's run begins with the item
+    int pad[2];
+};
+static_assert(sizeof(AttnSplit) == 32, "one sector");
+
+struct AttnParams {
+    const int32_t *cu, *lens, *page_table, *mask;
+    int64_t table_stride;
+    uint16_t* out;
+    int64_t out_ts, out_hs;
+    float* lse;
+    WsHeader* hdr;
+    AttnSplit* splits;                       // [gridDim.x]
+    float2* part_ml;                         // [gridDim.x][2][rows]: (m, l) of a piece's rows
+    float* part_o;                           // [gridDim.x][2][D / 4][rows][4]
+    int rows_max;                            // rows of a block at most
+    int N, B, Hq, Hkv, G, max_tokens, mask_words, n_pages, page_size, max_pages;
+    int tpt;                                 // tokens per row tile
+    int box_tokens;                          // tokens in a box of q
+    int whole;                               // 1: items are not cut
+    int n_stages;
+    uint32_t q_block, q_slot;                // bytes of 64 columns of a row tile; of a row tile
+    uint32_t q_tx, page_tx;                  // bytes of a q tile; of one box of keys
+    uint32_t shared_off, bar_off, withheld;              // withheld: see vt_test_withhold_copies
+    float scale, scale_log2;
+    unsigned long long wait_ns;
+};
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+// Descriptor of V as an operand whose columns (of the head) run fastest: 64 columns are one 128-byte swizzled row, 8 positions are 1024
+// bytes apart, the next 64 columns a block of 128 positions further on.
+__device__ __forceinline__ uint64_t attn_v_desc(uint32_t addr) {
+    uint64_t desc = 0;
+    desc |= (uint64_t)((addr & 0x3FFFFu) >> 4);
+    desc |= (uint64_t)((kAttnKeys * 128) >> 4) << 16;
+    desc |= (uint64_t)(1024 >> 4) << 32;
+    desc |= (uint64_t)1 << 46;
+    desc |= (uint64_t)2 << 61;
+    return desc;
+}
+__device__ __forceinline__ bool attn_elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t attn_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------ the cut
+struct AttnRequest {
+    int first, T, L;                         // first token, tokens, earlier positions
+};
+// Whatever the arrays hold, the tokens lie inside [0, N) and the positions inside the table.
+__device__ __forceinline__ AttnRequest attn_request(const AttnParams& p, int b) {
+    AttnRequest q;
+    const long long cap = (long long)p.max_pages * p.page_size;
+    q.first = min(max(p.cu[b], 0), p.N);
+    q.T = min(min(max(p.cu[b + 1], q.first), p.N) - q.first, p.max_tokens);
+    q.L = (int)min(min((long long)max(p.lens[b], 0), cap), 0x7FFF0000ll - q.T);
+    return q;
+}
+// The positions that tokens [.., t_end) of a request may attend, and the tiles they take.
+__device__ __forceinline__ int attn_keys(const AttnParams& p, const AttnRequest& q, int t_end) {
+    const long long cap = (long long)p.max_pages * p.page_size;
+    return (int)min((long long)q.L + (p.mask ? q.T : min(q.T, t_end)), cap);
+}
+__device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnRequest& q, int block) {
+    return max(1, (attn_keys(p, q, (block + 1) * 2 * p.tpt) + kAttnKeys - 1) / kAttnKeys);
+}
+__device__ __forceinline__ int attn_blocks(const AttnParams& p, const AttnRequest& q) { return (q.T + 2 * p.tpt - 1) / (2 * p.tpt); }
+// What a key head of a request adds to the work that is cut: its tiles (p.whole: its items).
+__device__ __forceinline__ long long attn_head_work(const AttnParams& p, const AttnRequest& q) {
+    long long n = 0;
+    const int blocks = attn_blocks(p, q);
+    if (p.whole) return blocks;
+    if (p.mask) return blocks > 0 ? (long long)blocks * attn_tiles(p, q, 0) : 0;
+    for (int i = 0; i < blocks; ++i) n += attn_tiles(p, q, i);
+    return n;
+}
+// Run c of C over W tiles.
+__device__ __forceinline__ long long attn_run(long long W, int C, int c) { return W * c / C; }
+
+// A CTA's way through its run, item by item.  Every role makes it for itself.
+struct AttnWalk {
+    int b, h, block;                         // the item
+    int t0, t1, tiles;                       // the CTA's tiles of it; all of them
+    long long left;                          // tiles (p.whole: items) of the run from t0 on
+    AttnRequest q;
+    int n_blocks;
+    int tok0, ntok;                          // the block's first token and their number
+    int keys;                                // positions of the item
+    bool dual;
+
+    __device__ __forceinline__ void place(const AttnParams& p) {
+        tok0 = block * 2 * p.tpt;
+        ntok = min(2 * p.tpt, q.T - tok0);
+        keys = attn_keys(p, q, tok0 + ntok);
+        tiles = attn_tiles(p, q, block);
+        dual = ntok > p.tpt;
+        t1 = p.whole ? tiles : (int)min((long long)tiles, t0 + left);
+    }
+    // b0: the request the run begins in, skip: tiles (items) of it that come before
+    __device__ __forceinline__ void begin(const AttnParams& p, int b0, long long skip, long long length) {
+        left = length;
+        if (left <= 0) return;
+        b = b0;
+        q = attn_request(p, b);
+        n_blocks = attn_blocks(p, q);
+        const long long per_head = attn_head_work(p, q);
+        h = (int)(skip / per_head);
+        skip -= h * per_head;
+        for (block = 0; block < n_blocks; ++block) {
+            const int n = p.whole ? 1 : attn_tiles(p, q, block);
+            if (skip < n) break;
+            skip -= n;
+        }
+        t0 = (int)skip;
+        place(p);
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ void next(const AttnParams& p) {
+        left -= p.whole ? 1 : t1 - t0;
+        if (left <= 0) return;
+        t0 = 0;
+        if (++block == n_blocks) {
+            block = 0;
+            if (++h == p.Hkv) {
+                h = 0;
+                do {
+                    ++b;
+                    q = attn_request(p, b);
+                } while (q.T <= 0 && b + 1 < p.B);
+                n_blocks = attn_blocks(p, q);
+            }
+        }
+        place(p);
+    }
+    // half-steps: products of one stream with one tile
+    __device__ __forceinline__ int steps() const { return (t1 - t0) << (dual ? 1 : 0); }
+    // whether some row may not attend some position of tile j
+    __device__ __forceinline__ bool masked(const AttnParams& p, int j) const {
+        return (long long)(j + 1) * kAttnKeys > min((long long)keys, (long long)q.L + (p.mask ? 0 : tok0 + 1));
+    }
+    // places of K(t0 + j) and V(t0 + j) in the order of loads: K0, K1, V0, K2, V1, ..., the last V
+    __device__ __forceinline__ uint32_t k_at(int j) const { return j == 0 ? 0u : 2u * j - 1u; }
+    __device__ __forceinline__ uint32_t v_at(int j) const { return j + 1 < t1 - t0 ? 2u * j + 2u : 2u * j + 1u; }
+};
+
+// Bits of the 32 positions from lens + u0 on that a token attends (u0 may be negative: earlier positions).
+__device__ __forceinline__ uint32_t attn_bits(const int32_t* row, int words, int t, int T, int u0) {
+    if (u0 <= -32) return 0xFFFFFFFFu;
+    const int up = u0 < 0 ? -u0 : 0;         // that many earlier positions come first
+    const int u = u0 + up;                   // >= 0
+    uint32_t bits;
+    if (row) {
+        const int w = u >> 5, s = u & 31;
+        const uint32_t lo = w < words ? (uint32_t)row[w] : 0u, hi = w + 1 < words ? (uint32_t)row[w + 1] : 0u;
+        bits = __funnelshift_r(lo, hi, s);
+        const int n = T - u;
+        bits &= n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+    } else {
+        const int n = t + 1 - u;
+        bits = n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+    }
+    return up ? bits << up | ((1u << up) - 1u) : bits;
+}
+
+struct AttnMaps {
+    CUtensorMap q, k, v;
+};
+
+struct AttnShared {
+    float2 ms[2][128];                       // (m, l) of the streams' rows, where one item has both
+    long long scan[kAttnThreads / 32];
+    long long start_skip;
+    int start_b;
+    uint32_t tmem;
+    int abort;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnParams p) {
+    constexpr uint32_t kTile = kAttnKeys * D * 2;            // bytes of a K or V tile: D / 64 blocks of 128 positions x 128 bytes
+    constexpr uint32_t kBlock = kAttnKeys * 128;
+    // D fp32, A and B bf16; S: 128 columns, both K-major; O: D columns, V with its columns fastest
+    constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnKeys >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    constexpr uint32_t kIdescO = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+
+    // q's two slots, the ring, then what AttnShared and the barriers take.  No static part, so that the whole begins at a multiple of 1024.
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem);
+    AttnShared& sh = *reinterpret_cast<AttnShared*>(smem + p.shared_off);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t ST = (uint32_t)p.n_stages;
+    const uint32_t q_smem = base, ring = base + 2u * p.q_slot;
+    const uint32_t bars = base + p.bar_off;
+    const uint32_t kv_full = bars, kv_empty = kv_full + 8u * ST, v_clean = kv_empty + 8u * ST;
+    const uint32_t q_full = v_clean + 8u * ST, q_empty = q_full + 16u, s_full = q_empty + 16u, p_full = s_full + 16u;
+    const uint32_t o_full = p_full + 16u, drain = o_full + 8u;
+    volatile int* abort_flag = &sh.abort;
+
+    if (tid == 0) {
+        for (uint32_t s = 0; s < ST; ++s) {
+            mbar_init(kv_full + 8u * s, 1);
+            mbar_init(kv_empty + 8u * s, 2);                 // the last product that reads it, and the cleaner
+            mbar_init(v_clean + 8u * s, 1);
+        }
+        for (uint32_t s = 0; s < 2; ++s) {
+            mbar_init(q_full + 8u * s, 1);
+            mbar_init(q_empty + 8u * s, 1);
+            mbar_init(s_full + 8u * s, 1);
+            mbar_init(p_full + 8u * s, 4);
+        }
+        mbar_init(o_full, 1);
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        sh.start_b = 0;
+        sh.start_skip = 0;
+        fence_mbar_init();
+    }
+    if (warp == kAttnProducer && lane < 3)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &maps.q : lane == 1 ? &maps.k : &maps.v) : "memory");
+    if (warp == kAttnIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_proxy_async();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    grid_dependency_wait();
+    if (tid == 0) grid_launch_dependents();
+
+    // ---- this CTA's run: tiles [g0, g1) of W, which begins at tile sh.start_skip of request sh.start_b
+    const int cta = (int)blockIdx.x;
+    int C = (int)gridDim.x;
+    long long W = 0, g0 = 0, g1 = 0, w_first = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+        long long before = 0;
+        for (int b0 = 0; b0 < p.B; b0 += kAttnThreads) {
+            long long w = w_first;
+            if ((pass == 0 || b0 > 0) && b0 + tid < p.B) {
+                const AttnRequest q = attn_request(p, b0 + tid);
+                w = attn_head_work(p, q) * p.Hkv;
+            } else if (b0 + tid >= p.B) {
+                w = 0;
+            }
+            if (pass == 0 && b0 == 0) w_first = w;
+            long long incl = w;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            if (lane == 31) sh.scan[warp] = incl;
+            __syncthreads();
+            long long ahead = before, all = before;
+            for (int i = 0; i < kAttnThreads / 32; ++i) {
+                if (i < warp) ahead += sh.scan[i];
+                all += sh.scan[i];
+            }
+            if (pass == 1) {
+                const long long at = ahead + incl - w;
+                if (g1 > g0 && at <= g0 && g0 < at + w) {
+                    sh.start_b = b0 + tid;
+                    sh.start_skip = g0 - at;
+                }
+            }
+            before = all;
+            __syncthreads();
+        }
+        if (pass == 0) {
+            W = before;
+            C = (int)min((long long)C, W);                   // no empty runs among them
+            if (cta < C) {
+                g0 = attn_run(W, C, cta);
+                g1 = attn_run(W, C, cta + 1);
+            }
+        }
+    }
+    AttnWalk first;
+    first.left = 0;
+    if (g1 > g0) first.begin(p, sh.start_b, sh.start_skip, g1 - g0);
+
+    auto fail = [&]() {
+        *abort_flag = 1;
+        atomicOr(&p.hdr->status, kStatusTimeout);
+    };
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        if (__all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, p.wait_ns))) return true;
+        fail();
+        return false;
+    };
+
+    uint32_t loads = 0;                                      // ring places used so far (by the items before)
+    uint32_t q_n = 0;                                        // q slots used so far
+    if (warp == kAttnProducer) {
+        // ---------------------------------------------------------------- producer
+        bool ok = true;
+        const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
+        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
+            const int n = w.t1 - w.t0, keys = w.keys;
+            // rows of q
+            for (int s = 0; s < (w.dual ? 2 : 1) && ok; ++s, ++q_n) {
+                const uint32_t slot = q_n & 1u, turn = q_n >> 1;
+                if (turn > 0 && !wait(q_empty + 8u * slot, (turn - 1u) & 1u)) { ok = false; break; }
+                if (attn_elect()) {
+                    const uint32_t bar = q_full + 8u * slot, to = q_smem + slot * p.q_slot;
+                    mbar_arrive_expect_tx(bar, p.q_tx + p.withheld);
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c)
+                        tma_load_3d(to + c * p.q_block, &maps.q, c * 64, w.h * p.G, w.q.first + w.tok0 + s * p.tpt, bar);
+                }
+                __syncwarp();
+            }
+            // a lane per box: column block lane / np, page lane % np of the tile; pages of the tile after next are looked up ahead
+            const int col = lane / np, pg = lane - col * np;
+            const bool mine = col < D / 64;
+            auto page_of = [&](int j) -> int {
+                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
+                if (j >= n || !mine || at >= keys) return -1;
+                return p.page_table[w.b * p.table_stride + (unsigned)at / (unsigned)p.page_size];
+            };
+            auto load = [&](const CUtensorMap* map, int j, int page, uint32_t place) -> bool {
+                const uint32_t s = place % ST, turn = place / ST;
+                if (turn > 0 && !wait(kv_empty + 8u * s, (turn - 1u) & 1u)) return false;
+                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
+                const bool there = mine && at < keys;
+                const uint32_t boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
+                if (lane == 0) mbar_arrive_expect_tx(kv_full + 8u * s, boxes * p.page_tx + p.withheld);
+                __syncwarp();
+                if (there) tma_load_4d(ring + s * kTile + col * kBlock + (uint32_t)(pg * pr) * 128u, map, col * 64, (int)((unsigned)at % (unsigned)p.page_size), w.h, page, kv_full + 8u * s);
+                __syncwarp();
+                return true;
+            };
+            int page0 = page_of(0), page1 = page_of(1);
+            bool bad = false;
+            ok = ok && load(&maps.k, 0, page0, loads + w.k_at(0));
+            for (int j = 0; j < n && ok; ++j) {
+                const int page2 = page_of(j + 2);
+                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
+                bad |= mine && at < keys && (unsigned)page0 >= (unsigned)p.n_pages;
+                if (j + 1 < n) ok = load(&maps.k, j + 1, page1, loads + w.k_at(j + 1));
+                ok = ok && load(&maps.v, j, page0, loads + w.v_at(j));
+                page0 = page1;
+                page1 = page2;
+                if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) ok = false;
+            }
+            if (bad) atomicOr(&p.hdr->status, kStatusPage);
+            loads += 2u * n;
+        }
+    } else if (warp == kAttnIssuer) {
+        // ---------------------------------------------------------------- MMA issuer
+        bool ok = true;
+        uint32_t p_phase = 0, clean_phase = 0;               // bit s: parity of stream s (of a ring stage)
+        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
+            const int n = w.t1 - w.t0, H = w.steps();
+            auto product_s = [&](int i) -> bool {
+                const int s = i & 1, j = w.dual ? i >> 1 : i;
+                const uint32_t place = loads + w.k_at(j), st = place % ST;
+                const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), slot = qn & 1u;
+                if (j == 0 && (w.dual || i == 0) && !wait(q_full + 8u * slot, (qn >> 1) & 1u)) return false;
+                if ((!w.dual || s == 0) && !wait(kv_full + 8u * st, (place / ST) & 1u)) return false;
+                tc_fence_after();
+                if (attn_elect()) {
+                    const uint64_t a = smem_desc_sw128(q_smem + slot * p.q_slot), bd = smem_desc_sw128(ring + st * kTile);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
+                                    bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), kIdescS, k > 0 ? 1u : 0u);
+                    if (!w.dual || s == 1) tc_commit(kv_empty + 8u * st);
+                    tc_commit(s_full + 8u * s);
+                    if (w.dual ? j == n - 1 : i == H - 1) tc_commit(q_empty + 8u * slot);
+                }
+                __syncwarp();
+                return true;
+            };
+            ok = product_s(0);
+            if (ok && H > 1) ok = product_s(1);
+            for (int i = 0; i < H && ok; ++i) {
+                const int s = i & 1, j = w.dual ? i >> 1 : i;
+                const uint32_t place = loads + w.v_at(j), st = place % ST;
+                if (!w.dual || s == 0) {
+                    if (!wait(kv_full + 8u * st, (place / ST) & 1u)) { ok = false; break; }
+                    if (w.masked(p, w.t0 + j)) {
+                        if (!wait(v_clean + 8u * st, clean_phase >> st & 1u)) { ok = false; break; }
+                        clean_phase ^= 1u << st;
+                    }
+                }
+                if (!wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
+                p_phase ^= 1u << s;
+                if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) { ok = false; break; }
+                tc_fence_after();
+                if (attn_elect()) {
+                    const uint64_t bd = attn_v_desc(ring + st * kTile);
+#pragma unroll
+                    for (int k = 0; k < kAttnKeys / 16; ++k)
+                        tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
+                                       i >= 2 || k > 0 ? 1u : 0u);
+                    if (!w.dual || s == 1) tc_commit(kv_empty + 8u * st);
+                    if (i == H - 1) tc_commit(o_full);
+                }
+                __syncwarp();
+                if (i + 2 < H) ok = product_s(i + 2);
+            }
+            loads += 2u * n;
+            q_n += w.dual ? 2u : 1u;
+        }
+    } else if (warp == kAttnCleaner) {
+        // ---------------------------------------------------------------- cleaner
+        bool ok = true;
+        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
+            const int n = w.t1 - w.t0;
+            for (uint32_t e = 0; e < 2u * n; ++e) {          // every place, in order: it is in no phase but the next
+                const uint32_t place = loads + e, st = place % ST;
+                if (!wait(kv_full + 8u * st, (place / ST) & 1u)) { ok = false; break; }
+                const int j = e == 2u * n - 1u ? n - 1 : (int)(e >> 1) - 1;      // of V, if it is one
+                if (e > 0 && e == w.v_at(j) && w.masked(p, w.t0 + j)) {
+                    // positions all rows attend stay as they are
+                    const int r0 = max(0, min(kAttnKeys, w.q.L - (w.t0 + j) * kAttnKeys));
+                    for (int c = 0; c < D / 64; ++c) {
+#pragma unroll 4
+                        for (int i = r0 * 8 + lane; i < kAttnKeys * 8; i += 32) {
+                            uint4* u = reinterpret_cast<uint4*>(smem + (ring - base) + st * kTile + c * kBlock + i * 16);
+                            uint4 x = *u;
+                            uint32_t* y = reinterpret_cast<uint32_t*>(&x);
+                            bool some = false;
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                if ((y[g] & 0x7F800000u) == 0x7F800000u) { y[g] = (y[g] & 0x8000FFFFu) | 0x7F7F0000u; some = true; }
+                                if ((y[g] & 0x00007F80u) == 0x00007F80u) { y[g] = (y[g] & 0xFFFF8000u) | 0x00007F7Fu; some = true; }
+                            }
+                            if (some) *u = x;
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(v_clean + 8u * st);
+                }
+                if (lane == 0) mbar_arrive(kv_empty + 8u * st);
+            }
+            loads += 2u * n;
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax, and the end of an item
+        // A warp whose wait has run out goes on through the same barriers without waiting, touching nothing.
+        const int s = warp >> 2, quad = warp & 3;
+        const int r = quad * 32 + lane;                      // the thread's lane of its stream's tiles
+        const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
+        const uint32_t t_s = tmem + kAttnTmemS + 128u * s + lane_at, t_o = tmem + kAttnTmemO + 128u * s + lane_at;
+        bool ok = true;
+        uint32_t s_phase = 0, item = 0;
+        for (AttnWalk w = first; w.more(); w.next(p), ++item) {
+            const int H = w.steps();
+            const int tile_tokens = w.dual ? (s ? w.ntok - p.tpt : p.tpt) : w.ntok;
+            const int rows = tile_tokens * p.G;              // of this stream's tile
+            const bool real = r < rows, busy = quad * 32 < rows;
+            const int t = w.tok0 + (w.dual ? s * p.tpt : 0) + (real ? r / p.G : 0);      // the row's token within its request
+            float m = -INFINITY, l = 0.0f;
+            for (int i = s; i < H; i += 2) {
+                if (ok) ok = wait(s_full + 8u * s, s_phase);
+                s_phase ^= 1u;
+                if (ok && busy) {
+                    tc_fence_after();
+                    const int j = w.t0 + (w.dual ? i >> 1 : i);
+                    uint32_t x[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tc_ld32(t_s + 32u * c, x[c]);
+                    tc_wait_ld();
+                    if (w.masked(p, j)) {
+                        const int32_t* row = p.mask ? p.mask + (int64_t)(w.q.first + t) * p.mask_words : nullptr;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int at = j * kAttnKeys + 32 * c;
+                            uint32_t bits = attn_bits(row, p.mask_words, t, w.q.T, at - w.q.L);
+                            const int n = w.keys - at;
+                            bits &= n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(bits >> e & 1u)) x[c][e] = 0xFF800000u;
+                        }
+                    }
+                    float top[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        top[c] = __uint_as_float(x[c][0]);
+#pragma unroll
+                        for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(x[c][e]));
+                    }
+                    const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    // (mx - m) is NaN while nothing has been attended yet
+                    const bool grow = real && mx > m && !((mx - m) * p.scale_log2 <= kAttnSlack);
+                    if (__any_sync(0xFFFFFFFFu, grow)) {
+                        const float f = grow ? ex2_approx((m - mx) * p.scale_log2) : 1.0f;
+                        if (grow) {
+                            m = mx;
+                            l *= f;
+                        }
+                        if (i >= 2) {
+#pragma unroll
+                            for (int c = 0; c < D / 32; ++c) {
+                                uint32_t o[32];
+                                tc_ld32(t_o + 32u * c, o);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tc_st32(t_o + 32u * c, o);
+                            }
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
+                    const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
+                    uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+                    for (int c = 0; c < 4; c += 2) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                float a, b;
+                                unpack2(fma2(pack2(__uint_as_float(x[c + h][e]), __uint_as_float(x[c + h][e + 1])), k2, r2), a, b);
+                                a = ex2_approx(a);
+                                b = ex2_approx(b);
+                                const uint64_t ab = pack2(a, b);
+                                if (e & 2) sum1 = add2(sum1, ab);
+                                else sum0 = add2(sum0, ab);
+                                pk[h * 16 + e / 2] = attn_bf16x2(a, b);
+                            }
+                        tc_st32(t_s + 16u * c, pk);
+                    }
+                    float a, b;
+                    unpack2(add2(sum0, sum1), a, b);
+                    l += a + b;
+                    tc_wait_st();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8u * s);
+            }
+            // ---- the item's end: a piece of it to the workspace, or its rows
+            if (ok) ok = wait(o_full, item & 1u);
+            tc_fence_after();
+            const bool both = !w.dual && H > 1;              // the streams hold different positions of the same rows
+            float f0 = 1.0f, f1 = 0.0f;                      // weights of stream 0's (of this stream's) and stream 1's O
+            if (!w.dual) {
+                sh.ms[s][r] = make_float2(m, l);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const float2 a = sh.ms[0][r], b = both ? sh.ms[1][r] : make_float2(-INFINITY, 0.0f);
+                m = fmaxf(a.x, b.x);
+                f0 = a.x == m ? 1.0f : ex2_approx((a.x - m) * p.scale_log2);
+                f1 = b.x == m ? 1.0f : ex2_approx((b.x - m) * p.scale_log2);
+                l = a.y * f0 + (both ? b.y * f1 : 0.0f);
+            }
+            if (ok && busy && (w.dual || both || s == 0)) {
+                const bool cut = w.t1 - w.t0 < w.tiles;
+                const int row = (w.dual ? s * p.tpt * p.G : 0) + r;
+                const uint32_t o_at = (w.dual ? t_o : tmem + kAttnTmemO + lane_at);
+                const int c0 = both ? s * (D / 64) : 0, c1 = both ? c0 + D / 64 : D / 32;        // runs of 32 columns
+                const float inv = cut ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+                const size_t piece = (size_t)(cta * 2 + (item == 0 ? 0 : 1));        // a run's first item, or its last
+                uint16_t* to = p.out + (int64_t)(w.q.first + t) * p.out_ts + (int64_t)(w.h * p.G + r % p.G) * p.out_hs;
+                for (int c = c0; c < c1; ++c) {
+                    __syncwarp();
+                    uint32_t o[32];
+                    tc_ld32(o_at + 32u * c, o);
+                    if (both) {
+                        uint32_t o1[32];
+                        tc_ld32(o_at + 128u + 32u * c, o1);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f0 + __uint_as_float(o1[e]) * f1);
+                    } else {
+                        tc_wait_ld();
+                    }
+                    if (!real) continue;
+                    if (cut) {
+                        float4* po = reinterpret_cast<float4*>(p.part_o) + (piece * (D / 4) + 8 * c) * p.rows_max + row;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            po[(size_t)e * p.rows_max] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]),
+                                                                     __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3]));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                v[u] = attn_bf16x2(__uint_as_float(o[e + 2 * u]) * inv, __uint_as_float(o[e + 2 * u + 1]) * inv);
+                            *reinterpret_cast<uint4*>(to + 32 * c + e) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                }
+                if (real && (w.dual || s == 0)) {
+                    if (cut) p.part_ml[piece * p.rows_max + row] = make_float2(m, l);
+                    else if (p.lse) p.lse[(int64_t)(w.q.first + t) * p.Hq + w.h * p.G + r % p.G] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+                }
+                tc_fence_before();
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");   // both streams' O and (m, l) have been read; neither is an item ahead
+        }
+    }
+
+    // ---- which item this CTA's run is the first to cut
+    if (tid == 0) {
+        AttnSplit d{};
+        if (g1 > g0 && first.t0 > 0) {
+            const long long start = g0 - first.t0, end = start + first.tiles;
+            int c0 = cta - 1;
+            while (attn_run(W, C, c0) > start) --c0;
+            if (c0 == cta - 1) {
+                int c1 = cta;
+                while (attn_run(W, C, c1 + 1) < end) ++c1;
+                d.rows = first.ntok * p.G;
+                d.token0 = first.q.first + first.tok0;
+                d.head0 = first.h * p.G;
+                d.first_cta = c0;
+                d.n_pieces = c1 - c0 + 1;
+                d.first_slot = attn_run(W, C, c0) == start ? 0 : 1;
+            }
+        }
+        if (!p.whole) p.splits[cta] = d;
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (__builtin_expect(*abort_flag != 0, 0)) {             // copies and MMAs in flight must end before their memory is given back
+        if (warp == kAttnIssuer && attn_elect()) {
+            tc_commit(drain);
+            (void)mbar_wait(drain, 0u, p.wait_ns);
+        }
+        if (warp == kAttnProducer && lane == 0) {            // longer than any copy takes
+            const unsigned long long now = global_timer_ns();
+            while (global_timer_ns() - now < 1000000ull) { }
+        }
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == kAttnIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------ joining an item's pieces
+// lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  A block takes
+// eight rows of an item at a time; which there are, each block works out from the runs' entries.
+constexpr int kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(256)
+attn_join_kernel(const __grid_constant__ AttnParams p, int C) {
+    __shared__ int ahead[kAttnCtas + 1];
+    __shared__ AttnSplit split[kAttnCtas];
+    grid_dependency_wait();
+    if (threadIdx.x == 0) grid_launch_dependents();
+    for (int i = threadIdx.x; i < C; i += 256) split[i] = p.splits[i];
+    __syncthreads();
+    if (threadIdx.x < 32) {                                  // running number of row groups
+        int before = 0;
+        for (int i = threadIdx.x; i - (int)threadIdx.x < C; i += 32) {
+            const int n = i < C ? (split[i].rows + kJoinRows - 1) / kJoinRows : 0;
+            int incl = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+                if ((int)threadIdx.x >= o) incl += v;
+            }
+            if (i < C) ahead[i] = before + incl - n;
+            before += __shfl_sync(0xFFFFFFFFu, incl, 31);
+        }
+        if (threadIdx.x == 0) ahead[C] = before;
+    }
+    __syncthreads();
+    const int all = ahead[C];
+    constexpr int kQuads = D / 4;                            // runs of four columns
+    for (int unit = blockIdx.x; unit < all; unit += gridDim.x) {
+        int lo = 0, hi = C;                                  // the last entry with ahead <= unit that has rows
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (ahead[mid] <= unit) lo = mid;
+            else hi = mid;
+        }
+        const AttnSplit d = split[lo];
+        const int row = (unit - ahead[lo]) * kJoinRows + (int)(threadIdx.x % kJoinRows);
+        if (row >= d.rows) continue;
+        for (int cq = threadIdx.x / kJoinRows; cq < kQuads; cq += 256 / kJoinRows) {
+            auto piece = [&](int i) { return (size_t)((d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0)); };
+            float m = -INFINITY;
+            for (int i = 0; i < d.n_pieces; ++i) m = fmaxf(m, p.part_ml[piece(i) * p.rows_max + row].x);
+            float l = 0.0f;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+            for (int i = 0; i < d.n_pieces; ++i) {
+                const float2 ml = p.part_ml[piece(i) * p.rows_max + row];
+                const float f = ml.x == m ? 1.0f : ex2_approx((ml.x - m) * p.scale_log2);
+                const float4 v = reinterpret_cast<const float4*>(p.part_o)[(piece(i) * kQuads + cq) * p.rows_max + row];
+                l += ml.y * f;
+                o.x += v.x * f;
+                o.y += v.y * f;
+                o.z += v.z * f;
+                o.w += v.w * f;
+            }
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int token = d.token0 + row / p.G, head = d.head0 + row % p.G;
+            *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq) =
+                make_uint2(attn_bf16x2(o.x * inv, o.y * inv), attn_bf16x2(o.z * inv, o.w * inv));
+            if (cq == 0 && p.lse) p.lse[(int64_t)token * p.Hq + head] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+        }
+    }
+}
+
+#endif  // __CUDACC__
+
+// ------------------------------------------------------------------------------------------ host
+static int attn_rows(int Hq, int heads, int max_tokens) {    // of a block, at most
+    const int G = Hq / heads, tpt = 128 / G;
+    return std::min(2 * tpt, max_tokens) * G;
+}
+struct AttnLayout {
+    size_t splits, ml, o, total;
+};
+static AttnLayout attn_layout(int Hq, int heads, int D, int max_tokens) {
+    const size_t rows = (size_t)attn_rows(Hq, heads, max_tokens), pieces = 2 * kAttnCtas;
+    AttnLayout a;
+    a.splits = kHeaderBytes;
+    a.ml = (a.splits + kAttnCtas * sizeof(AttnSplit) + 255) / 256 * 256;
+    a.o = (a.ml + pieces * rows * sizeof(float2) + 255) / 256 * 256;
+    a.total = (a.o + pieces * rows * D * sizeof(float) + 255) / 256 * 256;
+    return a;
+}
+size_t attn_workspace_bytes(int Hq, int heads, int D, int max_tokens) { return attn_layout(Hq, heads, D, max_tokens).total; }
+
+// (defined beside make_tensor_map_bf16)
+vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+
+static vt_status cache_map(CUtensorMap* map, const void* ptr, const vt_cache& a, int64_t token, int64_t head, int64_t page) {
+    const uint64_t dims[4] = {(uint64_t)a.head_dim, (uint64_t)a.page_size, (uint64_t)a.heads, (uint64_t)a.n_pages};
+    const uint64_t strides[3] = {(uint64_t)token * 2, (uint64_t)head * 2, (uint64_t)page * 2};
+    const uint32_t box[4] = {(uint32_t)kBoxK, (uint32_t)std::min(a.page_size, kAttnKeys), 1, 1};
+    return make_tensor_map_bf16_nd(map, ptr, 4, dims, strides, box);
+}
+
+template <int D>
+static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint32_t smem, cudaStream_t st) {
+    static std::atomic<unsigned long long> configured{0};
+    if (vt_status r = ensure_max_dyn_smem(reinterpret_cast<const void*>(attn_kernel<D>), kMaxDynSmem, &configured); r != VT_OK) return r;
+    cudaError_t e = launch_pdl(attn_kernel<D>, C, kAttnThreads, smem, st, maps, p);
+    count_launch();
+    if (e == cudaSuccess && !p.whole) {
+        e = launch_pdl(attn_join_kernel<D>, 2 * C, 256, 0, st, p, C);
+        count_launch();
+    }
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? VT_OK : cuda_fail(e);
+}
+
+vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
+    const vt_cache& a = *c.cache;
+    const int D = a.head_dim;
+    int sms = 0;
+    if (vt_status r = device_sm_count(&sms); r != VT_OK) return r;
+    const int C = std::min(sms, kAttnCtas);
+    AttnParams p{};
+    p.cu = c.cu_tokens;
+    p.lens = a.lens;
+    p.page_table = a.page_table;
+    p.table_stride = a.table_stride;
+    p.mask = c.mask;
+    p.mask_words = c.mask_words;
+    p.out = reinterpret_cast<uint16_t*>(c.out.ptr);
+    p.out_ts = c.out.token_stride;
+    p.out_hs = c.out.head_stride;
+    p.lse = c.lse;
+    const AttnLayout lay = attn_layout(c.Hq, a.heads, D, c.max_tokens);
+    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+    p.hdr = reinterpret_cast<WsHeader*>(ws);
+    p.splits = reinterpret_cast<AttnSplit*>(ws + lay.splits);
+    p.part_ml = reinterpret_cast<float2*>(ws + lay.ml);
+    p.part_o = reinterpret_cast<float*>(ws + lay.o);
+    p.rows_max = attn_rows(c.Hq, a.heads, c.max_tokens);
+    p.N = c.N;
+    p.B = a.B;
+    p.Hq = c.Hq;
+    p.Hkv = a.heads;
+    p.G = c.Hq / a.heads;
+    p.max_tokens = c.max_tokens;
+    p.n_pages = a.n_pages;
+    p.page_size = a.page_size;
+    p.max_pages = a.max_pages;
+    p.tpt = 128 / p.G;
+    p.box_tokens = std::min(p.tpt, c.max_tokens);
+    p.whole = (long long)a.max_pages * a.page_size <= (long long)kAttnWhole * kAttnKeys;
+    p.scale = c.scale;
+    p.scale_log2 = c.scale * kLog2e;
+    p.wait_ns = kWaitLimitNs;
+    if (const int us = gemm_withheld_us(); us > 0) {         // a test of the unwinding: copies fall 16 bytes short
+        p.withheld = 16;
+        p.wait_ns = (unsigned long long)us * 1000ull;
+    }
+    const uint32_t rows = (uint32_t)(p.box_tokens * p.G);
+    p.q_block = (rows + 7) / 8 * 1024;
+    p.q_slot = p.q_block * (D / 64);
+    p.q_tx = rows * 128u * (D / 64);
+    p.page_tx = (uint32_t)std::min(p.page_size, kAttnKeys) * 128u;
+    // five stages of 32 KB beside two full row tiles: 160 KB in flight
+    const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 10);
+    p.n_stages = (int)std::min((uint32_t)kAttnMaxStages, ((uint32_t)kMaxDynSmem - tail - 2 * p.q_slot) / tile);
+    p.shared_off = 2 * p.q_slot + p.n_stages * tile;
+    p.bar_off = p.shared_off + sizeof(AttnShared);
+    const uint32_t smem = p.shared_off + tail;
+    AttnMaps maps;
+    {
+        const uint64_t dims[3] = {(uint64_t)D, (uint64_t)c.Hq, (uint64_t)c.N};
+        const uint64_t strides[2] = {(uint64_t)c.q.head_stride * 2, (uint64_t)c.q.token_stride * 2};
+        const uint32_t box[3] = {(uint32_t)kBoxK, (uint32_t)p.G, (uint32_t)p.box_tokens};
+        if (vt_status r = make_tensor_map_bf16_nd(&maps.q, c.q.ptr, 3, dims, strides, box); r != VT_OK) return r;
+    }
+    if (vt_status r = cache_map(&maps.k, a.k, a, a.k_token_stride, a.k_head_stride, a.k_page_stride); r != VT_OK) return r;
+    if (vt_status r = cache_map(&maps.v, a.v, a, a.v_token_stride, a.v_head_stride, a.v_page_stride); r != VT_OK) return r;
+    return D == 64 ? run_attn<64>(maps, p, C, smem, st) : run_attn<128>(maps, p, C, smem, st);
+}
+
+}  // namespace vt

@@ -393,6 +393,24 @@ vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, i
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return cr == CUDA_SUCCESS ? VT_OK : driver_fail((int)cr);
 }
+// bf16 tensor of up to five dimensions, the first running fastest; strides in bytes, of the others; the box is kBoxK elements of the first.
+vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+    EncodeTiledFn enc;
+    vt_status r = get_encode(&enc);
+    if (r != VT_OK) return r;
+    cuuint64_t d[5], st[4];
+    cuuint32_t bx[5], elem[5];
+    for (int i = 0; i < rank; ++i) {
+        d[i] = dims[i];
+        if (i > 0) st[i - 1] = strides[i - 1];
+        bx[i] = box[i];
+        elem[i] = 1;
+    }
+    CUresult cr = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(ptr), d, st, bx, elem,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return cr == CUDA_SUCCESS ? VT_OK : driver_fail((int)cr);
+}
 vt_status make_tensor_map_bf16(CUtensorMap* map, const void* ptr, int rows, int d, int box_rows) {
     return make_tensor_map_bf16_ld(map, ptr, rows, d, d, box_rows);
 }
