@@ -19,8 +19,8 @@
 // O is rescaled only when a row's maximum grows by more than 2^8 over the one in use (P then stays below 2^8, its sum in fp32): the
 // rescale, done by the stream's own warps, is rare after the first tiles.
 //
-// Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (and the end of an item), warp 8 TMA producer, warp 9 MMA issuer, warp 10 the cleaner: in
-// tiles where something is masked it turns infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
+// Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (and the end of an item), warp 8 TMA producer, warp 9 MMA issuer,
+// warp 10 the cleaner: in tiles where something is masked it turns infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
 // All waits are bounded; one that runs out sets the status word and every role leaves.
 #include "vt_step.h"
 #include "vt_tc.cuh"
@@ -31,10 +31,12 @@ int gemm_withheld_us();                      // see vt_test_withhold_copies
 
 constexpr int kAttnKeys = 128;               // positions per tile
 constexpr int kAttnThreads = 11 * 32;
-constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10;
+constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10;       
+constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
 constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
 constexpr int kAttnMaxStages = 12;
+constexpr int kAttnItemCost = 2;             // what an item's beginning and end cost, in tiles
 constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
 constexpr uint32_t kAttnTmemO = 0, kAttnTmemS = 256;
 
@@ -61,7 +63,10 @@ struct AttnParams {
     int tpt;                                 // tokens per row tile
     int box_tokens;                          // tokens in a box of q
     int whole;                               // 1: items are not cut
+    int min_run;                             // the least weight of a CTA's run
+    int ctas;
     int n_stages;
+    uint32_t stages_inv;                     // 2^32 / n_stages, rounded up
     uint32_t q_block, q_slot;                // bytes of 64 columns of a row tile; of a row tile
     uint32_t q_tx, page_tx;                  // bytes of a q tile; of one box of keys
     uint32_t shared_off, bar_off, withheld;              // withheld: see vt_test_withhold_copies
@@ -87,6 +92,9 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32])
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[64]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -131,10 +139,35 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ uint32_t attn_bf16x2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// mbar_wait in few instructions.  The kernel's roles each run their code a handful of times in a short call, so its size is latency: the
+// first version, 167 KB with everything unrolled, spent more cycles on fetching instructions than on a short item.
+__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+    unsigned long long t0 = 0;
+    uint32_t spins = 0;
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity)) {
+        if ((++spins & 0xFFu) == 0) {
+            const unsigned long long now = global_timer_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > limit_ns) return false;
+        }
+    }
+    return true;
+}
+// n / d for n < 2^31 d.
+__device__ __noinline__ long long attn_div(long long n, long long d) {
+    return (n | d) <= 0xFFFFFFFFll ? (long long)((uint32_t)n / (uint32_t)d) : n / d;
 }
 
 // ------------------------------------------------------------------------------------------ the cut
@@ -155,86 +188,51 @@ __device__ __forceinline__ int attn_keys(const AttnParams& p, const AttnRequest&
     const long long cap = (long long)p.max_pages * p.page_size;
     return (int)min((long long)q.L + (p.mask ? q.T : min(q.T, t_end)), cap);
 }
-__device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnRequest& q, int block) {
-    return max(1, (attn_keys(p, q, (block + 1) * 2 * p.tpt) + kAttnKeys - 1) / kAttnKeys);
-}
+__device__ __forceinline__ int attn_tiles(int keys) { return max(1, (keys + kAttnKeys - 1) / kAttnKeys); }
 __device__ __forceinline__ int attn_blocks(const AttnParams& p, const AttnRequest& q) { return (q.T + 2 * p.tpt - 1) / (2 * p.tpt); }
-// What a key head of a request adds to the work that is cut: its tiles (p.whole: its items).
-__device__ __forceinline__ long long attn_head_work(const AttnParams& p, const AttnRequest& q) {
-    long long n = 0;
+// What a key head of a request weighs: its items' tiles, and kAttnItemCost for each item.
+__device__ __forceinline__ long long attn_head_weight(const AttnParams& p, const AttnRequest& q) {
     const int blocks = attn_blocks(p, q);
-    if (p.whole) return blocks;
-    if (p.mask) return blocks > 0 ? (long long)blocks * attn_tiles(p, q, 0) : 0;
-    for (int i = 0; i < blocks; ++i) n += attn_tiles(p, q, i);
+    long long n = (long long)blocks * kAttnItemCost;
+    if (p.mask) return blocks > 0 ? n + (long long)blocks * attn_tiles(attn_keys(p, q, q.T)) : 0;
+#pragma unroll 1
+    for (int i = 0; i < blocks; ++i) n += attn_tiles(attn_keys(p, q, (i + 1) * 2 * p.tpt));
     return n;
 }
-// Run c of C over W tiles.
-__device__ __forceinline__ long long attn_run(long long W, int C, int c) { return W * c / C; }
+// W units in C runs, the first `more` of them a unit longer than the others.
+struct AttnCut {
+    long long base, more;
+    __device__ __forceinline__ AttnCut(long long W, int C) {
+        base = attn_div(W, C);
+        more = W - base * C;
+    }
+    __device__ __forceinline__ long long start(int c) const { return base * c + min((long long)c, more); }
+    __device__ __forceinline__ int of(long long g) const {       // the run that unit g lies in
+        const long long at = more * (base + 1);
+        const long long n = g < at ? g : g - at, d = g < at ? base + 1 : base;
+        return (int)((g < at ? 0 : more) + attn_div(n, d));
+    }
+};
 
-// A CTA's way through its run, item by item.  Every role makes it for itself.
-struct AttnWalk {
-    int b, h, block;                         // the item
-    int t0, t1, tiles;                       // the CTA's tiles of it; all of them
-    long long left;                          // tiles (p.whole: items) of the run from t0 on
-    AttnRequest q;
-    int n_blocks;
-    int tok0, ntok;                          // the block's first token and their number
-    int keys;                                // positions of the item
-    bool dual;
+// What a CTA does of one item; the planner's message to the other roles.
+struct __align__(16) AttnPiece {
+    int n;                                   // key tiles; 0: nothing more
+    int b, h, t0;                            // request, key head, first tile
+    int keys, open;                          // positions of the item; tiles from `open` on hold some that some row may not attend
+    int L, T, first;                         // of the request: earlier positions, tokens, first token
+    int tok0, ntok;                          // the block's tokens
+    int dual;                                // two row tiles
+    int cut;                                 // others have pieces of the item, too
+    int slot;                                // in the workspace: 0 for the item the CTA's run begins in, 1 for the one it ends in
+    int pad[2];
 
-    __device__ __forceinline__ void place(const AttnParams& p) {
-        tok0 = block * 2 * p.tpt;
-        ntok = min(2 * p.tpt, q.T - tok0);
-        keys = attn_keys(p, q, tok0 + ntok);
-        tiles = attn_tiles(p, q, block);
-        dual = ntok > p.tpt;
-        t1 = p.whole ? tiles : (int)min((long long)tiles, t0 + left);
-    }
-    // b0: the request the run begins in, skip: tiles (items) of it that come before
-    __device__ __forceinline__ void begin(const AttnParams& p, int b0, long long skip, long long length) {
-        left = length;
-        if (left <= 0) return;
-        b = b0;
-        q = attn_request(p, b);
-        n_blocks = attn_blocks(p, q);
-        const long long per_head = attn_head_work(p, q);
-        h = (int)(skip / per_head);
-        skip -= h * per_head;
-        for (block = 0; block < n_blocks; ++block) {
-            const int n = p.whole ? 1 : attn_tiles(p, q, block);
-            if (skip < n) break;
-            skip -= n;
-        }
-        t0 = (int)skip;
-        place(p);
-    }
-    __device__ __forceinline__ bool more() const { return left > 0; }
-    __device__ __forceinline__ void next(const AttnParams& p) {
-        left -= p.whole ? 1 : t1 - t0;
-        if (left <= 0) return;
-        t0 = 0;
-        if (++block == n_blocks) {
-            block = 0;
-            if (++h == p.Hkv) {
-                h = 0;
-                do {
-                    ++b;
-                    q = attn_request(p, b);
-                } while (q.T <= 0 && b + 1 < p.B);
-                n_blocks = attn_blocks(p, q);
-            }
-        }
-        place(p);
-    }
     // half-steps: products of one stream with one tile
-    __device__ __forceinline__ int steps() const { return (t1 - t0) << (dual ? 1 : 0); }
-    // whether some row may not attend some position of tile j
-    __device__ __forceinline__ bool masked(const AttnParams& p, int j) const {
-        return (long long)(j + 1) * kAttnKeys > min((long long)keys, (long long)q.L + (p.mask ? 0 : tok0 + 1));
-    }
+    __device__ __forceinline__ int steps() const { return n << dual; }
     // places of K(t0 + j) and V(t0 + j) in the order of loads: K0, K1, V0, K2, V1, ..., the last V
     __device__ __forceinline__ uint32_t k_at(int j) const { return j == 0 ? 0u : 2u * j - 1u; }
-    __device__ __forceinline__ uint32_t v_at(int j) const { return j + 1 < t1 - t0 ? 2u * j + 2u : 2u * j + 1u; }
+    __device__ __forceinline__ uint32_t v_at(int j) const { return j + 1 < n ? 2u * j + 2u : 2u * j + 1u; }
+    // the j that place e holds V(t0 + j) of; -1 where it holds K((e + 1) / 2)
+    __device__ __forceinline__ int value_at(uint32_t e) const { return e + 1u == 2u * n ? n - 1 : e & 1u ? -1 : (int)(e >> 1) - 1; }
 };
 
 // Bits of the 32 positions from lens + u0 on that a token attends (u0 may be negative: earlier positions).
@@ -259,12 +257,9 @@ __device__ __forceinline__ uint32_t attn_bits(const int32_t* row, int words, int
 struct AttnMaps {
     CUtensorMap q, k, v;
 };
-
 struct AttnShared {
+    AttnPiece piece[kAttnPieces];
     float2 ms[2][128];                       // (m, l) of the streams' rows, where one item has both
-    long long scan[kAttnThreads / 32];
-    long long start_skip;
-    int start_b;
     uint32_t tmem;
     int abort;
 };
@@ -285,16 +280,16 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t ST = (uint32_t)p.n_stages;
     const uint32_t q_smem = base, ring = base + 2u * p.q_slot;
-    const uint32_t bars = base + p.bar_off;
-    const uint32_t kv_full = bars, kv_empty = kv_full + 8u * ST, v_clean = kv_empty + 8u * ST;
+    const uint32_t kv_full = base + p.bar_off, kv_empty = kv_full + 8u * ST, v_clean = kv_empty + 8u * ST;
     const uint32_t q_full = v_clean + 8u * ST, q_empty = q_full + 16u, s_full = q_empty + 16u, p_full = s_full + 16u;
-    const uint32_t o_full = p_full + 16u, drain = o_full + 8u;
+    const uint32_t o_full = p_full + 16u, meet = o_full + 8u, drain = meet + 8u;
+    const uint32_t piece_full = drain + 8u, piece_empty = piece_full + 8u * kAttnPieces;
     volatile int* abort_flag = &sh.abort;
 
     if (tid == 0) {
         for (uint32_t s = 0; s < ST; ++s) {
             mbar_init(kv_full + 8u * s, 1);
-            mbar_init(kv_empty + 8u * s, 2);                 // the last product that reads it, and the cleaner
+            mbar_init(kv_empty + 8u * s, 3);                 // the products of either stream, and the cleaner
             mbar_init(v_clean + 8u * s, 1);
         }
         for (uint32_t s = 0; s < 2; ++s) {
@@ -303,11 +298,14 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             mbar_init(s_full + 8u * s, 1);
             mbar_init(p_full + 8u * s, 4);
         }
+        for (uint32_t s = 0; s < kAttnPieces; ++s) {
+            mbar_init(piece_full + 8u * s, 1);
+            mbar_init(piece_empty + 8u * s, kAttnThreads / 32 - 1);
+        }
         mbar_init(o_full, 1);
+        mbar_init(meet, 8);
         mbar_init(drain, 1);
         *abort_flag = 0;
-        sh.start_b = 0;
-        sh.start_skip = 0;
         fence_mbar_init();
     }
     if (warp == kAttnProducer && lane < 3)
@@ -324,193 +322,250 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
     grid_dependency_wait();
     if (tid == 0) grid_launch_dependents();
 
-    // ---- this CTA's run: tiles [g0, g1) of W, which begins at tile sh.start_skip of request sh.start_b
-    const int cta = (int)blockIdx.x;
-    int C = (int)gridDim.x;
-    long long W = 0, g0 = 0, g1 = 0, w_first = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-        long long before = 0;
-        for (int b0 = 0; b0 < p.B; b0 += kAttnThreads) {
-            long long w = w_first;
-            if ((pass == 0 || b0 > 0) && b0 + tid < p.B) {
-                const AttnRequest q = attn_request(p, b0 + tid);
-                w = attn_head_work(p, q) * p.Hkv;
-            } else if (b0 + tid >= p.B) {
-                w = 0;
-            }
-            if (pass == 0 && b0 == 0) w_first = w;
-            long long incl = w;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (lane == 31) sh.scan[warp] = incl;
-            __syncthreads();
-            long long ahead = before, all = before;
-            for (int i = 0; i < kAttnThreads / 32; ++i) {
-                if (i < warp) ahead += sh.scan[i];
-                all += sh.scan[i];
-            }
-            if (pass == 1) {
-                const long long at = ahead + incl - w;
-                if (g1 > g0 && at <= g0 && g0 < at + w) {
-                    sh.start_b = b0 + tid;
-                    sh.start_skip = g0 - at;
-                }
-            }
-            before = all;
-            __syncthreads();
-        }
-        if (pass == 0) {
-            W = before;
-            C = (int)min((long long)C, W);                   // no empty runs among them
-            if (cta < C) {
-                g0 = attn_run(W, C, cta);
-                g1 = attn_run(W, C, cta + 1);
-            }
-        }
-    }
-    AttnWalk first;
-    first.left = 0;
-    if (g1 > g0) first.begin(p, sh.start_b, sh.start_skip, g1 - g0);
-
-    auto fail = [&]() {
+    // A warp whose wait runs out reports it and leaves its loop; so do the others when their own waits run out.
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        if (__all_sync(0xFFFFFFFFu, attn_wait(bar, parity, p.wait_ns))) return true;
         *abort_flag = 1;
         atomicOr(&p.hdr->status, kStatusTimeout);
-    };
-    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-        if (__all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, p.wait_ns))) return true;
-        fail();
         return false;
     };
+    // ring places by number: stage and parity of the turn
+    auto turn_of = [&](uint32_t place) { return __umulhi(place, p.stages_inv); };
+    uint32_t taken = 0;
+    auto take = [&](AttnPiece& w) -> bool {
+        const uint32_t s = taken % kAttnPieces;
+        if (!wait(piece_full + 8u * s, taken / kAttnPieces & 1u)) return false;
+        ++taken;
+        w = sh.piece[s];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(piece_empty + 8u * s);
+        return w.n > 0;
+    };
 
-    uint32_t loads = 0;                                      // ring places used so far (by the items before)
-    uint32_t q_n = 0;                                        // q slots used so far
+    uint32_t loads = 0;                                      // ring places used by the pieces before
+    uint32_t q_n = 0;                                        // q slots used by them
     if (warp == kAttnProducer) {
-        // ---------------------------------------------------------------- producer
-        bool ok = true;
-        const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
-        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
-            const int n = w.t1 - w.t0, keys = w.keys;
-            // rows of q
-            for (int s = 0; s < (w.dual ? 2 : 1) && ok; ++s, ++q_n) {
-                const uint32_t slot = q_n & 1u, turn = q_n >> 1;
-                if (turn > 0 && !wait(q_empty + 8u * slot, (turn - 1u) & 1u)) { ok = false; break; }
-                if (attn_elect()) {
-                    const uint32_t bar = q_full + 8u * slot, to = q_smem + slot * p.q_slot;
-                    mbar_arrive_expect_tx(bar, p.q_tx + p.withheld);
-#pragma unroll
-                    for (int c = 0; c < D / 64; ++c)
-                        tma_load_3d(to + c * p.q_block, &maps.q, c * 64, w.h * p.G, w.q.first + w.tok0 + s * p.tpt, bar);
-                }
-                __syncwarp();
-            }
-            // a lane per box: column block lane / np, page lane % np of the tile; pages of the tile after next are looked up ahead
-            const int col = lane / np, pg = lane - col * np;
-            const bool mine = col < D / 64;
-            auto page_of = [&](int j) -> int {
-                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
-                if (j >= n || !mine || at >= keys) return -1;
-                return p.page_table[w.b * p.table_stride + (unsigned)at / (unsigned)p.page_size];
-            };
-            auto load = [&](const CUtensorMap* map, int j, int page, uint32_t place) -> bool {
-                const uint32_t s = place % ST, turn = place / ST;
-                if (turn > 0 && !wait(kv_empty + 8u * s, (turn - 1u) & 1u)) return false;
-                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
-                const bool there = mine && at < keys;
-                const uint32_t boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
-                if (lane == 0) mbar_arrive_expect_tx(kv_full + 8u * s, boxes * p.page_tx + p.withheld);
-                __syncwarp();
-                if (there) tma_load_4d(ring + s * kTile + col * kBlock + (uint32_t)(pg * pr) * 128u, map, col * 64, (int)((unsigned)at % (unsigned)p.page_size), w.h, page, kv_full + 8u * s);
-                __syncwarp();
-                return true;
-            };
-            int page0 = page_of(0), page1 = page_of(1);
-            bool bad = false;
-            ok = ok && load(&maps.k, 0, page0, loads + w.k_at(0));
-            for (int j = 0; j < n && ok; ++j) {
-                const int page2 = page_of(j + 2);
-                const int at = (w.t0 + j) * kAttnKeys + pg * pr;
-                bad |= mine && at < keys && (unsigned)page0 >= (unsigned)p.n_pages;
-                if (j + 1 < n) ok = load(&maps.k, j + 1, page1, loads + w.k_at(j + 1));
-                ok = ok && load(&maps.v, j, page0, loads + w.v_at(j));
-                page0 = page1;
-                page1 = page2;
-                if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) ok = false;
-            }
-            if (bad) atomicOr(&p.hdr->status, kStatusPage);
-            loads += 2u * n;
+        // ---------------------------------------------------------------- producer: this CTA's run, piece by piece, and the copies for it
+        const int cta = (int)blockIdx.x, per = (p.B + 31) / 32;          // requests per lane
+        const int b0 = min(lane * per, p.B), b1 = min(b0 + per, p.B);
+        long long sum = 0;
+#pragma unroll 1
+        for (int b = b0; b < b1; ++b) sum += attn_head_weight(p, attn_request(p, b)) * p.Hkv;
+        long long at = sum;
+#pragma unroll 1
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xFFFFFFFFu, at, o);
+            if (lane >= o) at += v;
         }
-    } else if (warp == kAttnIssuer) {
-        // ---------------------------------------------------------------- MMA issuer
+        const long long W = __shfl_sync(0xFFFFFFFFu, at, 31);
+        at -= sum;
+        const int C = (int)max(1ll, min((long long)gridDim.x, attn_div(W, p.min_run)));
+        const AttnCut cut(W, C);
+        const long long g0 = cta < C ? cut.start(cta) : 0, g1 = cta < C ? cut.start(cta + 1) : 0;
+        uint32_t made = 0;
+        const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
+        // a lane per box: column block lane / np, page lane % np of the tile
+        const int col = lane / np, pg = lane - col * np;
+        const bool mine = col < D / 64;
+        bool bad = false;
+        AttnSplit split{};
+        auto publish = [&](const AttnPiece& w) -> bool {
+            const uint32_t s = made % kAttnPieces, turn = made / kAttnPieces;
+            if (turn > 0 && !wait(piece_empty + 8u * s, (turn - 1u) & 1u)) return false;
+            if (lane == 0) {
+                sh.piece[s] = w;
+                mbar_arrive(piece_full + 8u * s);
+            }
+            __syncwarp();
+            ++made;
+            return true;
+        };
         bool ok = true;
-        uint32_t p_phase = 0, clean_phase = 0;               // bit s: parity of stream s (of a ring stage)
-        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
-            const int n = w.t1 - w.t0, H = w.steps();
-            auto product_s = [&](int i) -> bool {
-                const int s = i & 1, j = w.dual ? i >> 1 : i;
-                const uint32_t place = loads + w.k_at(j), st = place % ST;
-                const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), slot = qn & 1u;
-                if (j == 0 && (w.dual || i == 0) && !wait(q_full + 8u * slot, (qn >> 1) & 1u)) return false;
-                if ((!w.dual || s == 0) && !wait(kv_full + 8u * st, (place / ST) & 1u)) return false;
-                tc_fence_after();
-                if (attn_elect()) {
-                    const uint64_t a = smem_desc_sw128(q_smem + slot * p.q_slot), bd = smem_desc_sw128(ring + st * kTile);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
-                                    bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), kIdescS, k > 0 ? 1u : 0u);
-                    if (!w.dual || s == 1) tc_commit(kv_empty + 8u * st);
-                    tc_commit(s_full + 8u * s);
-                    if (w.dual ? j == n - 1 : i == H - 1) tc_commit(q_empty + 8u * slot);
+        if (g1 > g0) {
+            const unsigned here = __ballot_sync(0xFFFFFFFFu, at <= g0 && g0 < at + sum);
+            const int from = __ffs((int)here) - 1;
+            long long s = __shfl_sync(0xFFFFFFFFu, at, from);            // where the request, then the item, begins
+            bool first = true;
+#pragma unroll 1
+            for (int b = __shfl_sync(0xFFFFFFFFu, b0, from); b < p.B && s < g1 && ok; ++b) {
+                const AttnRequest q = attn_request(p, b);
+                if (q.T <= 0) continue;
+                const long long weight = attn_head_weight(p, q);
+                int h = 0;
+                if (s + weight * p.Hkv <= g0) {
+                    s += weight * p.Hkv;
+                    continue;
                 }
-                __syncwarp();
-                return true;
-            };
-            ok = product_s(0);
-            if (ok && H > 1) ok = product_s(1);
-            for (int i = 0; i < H && ok; ++i) {
-                const int s = i & 1, j = w.dual ? i >> 1 : i;
-                const uint32_t place = loads + w.v_at(j), st = place % ST;
-                if (!w.dual || s == 0) {
-                    if (!wait(kv_full + 8u * st, (place / ST) & 1u)) { ok = false; break; }
-                    if (w.masked(p, w.t0 + j)) {
-                        if (!wait(v_clean + 8u * st, clean_phase >> st & 1u)) { ok = false; break; }
-                        clean_phase ^= 1u << st;
+                if (s < g0) {
+                    const long long skip = g0 - s;
+                    h = (int)attn_div(skip, weight);
+                    s += h * weight;
+                }
+                const int blocks = attn_blocks(p, q);
+#pragma unroll 1
+                for (; h < p.Hkv && s < g1 && ok; ++h) {
+#pragma unroll 1
+                    for (int i = 0; i < blocks && s < g1 && ok; ++i) {
+                        AttnPiece w;
+                        w.tok0 = i * 2 * p.tpt;
+                        w.ntok = min(2 * p.tpt, q.T - w.tok0);
+                        w.keys = attn_keys(p, q, w.tok0 + w.ntok);
+                        const int tiles = attn_tiles(w.keys);
+                        const long long s0 = s + kAttnItemCost;          // the first tile's place
+                        s = s0 + tiles;
+                        if (s <= g0) continue;
+                        // not cut: the item goes to the run it begins in
+                        const long long lo = p.whole ? (s0 - kAttnItemCost >= g0 ? 0 : tiles) : max(g0 - s0, 0ll);
+                        const long long hi = p.whole ? tiles : min(g1 - s0, (long long)tiles);
+                        const bool begun = s0 - kAttnItemCost < g0;      // the run begins inside the item
+                        if (hi <= lo) continue;
+                        w.n = (int)(hi - lo);
+                        w.t0 = (int)lo;
+                        w.b = b;
+                        w.h = h;
+                        w.open = min(w.keys, q.L + (p.mask ? 0 : w.tok0 + 1)) / kAttnKeys;
+                        w.L = q.L;
+                        w.T = q.T;
+                        w.first = q.first;
+                        w.dual = w.ntok > p.tpt;
+                        w.cut = w.n < tiles;
+                        w.slot = begun || s0 - kAttnItemCost == g0 ? 0 : 1;
+                        w.pad[0] = w.pad[1] = 0;
+                        ok = publish(w);
+                        if (!ok) break;
+                        auto place_of = [&](int j) { return (w.t0 + j) * kAttnKeys + pg * pr; };
+                        auto page_of = [&](int j) -> int {
+                            const int at = place_of(j);
+                            if (j >= w.n || !mine || at >= w.keys) return -1;
+                            return p.page_table[w.b * p.table_stride + (unsigned)at / (unsigned)p.page_size];
+                        };
+                        int page_k = page_of(0), page_v = page_k, page_last = page_k;        // of the next K and V, and of the last K
+#pragma unroll 1
+                        for (int s = 0; s < 1 + w.dual && ok; ++s, ++q_n) {          // rows of q
+                            const uint32_t slot = q_n & 1u, turn = q_n >> 1;
+                            if (turn > 0 && !wait(q_empty + 8u * slot, (turn - 1u) & 1u)) { ok = false; break; }
+                            if (attn_elect()) {
+                                const uint32_t bar = q_full + 8u * slot, to = q_smem + slot * p.q_slot;
+                                mbar_arrive_expect_tx(bar, p.q_tx + p.withheld);
+#pragma unroll
+                                for (int c = 0; c < D / 64; ++c)
+                                    tma_load_3d(to + c * p.q_block, &maps.q, c * 64, w.h * p.G, w.first + w.tok0 + s * p.tpt, bar);
+                            }
+                            __syncwarp();
+                        }
+                        int page_next = page_of(1);                      // one K ahead of its use
+#pragma unroll 1
+                        for (uint32_t e = 0; e < 2u * w.n && ok; ++e, ++loads) {
+                            const int jv = w.value_at(e), j = jv >= 0 ? jv : (int)(e + 1u) >> 1;
+                            const uint32_t turn = turn_of(loads), s = loads - turn * ST;
+                            if (turn > 0 && !wait(kv_empty + 8u * s, (turn - 1u) & 1u)) { ok = false; break; }
+                            const int at = place_of(j), page = jv >= 0 ? page_v : page_k;
+                            const bool there = mine && at < w.keys;
+                            const uint32_t boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
+                            if (lane == 0) mbar_arrive_expect_tx(kv_full + 8u * s, boxes * p.page_tx + p.withheld);
+                            __syncwarp();
+                            if (there) {
+                                bad |= (unsigned)page >= (unsigned)p.n_pages;
+                                tma_load_4d(ring + s * kTile + col * kBlock + (uint32_t)(pg * pr) * 128u, jv >= 0 ? &maps.v : &maps.k, col * 64,
+                                            (int)((unsigned)at % (unsigned)p.page_size), w.h, page, kv_full + 8u * s);
+                            }
+                            __syncwarp();
+                            if (jv >= 0) {
+                                page_v = page_last;                      // K(j + 1) is on its way
+                            } else {
+                                page_last = page_k;
+                                page_k = page_next;
+                                page_next = page_of(j + 2);
+                            }
+                        }
+                        // the first CTA whose run begins behind the item's first tile names it for the join
+                        if (first && w.t0 > 0) {
+                            const int c0 = cut.of(s0);
+                            if (c0 == cta - 1) {
+                                split.rows = w.ntok * p.G;
+                                split.token0 = q.first + w.tok0;
+                                split.head0 = h * p.G;
+                                split.first_cta = c0;
+                                split.n_pieces = cut.of(s - 1) - c0 + 1;
+                                split.first_slot = cut.start(c0) >= s0 - kAttnItemCost ? 0 : 1;
+                            }
+                        }
+                        first = false;
                     }
                 }
-                if (!wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
-                p_phase ^= 1u << s;
-                if (__any_sync(0xFFFFFFFFu, *abort_flag != 0)) { ok = false; break; }
-                tc_fence_after();
-                if (attn_elect()) {
-                    const uint64_t bd = attn_v_desc(ring + st * kTile);
-#pragma unroll
-                    for (int k = 0; k < kAttnKeys / 16; ++k)
-                        tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
-                                       i >= 2 || k > 0 ? 1u : 0u);
-                    if (!w.dual || s == 1) tc_commit(kv_empty + 8u * st);
-                    if (i == H - 1) tc_commit(o_full);
-                }
-                __syncwarp();
-                if (i + 2 < H) ok = product_s(i + 2);
             }
-            loads += 2u * n;
-            q_n += w.dual ? 2u : 1u;
+        }
+        if (ok) {
+            AttnPiece end;
+            end.n = 0;
+            (void)publish(end);
+        }
+        if (lane == 0 && !p.whole) p.splits[cta] = split;
+        if (bad) atomicOr(&p.hdr->status, kStatusPage);
+    } else if (warp == kAttnIssuer) {
+        // ---------------------------------------------------------------- MMA issuer
+        // One for both streams: P V and the next S of one, then of the other, so that the streams' scores are ready at different times.  (With an
+        // issuer each, both streams fall into step, and exponentials and products take turns instead of overlapping: two long
+        // documents under 60 drafted tokens 120 -> 133 us.)
+        bool ok = true;
+        uint32_t p_phase = 0;
+        for (AttnPiece w; ok && take(w);) {
+            const int H = w.steps();
+#pragma unroll 1
+            for (int i = -2; i < H; ++i) {                   // P V of half-step i, then S of the stream's next
+                const int s = i & 1;
+                if (i >= 0) {
+                    const uint32_t place = loads + w.v_at(i >> w.dual), turn = turn_of(place), st = place - turn * ST;
+                    if (!wait(v_clean + 8u * st, turn & 1u) || !wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
+                    p_phase ^= 1u << s;
+                    tc_fence_after();
+                    if (attn_elect()) {
+                        const uint64_t bd = attn_v_desc(ring + st * kTile);
+#pragma unroll
+                        for (int k = 0; k < kAttnKeys / 16; ++k)
+                            tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
+                                           i >= 2 || k > 0 ? 1u : 0u);
+                        tc_commit(kv_empty + 8u * st);
+                        if (i == H - 1) tc_commit(o_full);
+                    }
+                    __syncwarp();
+                }
+                if (i + 2 < H) {
+                    const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), q_at = qn & 1u;
+                    if (i + 2 <= w.dual && !wait(q_full + 8u * q_at, (qn >> 1) & 1u)) { ok = false; break; }
+                    const uint32_t place = loads + w.k_at((i + 2) >> w.dual), turn = turn_of(place), st = place - turn * ST;
+                    if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
+                    tc_fence_after();
+                    if (attn_elect()) {
+                        const uint64_t a = smem_desc_sw128(q_smem + q_at * p.q_slot), bd = smem_desc_sw128(ring + st * kTile);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+                            tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
+                                        bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), kIdescS, k > 0 ? 1u : 0u);
+                        tc_commit(s_full + 8u * s);
+                        tc_commit(kv_empty + 8u * st);
+                        if ((i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok) break;
+            loads += 2u * w.n;
+            q_n += 1u + w.dual;
         }
     } else if (warp == kAttnCleaner) {
         // ---------------------------------------------------------------- cleaner
         bool ok = true;
-        for (AttnWalk w = first; w.more() && ok; w.next(p)) {
-            const int n = w.t1 - w.t0;
-            for (uint32_t e = 0; e < 2u * n; ++e) {          // every place, in order: it is in no phase but the next
-                const uint32_t place = loads + e, st = place % ST;
-                if (!wait(kv_full + 8u * st, (place / ST) & 1u)) { ok = false; break; }
-                const int j = e == 2u * n - 1u ? n - 1 : (int)(e >> 1) - 1;      // of V, if it is one
-                if (e > 0 && e == w.v_at(j) && w.masked(p, w.t0 + j)) {
+        for (AttnPiece w; ok && take(w);) {
+#pragma unroll 1
+            for (uint32_t e = 0; e < 2u * w.n; ++e) {        // every place, in order: a barrier is never a phase ahead of it
+                const uint32_t place = loads + e, turn = turn_of(place), st = place - turn * ST;
+                if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
+                const int j = w.value_at(e);
+                if (j >= 0 && w.t0 + j >= w.open) {
                     // positions all rows attend stay as they are
-                    const int r0 = max(0, min(kAttnKeys, w.q.L - (w.t0 + j) * kAttnKeys));
+                    const int r0 = max(0, min(kAttnKeys, w.L - (w.t0 + j) * kAttnKeys));
+#pragma unroll 1
                     for (int c = 0; c < D / 64; ++c) {
 #pragma unroll 4
                         for (int i = r0 * 8 + lane; i < kAttnKeys * 8; i += 32) {
@@ -528,60 +583,75 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     }
                     fence_proxy_async();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(v_clean + 8u * st);
                 }
-                if (lane == 0) mbar_arrive(kv_empty + 8u * st);
+                if (lane == 0) {
+                    mbar_arrive(v_clean + 8u * st);
+                    // for the stream that does not read it, too
+                    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(kv_empty + 8u * st), "r"(w.dual ? 1u : 2u) : "memory");
+                }
             }
-            loads += 2u * n;
+            loads += 2u * w.n;
         }
     } else {
         // ---------------------------------------------------------------- softmax, and the end of an item
-        // A warp whose wait has run out goes on through the same barriers without waiting, touching nothing.
         const int s = warp >> 2, quad = warp & 3;
         const int r = quad * 32 + lane;                      // the thread's lane of its stream's tiles
         const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
         const uint32_t t_s = tmem + kAttnTmemS + 128u * s + lane_at, t_o = tmem + kAttnTmemO + 128u * s + lane_at;
         bool ok = true;
-        uint32_t s_phase = 0, item = 0;
-        for (AttnWalk w = first; w.more(); w.next(p), ++item) {
+        uint32_t s_phase = 0, o_phase = 0, meet_phase = 0;
+        auto meet_others = [&]() -> bool {                   // the eight warps here
+            __syncwarp();
+            if (lane == 0) mbar_arrive(meet);
+            meet_phase ^= 1u;
+            return wait(meet, meet_phase ^ 1u);
+        };
+        for (AttnPiece w; ok && take(w);) {
             const int H = w.steps();
             const int tile_tokens = w.dual ? (s ? w.ntok - p.tpt : p.tpt) : w.ntok;
             const int rows = tile_tokens * p.G;              // of this stream's tile
             const bool real = r < rows, busy = quad * 32 < rows;
             const int t = w.tok0 + (w.dual ? s * p.tpt : 0) + (real ? r / p.G : 0);      // the row's token within its request
             float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
             for (int i = s; i < H; i += 2) {
-                if (ok) ok = wait(s_full + 8u * s, s_phase);
+                if (!wait(s_full + 8u * s, s_phase)) { ok = false; break; }
                 s_phase ^= 1u;
-                if (ok && busy) {
+                if (busy) {
                     tc_fence_after();
-                    const int j = w.t0 + (w.dual ? i >> 1 : i);
-                    uint32_t x[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tc_ld32(t_s + 32u * c, x[c]);
-                    tc_wait_ld();
-                    if (w.masked(p, j)) {
-                        const int32_t* row = p.mask ? p.mask + (int64_t)(w.q.first + t) * p.mask_words : nullptr;
-#pragma unroll
+                    const int j = w.t0 + (i >> w.dual);
+                    if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
+                        const int32_t* row = p.mask ? p.mask + (int64_t)(w.first + t) * p.mask_words : nullptr;
+#pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            const int at = j * kAttnKeys + 32 * c;
-                            uint32_t bits = attn_bits(row, p.mask_words, t, w.q.T, at - w.q.L);
-                            const int n = w.keys - at;
+                            const int at = j * kAttnKeys + 32 * c, n = w.keys - at;
+                            uint32_t bits = attn_bits(row, p.mask_words, t, w.T, at - w.L);
                             bits &= n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+                            uint32_t x[32];
+                            __syncwarp();
+                            tc_ld32(t_s + 32u * c, x);
+                            tc_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (!(bits >> e & 1u)) x[c][e] = 0xFF800000u;
+                                if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
+                            tc_st32(t_s + 32u * c, x);
                         }
+                        tc_wait_st();
                     }
-                    float top[4];
+                    // The scores are read twice, half of them at a time, for their maximum and for the weights.  (One pass with the old maximum,
+                    // made again where it grew too much, has fewer instructions to issue but four times as many to fetch, as all weights wait in
+                    // registers: slower by 5 to 10 %.)
+                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t x[64];
+                        tc_ld64(t_s + 64u * c, x);
+                        tc_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        top[c] = __uint_as_float(x[c][0]);
-#pragma unroll
-                        for (int e = 1; e < 32; ++e) top[c] = fmaxf(top[c], __uint_as_float(x[c][e]));
+                        for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3(top[(e >> 1) & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                     }
                     const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                    // (mx - m) is NaN while nothing has been attended yet
+                    // (mx - m) is infinite while nothing has been attended yet
                     const bool grow = real && mx > m && !((mx - m) * p.scale_log2 <= kAttnSlack);
                     if (__any_sync(0xFFFFFFFFu, grow)) {
                         const float f = grow ? ex2_approx((m - mx) * p.scale_log2) : 1.0f;
@@ -590,7 +660,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             l *= f;
                         }
                         if (i >= 2) {
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D / 32; ++c) {
                                 uint32_t o[32];
                                 tc_ld32(t_o + 32u * c, o);
@@ -604,23 +674,22 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
                     const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
                     uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t x[64], pk[32];
+                        tc_ld64(t_s + 64u * c, x);
+                        tc_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < 4; c += 2) {
-                        uint32_t pk[32];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-#pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
-                                float a, b;
-                                unpack2(fma2(pack2(__uint_as_float(x[c + h][e]), __uint_as_float(x[c + h][e + 1])), k2, r2), a, b);
-                                a = ex2_approx(a);
-                                b = ex2_approx(b);
-                                const uint64_t ab = pack2(a, b);
-                                if (e & 2) sum1 = add2(sum1, ab);
-                                else sum0 = add2(sum0, ab);
-                                pk[h * 16 + e / 2] = attn_bf16x2(a, b);
-                            }
-                        tc_st32(t_s + 16u * c, pk);
+                        for (int e = 0; e < 64; e += 2) {
+                            float a, b;
+                            unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, r2), a, b);
+                            a = ex2_approx(a);
+                            b = ex2_approx(b);
+                            if (e & 2) sum1 = add2(sum1, pack2(a, b));
+                            else sum0 = add2(sum0, pack2(a, b));
+                            pk[e / 2] = attn_bf16x2(a, b);
+                        }
+                        tc_st32(t_s + 32u * c, pk);          // over scores that have been read
                     }
                     float a, b;
                     unpack2(add2(sum0, sum1), a, b);
@@ -632,27 +701,28 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 if (lane == 0) mbar_arrive(p_full + 8u * s);
             }
             // ---- the item's end: a piece of it to the workspace, or its rows
-            if (ok) ok = wait(o_full, item & 1u);
+            if (!ok || !wait(o_full, o_phase)) { ok = false; break; }
+            o_phase ^= 1u;
             tc_fence_after();
             const bool both = !w.dual && H > 1;              // the streams hold different positions of the same rows
             float f0 = 1.0f, f1 = 0.0f;                      // weights of stream 0's (of this stream's) and stream 1's O
-            if (!w.dual) {
+            if (both) {
                 sh.ms[s][r] = make_float2(m, l);
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                const float2 a = sh.ms[0][r], b = both ? sh.ms[1][r] : make_float2(-INFINITY, 0.0f);
+                if (!meet_others()) { ok = false; break; }
+                const float2 a = sh.ms[0][r], b = sh.ms[1][r];
                 m = fmaxf(a.x, b.x);
                 f0 = a.x == m ? 1.0f : ex2_approx((a.x - m) * p.scale_log2);
                 f1 = b.x == m ? 1.0f : ex2_approx((b.x - m) * p.scale_log2);
-                l = a.y * f0 + (both ? b.y * f1 : 0.0f);
+                l = a.y * f0 + b.y * f1;
             }
-            if (ok && busy && (w.dual || both || s == 0)) {
-                const bool cut = w.t1 - w.t0 < w.tiles;
-                const int row = (w.dual ? s * p.tpt * p.G : 0) + r;
-                const uint32_t o_at = (w.dual ? t_o : tmem + kAttnTmemO + lane_at);
+            if (busy && (w.dual || both || s == 0)) {
+                const int row = (w.dual ? s * p.tpt * p.G : 0) + r, head = w.h * p.G + (real ? r % p.G : 0);
+                const uint32_t o_at = w.dual ? t_o : tmem + kAttnTmemO + lane_at;
                 const int c0 = both ? s * (D / 64) : 0, c1 = both ? c0 + D / 64 : D / 32;        // runs of 32 columns
-                const float inv = cut ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-                const size_t piece = (size_t)(cta * 2 + (item == 0 ? 0 : 1));        // a run's first item, or its last
-                uint16_t* to = p.out + (int64_t)(w.q.first + t) * p.out_ts + (int64_t)(w.h * p.G + r % p.G) * p.out_hs;
+                const float inv = w.cut ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+                const size_t piece = (size_t)(blockIdx.x * 2 + w.slot);
+                uint16_t* to = p.out + (int64_t)(w.first + t) * p.out_ts + (int64_t)head * p.out_hs;
+#pragma unroll 1
                 for (int c = c0; c < c1; ++c) {
                     __syncwarp();
                     uint32_t o[32];
@@ -667,7 +737,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         tc_wait_ld();
                     }
                     if (!real) continue;
-                    if (cut) {
+                    if (w.cut) {
                         float4* po = reinterpret_cast<float4*>(p.part_o) + (piece * (D / 4) + 8 * c) * p.rows_max + row;
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
@@ -685,34 +755,13 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     }
                 }
                 if (real && (w.dual || s == 0)) {
-                    if (cut) p.part_ml[piece * p.rows_max + row] = make_float2(m, l);
-                    else if (p.lse) p.lse[(int64_t)(w.q.first + t) * p.Hq + w.h * p.G + r % p.G] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+                    if (w.cut) p.part_ml[piece * p.rows_max + row] = make_float2(m, l);
+                    else if (p.lse) p.lse[(int64_t)(w.first + t) * p.Hq + head] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
                 }
                 tc_fence_before();
             }
-            asm volatile("bar.sync 1, 256;" ::: "memory");   // both streams' O and (m, l) have been read; neither is an item ahead
+            if (!meet_others()) ok = false;                  // both streams' O and (m, l) have been read; neither is an item ahead
         }
-    }
-
-    // ---- which item this CTA's run is the first to cut
-    if (tid == 0) {
-        AttnSplit d{};
-        if (g1 > g0 && first.t0 > 0) {
-            const long long start = g0 - first.t0, end = start + first.tiles;
-            int c0 = cta - 1;
-            while (attn_run(W, C, c0) > start) --c0;
-            if (c0 == cta - 1) {
-                int c1 = cta;
-                while (attn_run(W, C, c1 + 1) < end) ++c1;
-                d.rows = first.ntok * p.G;
-                d.token0 = first.q.first + first.tok0;
-                d.head0 = first.h * p.G;
-                d.first_cta = c0;
-                d.n_pieces = c1 - c0 + 1;
-                d.first_slot = attn_run(W, C, c0) == start ? 0 : 1;
-            }
-        }
-        if (!p.whole) p.splits[cta] = d;
     }
 
     tc_fence_before();
@@ -736,68 +785,88 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 
 // ------------------------------------------------------------------------------------------ joining an item's pieces
 // lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  A block takes
-// eight rows of an item at a time; which there are, each block works out from the runs' entries.
-constexpr int kJoinRows = 8;
+// a few rows of an item at a time (1024 / D: a float4 of a row per thread); which there are, each block works out from the runs' entries.
 template <int D>
 __global__ void __launch_bounds__(256)
-attn_join_kernel(const __grid_constant__ AttnParams p, int C) {
-    __shared__ int ahead[kAttnCtas + 1];
+attn_join_kernel(const __grid_constant__ AttnParams p) {
+    constexpr int kRows = 1024 / D, kQuads = D / 4;
     __shared__ AttnSplit split[kAttnCtas];
+    __shared__ int ahead[kAttnCtas + 1];
+    __shared__ float2 weight[kAttnCtas][kRows];              // (m, l) of the pieces, then their weights
+    __shared__ float inv[kRows];
+    const int C = p.ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     grid_dependency_wait();
-    if (threadIdx.x == 0) grid_launch_dependents();
-    for (int i = threadIdx.x; i < C; i += 256) split[i] = p.splits[i];
+    if (tid == 0) grid_launch_dependents();
+    for (int i = tid; i < C; i += 256) split[i] = p.splits[i];
     __syncthreads();
-    if (threadIdx.x < 32) {                                  // running number of row groups
+    if (warp == 0) {                                         // running number of row groups
         int before = 0;
-        for (int i = threadIdx.x; i - (int)threadIdx.x < C; i += 32) {
-            const int n = i < C ? (split[i].rows + kJoinRows - 1) / kJoinRows : 0;
+        for (int i = lane; i - lane < C; i += 32) {
+            const int n = i < C ? (split[i].rows + kRows - 1) / kRows : 0;
             int incl = n;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if ((int)threadIdx.x >= o) incl += v;
+                if (lane >= o) incl += v;
             }
             if (i < C) ahead[i] = before + incl - n;
             before += __shfl_sync(0xFFFFFFFFu, incl, 31);
         }
-        if (threadIdx.x == 0) ahead[C] = before;
+        if (lane == 0) ahead[C] = before;
     }
     __syncthreads();
     const int all = ahead[C];
-    constexpr int kQuads = D / 4;                            // runs of four columns
     for (int unit = blockIdx.x; unit < all; unit += gridDim.x) {
-        int lo = 0, hi = C;                                  // the last entry with ahead <= unit that has rows
+        int lo = 0, hi = C;                                  // the last entry with ahead <= unit: it has rows
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (ahead[mid] <= unit) lo = mid;
             else hi = mid;
         }
         const AttnSplit d = split[lo];
-        const int row = (unit - ahead[lo]) * kJoinRows + (int)(threadIdx.x % kJoinRows);
-        if (row >= d.rows) continue;
-        for (int cq = threadIdx.x / kJoinRows; cq < kQuads; cq += 256 / kJoinRows) {
-            auto piece = [&](int i) { return (size_t)((d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0)); };
-            float m = -INFINITY;
-            for (int i = 0; i < d.n_pieces; ++i) m = fmaxf(m, p.part_ml[piece(i) * p.rows_max + row].x);
-            float l = 0.0f;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-            for (int i = 0; i < d.n_pieces; ++i) {
-                const float2 ml = p.part_ml[piece(i) * p.rows_max + row];
+        const int row0 = (unit - ahead[lo]) * kRows, rows = min(kRows, d.rows - row0);
+        auto piece = [&](int i) { return (size_t)((d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0)); };
+        for (int e = tid; e < d.n_pieces * kRows; e += 256) {
+            const int i = e / kRows, r = e % kRows;
+            if (r < rows) weight[i][r] = p.part_ml[piece(i) * p.rows_max + row0 + r];
+        }
+        __syncthreads();
+        for (int r = warp; r < rows; r += 8) {               // a warp per row
+            float m = -INFINITY, l = 0.0f;
+            for (int i = lane; i < d.n_pieces; i += 32) m = fmaxf(m, weight[i][r].x);
+            m = warp_max_f32(m);
+            for (int i = lane; i < d.n_pieces; i += 32) {
+                const float2 ml = weight[i][r];
                 const float f = ml.x == m ? 1.0f : ex2_approx((ml.x - m) * p.scale_log2);
-                const float4 v = reinterpret_cast<const float4*>(p.part_o)[(piece(i) * kQuads + cq) * p.rows_max + row];
                 l += ml.y * f;
+                weight[i][r].x = f;
+            }
+            l = warp_sum_f32(l);
+            if (lane == 0) {
+                inv[r] = l == 0.0f ? 0.0f : 1.0f / l;
+                const int row = row0 + r;
+                if (p.lse) p.lse[(int64_t)(d.token0 + row / p.G) * p.Hq + d.head0 + row % p.G] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+            }
+        }
+        __syncthreads();
+        const int r = tid % kRows, cq = tid / kRows;
+        if (r < rows) {
+            const int row = row0 + r;
+            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+            for (int i = 0; i < d.n_pieces; ++i) {
+                const float4 v = reinterpret_cast<const float4*>(p.part_o)[(piece(i) * kQuads + cq) * p.rows_max + row];
+                const float f = weight[i][r].x;
                 o.x += v.x * f;
                 o.y += v.y * f;
                 o.z += v.z * f;
                 o.w += v.w * f;
             }
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int token = d.token0 + row / p.G, head = d.head0 + row % p.G;
-            *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq) =
-                make_uint2(attn_bf16x2(o.x * inv, o.y * inv), attn_bf16x2(o.z * inv, o.w * inv));
-            if (cq == 0 && p.lse) p.lse[(int64_t)token * p.Hq + head] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+            const float n = inv[r];
+            *reinterpret_cast<uint2*>(p.out + (int64_t)(d.token0 + row / p.G) * p.out_ts + (int64_t)(d.head0 + row % p.G) * p.out_hs + 4 * cq) =
+                make_uint2(attn_bf16x2(o.x * n, o.y * n), attn_bf16x2(o.z * n, o.w * n));
         }
+        __syncthreads();
     }
 }
 
@@ -839,7 +908,7 @@ static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint
     cudaError_t e = launch_pdl(attn_kernel<D>, C, kAttnThreads, smem, st, maps, p);
     count_launch();
     if (e == cudaSuccess && !p.whole) {
-        e = launch_pdl(attn_join_kernel<D>, 2 * C, 256, 0, st, p, C);
+        e = launch_pdl(attn_join_kernel<D>, 2 * C, 256, 0, st, p);
         count_launch();
     }
     if (e == cudaSuccess) e = cudaGetLastError();
@@ -882,6 +951,8 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.tpt = 128 / p.G;
     p.box_tokens = std::min(p.tpt, c.max_tokens);
     p.whole = (long long)a.max_pages * a.page_size <= (long long)kAttnWhole * kAttnKeys;
+    p.ctas = C;
+    p.min_run = 1;
     p.scale = c.scale;
     p.scale_log2 = c.scale * kLog2e;
     p.wait_ns = kWaitLimitNs;
@@ -895,8 +966,9 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.q_tx = rows * 128u * (D / 64);
     p.page_tx = (uint32_t)std::min(p.page_size, kAttnKeys) * 128u;
     // five stages of 32 KB beside two full row tiles: 160 KB in flight
-    const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 10);
+    const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 11 + 2 * kAttnPieces);
     p.n_stages = (int)std::min((uint32_t)kAttnMaxStages, ((uint32_t)kMaxDynSmem - tail - 2 * p.q_slot) / tile);
+    p.stages_inv = (uint32_t)((0x100000000ull + p.n_stages - 1) / p.n_stages);
     p.shared_off = 2 * p.q_slot + p.n_stages * tile;
     p.bar_off = p.shared_off + sizeof(AttnShared);
     const uint32_t smem = p.shared_off + tail;
