@@ -554,7 +554,7 @@ def _heads(t: torch.Tensor, name: str, device: int) -> _VtHeads:
     """bf16 [tokens, heads, D] on the current device, the elements of a head in a row; anything else may be strided."""
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or t.get_device() != device or (t.stride(2) != 1 and t.shape[2] > 1):
+    if t.dim() != 3 or t.get_device() != device or (t.stride(2) != 1 and t.shape[2] > 1 and t.shape[0] > 0):
         raise ValueError(f"{name}: expected [tokens, heads, D] with contiguous heads on the current CUDA device")
     n, h, d = t.shape
     if n > 1 and h > 1:
@@ -773,7 +773,7 @@ def vt_verify_tokens(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.T
     distributed as if the target had generated alone; the rule is spelled out in ``include/vt.h``."""
     device = torch.cuda.current_device()
     for name, t in (("probs", probs), ("draft_probs", draft_probs)):
-        if t is not None and (t.dtype is not torch.float32 or t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.shape[1] > 1)):
+        if t is not None and (t.dtype is not torch.float32 or t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.shape[1] > 1 and t.shape[0] > 0)):
             raise ValueError(f"{name}: expected float32 [N, vocabulary] with contiguous rows on the current CUDA device")
     N, V = probs.shape
     B = u_sample.shape[0]
