@@ -27,7 +27,8 @@ _BINDING_NAMES = {
 
 def __getattr__(name):
     if name in _BINDING_NAMES:
-        return getattr(importlib.import_module(".binding", __name__), name)
+        value = globals()[name] = getattr(importlib.import_module(".binding", __name__), name)      # looked up once: 3 us a time
+        return value
     if name in ("inputs", "binding", "build"):
         return importlib.import_module("." + name, __name__)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -554,12 +554,12 @@ def _heads(t: torch.Tensor, name: str, device: int) -> _VtHeads:
     """bf16 [tokens, heads, D] on the current device, the elements of a head in a row; anything else may be strided."""
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or t.get_device() != device or (t.stride(2) != 1 and t.shape[2] > 1 and t.shape[0] > 0):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.get_device() != device or (stride[2] != 1 and shape[2] > 1 and shape[0] > 0):
         raise ValueError(f"{name}: expected [tokens, heads, D] with contiguous heads on the current CUDA device")
-    n, h, d = t.shape
-    if n > 1 and h > 1:
-        return _VtHeads(t.data_ptr(), t.stride(0), t.stride(1))
-    return _VtHeads(t.data_ptr(), t.stride(0) if n > 1 else max(h, 1) * d, t.stride(1) if h > 1 else d)     # the stride of one alone says nothing
+    n, h, d = shape
+    # the stride of one alone says nothing
+    return _VtHeads(t.data_ptr(), stride[0] if n > 1 else (h or 1) * d, stride[1] if h > 1 else d)
 
 
 def _vector(t: torch.Tensor, name: str, n: int | None, device: int, dtype: torch.dtype = torch.int32) -> int:
@@ -575,6 +575,10 @@ def _new_or_given(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.
     if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != shape:
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on the current CUDA device")
     return t
+
+
+def _stream_of(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 class VtRope(NamedTuple):
@@ -659,7 +663,7 @@ def _rope_args(q, k, positions, rope: VtRope):
 
 def _heads_out(t, name, like, device):
     if t is None:
-        t = torch.empty(like.shape, dtype=torch.bfloat16, device=like.device)
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
     elif t.shape != like.shape:
         raise ValueError(f"{name}: expected the shape of its input")
     return t, _heads(t, name, device)
@@ -682,7 +686,7 @@ def vt_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, ro
     _check(lib().vt_rope(ctypes.byref(hq), None if hk is None else ctypes.byref(hk), positions.data_ptr(), rope.table.data_ptr(), N, Hq,
                          0 if k is None else k.shape[1], D, rope.rot_dim, rope.amplitude,
                          (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), ctypes.byref(ho),
-                         None if ko is None else ctypes.byref(ko), _stream()), "vt_rope")
+                         None if ko is None else ctypes.byref(ko), _stream_of(device)), "vt_rope")
     return out_q, out_k
 
 
@@ -700,7 +704,7 @@ def vt_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions:
     out_q, ho = _heads_out(out_q, "out_q", q, device)
     _check(lib().vt_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), positions.data_ptr(), cu, rope.table.data_ptr(), q.shape[0],
                                 q.shape[1], rope.rot_dim, rope.amplitude, VT_ROPE_INTERLEAVED if rope.interleaved else 0, ctypes.byref(ho),
-                                cache._ref, _stream()), "vt_rope_append")
+                                cache._ref, _stream_of(device)), "vt_rope_append")
     return out_q
 
 
@@ -716,7 +720,7 @@ def vt_tree_mask(parents: torch.Tensor, cu_tokens: torch.Tensor, max_tokens: int
     pl = None if lens is None else _vector(lens, "lens", B, device)
     mask = _new_or_given(mask, "mask", (N, words), torch.int32, parents, device)
     positions = _new_or_given(positions, "positions", (N,), torch.int32, parents, device)
-    _check(lib().vt_tree_mask(pp, cu, pl, N, B, mask.data_ptr(), words, positions.data_ptr(), _stream()), "vt_tree_mask")
+    _check(lib().vt_tree_mask(pp, cu, pl, N, B, mask.data_ptr(), words, positions.data_ptr(), _stream_of(device)), "vt_tree_mask")
     return mask, positions
 
 
@@ -752,7 +756,7 @@ def vt_tree_attention(q: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache, 
         raise ValueError("workspace: expected a contiguous tensor on the current CUDA device")
     _check(lib().vt_tree_attention(ctypes.byref(hq), cu, cache._ref, None if mask is None else mask.data_ptr(), words, N, Hq, max_tokens,
                                    D ** -0.5 if scale is None else scale, ctypes.byref(ho), lse.data_ptr(), workspace.data_ptr(),
-                                   workspace.nbytes, _stream()), "vt_tree_attention")
+                                   workspace.nbytes, _stream_of(device)), "vt_tree_attention")
     return out, lse
 
 
@@ -797,7 +801,7 @@ def vt_verify_tokens(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.T
         for name, t, shape in zip(VtVerified._fields, out, ((B,), (B, max_tokens), (B, max_tokens))):
             _new_or_given(t, name, shape, torch.int32, tokens, device)
     _check(lib().vt_verify_tokens(probs.data_ptr(), probs.stride(0) if N > 1 else V, *args, pq, ldq, pi, pm, N, B, V, Vd, max_tokens,
-                                  out.n_accepted.data_ptr(), out.path.data_ptr(), out.tokens.data_ptr(), _stream()), "vt_verify_tokens")
+                                  out.n_accepted.data_ptr(), out.path.data_ptr(), out.tokens.data_ptr(), _stream_of(device)), "vt_verify_tokens")
     return out
 
 

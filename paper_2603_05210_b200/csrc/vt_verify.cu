@@ -4,14 +4,16 @@
 // p[parent][token] and q[parent][token], does not: all of them are fetched at once, and the way down the tree is then a walk through shared
 // memory that every CTA makes for itself.  Only the rows' sums need the cluster: each CTA owns an eighth of the vocabulary, adds up its part
 // in 64 bits in a fixed order and gives the sum to the others through distributed shared memory.  The token that follows is found from the
-// sums: the CTA, then the warp whose range the target falls into, then that warp's range once more, 32 ids at a time.
+// sums: the CTA, then the warp whose range the target falls into, then the lane's thirty-second of that, then the id.
 //
 // After j rejections at a node what is left is max(p - S q, 0) with one number S, because max(max(a - b, 0) - c, 0) = max(a - b - c, 0) for
-// c >= 0: no row is written anywhere.  q lives on the trimmed vocabulary, so a CTA lays the node's q out over its own ids in shared memory
-// first (it runs over the whole d2t, which all requests share in L2, and keeps the eighth that is its own: no exchange between CTAs).
+// c >= 0: no row is written anywhere.  q lives on the trimmed vocabulary, so the node's q is laid out over the CTAs' ids in shared memory
+// first: each CTA sends an eighth of q to where d2t says.
 // Drafts chosen without chance need no sums on the way (Z falls by p of each child), and a bitmap of rejected children in q's place.
 //
-// Bound: the latency of four dependent steps (offsets, gathers, the row, the range), then the bytes of one row of p (and q) per request.
+// Bound: latency.  Seven memory round trips follow one another (offsets, nodes, gathers, q, the row, a lane's part of it, the id); the bytes of
+// one row of p (and q) per request take a tenth of that for 16 requests.  (Going through the warp's range 32 ids at a time, each behind a load,
+// took 17 of 23 us.)
 #include "vt_step.h"
 #include "vt_tc.cuh"
 
@@ -27,7 +29,7 @@ struct VerifyParams {
     int share;                               // ids per CTA
 };
 
-// Adds up one value per thread (in the order of the lanes, then of the warps), then one per CTA of the cluster in the order of their ranks.
+// Adds up one value per thread (across lanes, then warps), then one per CTA of the cluster in the order of their ranks.
 // Every thread gets the total; warp_sums and cta_sums keep the parts.  cta_sums is written by the other CTAs: the caller alternates two.
 __device__ __forceinline__ double cluster_total(double x, double* warp_sums, double* cta_sums, uint32_t rank) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -36,10 +38,12 @@ __device__ __forceinline__ double cluster_total(double x, double* warp_sums, dou
     __syncthreads();                         // the last total's readers of warp_sums are done
     if (lane == 0) warp_sums[warp] = x;
     __syncthreads();
-    if (threadIdx.x < kVerifyCtas) {
-        double s = 0.0;
-        for (int w = 0; w < kVerifyWarps; ++w) s += warp_sums[w];
-        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_map_shared(smem_u32(cta_sums + rank), threadIdx.x)), "d"(s) : "memory");
+    if (warp == 0) {
+        double s = lane < kVerifyWarps ? warp_sums[lane] : 0.0;
+#pragma unroll
+        for (int o = kVerifyWarps / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        if (lane < kVerifyCtas)
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(cluster_map_shared(smem_u32(cta_sums + rank), (uint32_t)lane)), "d"(s) : "memory");
     }
     cluster_sync_all();
     double total = 0.0;
@@ -48,7 +52,7 @@ __device__ __forceinline__ double cluster_total(double x, double* warp_sums, dou
 }
 
 template <bool DRAWN>
-__global__ void __launch_bounds__(kVerifyThreads)
+__global__ void __launch_bounds__(kVerifyThreads, 2)
 verify_kernel(const __grid_constant__ VerifyParams prm) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ double warp_sums[kVerifyWarps], cta_sums[2][kVerifyCtas];
@@ -68,7 +72,12 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     int* node_parent = node_token + c.max_tokens;
     int* path = node_parent + c.max_tokens;
 
-    cluster_sync_all();                      // every CTA of the cluster runs before another writes into its shared memory
+    const int words = DRAWN ? prm.share : prm.share / 32;
+    auto clear = [&]() {
+        for (int i = 4 * tid; i < words; i += 4 * kVerifyThreads) *reinterpret_cast<uint4*>(out_bits + i) = make_uint4(0u, 0u, 0u, 0u);
+    };
+    clear();
+    cluster_sync_all();                      // every CTA of the cluster runs, and has cleared its own, before another writes into its shared memory
     grid_dependency_wait();
     if (tid == 0) grid_launch_dependents();
 
@@ -93,6 +102,7 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
         node_token[t] = token;
         node_parent[t] = in ? up : -1;
     }
+    const double u_follow = fmax((double)c.u_sample[b], 0.0);
     __syncthreads();
     if (!DRAWN) {                            // a child with the token of an earlier one: nothing is left of it by then
         for (int t = tid; t < T; t += kVerifyThreads) {
@@ -105,30 +115,42 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     }
 
     int buffer = 0;
-    // the node whose q (whose rejected children) are laid out
+    // lays out q of a node, or its children
+    bool cleared = true;
     auto lay_out = [&](int x) {
-        __syncthreads();
-        const int words = DRAWN ? prm.share : prm.share / 32;
-        for (int i = tid; i < words; i += kVerifyThreads) out_bits[i] = 0u;
-        __syncthreads();
+        if (!cleared) {
+            __syncthreads();                 // the last node's has been read
+            clear();
+            if (DRAWN) cluster_sync_all();
+            else __syncthreads();
+        }
+        cleared = false;
         if (DRAWN) {
             const float* q = c.draft_probs + (int64_t)(begin + x) * c.ld_draft;
             if (c.d2t) {
+                const int i0 = (int)((long long)c.Vd * rank / kVerifyCtas), i1 = (int)((long long)c.Vd * (rank + 1) / kVerifyCtas);
 #pragma unroll 8
-                for (int i = tid; i < c.Vd; i += kVerifyThreads) {
-                    const unsigned at = (unsigned)(c.d2t[i] - first_id);
-                    if (at < (unsigned)ids) left_q[at] = fmaxf(q[i], 0.0f);
+                for (int i = i0 + tid; i < i1; i += kVerifyThreads) {
+                    const int at = c.d2t[i];
+                    const float v = fmaxf(q[i], 0.0f);
+                    if ((unsigned)at < (unsigned)c.V) {
+                        const unsigned owner = (unsigned)at / (unsigned)prm.share;
+                        asm volatile("st.shared::cluster.f32 [%0], %1;"
+                                     ::"r"(cluster_map_shared(smem_u32(left_q + ((unsigned)at - owner * (unsigned)prm.share)), owner)), "f"(v) : "memory");
+                    }
                 }
+                cluster_sync_all();
             } else {
                 for (int i = tid; i < min(ids, c.Vd - first_id); i += kVerifyThreads) left_q[i] = fmaxf(q[first_id + i], 0.0f);
+                __syncthreads();
             }
         } else {
             for (int t = tid; t < T; t += kVerifyThreads) {
                 const unsigned at = (unsigned)(node_token[t] - first_id);
                 if (node_parent[t] == x && at < (unsigned)ids) atomicOr(&out_bits[at >> 5], 1u << (at & 31));
             }
+            __syncthreads();
         }
-        __syncthreads();
     };
     // what is left of id first_id + i, whose probability is p
     auto left = [&](float p, int i, double S, bool whole) -> double {
@@ -161,6 +183,7 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     // ---- down the tree; every thread of every CTA takes the same way
     int x = 0, n = 0, laid = -1;
     double S = 0.0, Z = 1.0;
+    bool summed = false;                     // Z is the sum of what is left, and its parts are in place
     for (int child = 1; T > 0;) {
         int next = T;                        // the next child of x
         for (int s = child; s < T; s += 32) {
@@ -179,12 +202,13 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
             x = next;
             S = 0.0;
             Z = 1.0;
+            summed = false;
         } else if (DRAWN) {
             S += Z;
             if (laid != x) lay_out(x);
             laid = x;
-            Z = cluster_total(part(x, S, false), warp_sums, cta_sums[buffer], rank);
-            buffer ^= 1;
+            Z = cluster_total(part(x, S, false), warp_sums, cta_sums[buffer ^= 1], rank);
+            summed = true;
         } else {
             Z -= p;
         }
@@ -193,16 +217,18 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
 
     // ---- the token that follows
     if (T > 0) {
-        bool whole = DRAWN ? S == 0.0 : false;
-        if (!whole && laid != x) lay_out(x);
-        double total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer], rank);
+        bool whole = DRAWN && !summed;
+        double total = Z;
+        if (!summed) {
+            if (!whole) lay_out(x);
+            total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer ^= 1], rank);
+        }
         if (!(total > 0.0) && !whole) {      // the same in every CTA
             whole = true;
-            buffer ^= 1;
-            total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer], rank);
+            total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer ^= 1], rank);
         }
         const double* sums = cta_sums[buffer];
-        const double target = fmax((double)c.u_sample[b], 0.0) * total;
+        const double target = u_follow * total;
         // the first CTA, then the first warp, whose range goes past the target; the last with anything in it when rounding leaves none
         int own = -1, last = -1;
         double before = 0.0;
@@ -225,20 +251,43 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
             if (w == warp) {
                 const float* row = c.probs + (int64_t)(begin + x) * c.ld_probs + first_id;
                 const int i0 = warp * per_warp, i1 = min(i0 + per_warp, ids);
-                int found = -1, latest = -1;
-                for (int i = i0; i < i1 && found < 0; i += 32) {
-                    const double l = i + lane < i1 ? left(row[i + lane], i + lane, S, whole) : 0.0;
-                    double cum = l;
+                // a lane per run of `len` consecutive ids: the run whose sum goes past the target (or the last with anything in it) ...
+                const int len = per_warp / 32, r0 = i0 + lane * len, r1 = min(r0 + len, i1);
+                double run = 0.0;
+                if (vector) {
+#pragma unroll 8
+                    for (int i = r0; i + 3 < r1; i += 4) {
+                        const float4 p = *reinterpret_cast<const float4*>(row + i);
+                        run += (left(p.x, i, S, whole) + left(p.y, i + 1, S, whole)) + (left(p.z, i + 2, S, whole) + left(p.w, i + 3, S, whole));
+                    }
+                    for (int i = r0 + (max(r1 - r0, 0) & ~3); i < r1; ++i) run += left(row[i], i, S, whole);
+                } else {
+#pragma unroll 8
+                    for (int i = r0; i < r1; ++i) run += left(row[i], i, S, whole);
+                }
+                auto up_to = [&](double v) {                 // sum over the lanes up to this one
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
-                        const double v = __shfl_up_sync(0xFFFFFFFFu, cum, o);
-                        if (lane >= o) cum += v;
+                        const double w = __shfl_up_sync(0xFFFFFFFFu, v, o);
+                        if (lane >= o) v += w;
                     }
-                    cum += before;
-                    const unsigned some = __ballot_sync(0xFFFFFFFFu, l > 0.0), over = __ballot_sync(0xFFFFFFFFu, !past_w && l > 0.0 && cum > target);
-                    if (over) found = i + __ffs((int)over) - 1;
-                    if (some) latest = i + 31 - __clz((int)some);
-                    before = __shfl_sync(0xFFFFFFFFu, cum, 31);
+                    return v;
+                };
+                const double cum = before + up_to(run);
+                const unsigned some = __ballot_sync(0xFFFFFFFFu, run > 0.0);
+                const unsigned over = __ballot_sync(0xFFFFFFFFu, !past_w && run > 0.0 && cum > target);
+                const int at = over ? __ffs((int)over) - 1 : some ? 31 - __clz((int)some) : 0;
+                const bool past_r = over == 0;
+                before = __shfl_sync(0xFFFFFFFFu, cum - run, at);
+                // ... and in it the id
+                int found = -1, latest = -1;
+                for (int i = i0 + at * len, e = min(i + len, i1); i < e && found < 0; i += 32) {
+                    const double l = i + lane < e ? left(row[i + lane], i + lane, S, whole) : 0.0;
+                    const double c32 = before + up_to(l);
+                    const unsigned any = __ballot_sync(0xFFFFFFFFu, l > 0.0), past = __ballot_sync(0xFFFFFFFFu, !past_r && l > 0.0 && c32 > target);
+                    if (past) found = i + __ffs((int)past) - 1;
+                    if (any) latest = i + 31 - __clz((int)any);
+                    before = __shfl_sync(0xFFFFFFFFu, c32, 31);
                 }
                 if (found < 0) found = latest;
                 if (lane == 0) c.out_tokens[(int64_t)b * c.max_tokens + n] = found < 0 ? -1 : first_id + found;
