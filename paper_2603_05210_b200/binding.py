@@ -564,7 +564,7 @@ def _heads(t: torch.Tensor, name: str, device: int) -> _VtHeads:
 
 def _vector(t: torch.Tensor, name: str, n: int | None, device: int, dtype: torch.dtype = torch.int32) -> int:
     """The address of a contiguous vector of n entries (None: any number) on the current device."""
-    if t.dtype is not dtype or t.dim() != 1 or t.get_device() != device or not t.is_contiguous() or (n is not None and t.shape[0] != n):
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or (t.shape != (n,) if n is not None else t.dim() != 1):
         raise ValueError(f"{name}: expected a contiguous {dtype} vector{'' if n is None else f' of {n}'} on the current CUDA device")
     return t.data_ptr()
 
@@ -649,22 +649,12 @@ class VtCache:
     lens = property(lambda self: self._lens)
 
 
-def _rope_args(q, k, positions, rope: VtRope):
-    device = torch.cuda.current_device()
-    hq = _heads(q, "q", device)
-    hk = None if k is None else _heads(k, "k", device)
-    if k is not None and (k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]):
-        raise ValueError("q and k disagree on tokens or D")
-    _vector(positions, "positions", q.shape[0], device)
-    if rope.table.get_device() != device:
-        raise ValueError("rope: its table lies on another device")
-    return device, hq, hk
-
-
-def _heads_out(t, name, like, device):
+def _heads_out(t, name, shape, like, device):
+    """(tensor, _VtHeads) of an output of the shape of `like`: the caller's, or a new one."""
     if t is None:
         t = torch.empty_like(like, memory_format=torch.contiguous_format)
-    elif t.shape != like.shape:
+        return t, _VtHeads(t.data_ptr(), (shape[1] or 1) * shape[2], shape[2])
+    if t.shape != shape:
         raise ValueError(f"{name}: expected the shape of its input")
     return t, _heads(t, name, device)
 
@@ -675,18 +665,27 @@ def vt_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, ro
 
     ``inverse`` turns back, which is the gradient's way: (grad_q, grad_k) = vt_rope(grad of q, grad of k, ..., inverse=True).  The outputs may
     be the inputs themselves."""
-    device, hq, hk = _rope_args(q, k, positions, rope)
-    out_q, ho = _heads_out(out_q, "out_q", q, device)
-    ko = None
+    device = torch.cuda.current_device()
+    hq, shape = _heads(q, "q", device), q.shape
+    N, Hq, D = shape
+    _vector(positions, "positions", N, device)
+    table = rope.table
+    if table.get_device() != device:
+        raise ValueError("rope: its table lies on another device")
+    out_q, ho = _heads_out(out_q, "out_q", shape, q, device)
+    Hkv, hk, ko = 0, None, None
     if k is not None:
-        out_k, ko = _heads_out(out_k, "out_k", k, device)
+        hk, kshape = _heads(k, "k", device), k.shape
+        if kshape[0] != N or kshape[2] != D:
+            raise ValueError("q and k disagree on tokens or D")
+        Hkv = kshape[1]
+        out_k, ko = _heads_out(out_k, "out_k", kshape, k, device)
+        hk, ko = ctypes.byref(hk), ctypes.byref(ko)
     elif out_k is not None:
         raise ValueError("out_k needs k")
-    N, Hq, D = q.shape
-    _check(lib().vt_rope(ctypes.byref(hq), None if hk is None else ctypes.byref(hk), positions.data_ptr(), rope.table.data_ptr(), N, Hq,
-                         0 if k is None else k.shape[1], D, rope.rot_dim, rope.amplitude,
-                         (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), ctypes.byref(ho),
-                         None if ko is None else ctypes.byref(ko), _stream_of(device)), "vt_rope")
+    _check(lib().vt_rope(ctypes.byref(hq), hk, positions.data_ptr(), table.data_ptr(), N, Hq, Hkv, D, rope.rot_dim, rope.amplitude,
+                         (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), ctypes.byref(ho), ko,
+                         _stream_of(device)), "vt_rope")
     return out_q, out_k
 
 
@@ -695,16 +694,20 @@ def vt_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions:
     """q [N, Hq, D] turned; k [N, heads, D] turned into the cache and v beside it, at places lens[b], lens[b] + 1, ... of each request.
 
     Request b has the tokens from ``cu_tokens``[b] to ``cu_tokens``[b + 1]; tokens outside all requests are padding, and left alone."""
-    device, hq, hk = _rope_args(q, k, positions, rope)
-    hv = _heads(v, "v", device)
-    c = cache._struct
-    if k.shape != v.shape or k.shape[1] != c.heads or k.shape[2] != c.head_dim or cache._device != device:
-        raise ValueError("k, v and the cache disagree on tokens, heads, D or device")
+    device = torch.cuda.current_device()
+    hq, hk, hv, shape, kshape, c = _heads(q, "q", device), _heads(k, "k", device), _heads(v, "v", device), q.shape, k.shape, cache._struct
+    N, Hq, D = shape
+    if kshape != v.shape or kshape[0] != N or kshape[1] != c.heads or kshape[2] != D or D != c.head_dim or cache._device != device:
+        raise ValueError("q, k, v and the cache disagree on tokens, heads, D or device")
+    _vector(positions, "positions", N, device)
     cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
-    out_q, ho = _heads_out(out_q, "out_q", q, device)
-    _check(lib().vt_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), positions.data_ptr(), cu, rope.table.data_ptr(), q.shape[0],
-                                q.shape[1], rope.rot_dim, rope.amplitude, VT_ROPE_INTERLEAVED if rope.interleaved else 0, ctypes.byref(ho),
-                                cache._ref, _stream_of(device)), "vt_rope_append")
+    table = rope.table
+    if table.get_device() != device:
+        raise ValueError("rope: its table lies on another device")
+    out_q, ho = _heads_out(out_q, "out_q", shape, q, device)
+    _check(lib().vt_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), positions.data_ptr(), cu, table.data_ptr(), N, Hq,
+                                rope.rot_dim, rope.amplitude, VT_ROPE_INTERLEAVED if rope.interleaved else 0, ctypes.byref(ho), cache._ref,
+                                _stream_of(device)), "vt_rope_append")
     return out_q
 
 
@@ -737,9 +740,8 @@ def vt_tree_attention(q: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache, 
     it a token attends itself and those before it.  ``scale`` is D^-0.5 unless it is given.  Rows outside all requests are left as they were.
     Time-outs and page ids outside the cache are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
     device = torch.cuda.current_device()
-    hq = _heads(q, "q", device)
-    N, Hq, D = q.shape
-    c = cache._struct
+    hq, shape, c = _heads(q, "q", device), q.shape, cache._struct
+    N, Hq, D = shape
     if D != c.head_dim or cache._device != device:
         raise ValueError("q and the cache disagree on D or device")
     cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
@@ -748,7 +750,7 @@ def vt_tree_attention(q: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache, 
         if mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != N or mask.get_device() != device or not mask.is_contiguous():
             raise ValueError("mask: expected a contiguous int32 tensor with a row per token on the current CUDA device")
         words = mask.shape[1]
-    out, ho = _heads_out(out, "out", q, device)
+    out, ho = _heads_out(out, "out", shape, q, device)
     lse = _new_or_given(lse, "lse", (N, Hq), torch.float32, q, device)
     if workspace is None:
         workspace = torch.empty(max(vt_tree_attention_workspace_bytes(Hq, c.heads, D, max_tokens), 256), dtype=torch.uint8, device=q.device)

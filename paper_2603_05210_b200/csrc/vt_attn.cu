@@ -36,7 +36,7 @@ constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
 constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
 constexpr int kAttnMaxStages = 12;
-constexpr int kAttnItemCost = 2;             // what an item's beginning and end cost, in tiles
+constexpr int kAttnItemCost = 3;             // what an item's beginning and end cost, in tiles
 constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
 constexpr uint32_t kAttnTmemO = 0, kAttnTmemS = 256;
 
@@ -64,7 +64,6 @@ struct AttnParams {
     int box_tokens;                          // tokens in a box of q
     int whole;                               // 1: items are not cut
     int min_run;                             // the least weight of a CTA's run
-    int ctas;
     int n_stages;
     uint32_t stages_inv;                     // 2^32 / n_stages, rounded up
     uint32_t q_block, q_slot;                // bytes of 64 columns of a row tile; of a row tile
@@ -95,6 +94,21 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t (&r)[32])
 }
 __device__ __forceinline__ void tc_ld64(uint32_t taddr, uint32_t (&r)[64]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -254,6 +268,11 @@ __device__ __forceinline__ uint32_t attn_bits(const int32_t* row, int words, int
     return up ? bits << up | ((1u << up) - 1u) : bits;
 }
 
+// Steps of 16 positions that hold any of the piece's j-th tile.
+__device__ __forceinline__ int attn_k_steps(const AttnPiece& w, int j) {
+    return min(kAttnKeys / 16, (w.keys - (w.t0 + j) * kAttnKeys + 15) >> 4);
+}
+
 struct AttnMaps {
     CUtensorMap q, k, v;
 };
@@ -264,13 +283,13 @@ struct AttnShared {
     int abort;
 };
 
-template <int D>
+template <int D, bool REP>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnParams p) {
     constexpr uint32_t kTile = kAttnKeys * D * 2;            // bytes of a K or V tile: D / 64 blocks of 128 positions x 128 bytes
     constexpr uint32_t kBlock = kAttnKeys * 128;
-    // D fp32, A and B bf16; S: 128 columns, both K-major; O: D columns, V with its columns fastest
-    constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kAttnKeys >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    // D fp32, A and B bf16; S: as many columns as positions (N / 8 from bit 17 on), both K-major; O: D columns, V with its columns fastest
+    constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);
     constexpr uint32_t kIdescO = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 
     // q's two slots, the ring, then what AttnShared and the barriers take.  No static part, so that the whole begins at a multiple of 1024.
@@ -294,7 +313,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         }
         for (uint32_t s = 0; s < 2; ++s) {
             mbar_init(q_full + 8u * s, 1);
-            mbar_init(q_empty + 8u * s, 1);
+            mbar_init(q_empty + 8u * s, REP ? 2 : 1);        // the last product that reads it, and the end of the item, which works in it
             mbar_init(s_full + 8u * s, 1);
             mbar_init(p_full + 8u * s, 4);
         }
@@ -449,7 +468,9 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                                 mbar_arrive_expect_tx(bar, p.q_tx + p.withheld);
 #pragma unroll
                                 for (int c = 0; c < D / 64; ++c)
-                                    tma_load_3d(to + c * p.q_block, &maps.q, c * 64, w.h * p.G, w.first + w.tok0 + s * p.tpt, bar);
+#pragma unroll
+                                    for (int k = 0; k < (REP ? 4 : 1); ++k)
+                                        tma_load_3d(to + c * p.q_block + k * 4096, &maps.q, c * 64, w.h * p.G, w.first + w.tok0 + s * p.tpt, bar);
                             }
                             __syncwarp();
                         }
@@ -521,9 +542,10 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     tc_fence_after();
                     if (attn_elect()) {
                         const uint64_t bd = attn_v_desc(ring + st * kTile);
+                        const int steps = attn_k_steps(w, i >> w.dual);
 #pragma unroll
                         for (int k = 0; k < kAttnKeys / 16; ++k)
-                            tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
+                            if (k < steps) tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
                                            i >= 2 || k > 0 ? 1u : 0u);
                         tc_commit(kv_empty + 8u * st);
                         if (i == H - 1) tc_commit(o_full);
@@ -537,11 +559,12 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
                     tc_fence_after();
                     if (attn_elect()) {
+                        const uint32_t idesc = kIdescS | ((uint32_t)attn_k_steps(w, (i + 2) >> w.dual) << 18);
                         const uint64_t a = smem_desc_sw128(q_smem + q_at * p.q_slot), bd = smem_desc_sw128(ring + st * kTile);
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)
                             tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
-                                        bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), kIdescS, k > 0 ? 1u : 0u);
+                                        bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
                         tc_commit(s_full + 8u * s);
                         tc_commit(kv_empty + 8u * st);
                         if ((i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
@@ -563,22 +586,27 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
                 const int j = w.value_at(e);
                 if (j >= 0 && w.t0 + j >= w.open) {
-                    // positions all rows attend stay as they are
-                    const int r0 = max(0, min(kAttnKeys, w.L - (w.t0 + j) * kAttnKeys));
+                    // positions all rows attend stay as they are, and no product reads past the last 16 that hold any
+                    const int tile0 = (w.t0 + j) * kAttnKeys;
+                    const int r0 = max(0, min(kAttnKeys, w.L - tile0)), r1 = attn_k_steps(w, j) * 16;
 #pragma unroll 1
                     for (int c = 0; c < D / 64; ++c) {
 #pragma unroll 4
-                        for (int i = r0 * 8 + lane; i < kAttnKeys * 8; i += 32) {
+                        for (int i = r0 * 8 + lane; i < r1 * 8; i += 32) {
                             uint4* u = reinterpret_cast<uint4*>(smem + (ring - base) + st * kTile + c * kBlock + i * 16);
                             uint4 x = *u;
-                            uint32_t* y = reinterpret_cast<uint32_t*>(&x);
-                            bool some = false;
+                            // an exponent of ones carries into the bit above it
+                            const uint32_t full = ((x.x & 0x7F807F80u) + 0x00800080u) | ((x.y & 0x7F807F80u) + 0x00800080u) |
+                                                  ((x.z & 0x7F807F80u) + 0x00800080u) | ((x.w & 0x7F807F80u) + 0x00800080u);
+                            if (__builtin_expect((full & 0x80008000u) != 0u, 0)) {
+                                uint32_t* y = reinterpret_cast<uint32_t*>(&x);
 #pragma unroll
-                            for (int g = 0; g < 4; ++g) {
-                                if ((y[g] & 0x7F800000u) == 0x7F800000u) { y[g] = (y[g] & 0x8000FFFFu) | 0x7F7F0000u; some = true; }
-                                if ((y[g] & 0x00007F80u) == 0x00007F80u) { y[g] = (y[g] & 0xFFFF8000u) | 0x00007F7Fu; some = true; }
+                                for (int g = 0; g < 4; ++g) {
+                                    if ((y[g] & 0x7F800000u) == 0x7F800000u) y[g] = (y[g] & 0x8000FFFFu) | 0x7F7F0000u;
+                                    if ((y[g] & 0x00007F80u) == 0x00007F80u) y[g] = (y[g] & 0xFFFF8000u) | 0x00007F7Fu;
+                                }
+                                *u = x;
                             }
-                            if (some) *u = x;
                         }
                     }
                     fence_proxy_async();
@@ -599,7 +627,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
         const uint32_t t_s = tmem + kAttnTmemS + 128u * s + lane_at, t_o = tmem + kAttnTmemO + 128u * s + lane_at;
         bool ok = true;
-        uint32_t s_phase = 0, o_phase = 0, meet_phase = 0;
+        uint32_t s_phase = 0, o_phase = 0, meet_phase = 0, item = 0;
         auto meet_others = [&]() -> bool {                   // the eight warps here
             __syncwarp();
             if (lane == 0) mbar_arrive(meet);
@@ -610,8 +638,9 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             const int H = w.steps();
             const int tile_tokens = w.dual ? (s ? w.ntok - p.tpt : p.tpt) : w.ntok;
             const int rows = tile_tokens * p.G;              // of this stream's tile
-            const bool real = r < rows, busy = quad * 32 < rows;
-            const int t = w.tok0 + (w.dual ? s * p.tpt : 0) + (real ? r / p.G : 0);      // the row's token within its request
+            const int my_row = REP ? lane : r;               // of the tile
+            const bool real = my_row < rows, busy = REP || quad * 32 < rows;
+            const int t = w.tok0 + (w.dual ? s * p.tpt : 0) + (real ? my_row / p.G : 0);      // its token within the request
             float m = -INFINITY, l = 0.0f;
 #pragma unroll 1
             for (int i = s; i < H; i += 2) {
@@ -620,13 +649,76 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 if (busy) {
                     tc_fence_after();
                     const int j = w.t0 + (i >> w.dual);
-                    if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
+                    // where a tile's row has grown past the maximum in use (mx - m is infinite while nothing has been attended yet)
+                    auto raise = [&](float mx) {
+                        const bool grow = real && mx > m && !((mx - m) * p.scale_log2 <= kAttnSlack);
+                        if (__any_sync(0xFFFFFFFFu, grow)) {
+                            const float f = grow ? ex2_approx((m - mx) * p.scale_log2) : 1.0f;
+                            if (grow) {
+                                m = mx;
+                                l *= f;
+                            }
+                            if (i >= 2) {
+#pragma unroll 1
+                                for (int c = 0; c < D / 32; ++c) {
+                                    uint32_t o[32];
+                                    tc_ld32(t_o + 32u * c, o);
+                                    tc_wait_ld();
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                    tc_st32(t_o + 32u * c, o);
+                                }
+                            }
+                        }
+                    };
+                    auto seen = [&](int c) -> uint32_t {     // which of the tile's positions 32 c .. the row attends
                         const int32_t* row = p.mask ? p.mask + (int64_t)(w.first + t) * p.mask_words : nullptr;
+                        const int at = j * kAttnKeys + 32 * c, n = w.keys - at;
+                        const uint32_t bits = attn_bits(row, p.mask_words, t, w.T, at - w.L);
+                        return bits & (n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u);
+                    };
+                  if constexpr (REP) {
+                    // the warp's own 32 positions of the tile; its weights of the others are 0
+                    uint32_t x[32], pk[16];
+                    tc_ld32(t_s + 32u * quad, x);
+                    tc_wait_ld();
+                    if (j >= w.open) {
+                        const uint32_t bits = seen(quad);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
+                    }
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) top[(e >> 1) & 1] = max3(top[(e >> 1) & 1], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                    __syncwarp();
+                    raise(fmaxf(top[0], top[1]));
+                    const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
+                    const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
+                    uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float a, b;
+                        unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, r2), a, b);
+                        a = ex2_approx(a);
+                        b = ex2_approx(b);
+                        if (e & 2) sum1 = add2(sum1, pack2(a, b));
+                        else sum0 = add2(sum0, pack2(a, b));
+                        pk[e / 2] = attn_bf16x2(a, b);
+                    }
+                    tc_st16(t_s + 16u * quad, pk);           // over scores of its own lanes, which it has read
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) pk[e] = 0u;
+#pragma unroll
+                    for (int k = 1; k < 4; ++k) tc_st16(t_s + 16u * ((quad + k) & 3), pk);
+                    float a, b;
+                    unpack2(add2(sum0, sum1), a, b);
+                    l += a + b;
+                  } else {
+                    if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            const int at = j * kAttnKeys + 32 * c, n = w.keys - at;
-                            uint32_t bits = attn_bits(row, p.mask_words, t, w.T, at - w.L);
-                            bits &= n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u;
+                            const uint32_t bits = seen(c);
                             uint32_t x[32];
                             __syncwarp();
                             tc_ld32(t_s + 32u * c, x);
@@ -650,27 +742,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3(top[(e >> 1) & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
                     }
-                    const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                    // (mx - m) is infinite while nothing has been attended yet
-                    const bool grow = real && mx > m && !((mx - m) * p.scale_log2 <= kAttnSlack);
-                    if (__any_sync(0xFFFFFFFFu, grow)) {
-                        const float f = grow ? ex2_approx((m - mx) * p.scale_log2) : 1.0f;
-                        if (grow) {
-                            m = mx;
-                            l *= f;
-                        }
-                        if (i >= 2) {
-#pragma unroll 1
-                            for (int c = 0; c < D / 32; ++c) {
-                                uint32_t o[32];
-                                tc_ld32(t_o + 32u * c, o);
-                                tc_wait_ld();
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tc_st32(t_o + 32u * c, o);
-                            }
-                        }
-                    }
+                    raise(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
                     const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
                     const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
                     uint64_t sum0 = 0ull, sum1 = 0ull;
@@ -694,6 +766,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     float a, b;
                     unpack2(add2(sum0, sum1), a, b);
                     l += a + b;
+                  }
                     tc_wait_st();
                     tc_fence_before();
                 }
@@ -705,6 +778,80 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             o_phase ^= 1u;
             tc_fence_after();
             const bool both = !w.dual && H > 1;              // the streams hold different positions of the same rows
+            const size_t piece = (size_t)(blockIdx.x * 2 + w.slot);
+            if constexpr (REP) {
+                // Eight parts of each row, by stream and warp, meet in the item's slot of q: all columns of up to 8 rows at a time, half of those
+                // of 16, a quarter of those of 32.  A thread adds up four columns of a row.
+                float4* xs = reinterpret_cast<float4*>(smem + (item++ & 1u) * p.q_slot);
+                const int log_rows = rows <= 8 ? 3 : rows <= 16 ? 4 : 5, rounds = 1 << (log_rows - 3), quads = (D / 4) >> (log_rows - 3);
+                sh.ms[s][r] = make_float2(m, l);
+#pragma unroll 1
+                for (int round = 0; round < rounds; ++round) {
+                    if (s == 0 || both) {
+                        const uint32_t at = t_o + (uint32_t)(round * quads * 4);
+#pragma unroll 1
+                        for (int c = 0; c < quads; c += 4) { // 16 columns at a time
+                            uint32_t o[16];
+                            tc_ld16(at + 4u * c, o);
+                            tc_wait_ld();
+                            if (real) {
+                                float4* to = xs + ((((s * 4 + quad) * quads + c) << log_rows) + lane);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    to[e << log_rows] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                                                    __uint_as_float(o[4 * e + 3]));
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    if (!meet_others()) { ok = false; break; }
+                    const int row = tid & ((1 << log_rows) - 1), parts = both ? 8 : 4;
+                    if (row < rows) {
+                        float2 ml[8];
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            ml[k] = sh.ms[k >> 2][(k & 3) * 32 + row];
+                            top = fmaxf(top, ml[k].x);
+                        }
+                        const float ref = top == -INFINITY ? 0.0f : top;
+                        float total = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            ml[k].x = ex2_approx((ml[k].x - ref) * p.scale_log2);
+                            total = fmaf(ml[k].y, ml[k].x, total);
+                        }
+                        const float inv = w.cut ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
+                        const int my_t = row / p.G, head = w.h * p.G + (row - my_t * p.G);
+                        const int64_t token = w.first + w.tok0 + my_t;
+                        for (int cq = tid >> log_rows; cq < quads; cq += 256 >> log_rows) {
+                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                if (k >= parts) break;
+                                const float4 u = xs[((k * quads + cq) << log_rows) + row];
+                                v = make_float4(fmaf(u.x, ml[k].x, v.x), fmaf(u.y, ml[k].x, v.y), fmaf(u.z, ml[k].x, v.z), fmaf(u.w, ml[k].x, v.w));
+                            }
+                            const int cq_all = round * quads + cq;
+                            if (w.cut) reinterpret_cast<float4*>(p.part_o)[(piece * (D / 4) + cq_all) * p.rows_max + row] = v;
+                            else
+                                *reinterpret_cast<uint2*>(p.out + token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq_all) =
+                                    make_uint2(attn_bf16x2(v.x * inv, v.y * inv), attn_bf16x2(v.z * inv, v.w * inv));
+                            if (cq_all == 0) {
+                                if (w.cut) p.part_ml[piece * p.rows_max + row] = make_float2(top, total);
+                                else if (p.lse) p.lse[token * p.Hq + head] = total == 0.0f ? -INFINITY : top * p.scale + logf(total);
+                            }
+                        }
+                    }
+                    if (round + 1 < rounds && !meet_others()) { ok = false; break; }
+                }
+                if (!ok) break;
+                fence_proxy_async();                         // the slot's next contents come by TMA
+                tc_fence_before();
+                if (!meet_others()) { ok = false; break; }
+                if (tid == 0) mbar_arrive(q_empty + 8u * ((item - 1u) & 1u));
+                continue;
+            }
             float f0 = 1.0f, f1 = 0.0f;                      // weights of stream 0's (of this stream's) and stream 1's O
             if (both) {
                 sh.ms[s][r] = make_float2(m, l);
@@ -720,7 +867,6 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 const uint32_t o_at = w.dual ? t_o : tmem + kAttnTmemO + lane_at;
                 const int c0 = both ? s * (D / 64) : 0, c1 = both ? c0 + D / 64 : D / 32;        // runs of 32 columns
                 const float inv = w.cut ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-                const size_t piece = (size_t)(blockIdx.x * 2 + w.slot);
                 uint16_t* to = p.out + (int64_t)(w.first + t) * p.out_ts + (int64_t)head * p.out_hs;
 #pragma unroll 1
                 for (int c = c0; c < c1; ++c) {
@@ -784,89 +930,78 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 }
 
 // ------------------------------------------------------------------------------------------ joining an item's pieces
-// lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  A block takes
-// a few rows of an item at a time (1024 / D: a float4 of a row per thread); which there are, each block works out from the runs' entries.
+// lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  Block (c, y) takes
+// the item that CTA c names, every gridDim.y-th group of its rows; a thread has four columns of two rows and asks for all it needs of four pieces
+// at once, so that an item of two pieces costs one memory round trip behind its entry.  Each thread works its rows' weights out for
+// itself: a step through shared memory, and finding the groups by a sum over all entries, took 25 us where this takes 8.
+constexpr int kJoinBatch = 4;
 template <int D>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnParams p) {
-    constexpr int kRows = 1024 / D, kQuads = D / 4;
-    __shared__ AttnSplit split[kAttnCtas];
-    __shared__ int ahead[kAttnCtas + 1];
-    __shared__ float2 weight[kAttnCtas][kRows];              // (m, l) of the pieces, then their weights
-    __shared__ float inv[kRows];
-    const int C = p.ctas, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kRows = 1024 / D, kQuads = D / 4;          // rows and runs of four columns that 256 threads cover
     grid_dependency_wait();
-    if (tid == 0) grid_launch_dependents();
-    for (int i = tid; i < C; i += 256) split[i] = p.splits[i];
-    __syncthreads();
-    if (warp == 0) {                                         // running number of row groups
-        int before = 0;
-        for (int i = lane; i - lane < C; i += 32) {
-            const int n = i < C ? (split[i].rows + kRows - 1) / kRows : 0;
-            int incl = n;
+    if (threadIdx.x == 0) grid_launch_dependents();
+    const AttnSplit d = p.splits[blockIdx.x];
+    const int cq = (int)threadIdx.x / kRows;
+    for (int row0 = (int)blockIdx.y * 2 * kRows + (int)threadIdx.x % kRows; row0 < d.rows; row0 += (int)gridDim.y * 2 * kRows) {
+        float m[2], l[2];
+        float4 o[2];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-                if (lane >= o) incl += v;
+        for (int u = 0; u < 2; ++u) {
+            m[u] = -INFINITY;
+            l[u] = 0.0f;
+            o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll 1
+        for (int i0 = 0; i0 < d.n_pieces; i0 += kJoinBatch) {
+            float2 ml[2][kJoinBatch];
+            float4 v[2][kJoinBatch];
+#pragma unroll
+            for (int k = 0; k < kJoinBatch; ++k) {
+                const int i = min(i0 + k, d.n_pieces - 1);   // (past the last: the last again, with no weight)
+                const size_t piece = (size_t)(d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0);
+                const float2* pm = p.part_ml + piece * p.rows_max;
+                const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece * kQuads + cq) * p.rows_max;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int row = min(row0 + u * kRows, d.rows - 1);
+                    ml[u][k] = pm[row];
+                    v[u][k] = po[row];
+                    if (i0 + k >= d.n_pieces) ml[u][k] = make_float2(-INFINITY, 0.0f);
+                }
             }
-            if (i < C) ahead[i] = before + incl - n;
-            before += __shfl_sync(0xFFFFFFFFu, incl, 31);
-        }
-        if (lane == 0) ahead[C] = before;
-    }
-    __syncthreads();
-    const int all = ahead[C];
-    for (int unit = blockIdx.x; unit < all; unit += gridDim.x) {
-        int lo = 0, hi = C;                                  // the last entry with ahead <= unit: it has rows
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (ahead[mid] <= unit) lo = mid;
-            else hi = mid;
-        }
-        const AttnSplit d = split[lo];
-        const int row0 = (unit - ahead[lo]) * kRows, rows = min(kRows, d.rows - row0);
-        auto piece = [&](int i) { return (size_t)((d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0)); };
-        for (int e = tid; e < d.n_pieces * kRows; e += 256) {
-            const int i = e / kRows, r = e % kRows;
-            if (r < rows) weight[i][r] = p.part_ml[piece(i) * p.rows_max + row0 + r];
-        }
-        __syncthreads();
-        for (int r = warp; r < rows; r += 8) {               // a warp per row
-            float m = -INFINITY, l = 0.0f;
-            for (int i = lane; i < d.n_pieces; i += 32) m = fmaxf(m, weight[i][r].x);
-            m = warp_max_f32(m);
-            for (int i = lane; i < d.n_pieces; i += 32) {
-                const float2 ml = weight[i][r];
-                const float f = ml.x == m ? 1.0f : ex2_approx((ml.x - m) * p.scale_log2);
-                l += ml.y * f;
-                weight[i][r].x = f;
-            }
-            l = warp_sum_f32(l);
-            if (lane == 0) {
-                inv[r] = l == 0.0f ? 0.0f : 1.0f / l;
-                const int row = row0 + r;
-                if (p.lse) p.lse[(int64_t)(d.token0 + row / p.G) * p.Hq + d.head0 + row % p.G] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                float top = m[u];
+#pragma unroll
+                for (int k = 0; k < kJoinBatch; ++k) top = fmaxf(top, ml[u][k].x);
+                const float ref = top == -INFINITY ? 0.0f : top;
+                const float f = ex2_approx((m[u] - ref) * p.scale_log2);
+                m[u] = top;
+                l[u] *= f;
+                o[u] = make_float4(o[u].x * f, o[u].y * f, o[u].z * f, o[u].w * f);
+#pragma unroll
+                for (int k = 0; k < kJoinBatch; ++k) {
+                    if (i0 + k >= d.n_pieces) break;         // (its O may be anything)
+                    const float w = ex2_approx((ml[u][k].x - ref) * p.scale_log2);
+                    l[u] = fmaf(ml[u][k].y, w, l[u]);
+                    o[u].x = fmaf(v[u][k].x, w, o[u].x);
+                    o[u].y = fmaf(v[u][k].y, w, o[u].y);
+                    o[u].z = fmaf(v[u][k].z, w, o[u].z);
+                    o[u].w = fmaf(v[u][k].w, w, o[u].w);
+                }
             }
         }
-        __syncthreads();
-        const int r = tid % kRows, cq = tid / kRows;
-        if (r < rows) {
-            const int row = row0 + r;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-            for (int i = 0; i < d.n_pieces; ++i) {
-                const float4 v = reinterpret_cast<const float4*>(p.part_o)[(piece(i) * kQuads + cq) * p.rows_max + row];
-                const float f = weight[i][r].x;
-                o.x += v.x * f;
-                o.y += v.y * f;
-                o.z += v.z * f;
-                o.w += v.w * f;
-            }
-            const float n = inv[r];
-            *reinterpret_cast<uint2*>(p.out + (int64_t)(d.token0 + row / p.G) * p.out_ts + (int64_t)(d.head0 + row % p.G) * p.out_hs + 4 * cq) =
-                make_uint2(attn_bf16x2(o.x * n, o.y * n), attn_bf16x2(o.z * n, o.w * n));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int row = row0 + u * kRows;
+            if (row >= d.rows) break;
+            const float n = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
+            const int t = row / p.G, token = d.token0 + t, head = d.head0 + (row - t * p.G);
+            *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq) =
+                make_uint2(attn_bf16x2(o[u].x * n, o[u].y * n), attn_bf16x2(o[u].z * n, o[u].w * n));
+            if (cq == 0 && p.lse) p.lse[(int64_t)token * p.Hq + head] = l[u] == 0.0f ? -INFINITY : m[u] * p.scale + logf(l[u]);
         }
-        __syncthreads();
     }
 }
 
@@ -901,14 +1036,23 @@ static vt_status cache_map(CUtensorMap* map, const void* ptr, const vt_cache& a,
     return make_tensor_map_bf16_nd(map, ptr, 4, dims, strides, box);
 }
 
-template <int D>
+template <int D, bool REP>
 static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint32_t smem, cudaStream_t st) {
     static std::atomic<unsigned long long> configured{0};
-    if (vt_status r = ensure_max_dyn_smem(reinterpret_cast<const void*>(attn_kernel<D>), kMaxDynSmem, &configured); r != VT_OK) return r;
-    cudaError_t e = launch_pdl(attn_kernel<D>, C, kAttnThreads, smem, st, maps, p);
+    if (vt_status r = ensure_max_dyn_smem(reinterpret_cast<const void*>(attn_kernel<D, REP>), kMaxDynSmem, &configured); r != VT_OK) return r;
+    cudaError_t e = launch_pdl(attn_kernel<D, REP>, C, kAttnThreads, smem, st, maps, p);
     count_launch();
     if (e == cudaSuccess && !p.whole) {
-        e = launch_pdl(attn_join_kernel<D>, 2 * C, 256, 0, st, p);
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)C, (unsigned)((p.rows_max + 2048 / D - 1) / (2048 / D)));
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, attn_join_kernel<D>, p);
         count_launch();
     }
     if (e == cudaSuccess) e = cudaGetLastError();
@@ -951,8 +1095,7 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.tpt = 128 / p.G;
     p.box_tokens = std::min(p.tpt, c.max_tokens);
     p.whole = (long long)a.max_pages * a.page_size <= (long long)kAttnWhole * kAttnKeys;
-    p.ctas = C;
-    p.min_run = 1;
+    p.min_run = p.rows_max > 128 ? 4 : 2;
     p.scale = c.scale;
     p.scale_log2 = c.scale * kLog2e;
     p.wait_ns = kWaitLimitNs;
@@ -961,9 +1104,10 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
         p.wait_ns = (unsigned long long)us * 1000ull;
     }
     const uint32_t rows = (uint32_t)(p.box_tokens * p.G);
-    p.q_block = (rows + 7) / 8 * 1024;
+    const bool few = p.rows_max <= 32;
+    p.q_block = few ? 16384u : (rows + 7) / 8 * 1024;
     p.q_slot = p.q_block * (D / 64);
-    p.q_tx = rows * 128u * (D / 64);
+    p.q_tx = rows * 128u * (D / 64) * (few ? 4u : 1u);
     p.page_tx = (uint32_t)std::min(p.page_size, kAttnKeys) * 128u;
     // five stages of 32 KB beside two full row tiles: 160 KB in flight
     const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 11 + 2 * kAttnPieces);
@@ -981,7 +1125,8 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     }
     if (vt_status r = cache_map(&maps.k, a.k, a, a.k_token_stride, a.k_head_stride, a.k_page_stride); r != VT_OK) return r;
     if (vt_status r = cache_map(&maps.v, a.v, a, a.v_token_stride, a.v_head_stride, a.v_page_stride); r != VT_OK) return r;
-    return D == 64 ? run_attn<64>(maps, p, C, smem, st) : run_attn<128>(maps, p, C, smem, st);
+    if (few) return D == 64 ? run_attn<64, true>(maps, p, C, smem, st) : run_attn<128, true>(maps, p, C, smem, st);
+    return D == 64 ? run_attn<64, false>(maps, p, C, smem, st) : run_attn<128, false>(maps, p, C, smem, st);
 }
 
 }  // namespace vt
