@@ -137,6 +137,8 @@ __device__ __forceinline__ bool attn_elect() {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
     return p != 0;
 }
+// fence_proxy_async for shared memory alone: it does not wait for stores of results.
+__device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -386,6 +388,9 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         // a lane per box: column block lane / np, page lane % np of the tile
         const int col = lane / np, pg = lane - col * np;
         const bool mine = col < D / 64;
+        const int tpp = p.page_size / kAttnKeys;             // tiles per page, 0 or 1 where a tile has whole pages
+        const uint32_t n_boxes = (uint32_t)np * (D / 64), box_at = (uint32_t)col * kBlock + (uint32_t)(pg * pr) * 128u;
+        uint32_t stage = 0, empty_phase = 1;
         bool bad = false;
         AttnSplit split{};
         auto publish = [&](const AttnPiece& w) -> bool {
@@ -452,11 +457,12 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         w.pad[0] = w.pad[1] = 0;
                         ok = publish(w);
                         if (!ok) break;
-                        auto place_of = [&](int j) { return (w.t0 + j) * kAttnKeys + pg * pr; };
+                        // a lane's page of tile t0 + j, where the tile has one there
+                        const int32_t* row = p.page_table + w.b * p.table_stride;
+                        const int end = (w.keys - pg * pr + kAttnKeys - 1) / kAttnKeys - w.t0;      // the lane's boxes end with this j
                         auto page_of = [&](int j) -> int {
-                            const int at = place_of(j);
-                            if (j >= w.n || !mine || at >= w.keys) return -1;
-                            return p.page_table[w.b * p.table_stride + (unsigned)at / (unsigned)p.page_size];
+                            if (j >= w.n || !mine || j >= end) return -1;
+                            return row[tpp > 1 ? (unsigned)(w.t0 + j) / (unsigned)tpp : (unsigned)((w.t0 + j) * np + pg)];
                         };
                         int page_k = page_of(0), page_v = page_k, page_last = page_k;        // of the next K and V, and of the last K
 #pragma unroll 1
@@ -475,22 +481,27 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             __syncwarp();
                         }
                         int page_next = page_of(1);                      // one K ahead of its use
+                        const int last_tile = attn_tiles(w.keys);
 #pragma unroll 1
-                        for (uint32_t e = 0; e < 2u * w.n && ok; ++e, ++loads) {
-                            const int jv = w.value_at(e), j = jv >= 0 ? jv : (int)(e + 1u) >> 1;
-                            const uint32_t turn = turn_of(loads), s = loads - turn * ST;
-                            if (turn > 0 && !wait(kv_empty + 8u * s, (turn - 1u) & 1u)) { ok = false; break; }
-                            const int at = place_of(j), page = jv >= 0 ? page_v : page_k;
-                            const bool there = mine && at < w.keys;
-                            const uint32_t boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
-                            if (lane == 0) mbar_arrive_expect_tx(kv_full + 8u * s, boxes * p.page_tx + p.withheld);
+                        for (uint32_t e = 0; e < 2u * w.n; ++e) {
+                            const int jv = w.value_at(e), j = jv >= 0 ? jv : (int)(e + 1u) >> 1, page = jv >= 0 ? page_v : page_k;
+                            if (!wait(kv_empty + 8u * stage, empty_phase)) { ok = false; break; }        // (at first there is nothing to wait for)
+                            const bool there = mine && j < end;
+                            uint32_t boxes = n_boxes;
+                            if (w.t0 + j + 1 == last_tile) boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
+                            const uint32_t bar = kv_full + 8u * stage;
+                            if (lane == 0) mbar_arrive_expect_tx(bar, boxes * p.page_tx + p.withheld);
                             __syncwarp();
                             if (there) {
                                 bad |= (unsigned)page >= (unsigned)p.n_pages;
-                                tma_load_4d(ring + s * kTile + col * kBlock + (uint32_t)(pg * pr) * 128u, jv >= 0 ? &maps.v : &maps.k, col * 64,
-                                            (int)((unsigned)at % (unsigned)p.page_size), w.h, page, kv_full + 8u * s);
+                                const int off = tpp > 1 ? (int)((unsigned)(w.t0 + j) % (unsigned)tpp) * kAttnKeys : 0;
+                                tma_load_4d(ring + stage * kTile + box_at, jv >= 0 ? &maps.v : &maps.k, col * 64, off, w.h, page, bar);
                             }
                             __syncwarp();
+                            if (++stage == ST) {
+                                stage = 0;
+                                empty_phase ^= 1u;
+                            }
                             if (jv >= 0) {
                                 page_v = page_last;                      // K(j + 1) is on its way
                             } else {
@@ -609,7 +620,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             }
                         }
                     }
-                    fence_proxy_async();
+                    fence_proxy_async_shared();
                     __syncwarp();
                 }
                 if (lane == 0) {
@@ -846,7 +857,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                     if (round + 1 < rounds && !meet_others()) { ok = false; break; }
                 }
                 if (!ok) break;
-                fence_proxy_async();                         // the slot's next contents come by TMA
+                fence_proxy_async_shared();                         // the slot's next contents come by TMA
                 tc_fence_before();
                 if (!meet_others()) { ok = false; break; }
                 if (tid == 0) mbar_arrive(q_empty + 8u * ((item - 1u) & 1u));
