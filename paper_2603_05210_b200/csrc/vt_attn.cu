@@ -30,8 +30,8 @@ namespace vt {
 int gemm_withheld_us();                      // see vt_test_withhold_copies
 
 constexpr int kAttnKeys = 128;               // positions per tile
-constexpr int kAttnThreads = 11 * 32;
-constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10;       
+constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10, kAttnIssuer1 = 11;      // (the last with few rows alone)
+constexpr int attn_threads(bool few) { return (few ? 12 : 11) * 32; }
 constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
 constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
@@ -286,7 +286,7 @@ struct AttnShared {
 };
 
 template <int D, bool REP>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(attn_threads(REP), 1)
 attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnParams p) {
     constexpr uint32_t kTile = kAttnKeys * D * 2;            // bytes of a K or V tile: D / 64 blocks of 128 positions x 128 bytes
     constexpr uint32_t kBlock = kAttnKeys * 128;
@@ -304,7 +304,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
     const uint32_t kv_full = base + p.bar_off, kv_empty = kv_full + 8u * ST, v_clean = kv_empty + 8u * ST;
     const uint32_t q_full = v_clean + 8u * ST, q_empty = q_full + 16u, s_full = q_empty + 16u, p_full = s_full + 16u;
     const uint32_t o_full = p_full + 16u, meet = o_full + 8u, drain = meet + 8u;
-    const uint32_t piece_full = drain + 8u, piece_empty = piece_full + 8u * kAttnPieces;
+    const uint32_t piece_full = drain + 16u, piece_empty = piece_full + 8u * kAttnPieces;
     volatile int* abort_flag = &sh.abort;
 
     if (tid == 0) {
@@ -315,17 +315,18 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         }
         for (uint32_t s = 0; s < 2; ++s) {
             mbar_init(q_full + 8u * s, 1);
-            mbar_init(q_empty + 8u * s, REP ? 2 : 1);        // the last product that reads it, and the end of the item, which works in it
+            mbar_init(q_empty + 8u * s, REP ? 3 : 1);        // the products that read it, and the end of the item, which works in it
             mbar_init(s_full + 8u * s, 1);
             mbar_init(p_full + 8u * s, 4);
         }
         for (uint32_t s = 0; s < kAttnPieces; ++s) {
             mbar_init(piece_full + 8u * s, 1);
-            mbar_init(piece_empty + 8u * s, kAttnThreads / 32 - 1);
+            mbar_init(piece_empty + 8u * s, attn_threads(REP) / 32 - 1);
         }
-        mbar_init(o_full, 1);
+        mbar_init(o_full, REP ? 2 : 1);
         mbar_init(meet, 8);
         mbar_init(drain, 1);
+        mbar_init(drain + 8u, 1);
         *abort_flag = 0;
         fence_mbar_init();
     }
@@ -534,17 +535,21 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         }
         if (lane == 0 && !p.whole) p.splits[cta] = split;
         if (bad) atomicOr(&p.hdr->status, kStatusPage);
-    } else if (warp == kAttnIssuer) {
-        // ---------------------------------------------------------------- MMA issuer
-        // One for both streams: P V and the next S of one, then of the other, so that the streams' scores are ready at different times.  (With an
-        // issuer each, both streams fall into step, and exponentials and products take turns instead of overlapping: two long
-        // documents under 60 drafted tokens 120 -> 133 us.)
+    } else if (warp == kAttnIssuer || (REP && warp == kAttnIssuer1)) {
+        // ---------------------------------------------------------------- MMA issuers
+        // Issuing takes 50 cycles a product and 120 a wait, 1400 per half-step.  Few rows: one issuer per stream, as one for both would be what
+        // all wait for.  Otherwise one for both: P V and the next S of one stream, then of the other, so that the streams' scores are ready at
+        // different times (with an issuer each, both fall into step, and exponentials and products take turns instead of overlapping: two long
+        // documents under 60 drafted tokens 120 -> 133 us).
         bool ok = true;
         uint32_t p_phase = 0;
+        uint32_t o_phase = 1, item = 0;
+        const int own = REP ? (warp == kAttnIssuer ? 0 : 1) : 0;             // the first half-step it issues
         for (AttnPiece w; ok && take(w);) {
             const int H = w.steps();
+            if (REP && !wait(q_full + 8u * (q_n & 1u), (q_n >> 1) & 1u)) break;
 #pragma unroll 1
-            for (int i = -2; i < H; ++i) {                   // P V of half-step i, then S of the stream's next
+            for (int i = own - 2; i < H; i += REP ? 2 : 1) { // P V of half-step i, then S of the stream's next
                 const int s = i & 1;
                 if (i >= 0) {
                     const uint32_t place = loads + w.v_at(i >> w.dual), turn = turn_of(place), st = place - turn * ST;
@@ -559,13 +564,13 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             if (k < steps) tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
                                            i >= 2 || k > 0 ? 1u : 0u);
                         tc_commit(kv_empty + 8u * st);
-                        if (i == H - 1) tc_commit(o_full);
+                        if (!REP && i == H - 1) tc_commit(o_full);
                     }
                     __syncwarp();
                 }
                 if (i + 2 < H) {
                     const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), q_at = qn & 1u;
-                    if (i + 2 <= w.dual && !wait(q_full + 8u * q_at, (qn >> 1) & 1u)) { ok = false; break; }
+                    if (!REP && i + 2 <= w.dual && !wait(q_full + 8u * q_at, (qn >> 1) & 1u)) { ok = false; break; }
                     const uint32_t place = loads + w.k_at((i + 2) >> w.dual), turn = turn_of(place), st = place - turn * ST;
                     if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
                     tc_fence_after();
@@ -578,12 +583,21 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                                         bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
                         tc_commit(s_full + 8u * s);
                         tc_commit(kv_empty + 8u * st);
-                        if ((i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
+                        if (!REP && (i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
                     }
                     __syncwarp();
                 }
             }
             if (!ok) break;
+            if constexpr (REP) {                             // also of a stream that has no part in the item: none is a phase ahead
+                if (item++ > 0 && !wait(o_full, o_phase)) break;
+                o_phase ^= 1u;
+                if (attn_elect()) {
+                    tc_commit(q_empty + 8u * (q_n & 1u));
+                    tc_commit(o_full);
+                }
+                __syncwarp();
+            }
             loads += 2u * w.n;
             q_n += 1u + w.dual;
         }
@@ -924,9 +938,10 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
     tc_fence_before();
     __syncthreads();
     if (__builtin_expect(*abort_flag != 0, 0)) {             // copies and MMAs in flight must end before their memory is given back
-        if (warp == kAttnIssuer && attn_elect()) {
-            tc_commit(drain);
-            (void)mbar_wait(drain, 0u, p.wait_ns);
+        if ((warp == kAttnIssuer || warp == kAttnIssuer1) && attn_elect()) {
+            const uint32_t bar = drain + (warp == kAttnIssuer ? 0u : 8u);
+            tc_commit(bar);
+            (void)mbar_wait(bar, 0u, p.wait_ns);
         }
         if (warp == kAttnProducer && lane == 0) {            // longer than any copy takes
             const unsigned long long now = global_timer_ns();
@@ -1038,20 +1053,22 @@ static AttnLayout attn_layout(int Hq, int heads, int D, int max_tokens) {
 size_t attn_workspace_bytes(int Hq, int heads, int D, int max_tokens) { return attn_layout(Hq, heads, D, max_tokens).total; }
 
 // (defined beside make_tensor_map_bf16)
-vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box,
+                                  bool alone);
 
 static vt_status cache_map(CUtensorMap* map, const void* ptr, const vt_cache& a, int64_t token, int64_t head, int64_t page) {
     const uint64_t dims[4] = {(uint64_t)a.head_dim, (uint64_t)a.page_size, (uint64_t)a.heads, (uint64_t)a.n_pages};
     const uint64_t strides[3] = {(uint64_t)token * 2, (uint64_t)head * 2, (uint64_t)page * 2};
     const uint32_t box[4] = {(uint32_t)kBoxK, (uint32_t)std::min(a.page_size, kAttnKeys), 1, 1};
-    return make_tensor_map_bf16_nd(map, ptr, 4, dims, strides, box);
+    // 64 columns whose neighbours in memory belong to another head, and to another time (24 x 8 over 10000, D = 64: 475 -> 410 us)
+    return make_tensor_map_bf16_nd(map, ptr, 4, dims, strides, box, a.head_dim == kBoxK && token != a.head_dim);
 }
 
 template <int D, bool REP>
 static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint32_t smem, cudaStream_t st) {
     static std::atomic<unsigned long long> configured{0};
     if (vt_status r = ensure_max_dyn_smem(reinterpret_cast<const void*>(attn_kernel<D, REP>), kMaxDynSmem, &configured); r != VT_OK) return r;
-    cudaError_t e = launch_pdl(attn_kernel<D, REP>, C, kAttnThreads, smem, st, maps, p);
+    cudaError_t e = launch_pdl(attn_kernel<D, REP>, C, attn_threads(REP), smem, st, maps, p);
     count_launch();
     if (e == cudaSuccess && !p.whole) {
         cudaLaunchConfig_t cfg{};
@@ -1121,7 +1138,7 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.q_tx = rows * 128u * (D / 64) * (few ? 4u : 1u);
     p.page_tx = (uint32_t)std::min(p.page_size, kAttnKeys) * 128u;
     // five stages of 32 KB beside two full row tiles: 160 KB in flight
-    const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 11 + 2 * kAttnPieces);
+    const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces);
     p.n_stages = (int)std::min((uint32_t)kAttnMaxStages, ((uint32_t)kMaxDynSmem - tail - 2 * p.q_slot) / tile);
     p.stages_inv = (uint32_t)((0x100000000ull + p.n_stages - 1) / p.n_stages);
     p.shared_off = 2 * p.q_slot + p.n_stages * tile;
@@ -1132,7 +1149,7 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
         const uint64_t dims[3] = {(uint64_t)D, (uint64_t)c.Hq, (uint64_t)c.N};
         const uint64_t strides[2] = {(uint64_t)c.q.head_stride * 2, (uint64_t)c.q.token_stride * 2};
         const uint32_t box[3] = {(uint32_t)kBoxK, (uint32_t)p.G, (uint32_t)p.box_tokens};
-        if (vt_status r = make_tensor_map_bf16_nd(&maps.q, c.q.ptr, 3, dims, strides, box); r != VT_OK) return r;
+        if (vt_status r = make_tensor_map_bf16_nd(&maps.q, c.q.ptr, 3, dims, strides, box, false); r != VT_OK) return r;
     }
     if (vt_status r = cache_map(&maps.k, a.k, a, a.k_token_stride, a.k_head_stride, a.k_page_stride); r != VT_OK) return r;
     if (vt_status r = cache_map(&maps.v, a.v, a, a.v_token_stride, a.v_head_stride, a.v_page_stride); r != VT_OK) return r;

@@ -394,7 +394,9 @@ vt_status make_tensor_map_bf16_ld(CUtensorMap* map, const void* ptr, int rows, i
     return cr == CUDA_SUCCESS ? VT_OK : driver_fail((int)cr);
 }
 // bf16 tensor of up to five dimensions, the first running fastest; strides in bytes, of the others; the box is kBoxK elements of the first.
-vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+// alone: what lies beside the box's 128-byte rows is not read soon, and is not brought into L2 with them.
+vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box,
+                                  bool alone) {
     EncodeTiledFn enc;
     vt_status r = get_encode(&enc);
     if (r != VT_OK) return r;
@@ -407,7 +409,7 @@ vt_status make_tensor_map_bf16_nd(CUtensorMap* map, const void* ptr, int rank, c
         elem[i] = 1;
     }
     CUresult cr = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(ptr), d, st, bx, elem,
-                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, alone ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return cr == CUDA_SUCCESS ? VT_OK : driver_fail((int)cr);
 }
