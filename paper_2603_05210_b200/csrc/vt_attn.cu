@@ -30,8 +30,8 @@ namespace vt {
 int gemm_withheld_us();                      // see vt_test_withhold_copies
 
 constexpr int kAttnKeys = 128;               // positions per tile
-constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10, kAttnIssuer1 = 11;      // (the last with few rows alone)
-constexpr int attn_threads(bool few) { return (few ? 12 : 11) * 32; }
+constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10, kAttnProducerV = 11, kAttnIssuer1 = 12;      // (the last with few rows alone)
+constexpr int attn_threads(bool few) { return (few ? 13 : 12) * 32; }
 constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
 constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
@@ -364,6 +364,46 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         return w.n > 0;
     };
 
+    // Copies of a piece's key tiles, or of its value tiles, from ring place `loads` on: a lane per box, column block lane / np, page lane % np of
+    // the tile.  A box costs the warp 100 cycles, so either kind has a warp of its own.
+    bool bad = false;
+    auto copy_tiles = [&](const AttnPiece& w, uint32_t loads, bool values) -> bool {
+        const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
+        const int col = lane / np, pg = lane - col * np;
+        const bool mine = col < D / 64;
+        const int tpp = p.page_size / kAttnKeys;             // tiles per page, 0 or 1 where a tile has whole pages
+        const uint32_t box_at = ring + (uint32_t)col * kBlock + (uint32_t)(pg * pr) * 128u;
+        const CUtensorMap* map = values ? &maps.v : &maps.k;
+        const int32_t* row = p.page_table + w.b * p.table_stride;
+        const int end = (w.keys - pg * pr + kAttnKeys - 1) / kAttnKeys - w.t0;      // the lane's boxes end with this j
+        auto page_of = [&](int j) -> int {
+            if (j >= w.n || !mine || j >= end) return -1;
+            return row[tpp > 1 ? (unsigned)(w.t0 + j) / (unsigned)tpp : (unsigned)((w.t0 + j) * np + pg)];
+        };
+        const int last_tile = attn_tiles(w.keys) - 1 - w.t0;
+        int page = page_of(0);
+#pragma unroll 1
+        for (int j = 0; j < w.n; ++j) {
+            const int page_next = page_of(j + 1);            // one ahead of its use
+            const uint32_t place = loads + (values ? w.v_at(j) : w.k_at(j)), turn = turn_of(place), stage = place - turn * ST;
+            if (!wait(kv_empty + 8u * stage, (turn & 1u) ^ 1u)) return false;        // (in the first turn there is nothing to wait for)
+            const bool there = mine && j < end;
+            uint32_t boxes = (uint32_t)np * (D / 64);
+            if (j == last_tile) boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
+            const uint32_t bar = kv_full + 8u * stage;
+            if (lane == 0) mbar_arrive_expect_tx(bar, boxes * p.page_tx + p.withheld);
+            __syncwarp();
+            if (there) {
+                bad |= (unsigned)page >= (unsigned)p.n_pages;
+                const int off = tpp > 1 ? (int)((unsigned)(w.t0 + j) % (unsigned)tpp) * kAttnKeys : 0;
+                tma_load_4d(box_at + stage * kTile, map, col * 64, off, w.h, page, bar);
+            }
+            __syncwarp();
+            page = page_next;
+        }
+        return true;
+    };
+
     uint32_t loads = 0;                                      // ring places used by the pieces before
     uint32_t q_n = 0;                                        // q slots used by them
     if (warp == kAttnProducer) {
@@ -385,14 +425,6 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         const AttnCut cut(W, C);
         const long long g0 = cta < C ? cut.start(cta) : 0, g1 = cta < C ? cut.start(cta + 1) : 0;
         uint32_t made = 0;
-        const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
-        // a lane per box: column block lane / np, page lane % np of the tile
-        const int col = lane / np, pg = lane - col * np;
-        const bool mine = col < D / 64;
-        const int tpp = p.page_size / kAttnKeys;             // tiles per page, 0 or 1 where a tile has whole pages
-        const uint32_t n_boxes = (uint32_t)np * (D / 64), box_at = (uint32_t)col * kBlock + (uint32_t)(pg * pr) * 128u;
-        uint32_t stage = 0, empty_phase = 1;
-        bool bad = false;
         AttnSplit split{};
         auto publish = [&](const AttnPiece& w) -> bool {
             const uint32_t s = made % kAttnPieces, turn = made / kAttnPieces;
@@ -458,14 +490,6 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         w.pad[0] = w.pad[1] = 0;
                         ok = publish(w);
                         if (!ok) break;
-                        // a lane's page of tile t0 + j, where the tile has one there
-                        const int32_t* row = p.page_table + w.b * p.table_stride;
-                        const int end = (w.keys - pg * pr + kAttnKeys - 1) / kAttnKeys - w.t0;      // the lane's boxes end with this j
-                        auto page_of = [&](int j) -> int {
-                            if (j >= w.n || !mine || j >= end) return -1;
-                            return row[tpp > 1 ? (unsigned)(w.t0 + j) / (unsigned)tpp : (unsigned)((w.t0 + j) * np + pg)];
-                        };
-                        int page_k = page_of(0), page_v = page_k, page_last = page_k;        // of the next K and V, and of the last K
 #pragma unroll 1
                         for (int s = 0; s < 1 + w.dual && ok; ++s, ++q_n) {          // rows of q
                             const uint32_t slot = q_n & 1u, turn = q_n >> 1;
@@ -481,36 +505,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             }
                             __syncwarp();
                         }
-                        int page_next = page_of(1);                      // one K ahead of its use
-                        const int last_tile = attn_tiles(w.keys);
-#pragma unroll 1
-                        for (uint32_t e = 0; e < 2u * w.n; ++e) {
-                            const int jv = w.value_at(e), j = jv >= 0 ? jv : (int)(e + 1u) >> 1, page = jv >= 0 ? page_v : page_k;
-                            if (!wait(kv_empty + 8u * stage, empty_phase)) { ok = false; break; }        // (at first there is nothing to wait for)
-                            const bool there = mine && j < end;
-                            uint32_t boxes = n_boxes;
-                            if (w.t0 + j + 1 == last_tile) boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
-                            const uint32_t bar = kv_full + 8u * stage;
-                            if (lane == 0) mbar_arrive_expect_tx(bar, boxes * p.page_tx + p.withheld);
-                            __syncwarp();
-                            if (there) {
-                                bad |= (unsigned)page >= (unsigned)p.n_pages;
-                                const int off = tpp > 1 ? (int)((unsigned)(w.t0 + j) % (unsigned)tpp) * kAttnKeys : 0;
-                                tma_load_4d(ring + stage * kTile + box_at, jv >= 0 ? &maps.v : &maps.k, col * 64, off, w.h, page, bar);
-                            }
-                            __syncwarp();
-                            if (++stage == ST) {
-                                stage = 0;
-                                empty_phase ^= 1u;
-                            }
-                            if (jv >= 0) {
-                                page_v = page_last;                      // K(j + 1) is on its way
-                            } else {
-                                page_last = page_k;
-                                page_k = page_next;
-                                page_next = page_of(j + 2);
-                            }
-                        }
+                        ok = ok && copy_tiles(w, loads, false);
+                        loads += 2u * w.n;
                         // the first CTA whose run begins behind the item's first tile names it for the join
                         if (first && w.t0 > 0) {
                             const int c0 = cut.of(s0);
@@ -534,6 +530,11 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             (void)publish(end);
         }
         if (lane == 0 && !p.whole) p.splits[cta] = split;
+        if (bad) atomicOr(&p.hdr->status, kStatusPage);
+    } else if (warp == kAttnProducerV) {
+        // ---------------------------------------------------------------- producer of values
+        bool ok = true;
+        for (AttnPiece w; ok && take(w); loads += 2u * w.n) ok = copy_tiles(w, loads, true);
         if (bad) atomicOr(&p.hdr->status, kStatusPage);
     } else if (warp == kAttnIssuer || (REP && warp == kAttnIssuer1)) {
         // ---------------------------------------------------------------- MMA issuers
@@ -943,7 +944,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             tc_commit(bar);
             (void)mbar_wait(bar, 0u, p.wait_ns);
         }
-        if (warp == kAttnProducer && lane == 0) {            // longer than any copy takes
+        if ((warp == kAttnProducer || warp == kAttnProducerV) && lane == 0) {        // longer than any copy takes
             const unsigned long long now = global_timer_ns();
             while (global_timer_ns() - now < 1000000ull) { }
         }
