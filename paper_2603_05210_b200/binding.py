@@ -16,6 +16,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libvt.so")
+MARSHAL_PATH = os.path.join(_HERE, "_vt_torch.so")
 
 VT_OK = 0
 VT_ERR_NULL, VT_ERR_SHAPE, VT_ERR_ALIGN, VT_ERR_RANGE, VT_ERR_DUP = 1, 2, 3, 4, 5
@@ -77,6 +78,7 @@ SYMBOLS = {
 }
 
 _lib = None
+_fast = None         # the compiled marshalling of the decode step's calls (csrc/vt_torch.cpp)
 
 
 class VtError(RuntimeError):
@@ -91,7 +93,7 @@ def lib() -> ctypes.CDLL:
     """Load ``libvt.so`` from the package directory, building it with nvcc first if it is absent."""
     global _lib
     if _lib is None:
-        if not os.path.exists(LIB_PATH):
+        if not os.path.exists(LIB_PATH) or not os.path.exists(MARSHAL_PATH):
             from .build import build
             build()
         cd = ctypes.CDLL(LIB_PATH)
@@ -100,6 +102,18 @@ def lib() -> ctypes.CDLL:
             fn.restype, fn.argtypes = res, args
         _lib = cd
     return _lib
+
+
+def _marshal():
+    """The compiled marshalling, told where the library's entry points are."""
+    global _fast
+    if _fast is None:
+        cd = lib()
+        from . import _vt_torch as fast
+        fast.init(*(ctypes.cast(getattr(cd, n), _p).value for n in (
+            "vt_rope", "vt_rope_append", "vt_tree_mask", "vt_tree_attention", "vt_tree_attention_workspace_bytes", "vt_verify_tokens")))
+        _fast = fast
+    return _fast
 
 
 def _check(status: int, what: str):
@@ -550,37 +564,6 @@ class _VtCacheStruct(ctypes.Structure):
         [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "heads", "head_dim", "B", "max_pages")]
 
 
-def _heads(t: torch.Tensor, name: str, device: int) -> _VtHeads:
-    """bf16 [tokens, heads, D] on the current device, the elements of a head in a row; anything else may be strided."""
-    if t.dtype is not torch.bfloat16:
-        raise TypeError(f"{name}: expected torch.bfloat16, got {t.dtype}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or t.get_device() != device or (stride[2] != 1 and shape[2] > 1 and shape[0] > 0):
-        raise ValueError(f"{name}: expected [tokens, heads, D] with contiguous heads on the current CUDA device")
-    n, h, d = shape
-    # the stride of one alone says nothing
-    return _VtHeads(t.data_ptr(), stride[0] if n > 1 else (h or 1) * d, stride[1] if h > 1 else d)
-
-
-def _vector(t: torch.Tensor, name: str, n: int | None, device: int, dtype: torch.dtype = torch.int32) -> int:
-    """The address of a contiguous vector of n entries (None: any number) on the current device."""
-    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or (t.shape != (n,) if n is not None else t.dim() != 1):
-        raise ValueError(f"{name}: expected a contiguous {dtype} vector{'' if n is None else f' of {n}'} on the current CUDA device")
-    return t.data_ptr()
-
-
-def _new_or_given(t: torch.Tensor | None, name: str, shape: tuple, dtype: torch.dtype, like: torch.Tensor, device: int) -> torch.Tensor:
-    if t is None:
-        return like.new_empty(shape, dtype=dtype)
-    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape} on the current CUDA device")
-    return t
-
-
-def _stream_of(device: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(device)
-
-
 class VtRope(NamedTuple):
     """Frequencies and layout of rotary positions, from ``vt_rope_table``."""
     table: torch.Tensor        # [rot_dim / 2] int64: turns per position, as fractions of 2^64
@@ -649,44 +632,15 @@ class VtCache:
     lens = property(lambda self: self._lens)
 
 
-def _heads_out(t, name, shape, like, device):
-    """(tensor, _VtHeads) of an output of the shape of `like`: the caller's, or a new one."""
-    if t is None:
-        t = torch.empty_like(like, memory_format=torch.contiguous_format)
-        return t, _VtHeads(t.data_ptr(), (shape[1] or 1) * shape[2], shape[2])
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected the shape of its input")
-    return t, _heads(t, name, device)
-
-
 def vt_rope(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, rope: VtRope, *, inverse: bool = False,
             out_q: torch.Tensor | None = None, out_k: torch.Tensor | None = None):
     """(q, k) turned to their ``positions`` [N] int32; q [N, Hq, D], k [N, Hkv, D] or None.
 
     ``inverse`` turns back, which is the gradient's way: (grad_q, grad_k) = vt_rope(grad of q, grad of k, ..., inverse=True).  The outputs may
     be the inputs themselves."""
-    device = torch.cuda.current_device()
-    hq, shape = _heads(q, "q", device), q.shape
-    N, Hq, D = shape
-    _vector(positions, "positions", N, device)
-    table = rope.table
-    if table.get_device() != device:
-        raise ValueError("rope: its table lies on another device")
-    out_q, ho = _heads_out(out_q, "out_q", shape, q, device)
-    Hkv, hk, ko = 0, None, None
-    if k is not None:
-        hk, kshape = _heads(k, "k", device), k.shape
-        if kshape[0] != N or kshape[2] != D:
-            raise ValueError("q and k disagree on tokens or D")
-        Hkv = kshape[1]
-        out_k, ko = _heads_out(out_k, "out_k", kshape, k, device)
-        hk, ko = ctypes.byref(hk), ctypes.byref(ko)
-    elif out_k is not None:
-        raise ValueError("out_k needs k")
-    _check(lib().vt_rope(ctypes.byref(hq), hk, positions.data_ptr(), table.data_ptr(), N, Hq, Hkv, D, rope.rot_dim, rope.amplitude,
-                         (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), ctypes.byref(ho), ko,
-                         _stream_of(device)), "vt_rope")
-    return out_q, out_k
+    r = (_fast or _marshal()).rope(q, k, positions, rope.table, rope.rot_dim, rope.amplitude,
+                                   (VT_ROPE_INTERLEAVED if rope.interleaved else 0) | (VT_ROPE_INVERSE if inverse else 0), out_q, out_k)
+    return r if type(r) is tuple else _check(r, "vt_rope")
 
 
 def vt_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache,
@@ -694,21 +648,9 @@ def vt_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions:
     """q [N, Hq, D] turned; k [N, heads, D] turned into the cache and v beside it, at places lens[b], lens[b] + 1, ... of each request.
 
     Request b has the tokens from ``cu_tokens``[b] to ``cu_tokens``[b + 1]; tokens outside all requests are padding, and left alone."""
-    device = torch.cuda.current_device()
-    hq, hk, hv, shape, kshape, c = _heads(q, "q", device), _heads(k, "k", device), _heads(v, "v", device), q.shape, k.shape, cache._struct
-    N, Hq, D = shape
-    if kshape != v.shape or kshape[0] != N or kshape[1] != c.heads or kshape[2] != D or D != c.head_dim or cache._device != device:
-        raise ValueError("q, k, v and the cache disagree on tokens, heads, D or device")
-    _vector(positions, "positions", N, device)
-    cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
-    table = rope.table
-    if table.get_device() != device:
-        raise ValueError("rope: its table lies on another device")
-    out_q, ho = _heads_out(out_q, "out_q", shape, q, device)
-    _check(lib().vt_rope_append(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), positions.data_ptr(), cu, table.data_ptr(), N, Hq,
-                                rope.rot_dim, rope.amplitude, VT_ROPE_INTERLEAVED if rope.interleaved else 0, ctypes.byref(ho), cache._ref,
-                                _stream_of(device)), "vt_rope_append")
-    return out_q
+    r = (_fast or _marshal()).rope_append(q, k, v, positions, cu_tokens, cache._ref, cache._device, rope.table, rope.rot_dim, rope.amplitude,
+                                          VT_ROPE_INTERLEAVED if rope.interleaved else 0, out_q)
+    return _check(r, "vt_rope_append") if type(r) is int else r
 
 
 def vt_tree_mask(parents: torch.Tensor, cu_tokens: torch.Tensor, max_tokens: int, *, lens: torch.Tensor | None = None,
@@ -716,15 +658,8 @@ def vt_tree_mask(parents: torch.Tensor, cu_tokens: torch.Tensor, max_tokens: int
     """(mask [N, ceil(max_tokens / 32)] int32, positions [N] int32) of drafted trees from ``parents`` [N] (index within the request, -1: none).
 
     A token's row has the bits of the tokens on its way up and its own; its position is lens[b] + its depth (without ``lens`` the depth)."""
-    device = torch.cuda.current_device()
-    N, words = parents.shape[0], (int(max_tokens) + 31) // 32
-    pp, cu = _vector(parents, "parents", N, device), _vector(cu_tokens, "cu_tokens", None, device)
-    B = cu_tokens.shape[0] - 1
-    pl = None if lens is None else _vector(lens, "lens", B, device)
-    mask = _new_or_given(mask, "mask", (N, words), torch.int32, parents, device)
-    positions = _new_or_given(positions, "positions", (N,), torch.int32, parents, device)
-    _check(lib().vt_tree_mask(pp, cu, pl, N, B, mask.data_ptr(), words, positions.data_ptr(), _stream_of(device)), "vt_tree_mask")
-    return mask, positions
+    r = (_fast or _marshal()).tree_mask(parents, cu_tokens, (int(max_tokens) + 31) // 32, lens, mask, positions)
+    return r if type(r) is tuple else _check(r, "vt_tree_mask")
 
 
 def vt_tree_attention_workspace_bytes(Hq: int, heads: int, D: int, max_tokens: int) -> int:
@@ -739,27 +674,8 @@ def vt_tree_attention(q: torch.Tensor, cu_tokens: torch.Tensor, cache: VtCache, 
     ``max_tokens`` bounds the tokens of a request.  ``mask`` [N, words] int32 (``vt_tree_mask``) says which drafted tokens each attends; without
     it a token attends itself and those before it.  ``scale`` is D^-0.5 unless it is given.  Rows outside all requests are left as they were.
     Time-outs and page ids outside the cache are only seen by ``vt_last_status`` of a workspace of the caller's (from ``new_workspace``)."""
-    device = torch.cuda.current_device()
-    hq, shape, c = _heads(q, "q", device), q.shape, cache._struct
-    N, Hq, D = shape
-    if D != c.head_dim or cache._device != device:
-        raise ValueError("q and the cache disagree on D or device")
-    cu = _vector(cu_tokens, "cu_tokens", c.B + 1, device)
-    words = 0
-    if mask is not None:
-        if mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != N or mask.get_device() != device or not mask.is_contiguous():
-            raise ValueError("mask: expected a contiguous int32 tensor with a row per token on the current CUDA device")
-        words = mask.shape[1]
-    out, ho = _heads_out(out, "out", shape, q, device)
-    lse = _new_or_given(lse, "lse", (N, Hq), torch.float32, q, device)
-    if workspace is None:
-        workspace = torch.empty(max(vt_tree_attention_workspace_bytes(Hq, c.heads, D, max_tokens), 256), dtype=torch.uint8, device=q.device)
-    elif workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError("workspace: expected a contiguous tensor on the current CUDA device")
-    _check(lib().vt_tree_attention(ctypes.byref(hq), cu, cache._ref, None if mask is None else mask.data_ptr(), words, N, Hq, max_tokens,
-                                   D ** -0.5 if scale is None else scale, ctypes.byref(ho), lse.data_ptr(), workspace.data_ptr(),
-                                   workspace.nbytes, _stream_of(device)), "vt_tree_attention")
-    return out, lse
+    r = (_fast or _marshal()).tree_attention(q, cu_tokens, cache._ref, cache._device, mask, max_tokens, scale, out, lse, workspace)
+    return r if type(r) is tuple else _check(r, "vt_tree_attention")
 
 
 class VtVerified(NamedTuple):
@@ -777,34 +693,10 @@ def vt_verify_tokens(probs: torch.Tensor, tokens: torch.Tensor, parents: torch.T
     Token 0 of a request is its root.  With ``draft_probs`` [N, Vd] the children of a token were drawn from its row (``draft_ids`` [N]: the tokens
     as draft indices, ``d2t`` [Vd] the draft-to-target map); without them they were picked without chance (``vt_tree_select``).  The result is
     distributed as if the target had generated alone; the rule is spelled out in ``include/vt.h``."""
-    device = torch.cuda.current_device()
-    for name, t in (("probs", probs), ("draft_probs", draft_probs)):
-        if t is not None and (t.dtype is not torch.float32 or t.dim() != 2 or t.get_device() != device or (t.stride(1) != 1 and t.shape[1] > 1 and t.shape[0] > 0)):
-            raise ValueError(f"{name}: expected float32 [N, vocabulary] with contiguous rows on the current CUDA device")
-    N, V = probs.shape
-    B = u_sample.shape[0]
-    f32 = torch.float32
-    args = (_vector(tokens, "tokens", N, device), _vector(parents, "parents", N, device), _vector(cu_tokens, "cu_tokens", B + 1, device),
-            _vector(u_accept, "u_accept", N, device, f32), _vector(u_sample, "u_sample", B, device, f32))
-    Vd, pq, ldq, pi, pm = 0, None, 0, None, None
-    if draft_probs is not None:
-        if draft_ids is None or draft_probs.shape[0] != N:
-            raise ValueError("draft_probs needs a row per token, and draft_ids")
-        Vd, pq, ldq = draft_probs.shape[1], draft_probs.data_ptr(), draft_probs.stride(0) if N > 1 else draft_probs.shape[1]
-        pi = _vector(draft_ids, "draft_ids", N, device)
-        pm = None if d2t is None else _vector(d2t, "d2t", Vd, device)
-    elif draft_ids is not None or d2t is not None:
-        raise ValueError("draft_ids and d2t need draft_probs")
-    if out is None:                # one allocation cut up
-        n = max(int(max_tokens), 0)
-        a, b, c = tokens.new_empty((B * (1 + 2 * n),)).split_with_sizes((B, B * n, B * n))
-        out = VtVerified(a, b.view(B, n), c.view(B, n))
-    else:
-        for name, t, shape in zip(VtVerified._fields, out, ((B,), (B, max_tokens), (B, max_tokens))):
-            _new_or_given(t, name, shape, torch.int32, tokens, device)
-    _check(lib().vt_verify_tokens(probs.data_ptr(), probs.stride(0) if N > 1 else V, *args, pq, ldq, pi, pm, N, B, V, Vd, max_tokens,
-                                  out.n_accepted.data_ptr(), out.path.data_ptr(), out.tokens.data_ptr(), _stream_of(device)), "vt_verify_tokens")
-    return out
+    n_accepted, path, out_tokens = out or (None, None, None)
+    r = (_fast or _marshal()).verify_tokens(probs, tokens, parents, cu_tokens, u_accept, u_sample, max_tokens, draft_probs, draft_ids, d2t,
+                                            n_accepted, path, out_tokens)
+    return VtVerified(*r) if type(r) is tuple else _check(r, "vt_verify_tokens")
 
 
 def vt_remap(draft_ids: torch.Tensor, d2t: torch.Tensor) -> torch.Tensor:

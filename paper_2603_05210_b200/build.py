@@ -1,15 +1,19 @@
-"""Builds ``libvt.so`` (the CUDA library behind ``include/vt.h``) in-tree with nvcc for sm_100a."""
+"""Builds ``libvt.so`` (the CUDA library behind ``include/vt.h``) in-tree with nvcc for sm_100a, and ``_vt_torch.so``, the compiled
+marshalling of torch tensors for some of its calls, with the host compiler."""
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libvt.so")
+MARSHAL = os.path.join(HERE, "_vt_torch.so")
 SOURCES = ["vt_api.cu", "vt_attn.cu", "vt_aux.cu", "vt_ffn.cu", "vt_gemm.cu", "vt_head_gemv.cu", "vt_head_mma.cu", "vt_head_mma_small.cu",
            "vt_merge.cu", "vt_probe.cu", "vt_rope.cu", "vt_score.cu", "vt_score_grad.cu", "vt_select.cu", "vt_verify.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -22,8 +26,8 @@ def _deps_mtime() -> float:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every ``.cu`` under ``csrc/`` and link ``libvt.so``; a no-op when the library is newer than its sources."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _deps_mtime():
+    """Compile every ``.cu`` under ``csrc/`` and link ``libvt.so``, and ``vt_torch.cpp``; a no-op when both are newer than their sources."""
+    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= _deps_mtime() for f in (LIB, MARSHAL)):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     os.makedirs(OBJ, exist_ok=True)
@@ -39,8 +43,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
+    def compile_marshal():
+        import torch
+        root, cuda = os.path.dirname(torch.__file__), os.path.dirname(os.path.dirname(shutil.which(nvcc) or "/usr/local/cuda/bin/nvcc"))
+        tmp = MARSHAL + f".{os.getpid()}.tmp"
+        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+               *(a for d in (sysconfig.get_paths()["include"], f"{root}/include", f"{root}/include/torch/csrc/api/include", f"{cuda}/include")
+                 for a in ("-isystem", d)),
+               os.path.join(CSRC, "vt_torch.cpp"), "-o", tmp, f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{cmd[0]} failed for vt_torch.cpp:\n{r.stdout}\n{r.stderr}")
+        os.replace(tmp, MARSHAL)
+
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
+        marshal = pool.submit(compile_marshal)
         objs = list(pool.map(compile_one, SOURCES))
+        marshal.result()
     tmp = LIB + f".{os.getpid()}.tmp"
     r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-lcudart"], capture_output=True, text=True)
     if r.returncode != 0:
