@@ -4,16 +4,21 @@
 // p[parent][token] and q[parent][token], does not: all of them are fetched at once, and the way down the tree is then a walk through shared
 // memory that every CTA makes for itself.  Only the rows' sums need the cluster: each CTA owns an eighth of the vocabulary, adds up its part
 // in 64 bits in a fixed order and gives the sum to the others through distributed shared memory.  The token that follows is found from the
-// sums: the CTA, then the warp whose range the target falls into, then the lane's thirty-second of that, then the id.
+// sums: the CTA, then the warp whose range the target falls into, then 128 ids of it, four of those, the id.
 //
 // After j rejections at a node what is left is max(p - S q, 0) with one number S, because max(max(a - b, 0) - c, 0) = max(a - b - c, 0) for
 // c >= 0: no row is written anywhere.  q lives on the trimmed vocabulary, so the node's q is laid out over the CTAs' ids in shared memory
 // first: each CTA sends an eighth of q to where d2t says.
 // Drafts chosen without chance need no sums on the way (Z falls by p of each child), and a bitmap of rejected children in q's place.
 //
-// Bound: latency.  Seven memory round trips follow one another (offsets, nodes, gathers, q, the row, a lane's part of it, the id); the bytes of
-// one row of p (and q) per request take a tenth of that for 16 requests.  (Going through the warp's range 32 ids at a time, each behind a load,
-// took 17 of 23 us.)
+// Bound: latency.  Seven memory round trips follow one another (offsets, nodes, gathers, q, the row, a part of it again, four ids), with two
+// to four synchronisations of a cluster between them; the bytes of one row of p (and q) per request take a tenth of that for 16 requests.
+// Measured with a vocabulary of 128256, in a graph: one chain of six drawn from 32000 ids 13.0 us, 16 trees of 60 best ones 10.7 us, 64 chains of
+// eight 37 us drawn and 22 us best.
+// The code is fetched as it goes, once per call and SM, so less of it is faster: the sum in one loop in place of a vector and a scalar one, and
+// the target sought by warp sums of 128 ids in place of lanes with runs of their own, took the 16 trees from 12.6 us to 10.7.  (Sums of 128 ids
+// kept by every warp for the search: 15 us.  1024 threads a CTA: 22 us.  q found through an index of the ids instead of laid out: a drawn chain
+// 15.0 us.  One id per lane and load, which needs no boundaries: 11.3 and 14.2 us.)
 #include "vt_step.h"
 #include "vt_tc.cuh"
 
@@ -22,6 +27,8 @@ namespace vt {
 constexpr int kVerifyCtas = 8;               // per request
 constexpr int kVerifyThreads = 512;
 constexpr int kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyBatch = 4;              // entries of q that a thread has on their way
+constexpr int kVerifyRuns = 4;               // runs of 128 ids that a warp looks through at once
 constexpr int kVerifyRun = kVerifyWarps * 128;       // a CTA's share of the vocabulary is a multiple of it: whole runs of 128 per warp
 
 struct VerifyParams {
@@ -60,7 +67,9 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_cta_rank();
     const int b = blockIdx.x / kVerifyCtas;
-    const int first_id = (int)rank * prm.share, ids = max(0, min(prm.share, c.V - first_id));
+    // A row of p is dealt out from the 16-byte boundary at or before its first id: with `skew` numbers before that, id i stands at i + skew, and
+    // this CTA has the places first .. first + share - 1.
+    const int first = (int)rank * prm.share;
     // this CTA's q (DRAWN), or a bit per id that is out; then the nodes
     float* left_q = reinterpret_cast<float*>(smem);
     uint32_t* out_bits = reinterpret_cast<uint32_t*>(smem);
@@ -115,6 +124,7 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     }
 
     int buffer = 0;
+    auto skew_of = [&](int x) { return (int)(reinterpret_cast<uintptr_t>(c.probs + (int64_t)(begin + x) * c.ld_probs) >> 2 & 3u); };
     // lays out q of a node, or its children
     bool cleared = true;
     auto lay_out = [&](int x) {
@@ -125,57 +135,94 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
             else __syncthreads();
         }
         cleared = false;
+        const int skew = skew_of(x);
         if (DRAWN) {
             const float* q = c.draft_probs + (int64_t)(begin + x) * c.ld_draft;
             if (c.d2t) {
                 const int i0 = (int)((long long)c.Vd * rank / kVerifyCtas), i1 = (int)((long long)c.Vd * (rank + 1) / kVerifyCtas);
-#pragma unroll 8
-                for (int i = i0 + tid; i < i1; i += kVerifyThreads) {
-                    const int at = c.d2t[i];
-                    const float v = fmaxf(q[i], 0.0f);
-                    if ((unsigned)at < (unsigned)c.V) {
-                        const unsigned owner = (unsigned)at / (unsigned)prm.share;
+#pragma unroll 1
+                for (int i = i0 + tid; i < i1; i += kVerifyBatch * kVerifyThreads) {
+                    int at[kVerifyBatch];
+                    float v[kVerifyBatch];
+#pragma unroll
+                    for (int k = 0; k < kVerifyBatch; ++k) {
+                        const int e = min(i + k * kVerifyThreads, i1 - 1);
+                        at[k] = c.d2t[e];
+                        v[k] = q[e];
+                    }
+#pragma unroll
+                    for (int k = 0; k < kVerifyBatch; ++k) {
+                        if (i + k * kVerifyThreads >= i1 || (unsigned)at[k] >= (unsigned)c.V) continue;
+                        const unsigned place = (unsigned)(at[k] + skew), owner = place / (unsigned)prm.share;
                         asm volatile("st.shared::cluster.f32 [%0], %1;"
-                                     ::"r"(cluster_map_shared(smem_u32(left_q + ((unsigned)at - owner * (unsigned)prm.share)), owner)), "f"(v) : "memory");
+                                     ::"r"(cluster_map_shared(smem_u32(left_q + (place - owner * (unsigned)prm.share)), owner)), "f"(fmaxf(v[k], 0.0f)) : "memory");
                     }
                 }
                 cluster_sync_all();
             } else {
-                for (int i = tid; i < min(ids, c.Vd - first_id); i += kVerifyThreads) left_q[i] = fmaxf(q[first_id + i], 0.0f);
+                for (int i = max(skew - first, 0) + tid; i < min(prm.share, c.Vd + skew - first); i += kVerifyThreads) left_q[i] = fmaxf(q[first + i - skew], 0.0f);
                 __syncthreads();
             }
         } else {
             for (int t = tid; t < T; t += kVerifyThreads) {
-                const unsigned at = (unsigned)(node_token[t] - first_id);
-                if (node_parent[t] == x && at < (unsigned)ids) atomicOr(&out_bits[at >> 5], 1u << (at & 31));
+                const unsigned at = (unsigned)node_token[t] + (unsigned)skew - (unsigned)first;
+                if (node_parent[t] == x && at < (unsigned)prm.share) atomicOr(&out_bits[at >> 5], 1u << (at & 31));
             }
             __syncthreads();
         }
     };
-    // what is left of id first_id + i, whose probability is p
-    auto left = [&](float p, int i, double S, bool whole) -> double {
-        if (whole) return p > 0.0f ? (double)p : 0.0;
-        if (DRAWN) return fmax((double)fmaxf(p, 0.0f) - S * (double)left_q[i], 0.0);
-        return p > 0.0f && !(out_bits[i >> 5] >> (i & 31) & 1u) ? (double)p : 0.0;
+    const int per_warp = prm.share / kVerifyWarps;
+    // what is left of this CTA's ids i .. i + 3 after node x, i a multiple of four; nothing of those outside start .. end - 1
+    auto left4 = [&](const float* row, int i, int start, int end, double S, bool whole, double (&l)[4]) {
+        float p[4];
+        if (i >= start && i + 3 < end) {
+            const float4 v = *reinterpret_cast<const float4*>(row + i);
+            p[0] = v.x, p[1] = v.y, p[2] = v.z, p[3] = v.w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[k] = i + k >= start && i + k < end ? row[i + k] : 0.0f;
+        }
+        const int in = min(i, prm.share - 4);                // where p is 0 past it all
+        if (DRAWN) {
+            const float4 v = *reinterpret_cast<const float4*>(left_q + in);
+            const float q[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const double d = (double)fmaxf(p[k], 0.0f), less = fmax(d - S * (double)q[k], 0.0);
+                l[k] = whole ? d : less;
+            }
+        } else {
+            const uint32_t out = whole ? 0u : out_bits[in >> 5] >> (in & 31);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) l[k] = out >> k & 1u ? 0.0 : (double)fmaxf(p[k], 0.0f);
+        }
     };
     // this thread's part of the sum of what is left after node x; a warp's ids are consecutive
-    const int per_warp = prm.share / kVerifyWarps;
-    const bool vector = (c.ld_probs & 3) == 0 && (reinterpret_cast<uintptr_t>(c.probs) & 15u) == 0;
     auto part = [&](int x, double S, bool whole) -> double {
-        const float* row = c.probs + (int64_t)(begin + x) * c.ld_probs + first_id;
-        const int i0 = warp * per_warp, i1 = min(i0 + per_warp, ids);
+        const int skew = skew_of(x), start = max(skew - first, 0), i0 = warp * per_warp, i1 = min(i0 + per_warp, c.V + skew - first);
+        const float* row = c.probs + (int64_t)(begin + x) * c.ld_probs + (first - skew);
         double sum = 0.0;
-        if (vector) {
+        if (DRAWN) {
+            auto left = [&](float p, int i) {
+                if (whole) return p > 0.0f ? (double)p : 0.0;
+                return fmax((double)fmaxf(p, 0.0f) - S * (double)left_q[i], 0.0);
+            };
+            const int ahead = start > i0 ? 4 : 0;
 #pragma unroll 8
-            for (int i = i0 + 4 * lane; i + 3 < i1; i += 128) {
+            for (int i = i0 + ahead + 4 * lane; i + 3 < i1; i += 128) {
                 const float4 p = *reinterpret_cast<const float4*>(row + i);
-                sum += (left(p.x, i, S, whole) + left(p.y, i + 1, S, whole)) + (left(p.z, i + 2, S, whole) + left(p.w, i + 3, S, whole));
+                sum += (left(p.x, i) + left(p.y, i + 1)) + (left(p.z, i + 2) + left(p.w, i + 3));
             }
-            const int rest = i0 + (max(i1 - i0, 0) & ~3) + lane;
-            if (rest < i1) sum += left(row[rest], rest, S, whole);
-        } else {
+            const int rest = max(i0 + ahead, i1 & ~3) + lane;
+            if (rest < i1) sum += left(row[rest], rest);
+            if (lane < ahead && lane >= start && lane < i1) sum += left(row[lane], lane);
+            return sum;
+        }
 #pragma unroll 8
-            for (int i = i0 + lane; i < i1; i += 32) sum += left(row[i], i, S, whole);
+        for (int i = i0 + 4 * lane; i < i1; i += 128) {
+            double l[4];
+            left4(row, i, start, i1, S, whole, l);
+            sum += (l[0] + l[1]) + (l[2] + l[3]);
         }
         return sum;
     };
@@ -218,14 +265,12 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
     // ---- the token that follows
     if (T > 0) {
         bool whole = DRAWN && !summed;
+        if (!DRAWN) lay_out(x);
         double total = Z;
-        if (!summed) {
-            if (!whole) lay_out(x);
-            total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer ^= 1], rank);
-        }
-        if (!(total > 0.0) && !whole) {      // the same in every CTA
+        for (bool known = summed;; known = false) {          // once more, of the whole row, where nothing is left; the same in every CTA
+            if (!known) total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer ^= 1], rank);
+            if (total > 0.0 || whole) break;
             whole = true;
-            total = cluster_total(part(x, S, whole), warp_sums, cta_sums[buffer ^= 1], rank);
         }
         const double* sums = cta_sums[buffer];
         const double target = u_follow * total;
@@ -249,48 +294,60 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
             const bool past_w = w < 0;
             if (past_w) w = last_w;
             if (w == warp) {
-                const float* row = c.probs + (int64_t)(begin + x) * c.ld_probs + first_id;
-                const int i0 = warp * per_warp, i1 = min(i0 + per_warp, ids);
-                // a lane per run of `len` consecutive ids: the run whose sum goes past the target (or the last with anything in it) ...
-                const int len = per_warp / 32, r0 = i0 + lane * len, r1 = min(r0 + len, i1);
-                double run = 0.0;
-                if (vector) {
-#pragma unroll 8
-                    for (int i = r0; i + 3 < r1; i += 4) {
-                        const float4 p = *reinterpret_cast<const float4*>(row + i);
-                        run += (left(p.x, i, S, whole) + left(p.y, i + 1, S, whole)) + (left(p.z, i + 2, S, whole) + left(p.w, i + 3, S, whole));
+                const int skew = skew_of(x), start = max(skew - first, 0), i0 = warp * per_warp, i1 = min(i0 + per_warp, c.V + skew - first);
+                const float* row = c.probs + (int64_t)(begin + x) * c.ld_probs + (first - skew);
+                // the 128 ids whose sum goes past the target (or the last with anything in them), four such runs at a time ...
+                int at = -1, last_at = -1;
+                double before_last = before;
+                for (int g = i0; g < i1 && at < 0; g += 128 * kVerifyRuns) {
+                    double run[kVerifyRuns];
+#pragma unroll
+                    for (int k = 0; k < kVerifyRuns; ++k) {
+                        double l[4];
+                        left4(row, g + 128 * k + 4 * lane, start, i1, S, whole, l);
+                        run[k] = (l[0] + l[1]) + (l[2] + l[3]);
                     }
-                    for (int i = r0 + (max(r1 - r0, 0) & ~3); i < r1; ++i) run += left(row[i], i, S, whole);
-                } else {
-#pragma unroll 8
-                    for (int i = r0; i < r1; ++i) run += left(row[i], i, S, whole);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+                        for (int k = 0; k < kVerifyRuns; ++k) run[k] += __shfl_xor_sync(0xFFFFFFFFu, run[k], o);
+#pragma unroll
+                    for (int k = 0; k < kVerifyRuns; ++k) {
+                        if (at >= 0 || !(run[k] > 0.0)) continue;
+                        last_at = g + 128 * k;
+                        before_last = before;
+                        if (!past_w && before + run[k] > target) at = last_at;
+                        else before += run[k];
+                    }
                 }
-                auto up_to = [&](double v) {                 // sum over the lanes up to this one
+                const bool past_r = at < 0;
+                // ... and in it the id: the lane of four, then the one
+                int found = -1;
+                if (last_at >= 0) {
+                    double l[4];
+                    const int i = last_at + 4 * lane;
+                    left4(row, i, start, i1, S, whole, l);
+                    double upto = (l[0] + l[1]) + (l[2] + l[3]);
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
-                        const double w = __shfl_up_sync(0xFFFFFFFFu, v, o);
-                        if (lane >= o) v += w;
+                        const double w = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                        if (lane >= o) upto += w;
                     }
-                    return v;
-                };
-                const double cum = before + up_to(run);
-                const unsigned some = __ballot_sync(0xFFFFFFFFu, run > 0.0);
-                const unsigned over = __ballot_sync(0xFFFFFFFFu, !past_w && run > 0.0 && cum > target);
-                const int at = over ? __ffs((int)over) - 1 : some ? 31 - __clz((int)some) : 0;
-                const bool past_r = over == 0;
-                before = __shfl_sync(0xFFFFFFFFu, cum - run, at);
-                // ... and in it the id
-                int found = -1, latest = -1;
-                for (int i = i0 + at * len, e = min(i + len, i1); i < e && found < 0; i += 32) {
-                    const double l = i + lane < e ? left(row[i + lane], i + lane, S, whole) : 0.0;
-                    const double c32 = before + up_to(l);
-                    const unsigned any = __ballot_sync(0xFFFFFFFFu, l > 0.0), past = __ballot_sync(0xFFFFFFFFu, !past_r && l > 0.0 && c32 > target);
-                    if (past) found = i + __ffs((int)past) - 1;
-                    if (any) latest = i + 31 - __clz((int)any);
-                    before = __shfl_sync(0xFFFFFFFFu, c32, 31);
+                    double c4 = before_last + __shfl_up_sync(0xFFFFFFFFu, upto, 1);
+                    if (lane == 0) c4 = before_last;
+                    int latest = -1;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        c4 += l[k];
+                        if (l[k] > 0.0) {
+                            latest = i + k;
+                            if (found < 0 && !past_r && c4 > target) found = i + k;
+                        }
+                    }
+                    const unsigned over = __ballot_sync(0xFFFFFFFFu, found >= 0), some = __ballot_sync(0xFFFFFFFFu, latest >= 0);
+                    found = over ? __shfl_sync(0xFFFFFFFFu, found, __ffs((int)over) - 1) : some ? __shfl_sync(0xFFFFFFFFu, latest, 31 - __clz((int)some)) : -1;
                 }
-                if (found < 0) found = latest;
-                if (lane == 0) c.out_tokens[(int64_t)b * c.max_tokens + n] = found < 0 ? -1 : first_id + found;
+                if (lane == 0) c.out_tokens[(int64_t)b * c.max_tokens + n] = found < 0 ? -1 : first + found - skew;
             }
         }
         if (own < 0 && rank == 0 && tid == 0) c.out_tokens[(int64_t)b * c.max_tokens + n] = -1;
@@ -311,7 +368,8 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
 vt_status launch_verify(const VerifyCall& c, cudaStream_t st) {
     VerifyParams p{c, 0};
     const bool drawn = c.draft_probs != nullptr;
-    p.share = (int)(((long long)c.V + kVerifyCtas * kVerifyRun - 1) / (kVerifyCtas * kVerifyRun)) * kVerifyRun;
+    const bool skewed = (c.ld_probs & 3) != 0 || (reinterpret_cast<uintptr_t>(c.probs) & 15u) != 0;
+    p.share = (int)(((long long)c.V + (skewed ? 3 : 0) + kVerifyCtas * kVerifyRun - 1) / (kVerifyCtas * kVerifyRun)) * kVerifyRun;
     const size_t smem = (drawn ? (size_t)p.share * 4 : (size_t)p.share / 8) + (size_t)c.max_tokens * 24;
     static std::atomic<unsigned long long> configured[2];
     void (*kernel)(VerifyParams) = drawn ? verify_kernel<true> : verify_kernel<false>;

@@ -82,6 +82,25 @@ def test_vocabularies(vt, V, Vd, tree, pad):
     check(vt, a, 33, pad)
 
 
+# rows that begin at each place between two 16-byte boundaries, their neighbours NaN; the last ids chosen, at the end of a CTA's or a warp's part
+@pytest.mark.parametrize("V,Vd", [(16384, 0), (16383, 0), (2046, 0), (2045, 77), (16384, 900), (16381, 16381)])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_rows_anywhere(vt, V, Vd, shift, odd):
+    a = make([3, 1, 12], V, Vd, True, seed=V + shift, identity=Vd == V)
+    a["u_sample"] = np.float32([0.0, 1.0, 0.9999])
+    want = so.verify(a["P"], a["tokens"], a["parents"], a["cu"], a["u_accept"], a["u_sample"], 12, a.get("Q"), a.get("draft_ids"), a.get("d2t"))
+    ld = V + 5 if odd else -(-(V + 3) // 4) * 4
+    flat = torch.full((16 * ld + 8,), float("nan"), device="cuda")
+    P = flat[shift:shift + 16 * ld].view(16, ld)[:, :V]
+    P.copy_(dev(a["P"], torch.float32))
+    kw = dict(draft_probs=dev(a["Q"], torch.float32), draft_ids=dev(a["draft_ids"]), d2t=dev(a["d2t"])) if Vd else {}
+    got = vt.vt_verify_tokens(P, dev(a["tokens"]), dev(a["parents"]), dev(a["cu"]), dev(a["u_accept"], torch.float32), dev(a["u_sample"], torch.float32),
+                              max_tokens=12, **kw)
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy(), w)
+
+
 @pytest.mark.parametrize("drawn", [False, True])
 def test_the_largest_vocabularies(vt, drawn):
     rng = np.random.default_rng(1)
