@@ -1,7 +1,8 @@
 // Attention of drafted tokens over a paged cache (see vt_tree_attention).
 //
 // out = sum_i e^{x_i - lse} v_i over the attended positions, x = scale q.k: one pass over keys and values, with the running maximum and sum
-// of each row, as two tcgen05 products per tile of 128 positions - S = Q K^T, then O += P V with P = 2^{(S - m) scale log2 e} in bf16.
+// of each row, as two tcgen05 products per tile of 128 positions - S = Q K^T, then O += P V with P = 2^{(S - m) scale log2 e} in bf16, the
+// operand type of the product (its sum l is of the weights before they are rounded).  Scores, maxima, sums and O are fp32.
 //
 // Rows.  All query heads of a key head and all drafted tokens of a request read the same keys, so they are the rows of one product: row
 // t G + g for token t and head g of G.  A block of rows is up to two tiles of 128 TMEM lanes (a TMA box of G heads x 128 / G tokens fills a tile
@@ -11,6 +12,10 @@
 // four warps work out one stream's exponentials, the tensor cores multiply for the other.  With two row tiles a stream is a row tile
 // and both read each key tile; with one, the streams take the key tiles in turn, and are joined when the rows are finished.
 //
+// Few rows (REP, 32 at most).  A tile of 128 lanes is a quarter full at best, and one warp of four would have all the exponentials.  So q stands in
+// all four groups of 32 lanes, each warp takes 32 of a tile's 128 positions (its weights of the others are 0), and the eight parts of O, by stream
+// and warp, are added up at the item's end.  The products cost the same, the exponentials a quarter (64 x 1 over 4096: 113 -> 100 us).
+//
 // Work.  The lengths are known on the device alone, so the cut is made there: all key tiles of all (request, key head, row block) in a row,
 // an equal run of them to each CTA.  A run begins and ends inside an item, and a long item lies in many runs: a CTA writes what it has
 // of such an item (unnormalised O, m, l in fp32) to the workspace, and a second kernel joins the pieces.  No atomics: the same bits every time.
@@ -19,9 +24,19 @@
 // O is rescaled only when a row's maximum grows by more than 2^8 over the one in use (P then stays below 2^8, its sum in fp32): the
 // rescale, done by the stream's own warps, is rare after the first tiles.
 //
-// Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (and the end of an item), warp 8 TMA producer, warp 9 MMA issuer,
-// warp 10 the cleaner: in tiles where something is masked it turns infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
+// Roles: warps 0-3 and 4-7 softmax of stream 0 and 1 (and the end of an item), warp 8 the planner and TMA producer of q and K, warp 11 that of V,
+// warp 9 MMA issuer (of stream 0 alone with few rows, stream 1 then has warp 12), warp 10 the cleaner: in tiles where something is masked it turns
+// infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
 // All waits are bounded; one that runs out sets the status word and every role leaves.
+//
+// Bound and measured (in a graph, a copy at 6.46 TB/s and 1673 TFLOP/s in bf16 as the floors; requests x tokens over positions, 32 heads over 8
+// of 128 where nothing else stands):
+//   2 x 8 over 100000             136 us   floor 127: bytes of the cache, 6.0 TB/s
+//   64 x 1 over 4096, ragged       99 us   floor 86: bytes, 5.6 TB/s
+//   24 x 8 over 2500, 32 heads of 64 each, ragged   63 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
+//   16 x 60 over 8000, ragged      95 us   floor 54: a stream's step is exponentials, then its products: 4140 cycles for a pair of 2 x 1024 each
+//   1 x 60 over 4000               28 us   floor 3: latency; 70 runs of four tiles and the join
+//   1 x 1 over 700                12.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
 #include "vt_step.h"
 #include "vt_tc.cuh"
 
@@ -180,6 +195,15 @@ __device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, unsigne
         }
     }
     return true;
+}
+__device__ __forceinline__ bool attn_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return __all_sync(0xFFFFFFFFu, ok != 0);
 }
 // n / d for n < 2^31 d.
 __device__ __noinline__ long long attn_div(long long n, long long d) {
@@ -538,10 +562,12 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         if (bad) atomicOr(&p.hdr->status, kStatusPage);
     } else if (warp == kAttnIssuer || (REP && warp == kAttnIssuer1)) {
         // ---------------------------------------------------------------- MMA issuers
-        // Issuing takes 50 cycles a product and 120 a wait, 1400 per half-step.  Few rows: one issuer per stream, as one for both would be what
-        // all wait for.  Otherwise one for both: P V and the next S of one stream, then of the other, so that the streams' scores are ready at
-        // different times (with an issuer each, both fall into step, and exponentials and products take turns instead of overlapping: two long
-        // documents under 60 drafted tokens 120 -> 133 us).
+        // A product takes 64 cycles, a wait 120.  Few rows: an issuer per stream, as one for both would be what all wait for.  Otherwise one for
+        // both: P V and the next S of one stream, then of the other, so that the streams' scores are ready at different times (with an issuer
+        // each, both fall into step, and exponentials and products take turns instead of overlapping: two long documents under 60 drafted
+        // tokens 120 -> 133 us).  Where the next keys are there, they are not asked for between the two products: 4520 -> 4140 cycles for
+        // both streams' half-steps, 2430 of them a stream's exponentials.  (The first half of P V as soon as half the weights are there: 115 ->
+        // 120 us.)  Such a call draws 1000 W: it runs at 1.97 GHz for some milliseconds and at 1.6 GHz when repeated for seconds.
         bool ok = true;
         uint32_t p_phase = 0;
         uint32_t o_phase = 1, item = 0;
@@ -552,40 +578,46 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 #pragma unroll 1
             for (int i = own - 2; i < H; i += REP ? 2 : 1) { // P V of half-step i, then S of the stream's next
                 const int s = i & 1;
+                const bool more = i + 2 < H;
+                const uint32_t k_place = loads + w.k_at((i + 2) >> w.dual), k_turn = turn_of(k_place), k_st = k_place - k_turn * ST;
+                const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), q_at = qn & 1u;
+                auto score = [&]() {
+                    const uint32_t idesc = kIdescS | ((uint32_t)attn_k_steps(w, (i + 2) >> w.dual) << 18);
+                    const uint64_t a = smem_desc_sw128(q_smem + q_at * p.q_slot), bd = smem_desc_sw128(ring + k_st * kTile);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
+                                    bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
+                    tc_commit(s_full + 8u * s);
+                    tc_commit(kv_empty + 8u * k_st);
+                    if (!REP && (i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
+                };
+                bool keys = false;                           // the next ones are there already: both products go out in one
                 if (i >= 0) {
                     const uint32_t place = loads + w.v_at(i >> w.dual), turn = turn_of(place), st = place - turn * ST;
-                    if (!wait(v_clean + 8u * st, turn & 1u) || !wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
+                    const int steps = attn_k_steps(w, i >> w.dual);
+                    if (!wait(v_clean + 8u * st, turn & 1u)) { ok = false; break; }
+                    if (!REP) keys = more && i + 2 > w.dual && attn_test(kv_full + 8u * k_st, k_turn & 1u);
+                    if (!wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
                     p_phase ^= 1u << s;
                     tc_fence_after();
                     if (attn_elect()) {
                         const uint64_t bd = attn_v_desc(ring + st * kTile);
-                        const int steps = attn_k_steps(w, i >> w.dual);
 #pragma unroll
                         for (int k = 0; k < kAttnKeys / 16; ++k)
                             if (k < steps) tc_mma_bf16_ts(tmem + kAttnTmemO + 128u * s, tmem + kAttnTmemS + 128u * s + 8u * k, bd + (uint64_t)(128 * k), kIdescO,
-                                           i >= 2 || k > 0 ? 1u : 0u);
+                                                          i >= 2 || k > 0 ? 1u : 0u);
                         tc_commit(kv_empty + 8u * st);
                         if (!REP && i == H - 1) tc_commit(o_full);
+                        if (keys) score();
                     }
                     __syncwarp();
                 }
-                if (i + 2 < H) {
-                    const uint32_t qn = q_n + (w.dual ? (uint32_t)s : 0u), q_at = qn & 1u;
+                if (more && !keys) {
                     if (!REP && i + 2 <= w.dual && !wait(q_full + 8u * q_at, (qn >> 1) & 1u)) { ok = false; break; }
-                    const uint32_t place = loads + w.k_at((i + 2) >> w.dual), turn = turn_of(place), st = place - turn * ST;
-                    if (!wait(kv_full + 8u * st, turn & 1u)) { ok = false; break; }
+                    if (!wait(kv_full + 8u * k_st, k_turn & 1u)) { ok = false; break; }
                     tc_fence_after();
-                    if (attn_elect()) {
-                        const uint32_t idesc = kIdescS | ((uint32_t)attn_k_steps(w, (i + 2) >> w.dual) << 18);
-                        const uint64_t a = smem_desc_sw128(q_smem + q_at * p.q_slot), bd = smem_desc_sw128(ring + st * kTile);
-#pragma unroll
-                        for (int k = 0; k < D / 16; ++k)
-                            tc_mma_bf16(tmem + kAttnTmemS + 128u * s, a + (uint64_t)((k >> 2) * (p.q_block >> 4) + (k & 3) * 2),
-                                        bd + (uint64_t)((k >> 2) * (kBlock >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
-                        tc_commit(s_full + 8u * s);
-                        tc_commit(kv_empty + 8u * st);
-                        if (!REP && (i + 2) >> w.dual == w.n - 1) tc_commit(q_empty + 8u * q_at);
-                    }
+                    if (attn_elect()) score();
                     __syncwarp();
                 }
             }
@@ -703,82 +735,27 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         const uint32_t bits = attn_bits(row, p.mask_words, t, w.T, at - w.L);
                         return bits & (n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u);
                     };
-                  if constexpr (REP) {
-                    // the warp's own 32 positions of the tile; its weights of the others are 0
-                    uint32_t x[32], pk[16];
-                    tc_ld32(t_s + 32u * quad, x);
-                    tc_wait_ld();
-                    if (j >= w.open) {
-                        const uint32_t bits = seen(quad);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
-                    }
-                    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) top[(e >> 1) & 1] = max3(top[(e >> 1) & 1], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-                    __syncwarp();
-                    raise(fmaxf(top[0], top[1]));
-                    const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
-                    const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
-                    uint64_t sum0 = 0ull, sum1 = 0ull;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        float a, b;
-                        unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, r2), a, b);
-                        a = ex2_approx(a);
-                        b = ex2_approx(b);
-                        if (e & 2) sum1 = add2(sum1, pack2(a, b));
-                        else sum0 = add2(sum0, pack2(a, b));
-                        pk[e / 2] = attn_bf16x2(a, b);
-                    }
-                    tc_st16(t_s + 16u * quad, pk);           // over scores of its own lanes, which it has read
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) pk[e] = 0u;
-#pragma unroll
-                    for (int k = 1; k < 4; ++k) tc_st16(t_s + 16u * ((quad + k) & 3), pk);
-                    float a, b;
-                    unpack2(add2(sum0, sum1), a, b);
-                    l += a + b;
-                  } else {
-                    if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            const uint32_t bits = seen(c);
-                            uint32_t x[32];
-                            __syncwarp();
-                            tc_ld32(t_s + 32u * c, x);
-                            tc_wait_ld();
+                    if constexpr (REP) {
+                        // the warp's own 32 positions of the tile; its weights of the others are 0
+                        uint32_t x[32], pk[16];
+                        tc_ld32(t_s + 32u * quad, x);
+                        tc_wait_ld();
+                        if (j >= w.open) {
+                            const uint32_t bits = seen(quad);
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
-                            tc_st32(t_s + 32u * c, x);
                         }
-                        tc_wait_st();
-                    }
-                    // The scores are read twice, half of them at a time, for their maximum and for the weights.  (One pass with the old maximum,
-                    // made again where it grew too much, has fewer instructions to issue but four times as many to fetch, as all weights wait in
-                    // registers: slower by 5 to 10 %.)
-                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t x[64];
-                        tc_ld64(t_s + 64u * c, x);
-                        tc_wait_ld();
+                        float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                        for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3(top[(e >> 1) & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-                    }
-                    raise(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-                    const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
-                    const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
-                    uint64_t sum0 = 0ull, sum1 = 0ull;
-#pragma unroll 1
-                    for (int c = 0; c < 2; ++c) {
-                        uint32_t x[64], pk[32];
-                        tc_ld64(t_s + 64u * c, x);
-                        tc_wait_ld();
+                        for (int e = 0; e < 32; e += 2) top[(e >> 1) & 1] = max3(top[(e >> 1) & 1], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                        __syncwarp();
+                        raise(fmaxf(top[0], top[1]));
+                        const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
+                        const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
+                        uint64_t sum0 = 0ull, sum1 = 0ull;
 #pragma unroll
-                        for (int e = 0; e < 64; e += 2) {
+                        for (int e = 0; e < 32; e += 2) {
                             float a, b;
                             unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, r2), a, b);
                             a = ex2_approx(a);
@@ -787,12 +764,67 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             else sum0 = add2(sum0, pack2(a, b));
                             pk[e / 2] = attn_bf16x2(a, b);
                         }
-                        tc_st32(t_s + 32u * c, pk);          // over scores that have been read
+                        tc_st16(t_s + 16u * quad, pk);           // over scores of its own lanes, which it has read
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) pk[e] = 0u;
+#pragma unroll
+                        for (int k = 1; k < 4; ++k) tc_st16(t_s + 16u * ((quad + k) & 3), pk);
+                        float a, b;
+                        unpack2(add2(sum0, sum1), a, b);
+                        l += a + b;
+                    } else {
+                        if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
+#pragma unroll 1
+                            for (int c = 0; c < 4; ++c) {
+                                const uint32_t bits = seen(c);
+                                uint32_t x[32];
+                                __syncwarp();
+                                tc_ld32(t_s + 32u * c, x);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (!(bits >> e & 1u)) x[e] = 0xFF800000u;
+                                tc_st32(t_s + 32u * c, x);
+                            }
+                            tc_wait_st();
+                        }
+                        // The scores are read twice, half of them at a time, for their maximum and for the weights.  (One pass with the old maximum,
+                        // made again where it grew too much, has fewer instructions to issue but four times as many to fetch, as all weights wait in
+                        // registers: slower by 5 to 10 %.)
+                        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t x[64];
+                            tc_ld64(t_s + 64u * c, x);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 64; e += 2) top[(e >> 1) & 3] = max3(top[(e >> 1) & 3], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                        }
+                        raise(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+                        const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
+                        const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
+                        uint64_t sum0 = 0ull, sum1 = 0ull;
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t x[64], pk[32];
+                            tc_ld64(t_s + 64u * c, x);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 64; e += 2) {
+                                float a, b;
+                                unpack2(fma2(pack2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), k2, r2), a, b);
+                                a = ex2_approx(a);
+                                b = ex2_approx(b);
+                                if (e & 2) sum1 = add2(sum1, pack2(a, b));
+                                else sum0 = add2(sum0, pack2(a, b));
+                                pk[e / 2] = attn_bf16x2(a, b);
+                            }
+                            tc_st32(t_s + 32u * c, pk);          // over scores that have been read
+                        }
+                        float a, b;
+                        unpack2(add2(sum0, sum1), a, b);
+                        l += a + b;
                     }
-                    float a, b;
-                    unpack2(add2(sum0, sum1), a, b);
-                    l += a + b;
-                  }
                     tc_wait_st();
                     tc_fence_before();
                 }
