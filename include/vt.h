@@ -33,7 +33,7 @@ typedef enum vt_status {
     VT_ERR_SHAPE = 2,      /* d < 8, d % 8 != 0, M < 1, V_trim < 1, V_trim > V_full, k < 1, k > V_trim,
                               k > VT_MAX_K, N < 0, a size beyond what an entry point states it takes  */
     VT_ERR_ALIGN = 3,      /* a bf16 matrix pointer is not 16-byte aligned, an id pointer not 4-byte  */
-    VT_ERR_RANGE = 4,      /* a keep id lies outside [0, V_full)                                      */
+    VT_ERR_RANGE = 4,      /* a keep id lies outside [0, V_full), or a page id outside [0, n_pages)    */
     VT_ERR_DUP = 5,        /* keep_ids names an id twice (V_d is a set, Section 2.1)                  */
     VT_ERR_EMPTY = 6,      /* vt_coverage with N == 0: Eq. 2 would be 0/0                             */
     VT_ERR_WORKSPACE = 7,  /* workspace NULL, misaligned (256 B) or smaller than the size function says */
@@ -393,8 +393,8 @@ vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v
  *
  * query head h reads key head h / (Hq / heads).  A token that attends nothing has out = 0 and lse = -infinity.  Keys and values of
  * positions that nobody attends, behind a request's end or out of every token's mask, may hold anything; where only some tokens attend one, the
- * others are not touched by it, but for those its value must be finite (infinities and NaN act as the largest finite number).  Products are
- * exact, sums fp32; the weights exp(x_i - m) are rounded to bf16 as an operand of the second product (not in lse), out once to bf16.
+ * others are not touched by it, but for those its value must be finite (infinities and NaN act as the largest finite number).  Queries of
+ * requests, attended keys and values, and the scores x_i must be finite.  Products are exact, sums fp32; the weights exp(x_i - m) are rounded to bf16 as an operand of the second product (not in lse), out once to bf16.
  *
  *   q        [N, Hq, D] as vt_heads                     out      [N, Hq, D] as vt_heads (out)      lse  dev [N, Hq] float (out) or NULL
  *   cu_tokens  dev [B + 1] int32, ascending, within [0, N]; rows outside all requests are left as they were

@@ -122,10 +122,12 @@ bool real(PyObject* o, float* out) {
     return true;
 }
 const vt_cache* cache_of(PyObject* o) { return reinterpret_cast<const vt_cache*>(PyLong_AsVoidPtr(o)); }
-bool table_of(PyObject* o, int* dev, const uint64_t** out) {
+bool table_of(PyObject* o, int rot_dim, int* dev, const uint64_t** out) {
     const at::Tensor* t;
     if (!tensor(o, "rope", &t)) return false;
     if (!here(*t, dev)) return refuse(PyExc_ValueError, "rope", "its table lies on another device");
+    if (t->scalar_type() != at::kLong || t->dim() != 1 || !t->is_contiguous() || t->size(0) != rot_dim / 2)
+        return refuse(PyExc_ValueError, "rope", "its table is not one of rot_dim / 2 frequencies");
     *out = reinterpret_cast<const uint64_t*>(t->data_ptr());
     return true;
 }
@@ -147,8 +149,8 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const uint64_t* table;
     float amplitude;
     const bool with_k = n == 9 && a[1] != Py_None;
-    if (!count(n, 9) || !heads(a[0], "q", &dev, &q) || !vector(a[2], "positions", q.n, at::kInt, &dev, &positions) || !table_of(a[3], &dev, &table) ||
-        !whole(a[4], "rot_dim", &rot) || !real(a[5], &amplitude) || !whole(a[6], "options", &options) ||
+    if (!count(n, 9) || !heads(a[0], "q", &dev, &q) || !vector(a[2], "positions", q.n, at::kInt, &dev, &positions) || !whole(a[4], "rot_dim", &rot) ||
+        !table_of(a[3], rot, &dev, &table) || !real(a[5], &amplitude) || !whole(a[6], "options", &options) ||
         !heads_out(a[7], "out_q", THPVariable_Unpack(a[0]), &dev, &out_q, &qo))
         return nullptr;
     if (with_k) {
@@ -190,7 +192,7 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return nullptr;
     }
     if (!vector(a[3], "positions", q.n, at::kInt, &dev, &positions) || !vector(a[4], "cu_tokens", (int64_t)c->B + 1, at::kInt, &dev, &cu) ||
-        !table_of(a[7], &dev, &table) || !whole(a[8], "rot_dim", &rot) || !real(a[9], &amplitude) || !whole(a[10], "options", &options) ||
+        !whole(a[8], "rot_dim", &rot) || !table_of(a[7], rot, &dev, &table) || !real(a[9], &amplitude) || !whole(a[10], "options", &options) ||
         !heads_out(a[11], "out_q", THPVariable_Unpack(a[0]), &dev, &out_q, &qo))
         return nullptr;
     void* stream = stream_of(dev);

@@ -174,3 +174,13 @@ def test_tree_mask(vt, N, words):
     owner = np.searchsorted(cu, np.arange(N), side="right") - 1
     assert np.array_equal(positions.cpu().numpy(), depth + lens[owner])
     assert np.array_equal(vt.vt_tree_mask(dev(parents), dev(cu), 32 * words)[1].cpu().numpy(), depth)
+
+
+def test_a_table_of_another_size_is_refused(vt):
+    rope = vt.vt_rope_table(64)
+    q = torch.zeros(3, 2, 128, dtype=torch.bfloat16, device="cuda")
+    positions = torch.arange(3, dtype=torch.int32, device="cuda")
+    for wrong in (rope._replace(rot_dim=128), rope._replace(table=rope.table[:-1]), rope._replace(table=rope.table[::2], rot_dim=32),
+                  rope._replace(table=rope.table.int()), rope._replace(table=rope.table.cpu())):
+        with pytest.raises(ValueError):
+            vt.vt_rope(q, None, positions, wrong)
