@@ -990,11 +990,12 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 
 // ------------------------------------------------------------------------------------------ joining an item's pieces
 // lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  Block (c, y) takes
-// the item that CTA c names, every gridDim.y-th group of its rows; a thread has four columns of two rows and asks for all it needs of four pieces
-// at once, so that an item of two pieces costs one memory round trip behind its entry.  Each thread works its rows' weights out for
+// the item that CTA c names, every gridDim.y-th group of its rows; a thread has four columns of a row and asks for all it needs of BATCH pieces
+// at once, so that an item of as many pieces costs one memory round trip behind its entry.  Each thread works its row's weights out for
 // itself: a step through shared memory, and finding the groups by a sum over all entries, took 25 us where this takes 8.
-constexpr int kJoinBatch = 4;
-template <int D>
+// Eight pieces at a time with few rows, where pieces are many and their latencies are what it costs (one token of eight heads on a key head over 60000: the
+// whole call 25.6 us, 29.7 with four); else four (16 x 60 over 8000: 86 us, 88 with eight).
+template <int D, int BATCH>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnParams p) {
     constexpr int kRows = 1024 / D, kQuads = D / 4;          // rows and runs of four columns that 256 threads cover
@@ -1002,65 +1003,44 @@ attn_join_kernel(const __grid_constant__ AttnParams p) {
     if (threadIdx.x == 0) grid_launch_dependents();
     const AttnSplit d = p.splits[blockIdx.x];
     const int cq = (int)threadIdx.x / kRows;
-    for (int row0 = (int)blockIdx.y * 2 * kRows + (int)threadIdx.x % kRows; row0 < d.rows; row0 += (int)gridDim.y * 2 * kRows) {
-        float m[2], l[2];
-        float4 o[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            m[u] = -INFINITY;
-            l[u] = 0.0f;
-            o[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
+    for (int row = (int)blockIdx.y * kRows + (int)threadIdx.x % kRows; row < d.rows; row += (int)gridDim.y * kRows) {
+        float m = -INFINITY, l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-        for (int i0 = 0; i0 < d.n_pieces; i0 += kJoinBatch) {
-            float2 ml[2][kJoinBatch];
-            float4 v[2][kJoinBatch];
+        for (int i0 = 0; i0 < d.n_pieces; i0 += BATCH) {
+            float2 ml[BATCH];
+            float4 v[BATCH];
 #pragma unroll
-            for (int k = 0; k < kJoinBatch; ++k) {
-                const int i = min(i0 + k, d.n_pieces - 1);   // (past the last: the last again, with no weight)
-                const size_t piece = (size_t)(d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0);
-                const float2* pm = p.part_ml + piece * p.rows_max;
-                const float4* po = reinterpret_cast<const float4*>(p.part_o) + (piece * kQuads + cq) * p.rows_max;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int row = min(row0 + u * kRows, d.rows - 1);
-                    ml[u][k] = pm[row];
-                    v[u][k] = po[row];
-                    if (i0 + k >= d.n_pieces) ml[u][k] = make_float2(-INFINITY, 0.0f);
+            for (int k = 0; k < BATCH; ++k) {
+                const int i = i0 + k;
+                ml[k] = make_float2(-INFINITY, 0.0f);
+                v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (i < d.n_pieces) {
+                    const size_t piece = (size_t)(d.first_cta + i) * 2 + (i == 0 ? d.first_slot : 0);
+                    ml[k] = p.part_ml[piece * p.rows_max + row];
+                    v[k] = reinterpret_cast<const float4*>(p.part_o)[(piece * kQuads + cq) * p.rows_max + row];
                 }
             }
+            float top = m;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float top = m[u];
+            for (int k = 0; k < BATCH; ++k) top = fmaxf(top, ml[k].x);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float f = ex2_approx((m - ref) * p.scale_log2);
+            m = top;
+            l *= f;
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
 #pragma unroll
-                for (int k = 0; k < kJoinBatch; ++k) top = fmaxf(top, ml[u][k].x);
-                const float ref = top == -INFINITY ? 0.0f : top;
-                const float f = ex2_approx((m[u] - ref) * p.scale_log2);
-                m[u] = top;
-                l[u] *= f;
-                o[u] = make_float4(o[u].x * f, o[u].y * f, o[u].z * f, o[u].w * f);
-#pragma unroll
-                for (int k = 0; k < kJoinBatch; ++k) {
-                    if (i0 + k >= d.n_pieces) break;         // (its O may be anything)
-                    const float w = ex2_approx((ml[u][k].x - ref) * p.scale_log2);
-                    l[u] = fmaf(ml[u][k].y, w, l[u]);
-                    o[u].x = fmaf(v[u][k].x, w, o[u].x);
-                    o[u].y = fmaf(v[u][k].y, w, o[u].y);
-                    o[u].z = fmaf(v[u][k].z, w, o[u].z);
-                    o[u].w = fmaf(v[u][k].w, w, o[u].w);
-                }
+            for (int k = 0; k < BATCH; ++k) {
+                const float w = ex2_approx((ml[k].x - ref) * p.scale_log2);
+                l = fmaf(ml[k].y, w, l);
+                o = make_float4(fmaf(v[k].x, w, o.x), fmaf(v[k].y, w, o.y), fmaf(v[k].z, w, o.z), fmaf(v[k].w, w, o.w));
             }
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int row = row0 + u * kRows;
-            if (row >= d.rows) break;
-            const float n = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
-            const int t = row / p.G, token = d.token0 + t, head = d.head0 + (row - t * p.G);
-            *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq) =
-                make_uint2(attn_bf16x2(o[u].x * n, o[u].y * n), attn_bf16x2(o[u].z * n, o[u].w * n));
-            if (cq == 0 && p.lse) p.lse[(int64_t)token * p.Hq + head] = l[u] == 0.0f ? -INFINITY : m[u] * p.scale + logf(l[u]);
-        }
+        const float n = l == 0.0f ? 0.0f : 1.0f / l;
+        const int t = row / p.G, token = d.token0 + t, head = d.head0 + (row - t * p.G);
+        *reinterpret_cast<uint2*>(p.out + (int64_t)token * p.out_ts + (int64_t)head * p.out_hs + 4 * cq) =
+            make_uint2(attn_bf16x2(o.x * n, o.y * n), attn_bf16x2(o.z * n, o.w * n));
+        if (cq == 0 && p.lse) p.lse[(int64_t)token * p.Hq + head] = l == 0.0f ? -INFINITY : m * p.scale + logf(l);
     }
 }
 
@@ -1105,7 +1085,7 @@ static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint
     count_launch();
     if (e == cudaSuccess && !p.whole) {
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)C, (unsigned)((p.rows_max + 2048 / D - 1) / (2048 / D)));
+        cfg.gridDim = dim3((unsigned)C, (unsigned)((p.rows_max + 1024 / D - 1) / (1024 / D)));
         cfg.blockDim = dim3(256);
         cfg.stream = st;
         cudaLaunchAttribute attr[1];
@@ -1113,7 +1093,7 @@ static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, attn_join_kernel<D>, p);
+        e = cudaLaunchKernelEx(&cfg, attn_join_kernel<D, REP ? 8 : 4>, p);
         count_launch();
     }
     if (e == cudaSuccess) e = cudaGetLastError();

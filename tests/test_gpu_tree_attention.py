@@ -112,6 +112,13 @@ def test_items_that_are_not_cut_and_items_in_many_pieces(vt):
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])         # the same bits
 
 
+# one long item in up to as many pieces as there are CTAs, and in one more or fewer than are fetched at a time
+@pytest.mark.parametrize("T,Hq,D,L", [(1, 8, 128, 40000), (1, 1, 64, 1100), (9, 4, 128, 2304), (33, 4, 64, 9000), (60, 4, 128, 2500)])
+def test_one_item_in_many_pieces(vt, T, Hq, D, L):
+    c = Case(vt, [L], [T], Hq, 1, D, 128, tree=T > 1)
+    c.check(*c.run())
+
+
 def test_many_requests(vt):
     rng = np.random.default_rng(3)
     lens, counts = rng.integers(0, 300, 700).tolist(), rng.integers(0, 4, 700).tolist()
