@@ -31,12 +31,13 @@
 //
 // Bound and measured (in a graph, a copy at 6.46 TB/s and 1673 TFLOP/s in bf16 as the floors; requests x tokens over positions, 32 heads over 8
 // of 128 where nothing else stands):
-//   2 x 8 over 100000             136 us   floor 127: bytes of the cache, 6.0 TB/s
-//   64 x 1 over 4096, ragged       99 us   floor 86: bytes, 5.6 TB/s
-//   24 x 8 over 2500, 32 heads of 64 each, ragged   63 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
-//   16 x 60 over 8000, ragged      95 us   floor 54: a stream's step is exponentials, then its products: 4140 cycles for a pair of 2 x 1024 each
-//   1 x 60 over 4000               28 us   floor 3: latency; 70 runs of four tiles and the join
-//   1 x 1 over 700                12.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
+//   2 x 8 over 100000             132 us   floor 127: bytes of the cache, 6.2 TB/s
+//   64 x 1 over 4096, ragged       98 us   floor 86: bytes, 5.7 TB/s
+//   24 x 8 over 2500, 32 heads of 64 each, ragged   61 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
+//   16 x 60 over 8000, ragged      88 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
+//                                          whose products, and whose exponentials, would each take 2048
+//   1 x 60 over 4000               26 us   floor 3: latency; 70 runs of four tiles and the join
+//   1 x 1 over 700                11.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
 #include "vt_step.h"
 #include "vt_tc.cuh"
 
@@ -790,7 +791,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         }
                         // The scores are read twice, half of them at a time, for their maximum and for the weights.  (One pass with the old maximum,
                         // made again where it grew too much, has fewer instructions to issue but four times as many to fetch, as all weights wait in
-                        // registers: slower by 5 to 10 %.)
+                        // registers: slower by 5 to 10 %.  All scores kept in registers from the first reading: 111 -> 123 us for two long documents
+                        // under 60 tokens, half of them 117; 32 at a time, the next on their way: the same.)
                         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
                         for (int c = 0; c < 2; ++c) {
