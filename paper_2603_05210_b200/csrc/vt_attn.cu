@@ -17,7 +17,7 @@
 // and warp, are added up at the item's end.  The products cost the same, the exponentials a quarter (64 x 1 over 4096: 113 -> 100 us).
 //
 // Work.  The lengths are known on the device alone, so the cut is made there: all key tiles of all (request, key head, row block) in a row,
-// an equal run of them to each CTA.  A run begins and ends inside an item, and a long item lies in many runs: a CTA writes what it has
+// a run of equal weight to each CTA.  A run begins and ends inside an item, and a long item lies in many runs: a CTA writes what it has
 // of such an item (unnormalised O, m, l in fp32) to the workspace, and a second kernel joins the pieces.  No atomics: the same bits every time.
 // Where the host can see that no item is longer than kAttnWhole tiles, items are not cut and there is one launch.
 //
@@ -33,10 +33,10 @@
 // of 128 where nothing else stands):
 //   2 x 8 over 100000             132 us   floor 127: bytes of the cache, 6.2 TB/s
 //   64 x 1 over 4096, ragged       98 us   floor 86: bytes, 5.7 TB/s
-//   24 x 8 over 2500, 32 heads of 64 each, ragged   61 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
-//   16 x 60 over 8000, ragged      88 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
+//   24 x 8 over 2500, 32 heads of 64 each, ragged   57 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
+//   16 x 60 over 8000, ragged      72 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
 //                                          whose products, and whose exponentials, would each take 2048
-//   1 x 60 over 4000               26 us   floor 3: latency; 70 runs of four tiles and the join
+//   1 x 60 over 4000               24 us   floor 3: latency; 93 runs of three tiles and the join
 //   1 x 1 over 700                11.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
 #include "vt_step.h"
 #include "vt_tc.cuh"
@@ -52,7 +52,7 @@ constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
 constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
 constexpr int kAttnMaxStages = 12;
-constexpr int kAttnItemCost = 3;             // what an item's beginning and end cost, in tiles
+constexpr int kAttnItemCost = 4;             // what an item's beginning and end cost, in its tiles (24 x 8 over 2500: 57 us; with 2 tiles 71, 3 60, 6 58)
 constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
 constexpr uint32_t kAttnTmemO = 0, kAttnTmemS = 256;
 
@@ -79,7 +79,7 @@ struct AttnParams {
     int tpt;                                 // tokens per row tile
     int box_tokens;                          // tokens in a box of q
     int whole;                               // 1: items are not cut
-    int min_run;                             // the least weight of a CTA's run
+    int min_run;                             // the least weight of a CTA's run, 2 at least
     int n_stages;
     uint32_t stages_inv;                     // 2^32 / n_stages, rounded up
     uint32_t q_block, q_slot;                // bytes of 64 columns of a row tile; of a row tile
@@ -231,13 +231,20 @@ __device__ __forceinline__ int attn_keys(const AttnParams& p, const AttnRequest&
 }
 __device__ __forceinline__ int attn_tiles(int keys) { return max(1, (keys + kAttnKeys - 1) / kAttnKeys); }
 __device__ __forceinline__ int attn_blocks(const AttnParams& p, const AttnRequest& q) { return (q.T + 2 * p.tpt - 1) / (2 * p.tpt); }
-// What a key head of a request weighs: its items' tiles, and kAttnItemCost for each item.
+// What a tile of a block of so many tokens weighs: with two row tiles twice as much is worked out for it (4 ragged trees of 40 over 30000: 87 us
+// when all weigh the same, 70 so).
+__device__ __forceinline__ int attn_tile_weight(const AttnParams& p, int tokens) { return tokens > p.tpt ? 2 : 1; }
+// What a key head of a request weighs: its items' tiles, and kAttnItemCost more for each item.
 __device__ __forceinline__ long long attn_head_weight(const AttnParams& p, const AttnRequest& q) {
     const int blocks = attn_blocks(p, q);
-    long long n = (long long)blocks * kAttnItemCost;
-    if (p.mask) return blocks > 0 ? n + (long long)blocks * attn_tiles(attn_keys(p, q, q.T)) : 0;
+    long long n = 0;
+    if (p.mask) {                            // all blocks but the last are full, and as long
+        const int last = attn_tile_weight(p, q.T - (blocks - 1) * 2 * p.tpt);
+        return blocks > 0 ? (2ll * (blocks - 1) + last) * (kAttnItemCost + attn_tiles(attn_keys(p, q, q.T))) : 0;
+    }
 #pragma unroll 1
-    for (int i = 0; i < blocks; ++i) n += attn_tiles(attn_keys(p, q, (i + 1) * 2 * p.tpt));
+    for (int i = 0; i < blocks; ++i)
+        n += (long long)attn_tile_weight(p, q.T - i * 2 * p.tpt) * (kAttnItemCost + attn_tiles(attn_keys(p, q, (i + 1) * 2 * p.tpt)));
     return n;
 }
 // W units in C runs, the first `more` of them a unit longer than the others.
@@ -492,14 +499,14 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         w.tok0 = i * 2 * p.tpt;
                         w.ntok = min(2 * p.tpt, q.T - w.tok0);
                         w.keys = attn_keys(p, q, w.tok0 + w.ntok);
-                        const int tiles = attn_tiles(w.keys);
-                        const long long s0 = s + kAttnItemCost;          // the first tile's place
-                        s = s0 + tiles;
+                        const int tiles = attn_tiles(w.keys), heavy = attn_tile_weight(p, w.ntok) - 1;
+                        const long long s1 = s, s0 = s1 + (kAttnItemCost << heavy);          // the item's place, and its first tile's
+                        s = s0 + ((long long)tiles << heavy);
                         if (s <= g0) continue;
-                        // not cut: the item goes to the run it begins in
-                        const long long lo = p.whole ? (s0 - kAttnItemCost >= g0 ? 0 : tiles) : max(g0 - s0, 0ll);
-                        const long long hi = p.whole ? tiles : min(g1 - s0, (long long)tiles);
-                        const bool begun = s0 - kAttnItemCost < g0;      // the run begins inside the item
+                        // a tile goes to the run that its place lies in; not cut: the item to the run it begins in
+                        const long long lo = p.whole ? (s1 >= g0 ? 0 : tiles) : (max(g0 - s0, 0ll) + heavy) >> heavy;
+                        const long long hi = p.whole ? tiles : min((g1 - s0 + heavy) >> heavy, (long long)tiles);
+                        const bool begun = s1 < g0;                      // the run begins inside the item
                         if (hi <= lo) continue;
                         w.n = (int)(hi - lo);
                         w.t0 = (int)lo;
@@ -511,7 +518,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         w.first = q.first;
                         w.dual = w.ntok > p.tpt;
                         w.cut = w.n < tiles;
-                        w.slot = begun || s0 - kAttnItemCost == g0 ? 0 : 1;
+                        w.slot = begun || s1 == g0 ? 0 : 1;
                         w.pad[0] = w.pad[1] = 0;
                         ok = publish(w);
                         if (!ok) break;
@@ -540,8 +547,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                                 split.token0 = q.first + w.tok0;
                                 split.head0 = h * p.G;
                                 split.first_cta = c0;
-                                split.n_pieces = cut.of(s - 1) - c0 + 1;
-                                split.first_slot = cut.start(c0) >= s0 - kAttnItemCost ? 0 : 1;
+                                split.n_pieces = cut.of(s - 1 - heavy) - c0 + 1;      // (the last tile's place)
+                                split.first_slot = cut.start(c0) >= s1 ? 0 : 1;
                             }
                         }
                         first = false;
@@ -996,7 +1003,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 // at once, so that an item of as many pieces costs one memory round trip behind its entry.  Each thread works its row's weights out for
 // itself: a step through shared memory, and finding the groups by a sum over all entries, took 25 us where this takes 8.
 // Eight pieces at a time with few rows, where pieces are many and their latencies are what it costs (one token of eight heads on a key head over 60000: the
-// whole call 25.6 us, 29.7 with four); else four (16 x 60 over 8000: 86 us, 88 with eight).
+// whole call 25.6 us, 29.7 with four); else four (16 x 60 over 8000: eight take 2 us more).
 template <int D, int BATCH>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnParams p) {
@@ -1138,7 +1145,7 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.tpt = 128 / p.G;
     p.box_tokens = std::min(p.tpt, c.max_tokens);
     p.whole = (long long)a.max_pages * a.page_size <= (long long)kAttnWhole * kAttnKeys;
-    p.min_run = p.rows_max > 128 ? 4 : 2;
+    p.min_run = p.rows_max > 128 ? 6 : 2;                      // 1 x 60 over 4000: 23.6 us, 24.7 with 8
     p.scale = c.scale;
     p.scale_log2 = c.scale * kLog2e;
     p.wait_ns = kWaitLimitNs;
