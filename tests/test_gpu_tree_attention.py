@@ -112,6 +112,22 @@ def test_items_that_are_not_cut_and_items_in_many_pieces(vt):
         assert torch.equal(out, again[0]) and torch.equal(lse, again[1])         # the same bits
 
 
+# ragged trees whose items weigh differently (one row tile and two, side by side in a run), runs that end between the places of a heavy tile
+@pytest.mark.parametrize("seed", range(4))
+def test_light_and_heavy_items_in_one_call(vt, seed):
+    rng = np.random.default_rng(seed)
+    B = int(rng.integers(2, 12))
+    lens, counts = rng.integers(0, 2500, B).tolist(), rng.integers(0, 75, B).tolist()
+    c = Case(vt, lens, counts, 8, 2, 128 if seed & 1 else 64, 32, tree=seed < 2)
+    c.check(*c.run())
+
+
+def test_a_bound_far_above_the_tokens(vt):
+    c = Case(vt, [700, 90], [1, 2], 8, 2, 128, 16, tree=True)
+    c.max_tokens = 5000
+    c.check(*c.run())
+
+
 # one long item in up to as many pieces as there are CTAs, and in one more or fewer than are fetched at a time
 @pytest.mark.parametrize("T,Hq,D,L", [(1, 8, 128, 40000), (1, 1, 64, 1100), (9, 4, 128, 2304), (33, 4, 64, 9000), (60, 4, 128, 2500)])
 def test_one_item_in_many_pieces(vt, T, Hq, D, L):

@@ -116,6 +116,25 @@ def test_the_largest_vocabularies(vt, drawn):
     check(vt, a, 4)
 
 
+def test_the_largest_drawn_vocabulary_with_rows_anywhere_and_the_most_tokens(vt):
+    rng = np.random.default_rng(4)
+    V, Vd, N = 393216, 1000, 5
+    P = rng.random((N, V), dtype=np.float32) ** 8
+    P /= P.sum(1, keepdims=True, dtype=np.float64).astype(np.float32)
+    Q = rng.random((N, Vd), dtype=np.float32)
+    Q /= Q.sum(1, keepdims=True)
+    d2t, ids = rng.permutation(V)[:Vd], np.array([0, 5, 70, 7, 999])
+    a = dict(P=P, parents=[-1, 0, 0, 1, 0], cu=[0, 5], u_accept=np.float32([0, .99, .99, .99, .99]), u_sample=np.float32([0.999999]), tokens=d2t[ids])
+    want = so.verify(P, a["tokens"], a["parents"], a["cu"], a["u_accept"], a["u_sample"], 1024, Q, ids, d2t)
+    flat = torch.full((N * (V + 1) + 1,), float("nan"), device="cuda")
+    rows = flat[1:].view(N, V + 1)[:, :V]
+    rows.copy_(dev(P, torch.float32))
+    got = vt.vt_verify_tokens(rows, dev(a["tokens"]), dev(a["parents"]), dev(a["cu"]), dev(a["u_accept"], torch.float32), dev(a["u_sample"], torch.float32),
+                              max_tokens=1024, draft_probs=dev(Q, torch.float32), draft_ids=dev(ids), d2t=dev(d2t))
+    for g, w in zip(got, want):
+        assert np.array_equal(g.cpu().numpy(), w)
+
+
 @pytest.mark.parametrize("drawn", [False, True])
 def test_many_random_trees(vt, drawn):
     for seed in range(12):
