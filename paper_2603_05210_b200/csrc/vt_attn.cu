@@ -36,7 +36,7 @@
 //   24 x 8 over 2500, 32 heads of 64 each, ragged   57 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
 //   16 x 60 over 8000, ragged      72 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
 //                                          whose products, and whose exponentials, would each take 2048
-//   1 x 60 over 4000               24 us   floor 3: latency; 93 runs of three tiles and the join
+//   1 x 60 over 4000             21.6 us   floor 3: latency; 93 runs of three tiles and the join
 //   1 x 1 over 700                11.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
 #include "vt_step.h"
 #include "vt_tc.cuh"
@@ -56,7 +56,7 @@ constexpr int kAttnItemCost = 4;             // what an item's beginning and end
 constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
 constexpr uint32_t kAttnTmemO = 0, kAttnTmemS = 256;
 
-struct AttnSplit {                           // a CTA's first item, where the CTA's run begins inside it and it is the first to do so
+struct AttnSplit {                           // an item that several CTAs have pieces of
     int rows;                                // 0: none
     int token0, head0, n_pieces, first_cta;
     int first_slot;                          // of the first piece: 0 where its CTA's run begins with the item
@@ -71,7 +71,7 @@ struct AttnParams {
     int64_t out_ts, out_hs;
     float* lse;
     WsHeader* hdr;
-    AttnSplit* splits;                       // [gridDim.x]
+    AttnSplit* splits;                       // [n_splits]
     float2* part_ml;                         // [gridDim.x][2][rows]: (m, l) of a piece's rows
     float* part_o;                           // [gridDim.x][2][D / 4][rows][4]
     int rows_max;                            // rows of a block at most
@@ -79,6 +79,8 @@ struct AttnParams {
     int tpt;                                 // tokens per row tile
     int box_tokens;                          // tokens in a box of q
     int whole;                               // 1: items are not cut
+    int blocks;                              // row blocks of a request at most
+    int entries, n_splits;                   // entries of the join: one for every item there may be, where rows are many and those no more than CTAs (else 0); all in all
     int min_run;                             // the least weight of a CTA's run, 2 at least
     int n_stages;
     uint32_t stages_inv;                     // 2^32 / n_stages, rounded up
@@ -259,6 +261,34 @@ struct AttnCut {
         const long long at = more * (base + 1);
         const long long n = g < at ? g : g - at, d = g < at ? base + 1 : base;
         return (int)((g < at ? 0 : more) + attn_div(n, d));
+    }
+};
+
+// Block i of a key head of a request, and its places from `at` on.
+struct AttnItem {
+    int tok0, ntok, keys, tiles, heavy;      // heavy: log2 of a tile's weight
+    long long begin, first, end;             // its place, its first tile's, the next item's
+    __device__ __forceinline__ AttnItem(const AttnParams& p, const AttnRequest& q, int i, long long at) {
+        tok0 = i * 2 * p.tpt;
+        ntok = min(2 * p.tpt, q.T - tok0);
+        keys = attn_keys(p, q, tok0 + ntok);
+        tiles = attn_tiles(keys);
+        heavy = attn_tile_weight(p, ntok) - 1;
+        begin = at;
+        first = at + (kAttnItemCost << heavy);
+        end = first + ((long long)tiles << heavy);
+    }
+    // what the join has to know where several runs have tiles of the item
+    __device__ __forceinline__ AttnSplit split(const AttnParams& p, const AttnRequest& q, int h, const AttnCut& cut) const {
+        AttnSplit r{};
+        const int c0 = cut.of(first);
+        r.n_pieces = cut.of(end - 1 - heavy) - c0 + 1;       // (to the last tile's place)
+        r.rows = r.n_pieces > 1 ? ntok * p.G : 0;
+        r.token0 = q.first + tok0;
+        r.head0 = h * p.G;
+        r.first_cta = c0;
+        r.first_slot = cut.start(c0) >= begin ? 0 : 1;
+        return r;
     }
 };
 
@@ -496,18 +526,16 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 #pragma unroll 1
                     for (int i = 0; i < blocks && s < g1 && ok; ++i) {
                         AttnPiece w;
-                        w.tok0 = i * 2 * p.tpt;
-                        w.ntok = min(2 * p.tpt, q.T - w.tok0);
-                        w.keys = attn_keys(p, q, w.tok0 + w.ntok);
-                        const int tiles = attn_tiles(w.keys), heavy = attn_tile_weight(p, w.ntok) - 1;
-                        const long long s1 = s, s0 = s1 + (kAttnItemCost << heavy);          // the item's place, and its first tile's
-                        s = s0 + ((long long)tiles << heavy);
+                        const AttnItem it(p, q, i, s);
+                        s = it.end;
                         if (s <= g0) continue;
                         // a tile goes to the run that its place lies in; not cut: the item to the run it begins in
-                        const long long lo = p.whole ? (s1 >= g0 ? 0 : tiles) : (max(g0 - s0, 0ll) + heavy) >> heavy;
-                        const long long hi = p.whole ? tiles : min((g1 - s0 + heavy) >> heavy, (long long)tiles);
-                        const bool begun = s1 < g0;                      // the run begins inside the item
+                        const long long lo = p.whole ? (it.begin >= g0 ? 0 : it.tiles) : (max(g0 - it.first, 0ll) + it.heavy) >> it.heavy;
+                        const long long hi = p.whole ? it.tiles : min((g1 - it.first + it.heavy) >> it.heavy, (long long)it.tiles);
                         if (hi <= lo) continue;
+                        w.tok0 = it.tok0;
+                        w.ntok = it.ntok;
+                        w.keys = it.keys;
                         w.n = (int)(hi - lo);
                         w.t0 = (int)lo;
                         w.b = b;
@@ -517,8 +545,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         w.T = q.T;
                         w.first = q.first;
                         w.dual = w.ntok > p.tpt;
-                        w.cut = w.n < tiles;
-                        w.slot = begun || s1 == g0 ? 0 : 1;
+                        w.cut = w.n < it.tiles;
+                        w.slot = it.begin <= g0 ? 0 : 1;
                         w.pad[0] = w.pad[1] = 0;
                         ok = publish(w);
                         if (!ok) break;
@@ -539,18 +567,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         }
                         ok = ok && copy_tiles(w, loads, false);
                         loads += 2u * w.n;
-                        // the first CTA whose run begins behind the item's first tile names it for the join
-                        if (first && w.t0 > 0) {
-                            const int c0 = cut.of(s0);
-                            if (c0 == cta - 1) {
-                                split.rows = w.ntok * p.G;
-                                split.token0 = q.first + w.tok0;
-                                split.head0 = h * p.G;
-                                split.first_cta = c0;
-                                split.n_pieces = cut.of(s - 1 - heavy) - c0 + 1;      // (the last tile's place)
-                                split.first_slot = cut.start(c0) >= s1 ? 0 : 1;
-                            }
-                        }
+                        // many items: the first CTA whose run begins behind the item's first tile names it for the join
+                        if (p.entries == 0 && first && w.t0 > 0 && cut.of(it.first) == cta - 1) split = it.split(p, q, h, cut);
                         first = false;
                     }
                 }
@@ -561,7 +579,20 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             end.n = 0;
             (void)publish(end);
         }
-        if (lane == 0 && !p.whole) p.splits[cta] = split;
+        if (!REP && cta < p.entries) {                       // few items: each has its entry
+            const int b = cta / (p.Hkv * p.blocks), h = cta / p.blocks - b * p.Hkv, i = cta % p.blocks, from = b / per;
+            long long s = __shfl_sync(0xFFFFFFFFu, at, from);
+#pragma unroll 1
+            for (int o = from * per; o < b; ++o) s += attn_head_weight(p, attn_request(p, o)) * p.Hkv;
+            const AttnRequest q = attn_request(p, b);
+            s += h * attn_head_weight(p, q);
+            if (q.T > 0 && i < attn_blocks(p, q)) {
+#pragma unroll 1
+                for (int j = 0; j < i; ++j) s = AttnItem(p, q, j, s).end;
+                split = AttnItem(p, q, i, s).split(p, q, h, cut);
+            }
+        }
+        if (lane == 0 && cta < p.n_splits) p.splits[cta] = split;
         if (bad) atomicOr(&p.hdr->status, kStatusPage);
     } else if (warp == kAttnProducerV) {
         // ---------------------------------------------------------------- producer of values
@@ -999,7 +1030,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
 
 // ------------------------------------------------------------------------------------------ joining an item's pieces
 // lse and out of rows that several CTAs have pieces of: weights 2^{(m_c - m) scale log2 e}, pieces in the order of the CTAs.  Block (c, y) takes
-// the item that CTA c names, every gridDim.y-th group of its rows; a thread has four columns of a row and asks for all it needs of BATCH pieces
+// entry c, every gridDim.y-th group of the item's rows; an entry is an item, where rows are many and there may be no more items than CTAs, or the item that CTA c
+// is the first to go on with; a thread has four columns of a row and asks for all it needs of BATCH pieces
 // at once, so that an item of as many pieces costs one memory round trip behind its entry.  Each thread works its row's weights out for
 // itself: a step through shared memory, and finding the groups by a sum over all entries, took 25 us where this takes 8.
 // Eight pieces at a time with few rows, where pieces are many and their latencies are what it costs (one token of eight heads on a key head over 60000: the
@@ -1094,7 +1126,7 @@ static vt_status run_attn(const AttnMaps& maps, const AttnParams& p, int C, uint
     count_launch();
     if (e == cudaSuccess && !p.whole) {
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)C, (unsigned)((p.rows_max + 1024 / D - 1) / (1024 / D)));
+        cfg.gridDim = dim3((unsigned)p.n_splits, (unsigned)((p.rows_max + 1024 / D - 1) / (1024 / D)));
         cfg.blockDim = dim3(256);
         cfg.stream = st;
         cudaLaunchAttribute attr[1];
@@ -1145,7 +1177,14 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.tpt = 128 / p.G;
     p.box_tokens = std::min(p.tpt, c.max_tokens);
     p.whole = (long long)a.max_pages * a.page_size <= (long long)kAttnWhole * kAttnKeys;
-    p.min_run = p.rows_max > 128 ? 6 : 2;                      // 1 x 60 over 4000: 23.6 us, 24.7 with 8
+    const bool few = p.rows_max <= 32;
+    p.blocks = (std::min(c.max_tokens, c.N) + 2 * p.tpt - 1) / (2 * p.tpt);
+    const long long items = (long long)a.B * a.heads * p.blocks;
+    // Most CTAs name no item where there are few: 30 blocks each for 240 rows, only to leave (1 x 60 over 4000: 24 us so, 21.6 with an entry per item).
+    // With few rows there are four at most, and the entries' code costs as much.
+    p.entries = !p.whole && !few && items <= C ? (int)items : 0;
+    p.n_splits = p.whole ? 0 : p.entries > 0 ? p.entries : C;
+    p.min_run = p.rows_max > 128 ? 6 : 2;                      // (1 x 60 over 4000: 24.7 us with 8, 23.6 with 6)
     p.scale = c.scale;
     p.scale_log2 = c.scale * kLog2e;
     p.wait_ns = kWaitLimitNs;
@@ -1154,7 +1193,6 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
         p.wait_ns = (unsigned long long)us * 1000ull;
     }
     const uint32_t rows = (uint32_t)(p.box_tokens * p.G);
-    const bool few = p.rows_max <= 32;
     p.q_block = few ? 16384u : (rows + 7) / 8 * 1024;
     p.q_slot = p.q_block * (D / 64);
     p.q_tx = rows * 128u * (D / 64) * (few ? 4u : 1u);

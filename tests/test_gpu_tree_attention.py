@@ -122,6 +122,16 @@ def test_light_and_heavy_items_in_one_call(vt, seed):
     c.check(*c.run())
 
 
+# more items than CTAs, as many, one less; some requests without tokens
+@pytest.mark.parametrize("B", [36, 37, 38, 60])
+def test_as_many_items_as_there_are_ctas(vt, B):
+    rng = np.random.default_rng(B)
+    lens, counts = rng.integers(0, 1500, B).tolist(), rng.integers(0, 12, B).tolist()
+    lens[0], counts[0] = 9000, 12
+    c = Case(vt, lens, counts, 16, 4, 64, 32, tree=True)
+    c.check(*c.run())
+
+
 def test_a_bound_far_above_the_tokens(vt):
     c = Case(vt, [700, 90], [1, 2], 8, 2, 128, 16, tree=True)
     c.max_tokens = 5000
