@@ -50,7 +50,7 @@ constexpr int kAttnProducer = 8, kAttnIssuer = 9, kAttnCleaner = 10, kAttnProduc
 constexpr int attn_threads(bool few) { return (few ? 13 : 12) * 32; }
 constexpr int kAttnPieces = 4;               // pieces the planner may be ahead
 constexpr int kAttnCtas = 148;               // runs at most
-constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting
+constexpr int kAttnWhole = 4;                // tiles of an item that is not worth cutting (16 x 60 over 440: 20 us, cut 24.5; 1 x 60 over 900: cut 18, 25 with 8 tiles)
 constexpr int kAttnMaxStages = 12;
 constexpr int kAttnItemCost = 4;             // what an item's beginning and end cost, in its tiles (24 x 8 over 2500: 57 us; with 2 tiles 71, 3 60, 6 58)
 constexpr float kAttnSlack = 8.0f;           // how far (in powers of two) a maximum may grow before O is rescaled
