@@ -29,6 +29,18 @@
 // infinities and NaN of V into the largest finite number, so that a weight of 0 keeps them out.
 // All waits are bounded; one that runs out sets the status word and every role leaves.
 //
+// Turns of the ring.  K and V tiles take places in one order (AttnPiece::k_at), place P stage P mod ST, turn P / ST, and the cleaner passes
+// every place in that order.  A wait names a turn by its parity and also passes when the turn before is not over, so whoever waits has to
+// know that it is; ST is 5 at least, and "passed" is said of the cleaner:
+//   a producer   waits for v_clean(P - ST), then kv_empty(P - ST).  Its last place lies 3 before P at most, so P - 3 - ST, and P - 2 ST with it,
+//                has been passed when it asks for v_clean; and P - ST is passed only when it was loaded, after its producer saw P - 2 ST empty.
+//   one issuer   takes all value places, 3 apart at most, and all key places behind the values before them: P - ST has been passed.
+//   two issuers  wait for the weights of a step before its values.  An item's first weights come behind the last item's O, so all of that one's
+//                places have been passed; V(0) lies at place 1 or 2 of the item and V(1) at 3 or 4, later values of a stream 3 or 4 behind its last.  K(j)
+//                follows the stream's V(j - 2), one place before it; K(0) and K(1) its last values, 2 places before the item at most, or, where the
+//                last item (of one tile) had none for it, the O of the item before.
+// (With the values first, or without a look at v_clean in the producers, copies of a slow stream's tiles were overtaken: no error, wrong values.)
+//
 // Bound and measured (in a graph, a copy at 6.46 TB/s and 1673 TFLOP/s in bf16 as the floors; requests x tokens over positions, 32 heads over 8
 // of 128 where nothing else stands):
 //   2 x 8 over 100000             132 us   floor 127: bytes of the cache, 6.2 TB/s
@@ -448,7 +460,8 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         for (int j = 0; j < w.n; ++j) {
             const int page_next = page_of(j + 1);            // one ahead of its use
             const uint32_t place = loads + (values ? w.v_at(j) : w.k_at(j)), turn = turn_of(place), stage = place - turn * ST;
-            if (!wait(kv_empty + 8u * stage, (turn & 1u) ^ 1u)) return false;        // (in the first turn there is nothing to wait for)
+            // (in the first turn there is nothing to wait for)
+            if (!wait(v_clean + 8u * stage, (turn & 1u) ^ 1u) || !wait(kv_empty + 8u * stage, (turn & 1u) ^ 1u)) return false;
             const bool there = mine && j < end;
             uint32_t boxes = (uint32_t)np * (D / 64);
             if (j == last_tile) boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
@@ -635,9 +648,12 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 if (i >= 0) {
                     const uint32_t place = loads + w.v_at(i >> w.dual), turn = turn_of(place), st = place - turn * ST;
                     const int steps = attn_k_steps(w, i >> w.dual);
-                    if (!wait(v_clean + 8u * st, turn & 1u)) { ok = false; break; }
-                    if (!REP) keys = more && i + 2 > w.dual && attn_test(kv_full + 8u * k_st, k_turn & 1u);
-                    if (!wait(p_full + 8u * s, p_phase >> s & 1u)) { ok = false; break; }
+                    auto weights = [&]() -> bool { return wait(p_full + 8u * s, p_phase >> s & 1u); };
+                    if ((REP && !weights()) || !wait(v_clean + 8u * st, turn & 1u)) { ok = false; break; }
+                    if (!REP) {
+                        keys = more && i + 2 > w.dual && attn_test(kv_full + 8u * k_st, k_turn & 1u);
+                        if (!weights()) { ok = false; break; }
+                    }
                     p_phase ^= 1u << s;
                     tc_fence_after();
                     if (attn_elect()) {
@@ -1200,6 +1216,8 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     // five stages of 32 KB beside two full row tiles: 160 KB in flight
     const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces);
     p.n_stages = (int)std::min((uint32_t)kAttnMaxStages, ((uint32_t)kMaxDynSmem - tail - 2 * p.q_slot) / tile);
+    static_assert((kMaxDynSmem - (sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces)) - 2 * 32768) / (kAttnKeys * 128 * 2) >= 5,
+                  "the order of waits in the ring takes five stages");
     p.stages_inv = (uint32_t)((0x100000000ull + p.n_stages - 1) / p.n_stages);
     p.shared_off = 2 * p.q_slot + p.n_stages * tile;
     p.bar_off = p.shared_off + sizeof(AttnShared);
