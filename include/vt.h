@@ -376,7 +376,7 @@ typedef struct vt_cache {
 /* vt_rope for serving: queries are turned into q_out, keys are turned and stored in the cache, values [N, Hkv, D] are stored beside them.
  * Token n belongs to the request b with cu_tokens[b] <= n < cu_tokens[b + 1] and goes to position lens[b] + n - cu_tokens[b]; lens
  * itself stays as it is.
- *   cu_tokens  dev [B + 1] int32, ascending          positions  dev [N] int32: what the angles go by (in a tree the depth, not the place)
+ *   cu_tokens  dev [B + 1] int32, ascending, within [0, N] (below 0 counts as 0)          positions  dev [N] int32: what the angles go by (in a tree the depth, not the place)
  * Tokens outside [cu_tokens[0], cu_tokens[B]) are padding: nothing of theirs is written.  A token whose position lies past the table, or
  * whose page id lies outside [0, n_pages), is not stored (its query is still turned).  Asynchronous. */
 vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v, const int32_t* positions, const int32_t* cu_tokens,
@@ -414,7 +414,7 @@ vt_status vt_tree_attention(const vt_heads* q, const int32_t* cu_tokens, const v
  * token n follows (an earlier one), or -1.  A token's mask row has the bits of itself and of all tokens on its way up; its depth is the
  * number of those above it.
  *   parents dev [N] int32        mask dev [N, mask_words] int32 (out) or NULL        positions dev [N] int32 (out) or NULL:
- *   lens[b] + depth (lens NULL: the depth)
+ *   lens[b] + depth (lens NULL: the depth)                cu_tokens dev [B + 1] int32, ascending, within [0, N] (below 0 counts as 0)
  * A parent that is not an earlier token of the request counts as -1.  Bits from 32 * mask_words on are dropped; rows outside all requests
  * are left as they were.  mask_words >= 1 where there is a mask.  Asynchronous. */
 vt_status vt_tree_mask(const int32_t* parents, const int32_t* cu_tokens, const int32_t* lens, int N, int B, int32_t* mask, int mask_words,

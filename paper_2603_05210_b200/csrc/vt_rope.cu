@@ -123,7 +123,7 @@ rope_kernel(const __grid_constant__ RopeParams p) {
         const int b = request_of(p.cu, p.B, (int)n);
         int64_t pk = -1, pv = -1;
         if (b >= 0) {
-            const int64_t at = (int64_t)p.lens[b] + n - p.cu[b];
+            const int64_t at = (int64_t)p.lens[b] + n - first_of(p.cu, b);
             const int64_t pg = at / p.page_size;
             if (at >= 0 && pg < p.max_pages) {
                 const int page = p.page_table[b * p.table_stride + pg];
@@ -202,7 +202,7 @@ __global__ void tree_mask_kernel(const int32_t* parents, const int32_t* cu, cons
     if (n >= N) return;
     const int b = request_of(cu, B, n);
     if (b < 0) return;
-    const int first = cu[b];
+    const int first = first_of(cu, b);
     int32_t* row = mask ? mask + (int64_t)n * words : nullptr;
     if (row)
         for (int w = 0; w < words; ++w) row[w] = 0;

@@ -62,6 +62,8 @@ __device__ __forceinline__ int request_of(const int32_t* cu, int B, int n) {
     }
     return lo;
 }
+// Its first token, as the attention and the verification take it: whatever cu holds, no earlier one than 0.
+__device__ __forceinline__ int first_of(const int32_t* cu, int b) { return max(cu[b], 0); }
 #endif
 
 }  // namespace vt
