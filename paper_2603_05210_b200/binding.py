@@ -8,6 +8,7 @@ fallback: if the library cannot be loaded the call raises.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import math
 import os
 from typing import NamedTuple
@@ -93,9 +94,9 @@ def lib() -> ctypes.CDLL:
     """Load ``libvt.so`` from the package directory, building it with nvcc first if it is absent."""
     global _lib
     if _lib is None:
-        if not os.path.exists(LIB_PATH) or not os.path.exists(MARSHAL_PATH):
-            from .build import build
-            build()
+        if not os.path.exists(LIB_PATH):
+            from .build import build_library
+            build_library()
         cd = ctypes.CDLL(LIB_PATH)
         for name, (res, args) in SYMBOLS.items():
             fn = getattr(cd, name)     # AttributeError if the library lacks a declared symbol
@@ -105,11 +106,19 @@ def lib() -> ctypes.CDLL:
 
 
 def _marshal():
-    """The compiled marshalling, told where the library's entry points are."""
+    """The compiled marshalling, told where the library's entry points are; built first if it is absent, or was built against another PyTorch."""
     global _fast
     if _fast is None:
         cd = lib()
-        from . import _vt_torch as fast
+        from .build import build_marshal
+        if not os.path.exists(MARSHAL_PATH):
+            build_marshal()
+        importlib.invalidate_caches()
+        try:
+            fast = importlib.import_module("._vt_torch", __package__)
+        except ImportError:
+            build_marshal(force=True)
+            fast = importlib.import_module("._vt_torch", __package__)
         fast.init(*(ctypes.cast(getattr(cd, n), _p).value for n in (
             "vt_rope", "vt_rope_append", "vt_tree_mask", "vt_tree_attention", "vt_tree_attention_workspace_bytes", "vt_verify_tokens")))
         _fast = fast

@@ -20,14 +20,44 @@ NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
 
-def _deps_mtime() -> float:
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "vt.h")]
-    return max(os.path.getmtime(p) for p in paths)
+MARSHAL_SOURCE = "vt_torch.cpp"
+
+
+def _newer(target: str, sources) -> bool:
+    paths = [os.path.join(CSRC, f) for f in sources] + [os.path.join(HERE, "..", "include", "vt.h")]
+    return os.path.exists(target) and os.path.getmtime(target) >= max(os.path.getmtime(p) for p in paths)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every ``.cu`` under ``csrc/`` and link ``libvt.so``, and ``vt_torch.cpp``; a no-op when both are newer than their sources."""
-    if not force and all(os.path.exists(f) and os.path.getmtime(f) >= _deps_mtime() for f in (LIB, MARSHAL)):
+    """``build_library`` and ``build_marshal`` side by side."""
+    with ThreadPoolExecutor(max_workers=1) as pool:
+        marshal = pool.submit(build_marshal, force)
+        lib = build_library(force, verbose)
+        marshal.result()
+    return lib
+
+
+def build_marshal(force: bool = False) -> str:
+    """Compile ``vt_torch.cpp`` against the installed PyTorch; a no-op when ``_vt_torch.so`` is newer than its source."""
+    if not force and _newer(MARSHAL, [MARSHAL_SOURCE]):
+        return MARSHAL
+    import torch
+    root, cuda = os.path.dirname(torch.__file__), os.path.dirname(os.path.dirname(shutil.which(os.environ.get("NVCC", "nvcc")) or "/usr/local/cuda/bin/nvcc"))
+    tmp = MARSHAL + f".{os.getpid()}.tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           *(a for d in (sysconfig.get_paths()["include"], f"{root}/include", f"{root}/include/torch/csrc/api/include", f"{cuda}/include")
+             for a in ("-isystem", d)),
+           os.path.join(CSRC, MARSHAL_SOURCE), "-o", tmp, f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for {MARSHAL_SOURCE}:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, MARSHAL)
+    return MARSHAL
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """Compile every ``.cu`` under ``csrc/`` and link ``libvt.so``; a no-op when the library is newer than its sources."""
+    if not force and _newer(LIB, [f for f in os.listdir(CSRC) if f != MARSHAL_SOURCE]):
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     os.makedirs(OBJ, exist_ok=True)
@@ -43,23 +73,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    def compile_marshal():
-        import torch
-        root, cuda = os.path.dirname(torch.__file__), os.path.dirname(os.path.dirname(shutil.which(nvcc) or "/usr/local/cuda/bin/nvcc"))
-        tmp = MARSHAL + f".{os.getpid()}.tmp"
-        cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-               *(a for d in (sysconfig.get_paths()["include"], f"{root}/include", f"{root}/include/torch/csrc/api/include", f"{cuda}/include")
-                 for a in ("-isystem", d)),
-               os.path.join(CSRC, "vt_torch.cpp"), "-o", tmp, f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"{cmd[0]} failed for vt_torch.cpp:\n{r.stdout}\n{r.stderr}")
-        os.replace(tmp, MARSHAL)
-
-    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
-        marshal = pool.submit(compile_marshal)
+    with ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
         objs = list(pool.map(compile_one, SOURCES))
-        marshal.result()
     tmp = LIB + f".{os.getpid()}.tmp"
     r = subprocess.run([nvcc, "-shared", "-o", tmp, *objs, "-lcudart"], capture_output=True, text=True)
     if r.returncode != 0:
