@@ -319,7 +319,7 @@ vt_status vt_gated_ffn_backward(const void* x, int64_t ldx, const void* W_gate, 
  *   VT_ROPE_RAMP        w_i = f_i (1 - s) + f_i / factor s,  s = (i - i0) / (i1 - i0) within [0, 1],
  *                       i0 = floor(e(high)), i1 = ceil(e(low)) within [0, rot_dim - 1],
  *                       e(turns) = rot_dim log(original_len / (2 pi turns)) / (2 log base): the pair that makes so many turns
- *                       (its usual amplitude is a = 0.1 log(factor) + 1)
+ *                       (its usual amplitude is a = 0.1 log(factor) + 1, and 1 for factors up to 1)
  *
  *   table  dev [rot_dim / 2] uint64 (out), 8-byte aligned
  * rot_dim a multiple of 16, 16 <= rot_dim <= 1024; base > 1, factor > 0, original_len > 0 and finite; low < high for WAVELENGTH,

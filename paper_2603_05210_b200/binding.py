@@ -590,13 +590,13 @@ def vt_rope_table(rot_dim: int, *, base: float = 10000.0, scaling: str = "none",
     """The plan of rotary positions over a head's first ``rot_dim`` elements, pairs (i, i + rot_dim / 2) or, ``interleaved``, (2 i, 2 i + 1).
 
     ``scaling`` stretches positions for contexts longer than ``original_len``: "linear", "base", "wavelength" (``low`` and ``high`` turns,
-    1 and 4) or "ramp" (1 and 32; the amplitude is then 0.1 log(factor) + 1 unless it is given).  Formulas: ``include/vt.h``."""
+    1 and 4) or "ramp" (1 and 32; the amplitude is then 0.1 log(factor) + 1, for factors above 1, unless it is given).  Formulas: ``include/vt.h``."""
     if scaling not in _ROPE_SCALINGS:
         raise ValueError(f"scaling: expected one of {', '.join(_ROPE_SCALINGS)}, got {scaling!r}")
     if high is None:
         high = 32.0 if scaling == "ramp" else 4.0
     if amplitude is None:
-        amplitude = 0.1 * math.log(factor) + 1.0 if scaling == "ramp" and factor > 0 else 1.0
+        amplitude = 0.1 * math.log(factor) + 1.0 if scaling == "ramp" and factor > 1 else 1.0
     table = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.int64, device=device or "cuda")
     if table.get_device() != torch.cuda.current_device():
         raise ValueError("device: expected the current CUDA device")
