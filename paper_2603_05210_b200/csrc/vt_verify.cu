@@ -125,14 +125,13 @@ verify_kernel(const __grid_constant__ VerifyParams prm) {
 
     int buffer = 0;
     auto skew_of = [&](int x) { return (int)(reinterpret_cast<uintptr_t>(c.probs + (int64_t)(begin + x) * c.ld_probs) >> 2 & 3u); };
-    // lays out q of a node, or its children
+    // lays out q of a node; without q the children of the last one, once
     bool cleared = true;
     auto lay_out = [&](int x) {
-        if (!cleared) {
+        if (DRAWN && !cleared) {
             __syncthreads();                 // the last node's has been read
             clear();
-            if (DRAWN) cluster_sync_all();
-            else __syncthreads();
+            cluster_sync_all();
         }
         cleared = false;
         const int skew = skew_of(x);
