@@ -32,13 +32,15 @@
 // Turns of the ring.  K and V tiles take places in one order (AttnPiece::k_at), place P stage P mod ST, turn P / ST, and the cleaner passes
 // every place in that order.  A wait names a turn by its parity and also passes when the turn before is not over, so whoever waits has to
 // know that it is; ST is 5 at least, and "passed" is said of the cleaner:
-//   a producer   waits for v_clean(P - ST), then kv_empty(P - ST).  Its last place lies 3 before P at most, so P - 3 - ST, and P - 2 ST with it,
-//                has been passed when it asks for v_clean; and P - ST is passed only when it was loaded, after its producer saw P - 2 ST empty.
+//   a producer   that loaded P - ST itself has seen P - 2 ST empty.  Otherwise it waits for v_clean(P - ST) before kv_empty(P - ST): that place is
+//                passed only when it was loaded, after the other producer saw P - 2 ST empty.  And P - 2 ST has been passed by then, as its own last place,
+//                3 before P at most, came behind the emptying of the place ST before that.
 //   one issuer   takes all value places, 3 apart at most, and all key places behind the values before them: P - ST has been passed.
-//   two issuers  wait for the weights of a step before its values.  An item's first weights come behind the last item's O, so all of that one's
-//                places have been passed; V(0) lies at place 1 or 2 of the item and V(1) at 3 or 4, later values of a stream 3 or 4 behind its last.  K(j)
-//                follows the stream's V(j - 2), one place before it; K(0) and K(1) its last values, 2 places before the item at most, or, where the
-//                last item (of one tile) had none for it, the O of the item before.
+//   two issuers  A stream's K(j) follows its V(j - 2), one place before it; later values of a stream are 3 or 4 behind its last.  K(0) and K(1), places 0
+//                and 1 of an item, follow its last values, 2 places before the item at most, or, where the last item (of one tile) had none for it,
+//                the O of the item before.  V(0) lies at 1 or 2, V(1) at 3 or 4: with 7 stages or more the same holds.  With fewer (heads of 128) an
+//                item's first weights are waited for before its values: they come behind the last item's O, so all of that one's places have been
+//                passed.  (For all steps and stages: 24 x 8 over 2500 57 -> 58.4 us.)
 // (With the values first, or without a look at v_clean in the producers, copies of a slow stream's tiles were overtaken: no error, wrong values.)
 //
 // Bound and measured (in a graph, a copy at 6.46 TB/s and 1673 TFLOP/s in bf16 as the floors; requests x tokens over positions, 32 heads over 8
@@ -441,6 +443,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
     // Copies of a piece's key tiles, or of its value tiles, from ring place `loads` on: a lane per box, column block lane / np, page lane % np of
     // the tile.  A box costs the warp 100 cycles, so either kind has a warp of its own.
     bool bad = false;
+    uint32_t own = 0, last_place = 0;                        // bit d of own: place last_place - d is this warp's
     auto copy_tiles = [&](const AttnPiece& w, uint32_t loads, bool values) -> bool {
         const int pr = min(p.page_size, kAttnKeys), np = kAttnKeys / pr;
         const int col = lane / np, pg = lane - col * np;
@@ -460,8 +463,11 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
         for (int j = 0; j < w.n; ++j) {
             const int page_next = page_of(j + 1);            // one ahead of its use
             const uint32_t place = loads + (values ? w.v_at(j) : w.k_at(j)), turn = turn_of(place), stage = place - turn * ST;
-            // (in the first turn there is nothing to wait for)
-            if (!wait(v_clean + 8u * stage, (turn & 1u) ^ 1u) || !wait(kv_empty + 8u * stage, (turn & 1u) ^ 1u)) return false;
+            own <<= place - last_place;
+            last_place = place;
+            // the other producer's tile in the stage: has it come?  Then, is the stage empty?  (In the first turn there is nothing to wait for.)
+            if ((!(own >> ST & 1u) && !wait(v_clean + 8u * stage, (turn & 1u) ^ 1u)) || !wait(kv_empty + 8u * stage, (turn & 1u) ^ 1u)) return false;
+            own |= 1u;
             const bool there = mine && j < end;
             uint32_t boxes = (uint32_t)np * (D / 64);
             if (j == last_tile) boxes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, there));
@@ -648,12 +654,14 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 if (i >= 0) {
                     const uint32_t place = loads + w.v_at(i >> w.dual), turn = turn_of(place), st = place - turn * ST;
                     const int steps = attn_k_steps(w, i >> w.dual);
-                    auto weights = [&]() -> bool { return wait(p_full + 8u * s, p_phase >> s & 1u); };
-                    if ((REP && !weights()) || !wait(v_clean + 8u * st, turn & 1u)) { ok = false; break; }
-                    if (!REP) {
-                        keys = more && i + 2 > w.dual && attn_test(kv_full + 8u * k_st, k_turn & 1u);
-                        if (!weights()) { ok = false; break; }
+                    uint32_t bar0 = v_clean + 8u * st, par0 = turn & 1u, bar1 = p_full + 8u * s, par1 = p_phase >> s & 1u;
+                    if (REP && D == 128 && i < 2) {      // an item's first weights before its values
+                        const uint32_t bar = bar0, par = par0;
+                        bar0 = bar1, par0 = par1, bar1 = bar, par1 = par;
                     }
+                    if (!wait(bar0, par0)) { ok = false; break; }
+                    if (!REP) keys = more && i + 2 > w.dual && attn_test(kv_full + 8u * k_st, k_turn & 1u);
+                    if (!wait(bar1, par1)) { ok = false; break; }
                     p_phase ^= 1u << s;
                     tc_fence_after();
                     if (attn_elect()) {
@@ -1216,8 +1224,8 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     // five stages of 32 KB beside two full row tiles: 160 KB in flight
     const uint32_t tile = kAttnKeys * D * 2, tail = sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces);
     p.n_stages = (int)std::min((uint32_t)kAttnMaxStages, ((uint32_t)kMaxDynSmem - tail - 2 * p.q_slot) / tile);
-    static_assert((kMaxDynSmem - (sizeof(AttnShared) + 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces)) - 2 * 32768) / (kAttnKeys * 128 * 2) >= 5,
-                  "the order of waits in the ring takes five stages");
+    constexpr int kRoom = kMaxDynSmem - (int)sizeof(AttnShared) - 8 * (3 * kAttnMaxStages + 12 + 2 * kAttnPieces);
+    static_assert((kRoom - 2 * 32768) / (kAttnKeys * 128 * 2) >= 5 && (kRoom - 2 * 16384) / (kAttnKeys * 64 * 2) >= 7, "see the turns of the ring");
     p.stages_inv = (uint32_t)((0x100000000ull + p.n_stages - 1) / p.n_stages);
     p.shared_off = 2 * p.q_slot + p.n_stages * tile;
     p.bar_off = p.shared_off + sizeof(AttnShared);

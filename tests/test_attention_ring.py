@@ -41,7 +41,7 @@ class Ring:
     """One CTA.  pieces: (tiles, two row tiles) of each item; few: an issuer per stream.
 
     Planted mistakes: clean_first, the few-rows issuer waits for the values before it waits for the weights; blind, the producers ask for a stage
-    without having seen that its last turn was loaded."""
+    without having seen that the other one's tile in it was loaded."""
 
     def __init__(self, pieces, stages, few, rng, clean_first=False, blind=False):
         self.pieces, self.ST, self.few, self.rng = pieces, stages, few, rng
@@ -65,6 +65,7 @@ class Ring:
 
     def producer(self, values):
         loads = q_n = 0
+        mine = set()
         for n, dual in self.pieces:
             if not values:
                 for _ in range(1 + dual):
@@ -77,9 +78,10 @@ class Ring:
                 place = loads + (self.v_at if values else self.k_at)(n, j)
                 turn, st = divmod(place, self.ST)
                 if turn > 0:
-                    if not self.blind:
+                    if not self.blind and place - self.ST not in mine:
                         yield self.clean[st], turn - 1
                     yield self.empty[st], turn - 1
+                mine.add(place)
                 self.full[st].arrive(expect=1)
                 self.copies.append((self.full[st], st, place))
             loads += 2 * n
@@ -118,7 +120,7 @@ class Ring:
                     place = loads + self.v_at(n, i >> dual)
                     turn, st = divmod(place, self.ST)
                     waits = [(self.clean[st], turn), (self.p_full[s], p_phase[s])]
-                    if self.few and not self.clean_first:
+                    if self.few and i < 2 and self.ST < 7 and not self.clean_first:
                         waits.reverse()
                     yield waits[0]
                     keys = False                 # the next keys are there already
