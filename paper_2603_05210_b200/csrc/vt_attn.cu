@@ -2,7 +2,10 @@
 //
 // out = sum_i e^{x_i - lse} v_i over the attended positions, x = scale q.k: one pass over keys and values, with the running maximum and sum
 // of each row, as two tcgen05 products per tile of 128 positions - S = Q K^T, then O += P V with P = 2^{(S - m) scale log2 e} in bf16, the
-// operand type of the product (its sum l is of the weights before they are rounded).  Scores, maxima, sums and O are fp32.
+// operand type of the product.  Scores, maxima, sums and O are fp32.  lse comes from the sum l of the weights before they are rounded.  With few rows O
+// is divided by the sum of the rounded ones: a weight far above the others then loses nothing (error of whole outputs over 4096 ragged positions 2.09e-3 ->
+// 1.88e-3, 1.65e-3 of it the rounding of out; 24 x 8 over 2500 +0.6 us).  With many, where a stream's exponentials are what it waits for, O is divided by l:
+// the second sum took 110 -> 113.6 us for two long documents under 60 tokens, and 58 -> 62.5 for 16 x 60 over 8000 with heads of 64.
 //
 // Rows.  All query heads of a key head and all drafted tokens of a request read the same keys, so they are the rows of one product: row
 // t G + g for token t and head g of G.  A block of rows is up to two tiles of 128 TMEM lanes (a TMA box of G heads x 128 / G tokens fills a tile
@@ -55,6 +58,8 @@
 #include "vt_step.h"
 #include "vt_tc.cuh"
 
+#include <cfloat>
+
 namespace vt {
 
 int gemm_withheld_us();                      // see vt_test_withhold_copies
@@ -101,7 +106,7 @@ struct AttnParams {
     uint32_t q_block, q_slot;                // bytes of 64 columns of a row tile; of a row tile
     uint32_t q_tx, page_tx;                  // bytes of a q tile; of one box of keys
     uint32_t shared_off, bar_off, withheld;              // withheld: see vt_test_withhold_copies
-    float scale, scale_log2;
+    float scale, scale_log2, scale_inv;      // scale_inv: 1 / scale_log2, 0 where that is no number
     unsigned long long wait_ns;
 };
 
@@ -186,6 +191,10 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     uint64_t r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+// adds two packed bf16 to two sums
+__device__ __forceinline__ void attn_add_bf16x2(float& lo, float& hi, uint32_t v) {
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}" : "+f"(lo), "+f"(hi) : "r"(v));
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
@@ -762,7 +771,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
             const int my_row = REP ? lane : r;               // of the tile
             const bool real = my_row < rows, busy = REP || quad * 32 < rows;
             const int t = w.tok0 + (w.dual ? s * p.tpt : 0) + (real ? my_row / p.G : 0);      // its token within the request
-            float m = -INFINITY, l = 0.0f;
+            float m = -INFINITY, l = 0.0f, lr = 0.0f;        // lr (few rows): of the rounded weights
 #pragma unroll 1
             for (int i = s; i < H; i += 2) {
                 if (!wait(s_full + 8u * s, s_phase)) { ok = false; break; }
@@ -778,6 +787,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             if (grow) {
                                 m = mx;
                                 l *= f;
+                                lr *= f;
                             }
                             if (i >= 2) {
 #pragma unroll 1
@@ -817,6 +827,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         const float ref = m == -INFINITY ? 0.0f : -m * p.scale_log2;
                         const uint64_t k2 = pack2(p.scale_log2, p.scale_log2), r2 = pack2(ref, ref);
                         uint64_t sum0 = 0ull, sum1 = 0ull;
+                        float lr0 = 0.0f, lr1 = 0.0f;
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float a, b;
@@ -826,6 +837,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                             if (e & 2) sum1 = add2(sum1, pack2(a, b));
                             else sum0 = add2(sum0, pack2(a, b));
                             pk[e / 2] = attn_bf16x2(a, b);
+                            attn_add_bf16x2(lr0, lr1, pk[e / 2]);
                         }
                         tc_st16(t_s + 16u * quad, pk);           // over scores of its own lanes, which it has read
 #pragma unroll
@@ -835,6 +847,7 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                         float a, b;
                         unpack2(add2(sum0, sum1), a, b);
                         l += a + b;
+                        lr += lr0 + lr1;
                     } else {
                         if (j >= w.open) {                       // what the row does not attend: -infinity, back in its place
 #pragma unroll 1
@@ -905,6 +918,13 @@ attn_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnP
                 // Eight parts of each row, by stream and warp, meet in the item's slot of q: all columns of up to 8 rows at a time, half of those
                 // of 16, a quarter of those of 32.  A thread adds up four columns of a row.
                 float4* xs = reinterpret_cast<float4*>(smem + (item++ & 1u) * p.q_slot);
+                // O has the rounded weights, so their sum lr is what it is divided by.  Instead of (m, l, lr) with l = 2^y lr, the rest of the way goes
+                // with (m + y / (scale log2 e), lr), which has both: lse comes from l, O / lr has weights that add up to 1.  |l / lr - 1| <= 2^-8.
+                if (lr > 0.0f && p.scale_inv > 0.0f) {
+                    const float d = __fdividef(l - lr, lr);
+                    m = fmaf(d * kLog2e * (1.0f - d * (0.5f - d * (1.0f / 3.0f))), p.scale_inv, m);
+                    l = lr;
+                }
                 const int log_rows = rows <= 8 ? 3 : rows <= 16 ? 4 : 5, rounds = 1 << (log_rows - 3), quads = (D / 4) >> (log_rows - 3);
                 sh.ms[s][r] = make_float2(m, l);
 #pragma unroll 1
@@ -1211,6 +1231,7 @@ vt_status launch_attn(const AttnCall& c, void* workspace, cudaStream_t st) {
     p.min_run = p.rows_max > 128 ? 6 : 2;                      // (1 x 60 over 4000: 24.7 us with 8, 23.6 with 6)
     p.scale = c.scale;
     p.scale_log2 = c.scale * kLog2e;
+    p.scale_inv = c.scale >= FLT_MIN ? 1.0f / p.scale_log2 : 0.0f;
     p.wait_ns = kWaitLimitNs;
     if (const int us = gemm_withheld_us(); us > 0) {         // a test of the unwinding: copies fall 16 bytes short
         p.withheld = 16;
