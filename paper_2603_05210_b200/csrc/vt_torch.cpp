@@ -248,8 +248,8 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[4] != Py_None) {
         const at::Tensor* m;
         if (!tensor(a[4], "mask", &m)) return nullptr;
-        if (m->scalar_type() != at::kInt || m->dim() != 2 || m->size(0) != q.n || !here(*m, &dev) || !m->is_contiguous() || m->size(1) > INT32_MAX) {
-            refuse(PyExc_ValueError, "mask", "expected a contiguous int32 tensor with a row per token on the current CUDA device");
+        if (m->scalar_type() != at::kInt || m->dim() != 2 || m->size(0) != q.n || !here(*m, &dev) || !m->is_contiguous() || m->size(1) < 1 || m->size(1) > INT32_MAX) {
+            refuse(PyExc_ValueError, "mask", "expected a contiguous int32 tensor with a row of words per token on the current CUDA device");
             return nullptr;
         }
         mask = (const int32_t*)m->data_ptr();
@@ -302,7 +302,7 @@ PyObject* verify_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t Vd = 0, ldq = 0;
     if (a[7] != Py_None) {
         if (!tensor(a[7], "draft_probs", &draft) || !rows(*draft, "draft_probs", &dev)) return nullptr;
-        if (a[8] == Py_None || draft->size(0) != N) {
+        if (a[8] == Py_None || draft->size(0) != N || draft->size(1) < 1) {
             refuse(PyExc_ValueError, "draft_probs", "needs a row per token, and draft_ids");
             return nullptr;
         }
