@@ -1,11 +1,12 @@
-"""Speculative decoding with a drafted tree, every step of it through the library.
+"""Speculative decoding with a drafted tree: the draft's layer, the choice of candidates and their verification through the library.
 
     python examples/decode_step.py [--rounds 4]
 
 A draft layer (queries, keys and values from the features, rotary positions, attention over a paged cache, the gated block, the
 trimmed head) grows a tree of candidates for each request (vt_rope_append, vt_tree_attention, vt_draft_head, vt_tree_select), the target
-scores it, and what stays is decided by vt_verify_tokens.  The target is a stand-in: a full head on the draft's own hidden states, with noise.
-Weights are random.
+scores it, and what stays is decided by vt_verify_tokens.  The target is a stand-in: the logits of a full head on the draft's own hidden states
+(vt_debug_logits) with noise, and torch.softmax.  Candidates are the best ones, so the form of the verification for drawn ones is not shown.  Weights
+are random.
 """
 from __future__ import annotations
 

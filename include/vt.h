@@ -376,7 +376,8 @@ typedef struct vt_cache {
 /* vt_rope for serving: queries are turned into q_out, keys are turned and stored in the cache, values [N, Hkv, D] are stored beside them.
  * Token n belongs to the request b with cu_tokens[b] <= n < cu_tokens[b + 1] and goes to position lens[b] + n - cu_tokens[b]; lens
  * itself stays as it is.
- *   cu_tokens  dev [B + 1] int32, ascending, within [0, N] (below 0 counts as 0)          positions  dev [N] int32: what the angles go by (in a tree the depth, not the place)
+ *   cu_tokens  dev [B + 1] int32, ascending, within [0, N] (below 0 counts as 0)
+ *   positions  dev [N] int32: what the angles go by (in a tree the depth, not the place)
  * Tokens outside [cu_tokens[0], cu_tokens[B]) are padding: nothing of theirs is written.  A token whose position lies past the table, or
  * whose page id lies outside [0, n_pages), is not stored (its query is still turned).  Asynchronous. */
 vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v, const int32_t* positions, const int32_t* cu_tokens,
@@ -394,7 +395,8 @@ vt_status vt_rope_append(const vt_heads* q, const vt_heads* k, const vt_heads* v
  * query head h reads key head h / (Hq / heads).  A token that attends nothing has out = 0 and lse = -infinity.  Keys and values of
  * positions that nobody attends, behind a request's end or out of every token's mask, may hold anything; where only some tokens attend one, the
  * others are not touched by it, but for those its value must be finite (infinities and NaN act as the largest finite number).  Queries of
- * requests, attended keys and values, and the scores x_i must be finite.  Products are exact, sums fp32; the weights exp(x_i - m) are rounded to bf16 as an operand of the second product (not in lse), out once to bf16.
+ * requests, attended keys and values, their products q . k_i and the scores x_i must be finite, scores and scale below 2^127.  Products are
+ * exact, sums fp32; the weights exp(x_i - m) are rounded to bf16 as an operand of the second product (not in lse), out once to bf16.
  *
  *   q        [N, Hq, D] as vt_heads                     out      [N, Hq, D] as vt_heads (out)      lse  dev [N, Hq] float (out) or NULL
  *   cu_tokens  dev [B + 1] int32, ascending, within [0, N]; rows outside all requests are left as they were

@@ -43,18 +43,20 @@
 //                and 1 of an item, follow its last values, 2 places before the item at most, or, where the last item (of one tile) had none for it,
 //                the O of the item before.  V(0) lies at 1 or 2, V(1) at 3 or 4: with 7 stages or more the same holds.  With fewer (heads of 128) an
 //                item's first weights are waited for before its values: they come behind the last item's O, so all of that one's places have been
-//                passed.  (For all steps and stages: 24 x 8 over 2500 57 -> 58.4 us.)
+//                passed.  (With heads of 64 too: 24 x 8 over 2500 57.4 -> 58.3 us.)
 // (With the values first, or without a look at v_clean in the producers, copies of a slow stream's tiles were overtaken: no error, wrong values.)
 //
 // Bound and measured (in a graph, a copy at 6.46 TB/s and 1673 TFLOP/s in bf16 as the floors; requests x tokens over positions, 32 heads over 8
 // of 128 where nothing else stands):
-//   2 x 8 over 100000             132 us   floor 127: bytes of the cache, 6.2 TB/s
+//   2 x 8 over 100000             134 us   floor 127: bytes of the cache, 6.1 TB/s
 //   64 x 1 over 4096, ragged       98 us   floor 86: bytes, 5.7 TB/s
-//   24 x 8 over 2500, 32 heads of 64 each, ragged   57 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
-//   16 x 60 over 8000, ragged      72 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
+//   24 x 8 over 2500, 32 heads of 64 each, ragged   58 us   floor 40: bytes, 768 items of 20 tiles at most, each with a beginning and an end
+//   16 x 60 over 8000, ragged      72 to 78 us   floor 54: a stream's exponentials and its products follow one another: 4140 cycles for a pair of steps
 //                                          whose products, and whose exponentials, would each take 2048
-//   1 x 60 over 4000             21.6 us   floor 3: latency; 93 runs of three tiles and the join
-//   1 x 1 over 700                11.5 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
+//   1 x 60 over 4000             21.6 us   floor 3: latency; 88 runs of two or three tiles and the join
+//   1 x 1 over 700                11.4 us  floor 0.5: latency of launch, plan, copy, two products, epilogue, join
+//   1 x 4099 over 0, a chain       171 us  floor 82: products, of 65 blocks with half a tile each that the chain cuts off; what else is not taken apart
+//   1 x 4099 over 120000           8.4 ms  floor 4.9: products and exponentials in turn, as with 16 x 60
 #include "vt_step.h"
 #include "vt_tc.cuh"
 

@@ -14,7 +14,7 @@
 // Bound: latency.  Seven memory round trips follow one another (offsets, nodes, gathers, q, the row, a part of it again, four ids), with two
 // to four synchronisations of a cluster between them; the bytes of one row of p (and q) per request take a tenth of that for 16 requests.
 // Measured with a vocabulary of 128256, in a graph: one chain of six drawn from 32000 ids 13.0 us, 16 trees of 60 best ones 10.7 us, 64 chains of
-// eight 37 us drawn and 22 us best.
+// eight 37 us drawn and 22 us best (bytes: 8 and 5): 512 CTAs at two per SM are 1.7 waves, each with the whole chain of round trips.
 // The code is fetched as it goes, once per call and SM, so less of it is faster: the sum in one loop in place of a vector and a scalar one, and
 // the target sought by warp sums of 128 ids in place of lanes with runs of their own, took the 16 trees from 12.6 us to 10.7.  (Sums of 128 ids
 // kept by every warp for the search: 15 us.  1024 threads a CTA: 22 us.  q found through an index of the ids instead of laid out: a drawn chain
