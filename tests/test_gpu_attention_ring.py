@@ -46,3 +46,19 @@ def test_long_items_behind_one_another(vt):  # noqa: F811
     c.check(out, lse)
     again = [c.run() for _ in range(50)]
     assert all(torch.equal(a, out) and torch.equal(b, lse) for a, b in again)
+
+
+def test_a_wait_that_runs_out_with_two_issuers_and_a_short_ring(vt):  # noqa: F811
+    # each copy is made to fall 16 bytes short of what is waited for (host side): every role leaves, and the next call is right
+    c = Case(vt, [3000, 700] * 12, [1, 3] * 12, 16, 4, 128, 32)
+    ws = vt.new_workspace(vt.vt_tree_attention_workspace_bytes(16, 4, 128, 3))
+    want = c.run()
+    try:
+        vt.vt_test_withhold_copies(2000)
+        c.run(workspace=ws)
+        assert vt.vt_last_status(ws) == vt.VT_ERR_TIMEOUT
+    finally:
+        vt.vt_test_withhold_copies(0)
+    got = c.run(workspace=ws)
+    assert vt.vt_last_status(ws) == vt.VT_OK
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
