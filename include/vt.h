@@ -440,7 +440,7 @@ vt_status vt_tree_mask(const int32_t* parents, const int32_t* cu_tokens, const i
  *   probs       dev [N, V] float, rows ld_probs apart     tokens  dev [N] int32: ids in the target's vocabulary
  *   parents     dev [N] int32: index within the request   cu_tokens  dev [B + 1] int32, ascending, within [0, N]
  *   u_accept    dev [N] float in [0, 1)                   u_sample   dev [B] float in [0, 1)
- *   draft_probs dev [N, Vd] float or NULL, rows ld_draft apart        draft_ids  dev [N] int32: tokens as draft indices
+ *   draft_probs dev [N, Vd] float or NULL, rows ld_draft apart        draft_ids  dev [N] int32: tokens as draft indices (what d2t maps to tokens[n])
  *   d2t         dev [Vd] int32: the draft-to-target map, distinct ids (NULL: a draft index is the target's id)
  *   n_accepted  dev [B] int32 (out)       path  dev [B, max_tokens] int32 (out): the accepted tokens' indices within the request, then -1
  *   out_tokens  dev [B, max_tokens] int32 (out): the accepted tokens, the one that follows them, then -1
